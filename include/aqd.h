@@ -349,6 +349,143 @@ size_t aqd_bn_level_stats_workspace_bytes(int32_t levels, int32_t c);
 aqd_status aqd_bn_level_stats(const float* const* z, const int64_t* pixels, int32_t levels, int32_t c, double* mean,
                               double* var, void* workspace, size_t ws_bytes, aqd_stream_t stream);
 
+/* ---- 8-bit language-model operators -------------------------------------------------- */
+
+/* The quantized path of a decoder's feed-forward and output layers beside the convolutions: every
+ * token's activations become int8 codes with one float32 scale per token (value = code * scale, Eq. 1's
+ * uniform quantizer with the interval taken from the row), layers multiply codes exactly as integers
+ * (Eq. 4), and the two scales return once per output. The paper's own layers are convolutions; these are the
+ * same quantizer and product on matrices of tokens.
+ *
+ * Matrices are row-major with a row stride in elements (ld); elements of a row are adjacent. Types: */
+enum { AQD_F32 = 0, AQD_F16 = 1, AQD_BF16 = 2, AQD_I32 = 3 };
+
+/* Where the quantizers write rows of 8-bit codes. codes or values may be NULL, not both. */
+typedef struct {
+  int8_t* codes;        /* [rows][ld_codes], in [-127, 127] */
+  int64_t ld_codes;
+  float* scales;        /* [rows] */
+  void* values;         /* the values that the codes stand for, code * scale rounded to values_dtype */
+  int64_t ld_values;
+  int32_t values_dtype; /* AQD_F32, AQD_F16 or AQD_BF16 */
+} aqd_row_codes;
+
+/* How a row u of float32 values becomes codes: a = max |u_k|, scale = a / 127, code = u / scale
+ * rounded to nearest, ties to even (computed as u * (127 / a)). A row with a < 2^-120 has scale 0 and codes 0. A row
+ * that holds a NaN or an infinity (or, under the norm, whose sum of squares passes float32's range)
+ * has scale NaN, codes 0 and values NaN, so the products that read it give NaN.
+ * All pointers are device pointers aligned to their element; rows that start at 16-byte boundaries
+ * take vector accesses. cols >= 1; rows may be 0. Every row stride of an output must be >= cols; an
+ * input's may be any value >= 0. Outputs do not overlap inputs, except where said. */
+
+/* u = x. */
+aqd_status aqd_quant_rows(int64_t rows, int32_t cols, const void* x, int64_t ldx, int32_t dtype,
+                          const aqd_row_codes* out, aqd_stream_t stream);
+
+/* The norm before a layer, with the residual's addition: h = x + residual (residual NULL: h = x),
+ *   u_k = h_k / sqrt(mean(h^2) + eps) * weight_k,
+ * in float32 throughout; `sum` (NULL: not wanted) receives h rounded to `dtype`, the type of x, residual
+ * and sum; the norm reads the unrounded h. sum may be x or residual itself (same pointer and ld): the residual
+ * stream updated in place. weight: cols values of weight_dtype. eps >= 0. */
+typedef struct {
+  int64_t rows;
+  int32_t cols, dtype;
+  const void* x;
+  int64_t ldx;
+  const void* residual;
+  int64_t ld_residual;
+  void* sum;
+  int64_t ld_sum;
+  const void* weight;
+  int32_t weight_dtype;
+  float eps;
+} aqd_rms_norm_args;
+aqd_status aqd_rms_norm_quant(const aqd_rms_norm_args* args, const aqd_row_codes* out, aqd_stream_t stream);
+
+/* Between a gated feed-forward's products: u = act(gate) * up in float32. act: AQD_ACT_SILU,
+ * g / (1 + e^-g), or AQD_ACT_GELU_TANH, g/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))). gate and up are matrices of
+ * one type (two halves of one product's output, say: same ld, up = gate + cols). */
+enum { AQD_ACT_SILU = 0, AQD_ACT_GELU_TANH = 1 };
+typedef struct {
+  int64_t rows;
+  int32_t cols, dtype;
+  const void* gate;
+  int64_t ld_gate;
+  const void* up;
+  int64_t ld_up;
+  int32_t act;
+} aqd_gated_act_args;
+aqd_status aqd_gated_act_quant(const aqd_gated_act_args* args, const aqd_row_codes* out, aqd_stream_t stream);
+
+/* Prepared weights of an 8-bit layer: n output channels of k int8 codes and a scale per channel. */
+typedef struct {
+  const void* data;    /* device buffer of aqd_linear_weights_bytes(n, k) bytes, 256-byte aligned */
+  const float* scales; /* [n] (device; read by every call, not copied) */
+  int32_t n, k;
+} aqd_linear_weights;
+
+/* Size of the prepared-weights buffer; 0 for sizes that are not supported (n or k < 1, k > 131,071, beyond which
+ * a sum of k products of two int8 codes could pass int32, or over 2^40 bytes). */
+size_t aqd_linear_weights_bytes(int32_t n, int32_t k);
+/* Lays codes[n][ld] (any int8 values) out at w->data, once per model load. */
+aqd_status aqd_linear_prepare_weights(const int8_t* codes, int64_t ld, const aqd_linear_weights* w, void* prepared,
+                                      size_t bytes, aqd_stream_t stream);
+
+/* y[m][n] = (sum_k x[m][k] w[n][k]) * x_scale[m] * w_scale[n] + bias[n]: the sum is the exact int32,
+ * converted to float32 once, then the products in this order and the addition in float32, rounded once to y_dtype. bias (float32) may be
+ * NULL. With y_dtype AQD_I32, y receives the integer sums and x_scale, the weights' scales and bias are not read.
+ * x: int8 codes, any ldx >= 0. workspace: aqd_linear_workspace_bytes(m, w) bytes or more, 256-byte aligned,
+ * or NULL; it must be zeroed once before its first use, and calls that share it must not overlap in time.
+ * Results are identical with and without it: it lets a product with few output tiles split its sums over k, and
+ * copies codes whose rows are not 16-byte aligned. */
+typedef struct {
+  int64_t m;
+  const int8_t* x;
+  int64_t ldx;
+  const float* x_scale;
+  const float* bias;
+  void* y;
+  int64_t ldy;
+  int32_t y_dtype;
+} aqd_linear_args;
+size_t aqd_linear_workspace_bytes(int64_t m, const aqd_linear_weights* w);
+aqd_status aqd_linear_int8(const aqd_linear_args* args, const aqd_linear_weights* w, void* workspace, size_t ws_bytes,
+                           aqd_stream_t stream);
+
+/* ---- distillation from a teacher's top logits ----------------------------------------- */
+
+/* The loss that trains a low-bit student from a float teacher of which only the `top` largest logits of each
+ * token are kept (teacher[t][j] float32, at vocabulary places index[t][j]):
+ *   p = softmax(teacher / tau) over the kept places, q = softmax(logits / tau) over the whole vocabulary,
+ *   loss[t] = row_weight[t] * sum_j p_j (ln p_j - ln q_index[j]),
+ *   grad[t][v] = d loss[t] / d logits[t][v] = row_weight[t] / tau * (q_v sum_j p_j - sum_{j: index[j] = v} p_j).
+ * A place whose index lies outside [0, vocab) is empty (a token may have fewer kept logits), as is one whose teacher
+ * logit is -infinity; a token with none has loss 0 and gradient 0. A place listed twice counts twice.
+ * A token of weight 0 has loss 0 and gradient 0 whatever its logits hold. A logit of -infinity has q = 0; where a
+ * kept place of p > 0 has it, the loss is +infinity. A NaN or +infinity among a token's logits or kept
+ * teacher logits makes its loss and gradient NaN, as do logits that are all -infinity. Statistics are
+ * float32; each thread sums a fixed share of a row and shares combine in a fixed order (deterministic).
+ *   loss, lse: [tokens] float32 or NULL; lse = ln sum_v exp(logits[v] / tau), which the backward reads.
+ *   grad: NULL (loss alone) or rows of the logits' type; it may be the logits themselves (same pointer and ld).
+ *   row_weight: [tokens] float32, or NULL for all 1. tau > 0. top: 1..1024. index: int64. */
+typedef struct {
+  int64_t tokens;
+  int32_t vocab, dtype;
+  const void* logits;
+  int64_t ld_logits;
+  const int64_t* index;  /* [tokens][top], rows adjacent */
+  const float* teacher;  /* [tokens][top], rows adjacent */
+  int32_t top;
+  float tau;
+  const float* row_weight;
+  void* grad;
+  int64_t ld_grad;
+} aqd_distill_args;
+aqd_status aqd_distill_topk(const aqd_distill_args* args, float* loss, float* lse, aqd_stream_t stream);
+/* The gradient alone, from the lse that aqd_distill_topk wrote; row_weight is the factor of each token's gradient
+ * (the weight times the gradient that arrives at its loss). */
+aqd_status aqd_distill_topk_backward(const aqd_distill_args* args, const float* lse, aqd_stream_t stream);
+
 /* ---- elementwise ------------------------------------------------------------------ */
 
 /* y = requant(sat32(acc + bias)) per channel at `level`: Eq. 6 + Eq. 2 on an int32

@@ -11,6 +11,7 @@ import functools
 import os
 import struct
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
@@ -62,7 +63,9 @@ EXPORTS = ["aqd_row_bytes", "aqd_quantize_multiplier", "aqd_status_string", "aqd
            "aqd_maxpool_codes", "aqd_maxpool_expand", "aqd_conv_int_static_workspace", "aqd_selftest_wait_timeout",
            "aqd_conv_tower_sync_bytes", "aqd_conv_int_grouped_tower", "aqd_fake_quant",
            "aqd_fake_quant_backward_workspace_bytes", "aqd_fake_quant_backward",
-           "aqd_bn_level_stats_workspace_bytes", "aqd_bn_level_stats"]
+           "aqd_bn_level_stats_workspace_bytes", "aqd_bn_level_stats", "aqd_quant_rows", "aqd_rms_norm_quant",
+           "aqd_gated_act_quant", "aqd_linear_weights_bytes", "aqd_linear_prepare_weights",
+           "aqd_linear_workspace_bytes", "aqd_linear_int8", "aqd_distill_topk", "aqd_distill_topk_backward"]
 
 _lib = None
 _hot = None  # the same library for the calls below that pass their structs as packed bytes
@@ -176,7 +179,16 @@ def load(build_if_missing: bool = True):
                        ("aqd_requant", [vp, vp, i32, vp, vp]),
                        ("aqd_residual_add_int", [vp, vp, vp, vp, i32, vp, vp]),
                        ("aqd_maxpool_codes", [vp, i32, i32, i32, vp, vp]),
-                       ("aqd_maxpool_expand", [vp, i32, i32, i32, vp, vp, i32, i32, vp, sz, vp])):
+                       ("aqd_maxpool_expand", [vp, i32, i32, i32, vp, vp, i32, i32, vp, sz, vp]),
+                       ("aqd_quant_rows", [i64, i32, vp, i64, i32, vp, vp]),
+                       ("aqd_rms_norm_quant", [vp, vp, vp]),
+                       ("aqd_gated_act_quant", [vp, vp, vp]),
+                       ("aqd_linear_weights_bytes", [i32, i32]),
+                       ("aqd_linear_prepare_weights", [vp, i64, vp, vp, sz, vp]),
+                       ("aqd_linear_workspace_bytes", [i64, vp]),
+                       ("aqd_linear_int8", [vp, vp, vp, sz, vp]),
+                       ("aqd_distill_topk", [vp, vp, vp, vp]),
+                       ("aqd_distill_topk_backward", [vp, vp, vp])):
         fn = getattr(hot, name)
         fn.argtypes = args
         fn.restype = sz if name.endswith("_bytes") else c_int
@@ -593,6 +605,278 @@ def bn_level_stats(zs, stream=None):
     _check(load().aqd_bn_level_stats(ptrs, pix, nlev, c, mean.data_ptr(), var.data_ptr(), ws.data_ptr(), ws.numel(),
                                      _stream(stream)), "aqd_bn_level_stats")
     return mean, var
+
+
+# ------------------------------------------------------------------ 8-bit language-model operators
+
+_F32, _F16, _BF16, _I32 = range(4)
+_DTYPE = {torch.float32: _F32, torch.float16: _F16, torch.bfloat16: _BF16}
+_OUT_DTYPE = {**_DTYPE, torch.int32: _I32}
+_ACT = {"silu": 0, "gelu_tanh": 1}
+
+_ROW_CODES = struct.Struct("=QqQQqi4x")            # aqd_row_codes
+_RMS_NORM = struct.Struct("=qiiQqQqQqQif")         # aqd_rms_norm_args
+_GATED_ACT = struct.Struct("=qiiQqQqi4x")           # aqd_gated_act_args
+_LINEAR_W = struct.Struct("=QQii")                 # aqd_linear_weights
+_LINEAR = struct.Struct("=qQqQQQqi4x")             # aqd_linear_args
+_DISTILL = struct.Struct("=qiiQqQQifQQq")          # aqd_distill_args
+
+
+class RowCodes(NamedTuple):
+    """Rows of 8-bit codes: codes int8 [..., cols], scales float32 [...], values (code x scale, or None) and,
+    from rms_norm_quant with a residual, the sum of x and the residual."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    values: torch.Tensor | None = None
+    summed: torch.Tensor | None = None
+
+
+def _rows_of(t: torch.Tensor, name: str, device=None):
+    """(rows, columns, row stride) of a CUDA tensor's last dimension, the others taken together; ValueError where
+    its rows are not evenly strided or their elements not adjacent."""
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name} must be a CUDA tensor on the call's device")
+    shape, nd = t.shape, t.dim()
+    if nd == 2:
+        m, c = shape
+        ld, last = t.stride()
+    elif nd == 1:
+        m, c, ld, last = 1, shape[0], shape[0], t.stride(0)
+    elif nd == 0:
+        raise ValueError(f"{name} needs at least one dimension")
+    else:
+        m, c = t.numel() // max(shape[-1], 1), shape[-1]
+        st = t.stride()
+        ld, last = st[-2], st[-1]
+        n = shape[-2]
+        for i in range(nd - 3, -1, -1):
+            if shape[i] > 1 and n > 1 and st[i] != n * ld:
+                raise ValueError(f"the rows of {name} are not evenly strided")
+            if n <= 1 and shape[i] > 1:
+                ld = st[i]
+            n *= shape[i]
+    if c < 1:
+        raise ValueError(f"{name} has no columns")
+    if last != 1 and c > 1:
+        raise ValueError(f"the elements of a row of {name} must be adjacent")
+    return m, c, (ld if m > 1 else max(ld, c))
+
+
+def _float_dtype(t: torch.Tensor, name: str) -> int:
+    d = _DTYPE.get(t.dtype)
+    if d is None:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16, got {t.dtype}")
+    return d
+
+
+def _vector(t: torch.Tensor, n: int, dtype, name: str, device) -> int:
+    """The address of a contiguous CUDA vector of n values."""
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} values on the call's device")
+    return t.data_ptr()
+
+
+def _new(shape, dtype, device, stream):
+    """A new tensor that belongs to the call's stream: memory that another stream may still be using is not written."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _row_codes_out(like: torch.Tensor, cols: int, codes: bool, values, dtype, stream):
+    """New outputs of a quantizer for rows shaped like `like`, and their aqd_row_codes."""
+    dev, shape = like.device, like.shape
+    c = _new(shape, torch.int8, dev, stream) if codes else None
+    s = _new(shape[:-1], torch.float32, dev, stream)
+    v, vd = None, 0
+    if values is not None and values is not False:
+        vt = dtype if values is True else values
+        vd = _DTYPE.get(vt)
+        if vd is None:
+            raise ValueError(f"values must be a bool, float32, float16 or bfloat16, got {values}")
+        v = _new(shape, vt, dev, stream)
+    elif not codes:
+        raise ValueError("at least one of codes and values is wanted")
+    return c, s, v, _ROW_CODES.pack(0 if c is None else c.data_ptr(), cols, s.data_ptr(),
+                                    0 if v is None else v.data_ptr(), cols, vd)
+
+
+def quant_rows(x: torch.Tensor, *, codes: bool = True, values=False, stream=None) -> RowCodes:
+    """8-bit codes of x's rows (its last dimension), one scale per row (aqd_quant_rows). values: True, or a type,
+    for the values that the codes stand for too."""
+    m, c, ld = _rows_of(x, "x")
+    d = _float_dtype(x, "x")
+    q, s, v, out = _row_codes_out(x, c, codes, values, x.dtype, stream)
+    _check(_calls().aqd_quant_rows(m, c, x.data_ptr(), ld, d, out, _stream(stream)), "aqd_quant_rows")
+    return RowCodes(q, s, v)
+
+
+def rms_norm_quant(x: torch.Tensor, weight: torch.Tensor, *, eps: float = 1e-6, residual: torch.Tensor | None = None,
+                   summed: torch.Tensor | None = None, codes: bool = True, values=False, stream=None) -> RowCodes:
+    """8-bit codes of rms_norm(x + residual) * weight (aqd_rms_norm_quant), one scale per row. With a residual the
+    sum comes back too, in `summed` where that is given (x or residual itself: in place)."""
+    m, c, ld = _rows_of(x, "x")
+    d = _float_dtype(x, "x")
+    dev = x.device
+    rp = rl = sp = sl = 0
+    if residual is not None:
+        if residual.shape != x.shape or residual.dtype != x.dtype:
+            raise ValueError("residual must have x's shape and type")
+        rl = _rows_of(residual, "residual", dev)[2]
+        rp = residual.data_ptr()
+        if summed is None:
+            summed = _new(x.shape, x.dtype, dev, stream)
+    if summed is not None:
+        if summed.shape != x.shape or summed.dtype != x.dtype:
+            raise ValueError("summed must have x's shape and type")
+        sl = _rows_of(summed, "summed", dev)[2]
+        sp = summed.data_ptr()
+    wd = _float_dtype(weight, "weight")
+    wp = _vector(weight, c, weight.dtype, "weight", dev)
+    q, s, v, out = _row_codes_out(x, c, codes, values, x.dtype, stream)
+    args = _RMS_NORM.pack(m, c, d, x.data_ptr(), ld, rp, rl, sp, sl, wp, wd, eps)
+    _check(_calls().aqd_rms_norm_quant(args, out, _stream(stream)), "aqd_rms_norm_quant")
+    return RowCodes(q, s, v, summed)
+
+
+def gated_act_quant(gate: torch.Tensor, up: torch.Tensor, *, act: str = "silu", codes: bool = True, values=False,
+                    stream=None) -> RowCodes:
+    """8-bit codes of act(gate) * up (aqd_gated_act_quant), one scale per row; act: "silu" or "gelu_tanh"."""
+    m, c, lg = _rows_of(gate, "gate")
+    d = _float_dtype(gate, "gate")
+    if up.shape != gate.shape or up.dtype != gate.dtype:
+        raise ValueError("up must have gate's shape and type")
+    lu = _rows_of(up, "up", gate.device)[2]
+    if act not in _ACT:
+        raise ValueError(f"act must be one of {sorted(_ACT)}, got {act!r}")
+    q, s, v, out = _row_codes_out(gate, c, codes, values, gate.dtype, stream)
+    args = _GATED_ACT.pack(m, c, d, gate.data_ptr(), lg, up.data_ptr(), lu, _ACT[act])
+    _check(_calls().aqd_gated_act_quant(args, out, _stream(stream)), "aqd_gated_act_quant")
+    return RowCodes(q, s, v)
+
+
+class LinearWeights:
+    """Prepared weights of an 8-bit layer: codes int8 [n, k] and a float32 scale per output channel (the scales are
+    read by every call, so a program may train them in place)."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, stream=None):
+        if codes.dim() != 2 or codes.dtype != torch.int8:
+            raise ValueError("codes must be an int8 matrix [n, k]")
+        n, k, ld = _rows_of(codes, "codes")
+        sp = _vector(scales, n, torch.float32, "scales", codes.device)
+        nbytes = int(_calls().aqd_linear_weights_bytes(n, k))
+        if nbytes == 0:
+            raise ValueError(f"unsupported weight shape {n} x {k}")
+        buf = _new(nbytes + 256, torch.uint8, codes.device, stream)
+        off = (-buf.data_ptr()) % 256
+        self.prepared = buf[off:off + nbytes]
+        self.n, self.k, self.scales, self.device = n, k, scales, codes.device
+        self.desc = _LINEAR_W.pack(self.prepared.data_ptr(), sp, n, k)
+        _check(_calls().aqd_linear_prepare_weights(codes.data_ptr(), ld, self.desc, self.prepared.data_ptr(), nbytes,
+                                                   _stream(stream)), "aqd_linear_prepare_weights")
+        self._codes = codes if stream is not None else None  # kept alive until that stream has consumed it
+
+    @classmethod
+    def from_float(cls, w: torch.Tensor, stream=None) -> "LinearWeights":
+        """Weights [n, k] in floating point, each output channel by its own largest magnitude."""
+        q = quant_rows(w, stream=stream)
+        return cls(q.codes, q.scales, stream=stream)
+
+
+def linear_workspace(m: int, w: LinearWeights) -> torch.Tensor | None:
+    """A workspace for linear_int8 with up to m tokens, zeroed as its first use needs; None where it needs none."""
+    n = int(_calls().aqd_linear_workspace_bytes(m, w.desc))
+    if n == 0:
+        return None
+    buf = torch.zeros(n + 256, dtype=torch.uint8, device=w.device)
+    off = (-buf.data_ptr()) % 256
+    return buf[off:off + n]
+
+
+def linear_int8(x: torch.Tensor, x_scale: torch.Tensor | None, w: LinearWeights, *, bias: torch.Tensor | None = None,
+                out: torch.Tensor | None = None, out_dtype=torch.bfloat16, workspace: torch.Tensor | None = None,
+                stream=None) -> torch.Tensor:
+    """x (int8 codes [..., k], one scale per row) times w's codes, scaled per token and channel (aqd_linear_int8).
+    out_dtype torch.int32: the integer sums. workspace: linear_workspace(m, w), which calls that may overlap in time must
+    not share."""
+    if x.dtype != torch.int8:
+        raise ValueError("x must hold int8 codes")
+    m, k, ld = _rows_of(x, "x", w.device)
+    if k != w.k:
+        raise ValueError(f"x has {k} columns, the weights {w.k}")
+    dev = x.device
+    if out is None:
+        out = _new((*x.shape[:-1], w.n), out_dtype, dev, stream)
+        ldy = w.n
+    else:
+        if out.shape != (*x.shape[:-1], w.n):
+            raise ValueError("out must have x's shape but for the last dimension, n")
+        ldy = _rows_of(out, "out", dev)[2]
+    yd = _OUT_DTYPE.get(out.dtype)
+    if yd is None:
+        raise ValueError(f"out must be float32, float16, bfloat16 or int32, got {out.dtype}")
+    xs = bp = 0
+    if yd != _I32:
+        if x_scale is None:
+            raise ValueError("x_scale is required")
+        xs = _vector(x_scale, m, torch.float32, "x_scale", dev)
+        if bias is not None:
+            bp = _vector(bias, w.n, torch.float32, "bias", dev)
+    wsp, wsb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    args = _LINEAR.pack(m, x.data_ptr(), ld, xs, bp, out.data_ptr(), ldy, yd)
+    _check(_calls().aqd_linear_int8(args, w.desc, wsp, wsb, _stream(stream)), "aqd_linear_int8")
+    return out
+
+
+class DistillLoss(NamedTuple):
+    loss: torch.Tensor
+    lse: torch.Tensor
+    grad: torch.Tensor | None = None
+
+
+def _distill_args(logits, index, teacher, row_weight, tau, grad):
+    m, v, ld = _rows_of(logits, "logits")
+    d = _float_dtype(logits, "logits")
+    dev = logits.device
+    top = teacher.shape[-1] if teacher.dim() else 0
+    if index.shape != teacher.shape or index.shape[:-1] != logits.shape[:-1]:
+        raise ValueError("index and teacher must have the logits' shape but for the last dimension")
+    ip = _vector(index, m * top, torch.int64, "index", dev)
+    tp = _vector(teacher, m * top, torch.float32, "teacher", dev)
+    wp = 0 if row_weight is None else _vector(row_weight, m, torch.float32, "row_weight", dev)
+    gp = lg = 0
+    if grad is not None:
+        if grad.shape != logits.shape or grad.dtype != logits.dtype:
+            raise ValueError("grad must have the logits' shape and type")
+        lg = _rows_of(grad, "grad", dev)[2]
+        gp = grad.data_ptr()
+    return m, _DISTILL.pack(m, v, d, logits.data_ptr(), ld, ip, tp, top, tau, wp, gp, lg)
+
+
+def distill_topk(logits: torch.Tensor, index: torch.Tensor, teacher: torch.Tensor, *, tau: float = 1.0,
+                 row_weight: torch.Tensor | None = None, grad: bool | torch.Tensor = False, stream=None) -> DistillLoss:
+    """The distillation loss of each token of logits [..., vocab] against a teacher's top logits (aqd_distill_topk):
+    teacher float32 [..., top] at the vocabulary places index int64 [..., top]. grad: True, or a tensor (the logits
+    themselves: in place), for the gradient of the losses' sum in the same pass."""
+    g = _new(logits.shape, logits.dtype, logits.device, stream) if grad is True else None if grad is False else grad
+    _, args = _distill_args(logits, index, teacher, row_weight, tau, g)
+    loss = _new(logits.shape[:-1], torch.float32, logits.device, stream)
+    lse = _new(logits.shape[:-1], torch.float32, logits.device, stream)
+    _check(_calls().aqd_distill_topk(args, loss.data_ptr(), lse.data_ptr(), _stream(stream)), "aqd_distill_topk")
+    return DistillLoss(loss, lse, g)
+
+
+def distill_topk_backward(logits: torch.Tensor, index: torch.Tensor, teacher: torch.Tensor, lse: torch.Tensor,
+                          row_weight: torch.Tensor | None = None, *, tau: float = 1.0,
+                          grad: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The gradient of distill_topk's losses from the lse that it returned; row_weight: the factor of each token's
+    gradient."""
+    g = _new(logits.shape, logits.dtype, logits.device, stream) if grad is None else grad
+    m, args = _distill_args(logits, index, teacher, row_weight, tau, g)
+    lp = _vector(lse, m, torch.float32, "lse", logits.device)
+    _check(_calls().aqd_distill_topk_backward(args, lp, _stream(stream)), "aqd_distill_topk_backward")
+    return g
 
 
 def device_status(stream=None) -> int:

@@ -886,6 +886,206 @@ aqd_status aqd_bn_level_stats(const float* const* z, const int64_t* pixels, int3
   return st ? fail((aqd_status)st, err) : AQD_OK;
 }
 
+// ---------------------------------------------------------------- 8-bit language-model operators
+
+// Bytes of one element of a floating type, or 0 for any other value.
+static int float_bytes(int32_t dtype) { return dtype == AQD_F32 ? 4 : (dtype == AQD_F16 || dtype == AQD_BF16 ? 2 : 0); }
+static bool misaligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
+
+// What is wrong with the quantizers' common arguments, or NULL; fills the output half of r.
+static const char* row_codes_fault(int64_t rows, int32_t cols, const aqd_row_codes* out, RowArgs* r) {
+  if (rows < 0 || rows > INT_MAX) return "rows must be in [0, 2^31)";
+  if (cols < 1) return "cols must be >= 1";
+  if (!out) return "out is NULL";
+  if (rows > 0 && !out->codes && !out->values) return "at least one of codes and values is required";
+  if (out->codes && out->ld_codes < cols) return "ld_codes < cols";
+  const int vb = out->values ? float_bytes(out->values_dtype) : 1;
+  if (vb == 0) return "values_dtype must be AQD_F32, AQD_F16 or AQD_BF16";
+  if (out->values && out->ld_values < cols) return "ld_values < cols";
+  if (out->values && misaligned(out->values, vb)) return "values must be aligned to its type";
+  if (rows > 0 && !out->scales) return "scales is NULL";
+  if (misaligned(out->scales, 4)) return "scales must be 4-byte aligned";
+  r->rows = rows; r->cols = cols;
+  r->codes = out->codes; r->ld_codes = out->ld_codes; r->scales = out->scales;
+  r->values = out->values; r->ld_values = out->ld_values; r->values_dtype = out->values_dtype;
+  return nullptr;
+}
+// An input matrix of a floating type.
+static const char* input_fault(const void* p, int64_t ld, int32_t dtype) {
+  const int b = float_bytes(dtype);
+  if (b == 0) return "dtype must be AQD_F32, AQD_F16 or AQD_BF16";
+  if (!p) return "an input is NULL";
+  if (ld < 0) return "an input's row stride is negative";
+  if (misaligned(p, b)) return "an input is not aligned to its type";
+  return nullptr;
+}
+static aqd_status run_rows(RowOp op, const RowArgs& r, aqd_stream_t stream) {
+  if (r.rows == 0) return AQD_OK;
+  std::string err;
+  const int st = launch_rows(op, r, static_cast<cudaStream_t>(stream), &err);
+  return st ? fail((aqd_status)st, err) : AQD_OK;
+}
+
+aqd_status aqd_quant_rows(int64_t rows, int32_t cols, const void* x, int64_t ldx, int32_t dtype,
+                          const aqd_row_codes* out, aqd_stream_t stream) {
+  RowArgs r{};
+  const char* f = row_codes_fault(rows, cols, out, &r);
+  if (!f && rows > 0) f = input_fault(x, ldx, dtype);
+  if (f) return fail(AQD_ERR_INVALID, f);
+  r.a = x; r.lda = ldx; r.dtype = dtype;
+  return run_rows(kRowPlain, r, stream);
+}
+
+aqd_status aqd_rms_norm_quant(const aqd_rms_norm_args* n, const aqd_row_codes* out, aqd_stream_t stream) {
+  if (!n) return fail(AQD_ERR_INVALID, "args is NULL");
+  RowArgs r{};
+  const char* f = row_codes_fault(n->rows, n->cols, out, &r);
+  if (!f && n->rows > 0) {
+    f = input_fault(n->x, n->ldx, n->dtype);
+    if (!f && n->residual) f = input_fault(n->residual, n->ld_residual, n->dtype);
+    if (!f) f = input_fault(n->weight, 0, n->weight_dtype);
+    if (!f && n->sum && misaligned(n->sum, float_bytes(n->dtype))) f = "sum must be aligned to its type";
+  }
+  if (!f && n->sum && n->ld_sum < n->cols) f = "ld_sum < cols";
+  if (!f && n->sum && ((n->sum == n->x && n->ld_sum != n->ldx) || (n->sum == n->residual && n->ld_sum != n->ld_residual)))
+    f = "sum in place needs its input's row stride";
+  if (!f && !(n->eps >= 0.0f && std::isfinite(n->eps))) f = "eps must be finite and >= 0";
+  if (f) return fail(AQD_ERR_INVALID, f);
+  r.a = n->x; r.lda = n->ldx; r.dtype = n->dtype;
+  r.b = n->residual; r.ldb = n->ld_residual;
+  r.sum = n->sum; r.ld_sum = n->ld_sum;
+  r.weight = n->weight; r.weight_dtype = n->weight_dtype; r.eps = n->eps;
+  return run_rows(kRowNorm, r, stream);
+}
+
+aqd_status aqd_gated_act_quant(const aqd_gated_act_args* g, const aqd_row_codes* out, aqd_stream_t stream) {
+  if (!g) return fail(AQD_ERR_INVALID, "args is NULL");
+  RowArgs r{};
+  const char* f = row_codes_fault(g->rows, g->cols, out, &r);
+  if (!f && g->rows > 0) {
+    f = input_fault(g->gate, g->ld_gate, g->dtype);
+    if (!f) f = input_fault(g->up, g->ld_up, g->dtype);
+  }
+  if (!f && g->act != AQD_ACT_SILU && g->act != AQD_ACT_GELU_TANH) f = "unknown act";
+  if (f) return fail(AQD_ERR_INVALID, f);
+  r.a = g->gate; r.lda = g->ld_gate; r.b = g->up; r.ldb = g->ld_up; r.dtype = g->dtype; r.act = g->act;
+  return run_rows(kRowGated, r, stream);
+}
+
+size_t aqd_linear_weights_bytes(int32_t n, int32_t k) {
+  if (n < 1 || k < 1 || k > 131071) return 0;
+  const int64_t bytes = (int64_t)kLinHeader + (int64_t)n * lin_pitch(k);
+  return bytes <= (1LL << 40) ? (size_t)bytes : 0;
+}
+
+static const char* linear_fault(const aqd_linear_weights* w) {
+  if (!w) return "weights descriptor is NULL";
+  if (aqd_linear_weights_bytes(w->n, w->k) == 0) return "unsupported weight shape";
+  return nullptr;
+}
+
+aqd_status aqd_linear_prepare_weights(const int8_t* codes, int64_t ld, const aqd_linear_weights* w, void* prepared,
+                                      size_t bytes, aqd_stream_t stream) {
+  const char* f = linear_fault(w);
+  if (!f && (!codes || !prepared)) f = "null pointer";
+  if (!f && ld < 0) f = "ld < 0";
+  if (!f && misaligned(prepared, 256)) f = "prepared must be 256-byte aligned";
+  if (!f && bytes < aqd_linear_weights_bytes(w->n, w->k)) f = "prepared buffer too small";
+  if (f) return fail(AQD_ERR_INVALID, f);
+  std::string err;
+  const int st = launch_linear_prepare(codes, ld, w->n, w->k, static_cast<uint8_t*>(prepared),
+                                       static_cast<cudaStream_t>(stream), &err);
+  return st ? fail((aqd_status)st, err) : AQD_OK;
+}
+
+size_t aqd_linear_workspace_bytes(int64_t m, const aqd_linear_weights* w) {
+  if (linear_fault(w) || m < 0 || m > INT_MAX) return 0;
+  return linear_workspace_bytes(m, w->n, w->k);
+}
+
+aqd_status aqd_linear_int8(const aqd_linear_args* l, const aqd_linear_weights* w, void* workspace, size_t ws_bytes,
+                           aqd_stream_t stream) {
+  const char* f = linear_fault(w);
+  if (!f && !l) f = "args is NULL";
+  if (!f && (l->m < 0 || l->m > INT_MAX)) f = "m must be in [0, 2^31)";
+  if (!f && l->y_dtype != AQD_I32 && float_bytes(l->y_dtype) == 0) f = "y_dtype must be AQD_F32, AQD_F16, AQD_BF16 or AQD_I32";
+  if (!f && l->ldx < 0) f = "ldx < 0";
+  if (!f && l->ldy < w->n) f = "ldy < n";
+  if (!f && misaligned(workspace, 256)) f = "workspace must be 256-byte aligned";
+  if (!f && l->m > 0) {
+    if (!w->data || misaligned(w->data, 256)) f = "weights data must be a 256-byte aligned device pointer";
+    else if (!l->x || !l->y) f = "x or y is NULL";
+    else if (misaligned(l->y, l->y_dtype == AQD_I32 ? 4 : float_bytes(l->y_dtype))) f = "y must be aligned to its type";
+    else if (l->y_dtype != AQD_I32 && (!l->x_scale || !w->scales)) f = "x_scale and the weights' scales are required";
+    else if (misaligned(l->x_scale, 4) || misaligned(w->scales, 4) || misaligned(l->bias, 4))
+      f = "x_scale, scales and bias must be 4-byte aligned";
+  }
+  if (f) return fail(AQD_ERR_INVALID, f);
+  if (l->m == 0) return AQD_OK;
+  std::string err;
+  LinArgs a{};
+  a.m = l->m; a.n = w->n; a.k = w->k;
+  a.x = l->x; a.ldx = l->ldx; a.x_scale = l->x_scale;
+  a.w = static_cast<const uint8_t*>(w->data); a.w_scale = w->scales;
+  a.bias = l->y_dtype == AQD_I32 ? nullptr : l->bias;
+  a.y = l->y; a.ldy = l->ldy; a.y_dtype = l->y_dtype;
+  a.ws = static_cast<uint8_t*>(workspace); a.ws_bytes = workspace ? ws_bytes : 0;
+  a.status = status_ptr(&err);
+  if (!a.status) return fail(AQD_ERR_CUDA, err);
+  const int st = launch_linear(a, static_cast<cudaStream_t>(stream), &err);
+  return st ? fail((aqd_status)st, err) : AQD_OK;
+}
+
+// What is wrong with a distillation call, or NULL; fills a.
+static const char* distill_fault(const aqd_distill_args* d, DistillArgs* a) {
+  if (!d) return "args is NULL";
+  if (d->tokens < 0 || d->tokens > INT_MAX) return "tokens must be in [0, 2^31)";
+  if (d->vocab < 1) return "vocab must be >= 1";
+  const int b = float_bytes(d->dtype);
+  if (b == 0) return "dtype must be AQD_F32, AQD_F16 or AQD_BF16";
+  if (d->top < 1 || d->top > 1024) return "top must be in [1, 1024]";
+  if (!(d->tau > 0.0f) || !std::isfinite(d->tau) || !std::isfinite(1.0f / d->tau)) return "tau must be positive and finite";
+  if (d->grad && d->ld_grad < d->vocab) return "ld_grad < vocab";
+  if (d->grad && d->grad == d->logits && d->ld_grad != d->ld_logits) return "grad in place needs the logits' row stride";
+  if (d->tokens > 0) {
+    if (const char* f = input_fault(d->logits, d->ld_logits, d->dtype)) return f;
+    if (!d->index || !d->teacher) return "index and teacher are required";
+    if (misaligned(d->index, 8)) return "index must be 8-byte aligned";
+    if (misaligned(d->teacher, 4) || misaligned(d->row_weight, 4)) return "teacher and row_weight must be 4-byte aligned";
+    if (d->grad && misaligned(d->grad, b)) return "grad must be aligned to its type";
+  }
+  a->tokens = d->tokens; a->vocab = d->vocab; a->dtype = d->dtype; a->top = d->top;
+  a->logits = d->logits; a->ld_logits = d->ld_logits; a->index = d->index; a->teacher = d->teacher;
+  a->tau = d->tau; a->row_weight = d->row_weight; a->grad = d->grad; a->ld_grad = d->ld_grad;
+  return nullptr;
+}
+
+aqd_status aqd_distill_topk(const aqd_distill_args* args, float* loss, float* lse, aqd_stream_t stream) {
+  DistillArgs a{};
+  const char* f = distill_fault(args, &a);
+  if (!f && args->tokens > 0 && !loss && !lse && !args->grad) f = "at least one of loss, lse and grad is required";
+  if (!f && (misaligned(loss, 4) || misaligned(lse, 4))) f = "loss and lse must be 4-byte aligned";
+  if (f) return fail(AQD_ERR_INVALID, f);
+  if (a.tokens == 0) return AQD_OK;
+  a.loss = loss; a.lse = lse;
+  std::string err;
+  const int st = launch_distill(a, static_cast<cudaStream_t>(stream), &err);
+  return st ? fail((aqd_status)st, err) : AQD_OK;
+}
+
+aqd_status aqd_distill_topk_backward(const aqd_distill_args* args, const float* lse, aqd_stream_t stream) {
+  DistillArgs a{};
+  const char* f = distill_fault(args, &a);
+  if (!f && args->tokens > 0 && (!lse || !args->grad)) f = "lse and grad are required";
+  if (!f && misaligned(lse, 4)) f = "lse must be 4-byte aligned";
+  if (f) return fail(AQD_ERR_INVALID, f);
+  if (a.tokens == 0) return AQD_OK;
+  a.lse_in = lse;
+  std::string err;
+  const int st = launch_distill(a, static_cast<cudaStream_t>(stream), &err);
+  return st ? fail((aqd_status)st, err) : AQD_OK;
+}
+
 }  // extern "C"
 
 // ---------------------------------------------------------------- static workspace

@@ -173,6 +173,68 @@ int bn_stats_blocks(int32_t levels);
 int launch_bn_level_stats(const float* const* z, const int64_t* pixels, int32_t levels, int32_t c, double* mean,
                           double* var, double* work, cudaStream_t stream, std::string* err);
 
+// 8-bit language-model operators (lm_rows.cu, lm_linear.cu) and distillation (lm_distill.cu); types are AQD_F32 etc.
+struct RowArgs {
+  int64_t rows;
+  int32_t cols, dtype;
+  const void *a, *b;      // x and residual; gate and up; x and NULL
+  int64_t lda, ldb;
+  void* sum;              // norm: h, or NULL
+  int64_t ld_sum;
+  const void* weight;     // norm
+  int32_t weight_dtype;
+  float eps;
+  int32_t act;            // gated: AQD_ACT_*
+  int8_t* codes;
+  int64_t ld_codes;
+  float* scales;
+  void* values;
+  int64_t ld_values;
+  int32_t values_dtype;
+};
+enum RowOp { kRowPlain = 0, kRowNorm = 1, kRowGated = 2 };
+int launch_rows(RowOp op, const RowArgs& a, cudaStream_t stream, std::string* err);
+
+// Prepared weights: a header (kLinHeader bytes), then n rows of lin_pitch(k) bytes, zero past k.
+constexpr size_t kLinHeader = 256;
+inline int64_t lin_pitch(int32_t k) { return ((int64_t)k + 127) / 128 * 128; }
+struct LinArgs {
+  int64_t m;
+  int32_t n, k;
+  const int8_t* x;
+  int64_t ldx;
+  const float* x_scale;
+  const uint8_t* w;       // prepared weights
+  const float* w_scale;
+  const float* bias;
+  void* y;
+  int64_t ldy;
+  int32_t y_dtype;
+  uint8_t* ws;
+  size_t ws_bytes;
+  uint32_t* status;
+};
+int launch_linear_prepare(const int8_t* codes, int64_t ld, int32_t n, int32_t k, uint8_t* out, cudaStream_t stream,
+                          std::string* err);
+size_t linear_workspace_bytes(int64_t m, int32_t n, int32_t k);
+int launch_linear(const LinArgs& a, cudaStream_t stream, std::string* err);
+
+struct DistillArgs {
+  int64_t tokens;
+  int32_t vocab, dtype, top;
+  const void* logits;
+  int64_t ld_logits;
+  const int64_t* index;
+  const float* teacher;
+  float tau;
+  const float* row_weight;
+  void* grad;
+  int64_t ld_grad;
+  float *loss, *lse;        // forward
+  const float* lse_in;      // backward
+};
+int launch_distill(const DistillArgs& a, cudaStream_t stream, std::string* err);
+
 // the bounded-wait self-test (selftest.cu): out receives 5 int64 values
 int launch_wait_selftest(uint32_t* status, int64_t* out, cudaStream_t stream, std::string* err);
 
