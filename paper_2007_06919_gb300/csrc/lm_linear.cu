@@ -12,14 +12,44 @@
 namespace aqd {
 namespace lin {
 
-__global__ void prepare_kernel(const int8_t* __restrict__ codes, int64_t ld, int32_t n, int32_t k, int64_t pitch,
-                               uint8_t* __restrict__ out) {
-  const int64_t total = (int64_t)n * pitch;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
-    const int64_t row = i / pitch;
-    const int64_t c = i - row * pitch;
-    out[kLinHeader + i] = c < k ? (uint8_t)codes[row * ld + c] : 0;
+// Rows of k codes plus 128, as bytes (what the conversion to F16 starts from), padded with code 0 to whole chunks of
+// 128; and the header's first word, the most chunks in a row that any row of weights lets an FP32 accumulator sum exactly:
+// those of every window of that length have sum |w| * 128 <= 2^24. (8 chunks always do.) One warp per row.
+__global__ void __launch_bounds__(128) prepare_kernel(const int8_t* __restrict__ codes, int64_t ld, int32_t n, int32_t k,
+                                                      int64_t pitch, uint8_t* __restrict__ out) {
+  __shared__ uint16_t sums[4][1024];  // sum |w| of each chunk (at most 128 * 128)
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int chunks = (int)(pitch / 128);
+  int most = chunks;
+  for (int64_t row = (int64_t)blockIdx.x * 4 + warp; row < n; row += (int64_t)gridDim.x * 4) {
+    for (int c = 0; c < chunks; ++c) {
+      uint32_t word = 0;
+      int s = 0;
+      for (int j = 0; j < 4; ++j) {
+        const int i = c * 128 + lane * 4 + j;
+        const int w = i < k ? codes[row * ld + i] : 0;
+        s += w < 0 ? -w : w;
+        word |= (uint32_t)(uint8_t)(w + 128) << (8 * j);
+      }
+      *reinterpret_cast<uint32_t*>(out + kLinHeader + row * pitch + c * 128 + lane * 4) = word;
+      s = __reduce_add_sync(0xffffffffu, s);
+      if (lane == 0) sums[warp][c] = (uint16_t)s;
+    }
+    __syncwarp();
+    if (lane == 0) {  // windows (lo, hi]: each hi's longest with a sum in range; the shortest of those that could not grow
+      int lo = 0, sum = 0;
+      for (int hi = 0; hi < chunks; ++hi) {
+        sum += sums[warp][hi];
+        while (sum > 131072) {
+          sum -= sums[warp][lo++];
+          const int len = hi - lo + 1;
+          if (len < most) most = len;
+        }
+      }
+    }
+    __syncwarp();
   }
+  if (lane == 0) atomicMin(reinterpret_cast<int*>(out), most);
 }
 
 __device__ __forceinline__ void store_y(const LinArgs& p, int64_t m, int n, int acc) {
@@ -53,7 +83,7 @@ __global__ void __launch_bounds__(256) linear_direct_kernel(const LinArgs p) {
     }
     for (int i = threadIdx.x; i < kTN * kTK / 4; i += 256) {
       const int r = i / (kTK / 4), c = i % (kTK / 4);
-      sw[r][c] = n0 + r < p.n ? *reinterpret_cast<const int*>(p.w + kLinHeader + (n0 + r) * pitch + k0 + 4 * c) : 0;
+      sw[r][c] = n0 + r < p.n ? (int)(*reinterpret_cast<const uint32_t*>(p.w + kLinHeader + (n0 + r) * pitch + k0 + 4 * c) ^ 0x80808080u) : 0;
     }
     __syncthreads();
 #pragma unroll
@@ -87,13 +117,16 @@ static int launched(const char* what, std::string* err) {
 
 int launch_linear_prepare(const int8_t* codes, int64_t ld, int32_t n, int32_t k, uint8_t* out, cudaStream_t stream,
                           std::string* err) {
-  lin::prepare_kernel<<<1216, 256, 0, stream>>>(codes, ld, n, k, lin_pitch(k), out);
+  const cudaError_t e = cudaMemsetAsync(out, 0x7f, 4, stream);
+  if (e != cudaSuccess) { *err = std::string("weight preparation: ") + cudaGetErrorString(e); return AQD_ERR_CUDA; }
+  lin::prepare_kernel<<<n < 4864 ? (n + 3) / 4 : 1216, 128, 0, stream>>>(codes, ld, n, k, lin_pitch(k), out);
   return launched("weight preparation launch: ", err);
 }
 
-size_t linear_workspace_bytes(int64_t m, int32_t n, int32_t k) { return 0; }
+size_t linear_workspace_bytes(int64_t m, int32_t n, int32_t k) { return linear_tc_workspace_bytes(m, n); }
 
 int launch_linear(const LinArgs& a, cudaStream_t stream, std::string* err) {
+  if (a.m > 8 && linear_tc_takes(a)) return launch_linear_tc(a, stream, err);
   // rows of blocks in pieces of the grid's second dimension
   constexpr int64_t kRows = 65535LL * lin::kTM;
   const size_t es = a.y_dtype == AQD_F32 || a.y_dtype == AQD_I32 ? 4 : 2;
