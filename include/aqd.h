@@ -435,9 +435,9 @@ aqd_status aqd_linear_prepare_weights(const int8_t* codes, int64_t ld, const aqd
  * converted to float32 once, then the products in this order and the addition in float32, rounded once to y_dtype. bias (float32) may be
  * NULL. With y_dtype AQD_I32, y receives the integer sums and x_scale, the weights' scales and bias are not read.
  * x: int8 codes, any ldx >= 0. workspace: aqd_linear_workspace_bytes(m, w) bytes or more, 256-byte aligned,
- * or NULL; it must be zeroed once before its first use, and calls that share it must not overlap in time.
- * Results are identical with and without it: it lets a product with few output tiles split its sums over k, and
- * copies codes whose rows are not 16-byte aligned. */
+ * or NULL; its contents do not matter, and calls that share it must not overlap in time. Results are identical with
+ * and without it: with more than 64 tokens, or rows of codes that are not 16-byte aligned, it holds the codes as the tensor cores read
+ * them and the sums of tiles that several blocks share, and a call without it runs on slower kernels. */
 typedef struct {
   int64_t m;
   const int8_t* x;

@@ -785,11 +785,11 @@ class LinearWeights:
 
 
 def linear_workspace(m: int, w: LinearWeights) -> torch.Tensor | None:
-    """A workspace for linear_int8 with up to m tokens, zeroed as its first use needs; None where it needs none."""
+    """A workspace for linear_int8 with up to m tokens; None where it needs none."""
     n = int(_calls().aqd_linear_workspace_bytes(m, w.desc))
     if n == 0:
         return None
-    buf = torch.zeros(n + 256, dtype=torch.uint8, device=w.device)
+    buf = torch.empty(n + 256, dtype=torch.uint8, device=w.device)
     off = (-buf.data_ptr()) % 256
     return buf[off:off + n]
 

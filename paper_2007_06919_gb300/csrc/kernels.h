@@ -218,9 +218,9 @@ int launch_linear_prepare(const int8_t* codes, int64_t ld, int32_t n, int32_t k,
                           std::string* err);
 size_t linear_workspace_bytes(int64_t m, int32_t n, int32_t k);
 int launch_linear(const LinArgs& a, cudaStream_t stream, std::string* err);
-// the tensor-core kernel: whether it takes x's rows (16-byte aligned), its workspace, its launch
-bool linear_tc_takes(const LinArgs& a);
-size_t linear_tc_workspace_bytes(int64_t m, int32_t n);
+// the tcgen05 kernel: its estimated time (us; infinite where it does not take the call), its workspace, its launch
+float linear_tc_estimate(const LinArgs& a);
+size_t linear_tc_workspace_bytes(int64_t m, int32_t k);
 int launch_linear_tc(const LinArgs& a, cudaStream_t stream, std::string* err);
 
 struct DistillArgs {

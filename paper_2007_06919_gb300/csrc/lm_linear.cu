@@ -4,10 +4,13 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <cmath>
 #include <cstdint>
 
 #include "../../include/aqd.h"
+#include "common.cuh"
 #include "kernels.h"
+#include "tc_ptx.cuh"
 
 namespace aqd {
 namespace lin {
@@ -106,6 +109,187 @@ __global__ void __launch_bounds__(256) linear_direct_kernel(const LinArgs p) {
     }
 }
 
+// ---------------------------------------------------------------- few tokens
+
+__device__ __forceinline__ uint4 ld_weights(const uint8_t* p) {  // read once: past L1
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.L2::128B.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+// Four codes with 128 added, as bytes, to F16: a byte u under the exponent byte 0x64 is 1024 + u, and 1024 + u - 1152 the code.
+__device__ __forceinline__ void bytes_to_f16(uint32_t u, uint32_t& lo, uint32_t& hi) {
+  const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(lo) : "r"(a), "r"(0x64806480u));
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(b), "r"(0x64806480u));
+}
+__device__ __forceinline__ void piece_to_f16(const uint4& v, uint32_t flip, uint32_t (&f)[8]) {
+  bytes_to_f16(v.x ^ flip, f[0], f[1]);
+  bytes_to_f16(v.y ^ flip, f[2], f[3]);
+  bytes_to_f16(v.z ^ flip, f[4], f[5]);
+  bytes_to_f16(v.w ^ flip, f[6], f[7]);
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+constexpr int kSmallWarps = 8;
+
+constexpr int small_bytes(int g, int r, int depth) {
+  const int ring = kSmallWarps * depth * (2 * r + g) * 512, part = kSmallWarps * g * 8 * (16 * r + 1) * 4;
+  return ring > part ? ring : part;
+}
+
+// Up to 8 kG tokens: bound by the weights' bytes. A block takes 16 kR channels and all tokens, and its warps take 64-K pieces
+// of the rows in turn, as operands of mma.sync. The order of K within a piece is free, so a lane's 16 adjacent codes
+// of a row are its fragments of four MMAs: each lane copies the bytes that it will itself multiply into its own places of a ring in
+// shared memory (kDepth pieces ahead, no barrier between lanes) and turns them into F16 in registers. Sums are exact in FP32 over
+// 1024 K, then add up in int32 (kLong: a warp has more than that), across warps in shared memory.
+// (Measured: loads straight into registers, a round of them at a time, 24 x 4096 x 12288 23.3 us against 18.2; weights by bulk
+// copies, the tokens' loads then waited for at each stage, 33; tokens as F16 once per block and K split
+// over a cluster, 20.)
+template <int kG, int kR, int kDepth, bool kLong>
+__global__ void __launch_bounds__(kSmallWarps * 32, 2) linear_ring_kernel(const LinArgs p) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int64_t pitch = ((int64_t)p.k + 127) / 128 * 128;
+  const int n0 = blockIdx.x * 16 * kR;
+  const int64_t m0 = (int64_t)blockIdx.y * (8 * kG);
+  constexpr int kPieces = 2 * kR + kG;
+  const uint32_t ring = tc::smem_u32(smem) + (uint32_t)warp * (kDepth * kPieces * 512) + (uint32_t)lane * 16;
+  tc::grid_dep_wait();
+  const uint8_t* w = p.w + kLinHeader + (int64_t)(n0 + g) * pitch + t * 16;
+  const int8_t* x = p.x + (m0 + g) * p.ldx + t * 16;
+  const int rows = p.n - n0 - g, tokens = (int)min((int64_t)(8 * kG), p.m - m0) - g;
+  const int blocks = (p.k + 63) / 64;
+  const int mine = (blocks - warp + kSmallWarps - 1) / kSmallWarps;  // this warp's blocks: warp, warp + 8, ...
+  auto fetch = [&](int i) {
+    if (i < mine) {
+      const int k = (warp + i * kSmallWarps) * 64;
+      const uint32_t to = ring + (uint32_t)(i % kDepth) * (kPieces * 512);
+      // (rows and tokens past the last, and codes past a row's end: zeros, from an address that is not read)
+#pragma unroll
+      for (int r = 0; r < 2 * kR; ++r) {
+        const bool in = r * 8 < rows;
+        asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;"
+                     ::"r"(to + r * 512), "l"(in ? w + (r * 8 * pitch + k) : p.w), "r"(in ? 16 : 0) : "memory");
+      }
+      const int left = p.k - k - t * 16, bytes = left < 0 ? 0 : (left < 16 ? left : 16);
+#pragma unroll
+      for (int j = 0; j < kG; ++j) {
+        const bool in = j * 8 < tokens && bytes > 0;
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;"
+                     ::"r"(to + (2 * kR + j) * 512), "l"(in ? x + (j * 8 * p.ldx + k) : p.x), "r"(in ? bytes : 0) : "memory");
+      }
+    }
+    tc::cp_async_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < kDepth - 1; ++i) fetch(i);
+  int sum[kR][kG][4];
+  float d[kR][kG][4] = {};
+  if constexpr (kLong) {
+#pragma unroll
+    for (int r = 0; r < kR; ++r)
+#pragma unroll
+      for (int j = 0; j < kG; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sum[r][j][q] = 0;
+  }
+  for (int i = 0; i < mine; ++i) {
+    tc::cp_async_wait<kDepth - 2>();
+    const uint32_t from = ring + (uint32_t)(i % kDepth) * (kPieces * 512);
+    uint32_t wf[2 * kR][8];
+#pragma unroll
+    for (int r = 0; r < 2 * kR; ++r) piece_to_f16(lds128(from + r * 512), 0u, wf[r]);
+#pragma unroll
+    for (int j = 0; j < kG; ++j) {
+      uint32_t xf[8];
+      piece_to_f16(lds128(from + (2 * kR + j) * 512), 0x80808080u, xf);
+#pragma unroll
+      for (int r = 0; r < kR; ++r)
+#pragma unroll
+        for (int q = 0; q < 8; q += 2)
+          mma_16816(d[r][j], wf[2 * r][q], wf[2 * r + 1][q], wf[2 * r][q + 1], wf[2 * r + 1][q + 1], xf[q], xf[q + 1]);
+    }
+    fetch(i + kDepth - 1);
+    if (kLong && (i & 15) == 15) {
+#pragma unroll
+      for (int r = 0; r < kR; ++r)
+#pragma unroll
+        for (int j = 0; j < kG; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) { sum[r][j][q] += __float2int_rn(d[r][j][q]); d[r][j][q] = 0.0f; }
+    }
+  }
+  __syncthreads();  // (every fetched stage has been waited for; the sums take the ring's place)
+  int* part = reinterpret_cast<int*>(smem);
+  constexpr int kRow = 16 * kR + 1, kPart = kG * 8 * kRow;
+#pragma unroll
+  for (int r = 0; r < kR; ++r)
+#pragma unroll
+    for (int i = 0; i < kG; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        part[warp * kPart + (i * 8 + 2 * t + (j & 1)) * kRow + r * 16 + g + (j >> 1) * 8] = (kLong ? sum[r][i][j] : 0) + __float2int_rn(d[r][i][j]);
+  __syncthreads();
+  for (int i = threadIdx.x; i < kG * 8 * 16 * kR; i += kSmallWarps * 32) {
+    const int c = i % (16 * kR), m = i / (16 * kR);
+    int s = 0;
+#pragma unroll
+    for (int v = 0; v < kSmallWarps; ++v) s += part[v * kPart + m * kRow + c];
+    if (m0 + m < p.m && n0 + c < p.n) store_y(p, m0 + m, n0 + c, s);
+  }
+}
+
+template <int kG, int kR, int kDepth, bool kLong>
+static cudaError_t run_ring(const LinArgs& a, cudaStream_t stream) {
+  constexpr int smem = small_bytes(kG, kR, kDepth);
+  const cudaError_t e = cudaFuncSetAttribute(linear_ring_kernel<kG, kR, kDepth, kLong>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(((int64_t)a.n + 16 * kR - 1) / (16 * kR)), (unsigned)((a.m + 8 * kG - 1) / (8 * kG)));
+  cfg.blockDim = dim3(kSmallWarps * 32);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, linear_ring_kernel<kG, kR, kDepth, kLong>, a);
+}
+
+// Time of this kernel (us) for more than 16 tokens, fitted to n 1024 .. 16384, k 1024 .. 4096: throughput of a warp's pieces, or a warp's own chain.
+static float ring_estimate(const LinArgs& a) {
+  const float k64 = (float)((a.k + 63) / 64), n = (float)a.n;
+  const float work = a.m <= 32 ? (n > 32 * 120 ? n / 32 * 0.62f : n / 16 * 0.5f) : n / 16 * 0.9f * (float)((a.m + 63) / 64);
+  return 3.0f + fmaxf(1e-3f * k64 * work, 0.05f * k64);
+}
+
+// Two row tiles a warp halve the work on the tokens' codes for each weight, and the blocks: they pay from about a block per SM on (16
+// tokens, K 4096: n 1024 2.7 us against 2.2, n 4096 6.5 against 6.8; 24 tokens, n 12288 18.2 against 22.4; one to eight tokens, n 12288 12.9
+// against 11.2: not there).
+static int launch_ring(const LinArgs& a, cudaStream_t stream, std::string* err) {
+  const bool longk = a.k > 16 * 64 * kSmallWarps, wide = a.n > 32 * 120;
+  cudaError_t e;
+  if (a.m <= 8) e = longk ? run_ring<1, 1, 4, true>(a, stream) : run_ring<1, 1, 4, false>(a, stream);
+  else if (a.m <= 16 && wide) e = longk ? run_ring<2, 2, 4, true>(a, stream) : run_ring<2, 2, 4, false>(a, stream);
+  else if (a.m <= 16) e = longk ? run_ring<2, 1, 4, true>(a, stream) : run_ring<2, 1, 4, false>(a, stream);
+  else if (a.m <= 32 && wide && !longk) e = run_ring<4, 2, 3, false>(a, stream);  // (longk would spill)
+  else if (a.m <= 32) e = longk ? run_ring<4, 1, 4, true>(a, stream) : run_ring<4, 1, 4, false>(a, stream);
+  else e = longk ? run_ring<8, 1, 3, true>(a, stream) : run_ring<8, 1, 3, false>(a, stream);
+  if (e == cudaSuccess) e = cudaGetLastError();
+  if (e != cudaSuccess) { *err = std::string("8-bit product launch: ") + cudaGetErrorString(e); return AQD_ERR_CUDA; }
+  return 0;
+}
+
 }  // namespace lin
 
 static int launched(const char* what, std::string* err) {
@@ -123,22 +307,30 @@ int launch_linear_prepare(const int8_t* codes, int64_t ld, int32_t n, int32_t k,
   return launched("weight preparation launch: ", err);
 }
 
-size_t linear_workspace_bytes(int64_t m, int32_t n, int32_t k) { return linear_tc_workspace_bytes(m, n); }
+size_t linear_workspace_bytes(int64_t m, int32_t n, int32_t k) { return linear_tc_workspace_bytes(m, k); }
 
 int launch_linear(const LinArgs& a, cudaStream_t stream, std::string* err) {
-  if (a.m > 8 && linear_tc_takes(a)) return launch_linear_tc(a, stream, err);
-  // rows of blocks in pieces of the grid's second dimension
-  constexpr int64_t kRows = 65535LL * lin::kTM;
+  const bool aligned = a.ldx % 16 == 0 && (reinterpret_cast<uintptr_t>(a.x) & 15) == 0;
+  if (aligned && a.m <= 16) return lin::launch_ring(a, stream, err);
+  const float tc = linear_tc_estimate(a);
+  if (tc < INFINITY && (!aligned || tc < lin::ring_estimate(a))) return launch_linear_tc(a, stream, err);
+  // the tokens in pieces of the grid's second dimension
+  const int64_t most = 65535LL * (aligned ? 64 : lin::kTM);
   const size_t es = a.y_dtype == AQD_F32 || a.y_dtype == AQD_I32 ? 4 : 2;
-  for (int64_t m = 0; m < a.m; m += kRows) {
+  for (int64_t m = 0; m < a.m; m += most) {
     LinArgs p = a;
-    p.m = a.m - m < kRows ? a.m - m : kRows;
+    p.m = a.m - m < most ? a.m - m : most;
     p.x += m * a.ldx;
     if (p.x_scale) p.x_scale += m;
     p.y = static_cast<uint8_t*>(p.y) + (size_t)m * a.ldy * es;
-    const dim3 grid((unsigned)((p.n + lin::kTN - 1) / lin::kTN), (unsigned)((p.m + lin::kTM - 1) / lin::kTM));
-    lin::linear_direct_kernel<<<grid, 256, 0, stream>>>(p);
-    if (const int st = launched("8-bit product launch: ", err)) return st;
+    int st = 0;
+    if (aligned) st = lin::launch_ring(p, stream, err);
+    else {
+      const dim3 grid((unsigned)(((int64_t)p.n + lin::kTN - 1) / lin::kTN), (unsigned)((p.m + lin::kTM - 1) / lin::kTM));
+      lin::linear_direct_kernel<<<grid, 256, 0, stream>>>(p);
+      st = launched("8-bit product launch: ", err);
+    }
+    if (st) return st;
   }
   return 0;
 }
