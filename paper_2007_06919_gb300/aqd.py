@@ -631,29 +631,28 @@ class RowCodes(NamedTuple):
     summed: torch.Tensor | None = None
 
 
-def _rows_of(t: torch.Tensor, name: str, device=None):
+def _rows_of(t: torch.Tensor, name: str, device: int | None = None):
     """(rows, columns, row stride) of a CUDA tensor's last dimension, the others taken together; ValueError where
-    its rows are not evenly strided or their elements not adjacent."""
-    if not t.is_cuda or (device is not None and t.device != device):
+    its rows are not evenly strided or their elements not adjacent. device: the index of the call's device."""
+    if not t.is_cuda or (device is not None and t.get_device() != device):
         raise ValueError(f"{name} must be a CUDA tensor on the call's device")
-    shape, nd = t.shape, t.dim()
-    if nd == 2:
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 2:
         m, c = shape
-        ld, last = t.stride()
-    elif nd == 1:
-        m, c, ld, last = 1, shape[0], shape[0], t.stride(0)
-    elif nd == 0:
+        ld, last = strides
+    elif len(shape) == 1:
+        m, c, ld, last = 1, shape[0], shape[0], strides[0]
+    elif not shape:
         raise ValueError(f"{name} needs at least one dimension")
     else:
-        m, c = t.numel() // max(shape[-1], 1), shape[-1]
-        st = t.stride()
-        ld, last = st[-2], st[-1]
-        n = shape[-2]
-        for i in range(nd - 3, -1, -1):
-            if shape[i] > 1 and n > 1 and st[i] != n * ld:
+        c, n = shape[-1], shape[-2]
+        m = t.numel() // max(c, 1)
+        ld, last = strides[-2], strides[-1]
+        for i in range(len(shape) - 3, -1, -1):
+            if shape[i] > 1 and n > 1 and strides[i] != n * ld:
                 raise ValueError(f"the rows of {name} are not evenly strided")
             if n <= 1 and shape[i] > 1:
-                ld = st[i]
+                ld = strides[i]
             n *= shape[i]
     if c < 1:
         raise ValueError(f"{name} has no columns")
@@ -669,37 +668,43 @@ def _float_dtype(t: torch.Tensor, name: str) -> int:
     return d
 
 
-def _vector(t: torch.Tensor, n: int, dtype, name: str, device) -> int:
+def _vector(t: torch.Tensor, n: int, dtype, name: str, device: int) -> int:
     """The address of a contiguous CUDA vector of n values."""
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != device:
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda or t.get_device() != device:
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} values on the call's device")
     return t.data_ptr()
+
+
+_empty = torch.empty
 
 
 def _new(shape, dtype, device, stream):
     """A new tensor that belongs to the call's stream: memory that another stream may still be using is not written."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _empty(shape, dtype=dtype, device=device)
 
 
-def _row_codes_out(like: torch.Tensor, cols: int, codes: bool, values, dtype, stream):
+def _row_codes_out(like: torch.Tensor, cols: int, codes: bool, values, stream):
     """New outputs of a quantizer for rows shaped like `like`, and their aqd_row_codes."""
     dev, shape = like.device, like.shape
-    c = _new(shape, torch.int8, dev, stream) if codes else None
     s = _new(shape[:-1], torch.float32, dev, stream)
-    v, vd = None, 0
-    if values is not None and values is not False:
-        vt = dtype if values is True else values
+    c = v = None
+    cp = vp = vd = 0
+    if codes:
+        c = _new(shape, torch.int8, dev, stream)
+        cp = c.data_ptr()
+    elif not values:
+        raise ValueError("at least one of codes and values is wanted")
+    if values is not False and values is not None:
+        vt = like.dtype if values is True else values
         vd = _DTYPE.get(vt)
         if vd is None:
             raise ValueError(f"values must be a bool, float32, float16 or bfloat16, got {values}")
         v = _new(shape, vt, dev, stream)
-    elif not codes:
-        raise ValueError("at least one of codes and values is wanted")
-    return c, s, v, _ROW_CODES.pack(0 if c is None else c.data_ptr(), cols, s.data_ptr(),
-                                    0 if v is None else v.data_ptr(), cols, vd)
+        vp = v.data_ptr()
+    return c, s, v, _ROW_CODES.pack(cp, cols, s.data_ptr(), vp, cols, vd)
 
 
 def quant_rows(x: torch.Tensor, *, codes: bool = True, values=False, stream=None) -> RowCodes:
@@ -707,7 +712,7 @@ def quant_rows(x: torch.Tensor, *, codes: bool = True, values=False, stream=None
     for the values that the codes stand for too."""
     m, c, ld = _rows_of(x, "x")
     d = _float_dtype(x, "x")
-    q, s, v, out = _row_codes_out(x, c, codes, values, x.dtype, stream)
+    q, s, v, out = _row_codes_out(x, c, codes, values, stream)
     _check(_calls().aqd_quant_rows(m, c, x.data_ptr(), ld, d, out, _stream(stream)), "aqd_quant_rows")
     return RowCodes(q, s, v)
 
@@ -718,23 +723,24 @@ def rms_norm_quant(x: torch.Tensor, weight: torch.Tensor, *, eps: float = 1e-6, 
     sum comes back too, in `summed` where that is given (x or residual itself: in place)."""
     m, c, ld = _rows_of(x, "x")
     d = _float_dtype(x, "x")
-    dev = x.device
+    dev = x.get_device()
     rp = rl = sp = sl = 0
     if residual is not None:
-        if residual.shape != x.shape or residual.dtype != x.dtype:
+        if residual.shape != x.shape or residual.dtype is not x.dtype:
             raise ValueError("residual must have x's shape and type")
         rl = _rows_of(residual, "residual", dev)[2]
         rp = residual.data_ptr()
         if summed is None:
-            summed = _new(x.shape, x.dtype, dev, stream)
-    if summed is not None:
-        if summed.shape != x.shape or summed.dtype != x.dtype:
+            summed = _new(x.shape, x.dtype, x.device, stream)
+            sp, sl = summed.data_ptr(), c
+    if summed is not None and not sp:
+        if summed.shape != x.shape or summed.dtype is not x.dtype:
             raise ValueError("summed must have x's shape and type")
         sl = _rows_of(summed, "summed", dev)[2]
         sp = summed.data_ptr()
     wd = _float_dtype(weight, "weight")
     wp = _vector(weight, c, weight.dtype, "weight", dev)
-    q, s, v, out = _row_codes_out(x, c, codes, values, x.dtype, stream)
+    q, s, v, out = _row_codes_out(x, c, codes, values, stream)
     args = _RMS_NORM.pack(m, c, d, x.data_ptr(), ld, rp, rl, sp, sl, wp, wd, eps)
     _check(_calls().aqd_rms_norm_quant(args, out, _stream(stream)), "aqd_rms_norm_quant")
     return RowCodes(q, s, v, summed)
@@ -745,12 +751,12 @@ def gated_act_quant(gate: torch.Tensor, up: torch.Tensor, *, act: str = "silu", 
     """8-bit codes of act(gate) * up (aqd_gated_act_quant), one scale per row; act: "silu" or "gelu_tanh"."""
     m, c, lg = _rows_of(gate, "gate")
     d = _float_dtype(gate, "gate")
-    if up.shape != gate.shape or up.dtype != gate.dtype:
+    if up.shape != gate.shape or up.dtype is not gate.dtype:
         raise ValueError("up must have gate's shape and type")
-    lu = _rows_of(up, "up", gate.device)[2]
+    lu = _rows_of(up, "up", gate.get_device())[2]
     if act not in _ACT:
         raise ValueError(f"act must be one of {sorted(_ACT)}, got {act!r}")
-    q, s, v, out = _row_codes_out(gate, c, codes, values, gate.dtype, stream)
+    q, s, v, out = _row_codes_out(gate, c, codes, values, stream)
     args = _GATED_ACT.pack(m, c, d, gate.data_ptr(), lg, up.data_ptr(), lu, _ACT[act])
     _check(_calls().aqd_gated_act_quant(args, out, _stream(stream)), "aqd_gated_act_quant")
     return RowCodes(q, s, v)
@@ -764,14 +770,14 @@ class LinearWeights:
         if codes.dim() != 2 or codes.dtype != torch.int8:
             raise ValueError("codes must be an int8 matrix [n, k]")
         n, k, ld = _rows_of(codes, "codes")
-        sp = _vector(scales, n, torch.float32, "scales", codes.device)
+        sp = _vector(scales, n, torch.float32, "scales", codes.get_device())
         nbytes = int(_calls().aqd_linear_weights_bytes(n, k))
         if nbytes == 0:
             raise ValueError(f"unsupported weight shape {n} x {k}")
         buf = _new(nbytes + 256, torch.uint8, codes.device, stream)
         off = (-buf.data_ptr()) % 256
         self.prepared = buf[off:off + nbytes]
-        self.n, self.k, self.scales, self.device = n, k, scales, codes.device
+        self.n, self.k, self.scales, self.device, self.index = n, k, scales, codes.device, codes.get_device()
         self.desc = _LINEAR_W.pack(self.prepared.data_ptr(), sp, n, k)
         _check(_calls().aqd_linear_prepare_weights(codes.data_ptr(), ld, self.desc, self.prepared.data_ptr(), nbytes,
                                                    _stream(stream)), "aqd_linear_prepare_weights")
@@ -800,32 +806,33 @@ def linear_int8(x: torch.Tensor, x_scale: torch.Tensor | None, w: LinearWeights,
     """x (int8 codes [..., k], one scale per row) times w's codes, scaled per token and channel (aqd_linear_int8).
     out_dtype torch.int32: the integer sums. workspace: linear_workspace(m, w), which calls that may overlap in time must
     not share."""
-    if x.dtype != torch.int8:
+    if x.dtype is not torch.int8:
         raise ValueError("x must hold int8 codes")
-    m, k, ld = _rows_of(x, "x", w.device)
+    dev = w.index
+    m, k, ld = _rows_of(x, "x", dev)
+    n = w.n
     if k != w.k:
         raise ValueError(f"x has {k} columns, the weights {w.k}")
-    dev = x.device
+    yd = _OUT_DTYPE.get(out_dtype if out is None else out.dtype)
+    if yd is None:
+        raise ValueError("the output must be float32, float16, bfloat16 or int32")
     if out is None:
-        out = _new((*x.shape[:-1], w.n), out_dtype, dev, stream)
-        ldy = w.n
+        out = _new((m, n) if x.dim() == 2 else (*x.shape[:-1], n), out_dtype, w.device, stream)
+        ldy = n
     else:
-        if out.shape != (*x.shape[:-1], w.n):
+        if out.shape != (*x.shape[:-1], n):
             raise ValueError("out must have x's shape but for the last dimension, n")
         ldy = _rows_of(out, "out", dev)[2]
-    yd = _OUT_DTYPE.get(out.dtype)
-    if yd is None:
-        raise ValueError(f"out must be float32, float16, bfloat16 or int32, got {out.dtype}")
     xs = bp = 0
     if yd != _I32:
         if x_scale is None:
             raise ValueError("x_scale is required")
         xs = _vector(x_scale, m, torch.float32, "x_scale", dev)
         if bias is not None:
-            bp = _vector(bias, w.n, torch.float32, "bias", dev)
+            bp = _vector(bias, n, torch.float32, "bias", dev)
     wsp, wsb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
-    args = _LINEAR.pack(m, x.data_ptr(), ld, xs, bp, out.data_ptr(), ldy, yd)
-    _check(_calls().aqd_linear_int8(args, w.desc, wsp, wsb, _stream(stream)), "aqd_linear_int8")
+    _check(_calls().aqd_linear_int8(_LINEAR.pack(m, x.data_ptr(), ld, xs, bp, out.data_ptr(), ldy, yd), w.desc, wsp, wsb,
+                                    _stream(stream)), "aqd_linear_int8")
     return out
 
 
@@ -838,7 +845,7 @@ class DistillLoss(NamedTuple):
 def _distill_args(logits, index, teacher, row_weight, tau, grad):
     m, v, ld = _rows_of(logits, "logits")
     d = _float_dtype(logits, "logits")
-    dev = logits.device
+    dev = logits.get_device()
     top = teacher.shape[-1] if teacher.dim() else 0
     if index.shape != teacher.shape or index.shape[:-1] != logits.shape[:-1]:
         raise ValueError("index and teacher must have the logits' shape but for the last dimension")
@@ -847,7 +854,7 @@ def _distill_args(logits, index, teacher, row_weight, tau, grad):
     wp = 0 if row_weight is None else _vector(row_weight, m, torch.float32, "row_weight", dev)
     gp = lg = 0
     if grad is not None:
-        if grad.shape != logits.shape or grad.dtype != logits.dtype:
+        if grad.shape != logits.shape or grad.dtype is not logits.dtype:
             raise ValueError("grad must have the logits' shape and type")
         lg = _rows_of(grad, "grad", dev)[2]
         gp = grad.data_ptr()
@@ -874,7 +881,7 @@ def distill_topk_backward(logits: torch.Tensor, index: torch.Tensor, teacher: to
     gradient."""
     g = _new(logits.shape, logits.dtype, logits.device, stream) if grad is None else grad
     m, args = _distill_args(logits, index, teacher, row_weight, tau, g)
-    lp = _vector(lse, m, torch.float32, "lse", logits.device)
+    lp = _vector(lse, m, torch.float32, "lse", logits.get_device())
     _check(_calls().aqd_distill_topk_backward(args, lp, _stream(stream)), "aqd_distill_topk_backward")
     return g
 

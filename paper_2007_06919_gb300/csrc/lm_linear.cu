@@ -251,8 +251,10 @@ __global__ void __launch_bounds__(kSmallWarps * 32, 2) linear_ring_kernel(const 
 template <int kG, int kR, int kDepth, bool kLong>
 static cudaError_t run_ring(const LinArgs& a, cudaStream_t stream) {
   constexpr int smem = small_bytes(kG, kR, kDepth);
-  const cudaError_t e = cudaFuncSetAttribute(linear_ring_kernel<kG, kR, kDepth, kLong>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
+  if constexpr (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(linear_ring_kernel<kG, kR, kDepth, kLong>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(((int64_t)a.n + 16 * kR - 1) / (16 * kR)), (unsigned)((a.m + 8 * kG - 1) / (8 * kG)));
   cfg.blockDim = dim3(kSmallWarps * 32);
