@@ -1,9 +1,10 @@
 // lm_distill.cu -- distillation from a teacher's top logits: the loss of each token, its normalizer, and the gradient.
 //
-// Bound by memory: the logits are read once and the gradient written once. A token's logits stay in registers between the
-// normalizer's sum and the gradient: 16-byte vectors, eight a thread at most, spread over the threads of up to eight blocks of a
-// cluster, which join their (maximum, sum) through distributed shared memory. Tokens of a larger vocabulary than that holds
-// (262,144 logits of 16 bits, 131,072 of 32) are read a second time for the gradient.
+// Bound by memory: the logits are read once and the gradient written once. Between the normalizer's sum and the gradient a token's
+// logits stay in shared memory, spread over the blocks of a cluster (about 32 KB each, so that several blocks share an SM and
+// one's copies overlap another's sums and barriers), which join their (maximum, sum) through distributed shared memory. Every thread
+// reads only what it copied itself (cp.async), so the copies need no barrier. Tokens of a larger vocabulary than eight blocks
+// hold (1.6 MB of logits) are read a second time for the gradient.
 //
 // Exponentials are taken to base 2 (one multiply-add and one ex2.approx, within 2 units of 2^-23 of its value): with c = log2(e) / tau,
 // q_v = 2^(x_v c - lse2). A row may start at any element: its first and last vectors are read and
@@ -22,8 +23,9 @@
 namespace aqd {
 namespace distill {
 
-constexpr int kMaxThreads = 512, kMaxTop = 1024, kMaxSplits = 8;
-constexpr int kHold = 8;  // vectors of a thread that stay in registers
+constexpr int kMaxThreads = 256, kMaxTop = 1024, kMaxSplits = 8;
+constexpr int kMaxWarps = kMaxThreads / 32;
+constexpr int kSlice = 32 * 1024, kMaxSlice = 200 * 1024;  // bytes of a block's logits: wanted, at most
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float load_f32(const float* p) { return *p; }
@@ -48,6 +50,9 @@ struct Vec<float> {
   static __device__ __forceinline__ void unpack(const uint4& v, float (&f)[4]) {
     f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
   }
+  static __device__ __forceinline__ float top(const uint4& v, float m) {
+    return fmaxf(fmaxf(fmaxf(m, __uint_as_float(v.x)), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+  }
   static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
     return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
   }
@@ -59,6 +64,12 @@ struct Vec<__half> {
   static __device__ __forceinline__ void two(uint32_t w, float& a, float& b) {
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
     a = f.x; b = f.y;
+  }
+  // the larger of m and v's values (a NaN counts only where nothing else is there)
+  static __device__ __forceinline__ float top(const uint4& v, float m) {
+    const __half2* h = reinterpret_cast<const __half2*>(&v);
+    const __half2 t = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return fmaxf(m, fmaxf(__low2float(t), __high2float(t)));
   }
   static __device__ __forceinline__ uint32_t one(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
@@ -77,6 +88,11 @@ struct Vec<__nv_bfloat16> {
   static constexpr uint32_t kLow = 0xff80ff80u;
   static __device__ __forceinline__ void two(uint32_t w, float& a, float& b) {
     a = __uint_as_float(w << 16); b = __uint_as_float(w & 0xffff0000u);
+  }
+  static __device__ __forceinline__ float top(const uint4& v, float m) {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+    const __nv_bfloat162 t = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return fmaxf(m, fmaxf(__low2float(t), __high2float(t)));
   }
   static __device__ __forceinline__ uint32_t one(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
@@ -113,7 +129,7 @@ __device__ __forceinline__ void store_vec(T* g, int64_t first, int vocab, bool w
 }
 
 // The maximum m and the sum s of 2^(z - m) of a share of a softmax's terms; an empty share is (-inf, 0).
-struct Soft {
+struct alignas(8) Soft {
   float m, s;
 };
 __device__ __forceinline__ Soft join(Soft a, Soft b) {
@@ -121,42 +137,50 @@ __device__ __forceinline__ Soft join(Soft a, Soft b) {
   if (m == -INFINITY) return {m, a.s + b.s};  // nothing yet (or NaN sums, which stay)
   return {m, a.s * ex2(a.m - m) + b.s * ex2(b.m - m)};
 }
-__device__ Soft block_join(Soft v, Soft* sh) {  // (in a fixed order: lanes, then warps)
+__device__ __forceinline__ Soft lanes_join(Soft v) {  // (a fixed order: every lane gets the same)
+#pragma unroll
   for (int o = 16; o > 0; o >>= 1)
     v = join(v, Soft{__shfl_xor_sync(0xffffffffu, v.m, o), __shfl_xor_sync(0xffffffffu, v.s, o)});
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
-  __syncthreads();
-  const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-  v = lane < warps ? sh[lane] : Soft{-INFINITY, 0.0f};
-  for (int o = 8; o > 0; o >>= 1)
-    v = join(v, Soft{__shfl_xor_sync(0xffffffffu, v.m, o), __shfl_xor_sync(0xffffffffu, v.s, o)});
-  return v;  // (of lane 0 .. 15: 16 warps at most)
+  return v;
 }
-template <int kE>
-__device__ __forceinline__ Soft add(Soft a, const float (&f)[kE], float c) {
-  float top = f[0];
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// A share and one more term z.
+__device__ __forceinline__ Soft add(Soft a, float z) {
+  const float m = fmaxf(a.m, z), zero = m == -INFINITY ? 0.0f : m;
+  return {m, a.s * ex2(a.m - zero) + ex2(z - zero)};
+}
+// sum 2^(x c - zero) over a vector
+template <class T>
+__device__ __forceinline__ float terms(const uint4& v, float c, float zero) {
+  constexpr int kE = Vec<T>::kE;
+  float f[kE];
+  Vec<T>::unpack(v, f);
 #pragma unroll
-  for (int e = 1; e < kE; ++e) top = fmaxf(top, f[e]);
-  const float m = fmaxf(a.m, top * c);
-  const float zero = m == -INFINITY ? 0.0f : m;  // (nothing but -inf so far: every term below is 0)
-  float s = a.s * ex2(a.m - zero);
+  for (int e = 0; e < kE; ++e) f[e] = ex2(fmaf(f[e], c, -zero));
 #pragma unroll
-  for (int e = 0; e < kE; ++e) s += ex2(fmaf(f[e], c, -zero));
-  return {m, s};
+  for (int d = kE / 2; d > 0; d >>= 1)
+#pragma unroll
+    for (int e = 0; e < d; ++e) f[e] += f[e + d];
+  return f[0];
 }
 
-// A token per cluster of `splits` blocks, each a range of its vectors. kRegs: the range stays in registers.
-template <class T, bool kRegs>
-__global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillArgs p, const int splits) {
-  __shared__ int sidx[kMaxTop];
-  __shared__ float sp[kMaxTop], slz[kMaxTop];
-  __shared__ Soft ssoft[kMaxThreads / 32], sranks[kMaxSplits];
+// A token per cluster of `splits` blocks, each a range of its vectors. kStay: the range stays in shared memory.
+template <class T, bool kStay>
+__global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 5) distill_kernel(const DistillArgs p, const int splits) {
+  extern __shared__ __align__(16) uint8_t smem[];  // the kept places' logits, shares and indices, then the range
+  __shared__ Soft swt[kMaxWarps], sws[kMaxSplits * kMaxWarps];  // the warps' shares: of the kept places, of the logits (all blocks')
   __shared__ float ssum[kMaxThreads / 32];
   constexpr int kE = Vec<T>::kE;
-  const int threads = blockDim.x;
+  const int threads = blockDim.x, tops = (p.top + 3) & ~3;
+  float* slz = reinterpret_cast<float*>(smem);
+  float* sp = slz + tops;
+  int* sidx = reinterpret_cast<int*>(sp + tops);
+  const uint4* held = reinterpret_cast<const uint4*>(sidx + tops);
   const int64_t row = blockIdx.x / (unsigned)splits;
   const int rank = (int)(blockIdx.x - (unsigned)row * (unsigned)splits);
+  if (splits > 1) cluster_arrive();  // (waited for before the first store into another block: all have started)
   tc::grid_dep_wait();
   const T* x = static_cast<const T*>(p.logits) + row * p.ld_logits;
   T* g = p.grad ? static_cast<T*>(p.grad) + row * p.ld_grad : nullptr;
@@ -167,15 +191,16 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
   const float rt = 1.0f / p.tau, c = kLog2e * rt;
   const float w = p.row_weight ? p.row_weight[row] : 1.0f;
   const bool sums = !p.lse_in && (w != 0.0f || p.lse);  // the normalizer is computed here
-  uint4 raw[kRegs ? kHold : 1];
-  if constexpr (kRegs) {
+  if constexpr (kStay) {
     if (sums || (g && w != 0.0f)) {
-#pragma unroll
-      for (int j = 0; j < kHold; ++j) {
-        const int v = v0 + (int)threadIdx.x + j * threads;
-        raw[j] = v < v1 ? load_vec(x, (int64_t)v * kE - off, p.vocab) : make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
+      for (int v = v0 + (int)threadIdx.x; v < v1; v += threads) {
+        const int64_t first = (int64_t)v * kE - off;
+        const uint32_t to = tc::smem_u32(held + (v - v0));
+        if (first >= 0 && first + kE <= p.vocab) tc::cp_async<16>(to, x + first, true);
+        else *const_cast<uint4*>(held + (v - v0)) = load_vec(x, first, p.vocab);
       }
     }
+    tc::cp_async_commit();
   }
   // the kept places, in base 2; an empty one has index -1
   Soft t{-INFINITY, 0.0f};
@@ -186,47 +211,61 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
     sidx[j] = in ? (int)i : -1;
     sp[j] = z;
     slz[j] = in ? load_f32(x + i) * c : 0.0f;
-    if (in) {
-      const float one[1] = {z};
-      t = add<1>(t, one, 1.0f);
-    }
+    if (in) t = add(t, z);
   }
-  t = block_join(t, ssoft);
-  t = Soft{__shfl_sync(0xffffffffu, t.m, 0), __shfl_sync(0xffffffffu, t.s, 0)};
-  const bool live = w != 0.0f && (t.m != -INFINITY || t.s != 0.0f);
   float lse2 = 0.0f;
   if (p.lse_in) lse2 = p.lse_in[row] * kLog2e;
   Soft s{-INFINITY, 0.0f};
+  if constexpr (kStay) tc::cp_async_wait<0>();
   if (sums) {
-    if constexpr (kRegs) {
+    // a few vectors at a time: their maximum, then their terms
+    constexpr int kU = kStay ? 2 : 4;
+    for (int v = v0 + (int)threadIdx.x; v < v1; v += kU * threads) {
+      uint4 raw[kU];
 #pragma unroll
-      for (int j = 0; j < kHold; ++j) {
-        if (v0 + j * threads >= v1) break;
-        float f[kE];
-        Vec<T>::unpack(raw[j], f);
-        s = add<kE>(s, f, c);
+      for (int u = 0; u < kU; ++u) {
+        const int at = v + u * threads;
+        if (at >= v1) raw[u] = make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
+        else if (kStay) raw[u] = held[at - v0];
+        else raw[u] = load_vec(x, (int64_t)at * kE - off, p.vocab);
       }
-    } else {
-      for (int v = v0 + (int)threadIdx.x; v < v1; v += threads) {
-        float f[kE];
-        Vec<T>::unpack(load_vec(x, (int64_t)v * kE - off, p.vocab), f);
-        s = add<kE>(s, f, c);
+      float top = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < kU; ++u) top = Vec<T>::top(raw[u], top);
+      const float m = fmaxf(s.m, top * c), zero = m == -INFINITY ? 0.0f : m;  // (nothing but -inf so far: every term is 0)
+      s = Soft{m, s.s * ex2(s.m - zero)};
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        if (v + u * threads >= v1) break;
+        s.s += terms<T>(raw[u], c, zero);
       }
     }
-    s = block_join(s, ssoft);
   }
-  if (splits > 1) {  // (also: no block writes a gradient in place before all have read their kept places' logits)
-    if (threadIdx.x < (unsigned)splits) {
-      const uint32_t to = tc::mapa_shared(tc::smem_u32(&sranks[rank]), threadIdx.x);
+  // Every warp's share to every block of the cluster, then one barrier. (Also: no gradient is written in place before all
+  // blocks have read their kept places' logits.)
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = threads >> 5;
+  t = lanes_join(t);
+  s = lanes_join(s);
+  if (lane == 0) swt[warp] = t;
+  if (splits > 1) {
+    cluster_wait();
+    if (lane < splits) {
+      const uint32_t to = tc::mapa_shared(tc::smem_u32(&sws[rank * warps + warp]), (uint32_t)lane);
       asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(s.m), "f"(s.s) : "memory");
     }
     tc::cluster_sync();
-    s = sranks[0];
-    for (int r = 1; r < splits; ++r) s = join(s, sranks[r]);
   } else {
-    s = Soft{__shfl_sync(0xffffffffu, s.m, 0), __shfl_sync(0xffffffffu, s.s, 0)};
+    if (lane == 0) sws[warp] = s;
     __syncthreads();
   }
+  t = lanes_join(lane < warps ? swt[lane] : Soft{-INFINITY, 0.0f});
+  s = Soft{-INFINITY, 0.0f};
+  if (sums) {
+    if (lane < splits * warps) s = sws[lane];
+    if (lane + 32 < splits * warps) s = join(s, sws[lane + 32]);
+    s = lanes_join(s);
+  }
+  const bool live = w != 0.0f && (t.m != -INFINITY || t.s != 0.0f);
   if (sums) {
     lse2 = s.m == -INFINITY && s.s == 0.0f ? -INFINITY : s.m + log2f(s.s);
     if (p.lse && rank == 0 && threadIdx.x == 0) p.lse[row] = lse2 * kLn2;
@@ -255,25 +294,13 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
     p.loss[row] = 0.0f;
   }
   if (!g) return;
-  if constexpr (kRegs) {
+  for (int v = v0 + (int)threadIdx.x; v < v1; v += threads) {
+    float f[kE];
+    const int64_t first = (int64_t)v * kE - off;
+    if (live) Vec<T>::unpack(kStay ? held[v - v0] : load_vec(x, first, p.vocab), f);
 #pragma unroll
-    for (int j = 0; j < kHold; ++j) {
-      const int v = v0 + (int)threadIdx.x + j * threads;
-      if (v >= v1) break;
-      float f[kE];
-      Vec<T>::unpack(raw[j], f);
-#pragma unroll
-      for (int e = 0; e < kE; ++e) f[e] = live ? f0 * ex2(fmaf(f[e], c, -lse2)) : 0.0f;
-      store_vec(g, (int64_t)v * kE - off, p.vocab, whole, f);
-    }
-  } else {
-    for (int v = v0 + (int)threadIdx.x; v < v1; v += threads) {
-      float f[kE];
-      if (live) Vec<T>::unpack(load_vec(x, (int64_t)v * kE - off, p.vocab), f);
-#pragma unroll
-      for (int e = 0; e < kE; ++e) f[e] = live ? f0 * ex2(fmaf(f[e], c, -lse2)) : 0.0f;
-      store_vec(g, (int64_t)v * kE - off, p.vocab, whole, f);
-    }
+    for (int e = 0; e < kE; ++e) f[e] = live ? f0 * ex2(fmaf(f[e], c, -lse2)) : 0.0f;
+    store_vec(g, first, p.vocab, whole, f);
   }
   if (!live) return;
   __syncthreads();
@@ -292,16 +319,23 @@ template <class T>
 static cudaError_t run(const DistillArgs& a, cudaStream_t stream) {
   constexpr int kE = Vec<T>::kE;
   const int64_t vecs = ((int64_t)a.vocab + 2 * kE - 2) / kE;  // at most
-  int64_t splits = (vecs + kHold * kMaxThreads - 1) / (kHold * kMaxThreads);
-  const bool regs = splits <= kMaxSplits;
-  if (!regs) splits = kMaxSplits;
+  const int64_t bytes = vecs * 16;
+  int64_t splits = (bytes + kSlice - 1) / kSlice;
   // few tokens: more blocks a token, down to a vector a thread
-  const int64_t room = 304 / a.tokens, wide = vecs / kMaxThreads;
+  const int64_t room = 608 / a.tokens, wide = vecs / kMaxThreads;
   if (splits < room && splits < wide) splits = room < wide ? room : wide;
   if (splits > kMaxSplits) splits = kMaxSplits;
+  const int64_t per = (vecs + splits - 1) / splits;
+  const bool stay = per * 16 <= kMaxSlice;
   // about four vectors a thread where they are that few
-  int64_t threads = ((vecs + splits - 1) / splits + 3) / 4;
+  int64_t threads = (per + 3) / 4;
   threads = threads < 64 ? 64 : (threads > kMaxThreads ? kMaxThreads : (threads + 31) / 32 * 32);
+  const size_t smem = (size_t)((a.top + 3) / 4 * 4) * 12 + (stay ? (size_t)per * 16 : 0);
+  void (*kernel)(DistillArgs, int) = stay ? distill_kernel<T, true> : distill_kernel<T, false>;
+  if (smem > 40 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlice + kMaxTop * 12);
+    if (e != cudaSuccess) return e;
+  }
   // (a grid holds 2^31 - 1 blocks: the tokens in pieces)
   const int64_t most = 2147483647LL / splits;
   for (int64_t m = 0; m < a.tokens; m += most) {
@@ -318,6 +352,7 @@ static cudaError_t run(const DistillArgs& a, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(p.tokens * splits));
     cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -328,8 +363,7 @@ static cudaError_t run(const DistillArgs& a, cudaStream_t stream) {
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = splits > 1 ? 2 : 1;
-    const cudaError_t e = regs ? cudaLaunchKernelEx(&cfg, distill_kernel<T, true>, p, (int)splits)
-                               : cudaLaunchKernelEx(&cfg, distill_kernel<T, false>, p, (int)splits);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p, (int)splits);
     if (e != cudaSuccess) return e;
   }
   return cudaGetLastError();

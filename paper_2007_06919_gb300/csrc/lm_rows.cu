@@ -5,9 +5,10 @@
 // u_k = h_k w_k / rms(h): the factor 1 / rms cancels in the codes, so they need only max_k |h_k w_k|, which the same pass
 // over the row gives as sum h^2; the scale takes the factor.
 //
-// All three are bound by memory. rows_kernel keeps a row in registers between its statistics and its codes, so it is
-// read once: a warp per short row, a block per longer one, 16-byte accesses where all tensors allow them. Rows
-// longer than a block's registers hold (16,384 values) take rows_long_kernel, which reads them twice (the second time from L2).
+// All three are bound by memory, and a row's codes need all of it: it waits on chip in between, so it is read once. Short rows
+// wait in registers (rows_kernel: a warp or a block each), longer ones in shared memory (rows_held_kernel), and rows longer
+// than that are read twice, the second time from L2 (rows_long_kernel). 16-byte accesses where all tensors allow them.
+// (4096 x 4096 bf16, the norm with its residual, codes and values: 26 us, 5.8 TB/s; 4096 x 12288 f16, gated: 56 us, 6.2 TB/s.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -16,12 +17,15 @@
 #include <type_traits>
 
 #include "../../include/aqd.h"
+#include "common.cuh"
 #include "kernels.h"
+#include "tc_ptx.cuh"
 
 namespace aqd {
 namespace rows {
 
 constexpr float kTiny = 7.52316385e-37f;  // 2^-120: 127 / a stays finite above it
+constexpr int kHeldBytes = 72 * 1024;
 constexpr float kRound = 12582912.0f;     // 1.5 * 2^23: x + kRound has x rounded to nearest even in its low bits, for |x| < 2^22
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
@@ -96,10 +100,14 @@ __device__ __forceinline__ void store_vec_any(void* p, int64_t i, int dtype, con
 }
 
 // Both activations are g times a logistic function: (1 + tanh z) / 2 = 1 / (1 + e^-2z), which loses nothing for z << 0 as 1 + tanh z
-// does. e^x and the quotient by the fast hardware functions: within 2^-21 of their size for |x| <= 8, far inside half a code's step.
+// does. The exponential and the reciprocal are the fast hardware functions': together within 2^-21 of their size for |z| <= 8, far inside
+// half a code's step. (1 + e^-z infinite gives 0.)
 __device__ __forceinline__ float activate(float g, int act) {
   const float z = act == AQD_ACT_SILU ? g : 1.5957691216f * fmaf(0.044715f * g * g, g, g);  // 2 sqrt(2 / pi)
-  return __fdividef(g, 1.0f + __expf(-z));
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-1.4426950409f * z));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+  return g * r;
 }
 
 // A row's codes: u * inv rounded; its scale. (rms: of the row, under the norm, else 1 / rms is 1)
@@ -113,13 +121,13 @@ __device__ __forceinline__ void row_scale(float a, float ss, float rrms, float& 
   }
 }
 
-// The codes and values of kE adjacent u (which they replace).
+// The codes and values of kE adjacent u (which they replace), all finite or inv and u 0.
 template <int kE>
 __device__ __forceinline__ void write_codes(const RowArgs& p, int64_t row, int64_t k, float inv, float scale, float (&u)[kE]) {
   uint32_t q[kE];
 #pragma unroll
   for (int j = 0; j < kE; ++j) {
-    const float t = inv == 0.0f ? kRound : fmaf(u[j], inv, kRound);
+    const float t = fmaf(u[j], inv, kRound);
     q[j] = __float_as_uint(t);
     u[j] = (t - kRound) * scale;
   }
@@ -137,11 +145,27 @@ __device__ __forceinline__ void write_codes(const RowArgs& p, int64_t row, int64
   if (p.values) store_vec_any<kE>(p.values, row * p.ld_values + k, p.values_dtype, u);
 }
 
+// Statistics of a block's threads, in a fixed order: lanes, then warps.
+template <bool kSum>
+__device__ __forceinline__ void block_stats(uint32_t& top, float& ss) {
+  __shared__ float ssum[32];
+  __shared__ uint32_t smax[32];
+  const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  top = __reduce_max_sync(0xffffffffu, top);
+  if (kSum)
+    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+  if (lane == 0) { ssum[threadIdx.x >> 5] = ss; smax[threadIdx.x >> 5] = top; }
+  __syncthreads();
+  top = __reduce_max_sync(0xffffffffu, lane < warps ? smax[lane] : 0u);
+  if (kSum) {
+    ss = lane < warps ? ssum[lane] : 0.0f;
+    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+  }
+}
+
 // kWarpRow: a warp per row, else a block; kV vectors of kE elements a thread (32 values of 32 bits take a block of at most 512).
 template <class T, RowOp kOp, int kE, int kV, bool kWarpRow>
 __global__ void __launch_bounds__(kWarpRow ? 256 : (kV * kE >= 32 ? 512 : 1024)) rows_kernel(const RowArgs p) {
-  __shared__ float ssum[32];
-  __shared__ uint32_t smax[32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t row = kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + warp : (int64_t)blockIdx.x;
@@ -193,22 +217,22 @@ __global__ void __launch_bounds__(kWarpRow ? 256 : (kV * kE >= 32 ? 512 : 1024))
 #pragma unroll
     for (int j = 0; j < kE; ++j) top = max(top, __float_as_uint(fabsf(u[i][j])));
   }
-  top = __reduce_max_sync(0xffffffffu, top);
-  if (kOp == kRowNorm)
-    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-  if constexpr (!kWarpRow) {
-    if (lane == 0) { ssum[warp] = ss; smax[warp] = top; }
-    __syncthreads();
-    const int warps = blockDim.x >> 5;
-    top = __reduce_max_sync(0xffffffffu, lane < warps ? smax[lane] : 0u);
-    if (kOp == kRowNorm) {
-      ss = lane < warps ? ssum[lane] : 0.0f;
+  if constexpr (kWarpRow) {
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (kOp == kRowNorm)
       for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    }
+  } else {
+    block_stats<kOp == kRowNorm>(top, ss);
   }
   float inv, scale;
   row_scale(__uint_as_float(top), ss, kOp == kRowNorm ? rsqrtf(ss / (float)p.cols + p.eps) : 1.0f, inv, scale);
   if (first == 0) p.scales[row] = scale;
+  if (isnan(scale)) {
+#pragma unroll
+    for (int i = 0; i < kV; ++i)
+#pragma unroll
+      for (int j = 0; j < kE; ++j) u[i][j] = 0.0f;
+  }
 #pragma unroll
   for (int i = 0; i < kV; ++i) {
     const int k = first + i * step;
@@ -243,11 +267,8 @@ __device__ __forceinline__ void units(const RowArgs& p, int64_t row, int64_t k, 
 // is written in the second pass, by the thread that reads the inputs there.)
 template <class T, RowOp kOp, int kE>
 __global__ void __launch_bounds__(512) rows_long_kernel(const RowArgs p) {
-  __shared__ float ssum[16];
-  __shared__ uint32_t smax[16];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int64_t row = blockIdx.x;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   float ss = 0.0f, u[kE], h[kE];
   uint32_t top = 0;
   for (int64_t k = (int64_t)threadIdx.x * kE; k < p.cols; k += 512 * kE) {
@@ -258,20 +279,114 @@ __global__ void __launch_bounds__(512) rows_long_kernel(const RowArgs p) {
       top = max(top, __float_as_uint(fabsf(u[j])));
     }
   }
-  top = __reduce_max_sync(0xffffffffu, top);
-  for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-  if (lane == 0) { ssum[warp] = ss; smax[warp] = top; }
-  __syncthreads();
-  top = __reduce_max_sync(0xffffffffu, smax[lane & 15]);
-  ss = lane < 16 ? ssum[lane] : 0.0f;
-  for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+  block_stats<kOp == kRowNorm>(top, ss);
   float inv, scale;
   row_scale(__uint_as_float(top), ss, kOp == kRowNorm ? rsqrtf(ss / (float)p.cols + p.eps) : 1.0f, inv, scale);
   if (threadIdx.x == 0) p.scales[row] = scale;
   for (int64_t k = (int64_t)threadIdx.x * kE; k < p.cols; k += 512 * kE) {
     units<T, kOp, kE>(p, row, k, u, h);
     if (kOp == kRowNorm && p.sum) store_vec<kE>(static_cast<T*>(p.sum) + row * p.ld_sum + k, h);
+    if (isnan(scale)) {
+#pragma unroll
+      for (int j = 0; j < kE; ++j) u[j] = 0.0f;
+    }
     write_codes<kE>(p, row, k, inv, scale, u);
+  }
+}
+
+// One block per row, which waits in shared memory: all of it is on its way at once, and few registers let several blocks share an SM. kVec: a
+// thread copies, and later reads, its own vectors, and u takes the place of the two inputs that it came from (a single
+// input of 16 bits is read twice instead). Else rows at any address: whole vectors of the aligned memory that holds them, their edges element by
+// element, and u in a place of its own; the threads then take the row's elements in turn.
+template <class T, RowOp kOp, bool kVec>
+__global__ void __launch_bounds__(512, 3) rows_held_kernel(const RowArgs p, const int bytes) {
+  extern __shared__ __align__(16) uint8_t smem[];  // a, then b (`bytes` each), then u (not kVec)
+  constexpr int kE = 16 / sizeof(T);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int64_t row = blockIdx.x;
+  const bool two = kOp == kRowGated || (kOp == kRowNorm && p.b);
+  const T* ab[2] = {static_cast<const T*>(p.a) + row * p.lda, static_cast<const T*>(p.b) + row * p.ldb};
+  int off[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (i == 1 && !two) break;
+    uint8_t* to = smem + i * bytes;
+    int v0 = 0, v1 = p.cols / kE;
+    if constexpr (!kVec) {
+      off[i] = (int)((reinterpret_cast<uintptr_t>(ab[i]) & 15) / sizeof(T));
+      v0 = off[i] > 0;
+      v1 = (off[i] + p.cols) / kE;
+      // the edges, an element a thread: the first kE - off, and those from vector v1 on
+      const int t = threadIdx.x, k = t < 32 ? t : v1 * kE - off[i] + t - 32;
+      if (t < 32 ? v0 > 0 && k < kE - off[i] && k < p.cols : t < 32 + kE && k >= 0 && k < p.cols)
+        reinterpret_cast<T*>(to)[off[i] + k] = ab[i][k];
+    }
+    for (int v = v0 + (int)threadIdx.x; v < v1; v += blockDim.x) tc::cp_async<16>(tc::smem_u32(to + v * 16), ab[i] + v * kE - off[i], true);
+  }
+  tc::cp_async_commit();
+  tc::cp_async_wait<0>();
+  if (!kVec) __syncthreads();
+  float ss = 0.0f;
+  uint32_t top = 0;
+  constexpr int kU = kVec ? kE : 1;
+  const bool again = kVec && sizeof(T) == 2 && !two;  // u is computed twice
+  float* us = reinterpret_cast<float*>(smem + 2 * bytes);
+  // kU values from element k on: u and, under the norm, h
+  auto units_of = [&](int k, float (&u)[kU], float (&h)[kU]) {
+    load_vec<kU>(reinterpret_cast<const T*>(smem) + off[0] + k, u);
+    if constexpr (kOp != kRowPlain) {
+      float v[kU];
+      if (two) load_vec<kU>(reinterpret_cast<const T*>(smem + bytes) + off[1] + k, v);
+      if constexpr (kOp == kRowNorm) {
+        if (two) {
+#pragma unroll
+          for (int j = 0; j < kU; ++j) u[j] += v[j];
+        }
+        load_vec_any<kU>(p.weight, k, p.weight_dtype, v);
+#pragma unroll
+        for (int j = 0; j < kU; ++j) { h[j] = u[j]; u[j] *= v[j]; }
+      } else {
+#pragma unroll
+        for (int j = 0; j < kU; ++j) u[j] = activate(u[j], p.act) * v[j];
+      }
+    }
+  };
+  for (int k = (int)threadIdx.x * kU; k < p.cols; k += (int)blockDim.x * kU) {
+    float u[kU], h[kU];
+    units_of(k, u, h);
+    if (kOp == kRowNorm && p.sum) store_vec<kU>(static_cast<T*>(p.sum) + row * p.ld_sum + k, h);
+#pragma unroll
+    for (int j = 0; j < kU; ++j) {
+      if (kOp == kRowNorm) ss = fmaf(h[j], h[j], ss);
+      top = max(top, __float_as_uint(fabsf(u[j])));
+    }
+    if constexpr (!kVec) us[k] = u[0];
+    else if (!again) {
+      uint4* at = reinterpret_cast<uint4*>(smem) + k / kE;
+      at[0] = make_uint4(__float_as_uint(u[0]), __float_as_uint(u[1]), __float_as_uint(u[2]), __float_as_uint(u[3]));
+      if constexpr (kE == 8)
+        *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(at) + bytes) = make_uint4(__float_as_uint(u[4]), __float_as_uint(u[5]), __float_as_uint(u[6]), __float_as_uint(u[7]));
+    }
+  }
+  block_stats<kOp == kRowNorm>(top, ss);
+  float inv, scale;
+  row_scale(__uint_as_float(top), ss, kOp == kRowNorm ? rsqrtf(ss / (float)p.cols + p.eps) : 1.0f, inv, scale);
+  if (threadIdx.x == 0) p.scales[row] = scale;
+  for (int k = (int)threadIdx.x * kU; k < p.cols; k += (int)blockDim.x * kU) {
+    float u[kU], h[kU];
+    if constexpr (!kVec) u[0] = us[k];
+    else if (again) units_of(k, u, h);
+    else {
+      const uint4* at = reinterpret_cast<const uint4*>(smem) + k / kE;
+      load_vec<4>(reinterpret_cast<const float*>(at), *reinterpret_cast<float(*)[4]>(&u[0]));
+      if constexpr (kE == 8)
+        load_vec<4>(reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(at) + bytes), *reinterpret_cast<float(*)[4]>(&u[kE / 2]));
+    }
+    if (isnan(scale)) {
+#pragma unroll
+      for (int j = 0; j < kU; ++j) u[j] = 0.0f;
+    }
+    write_codes<kU>(p, row, k, inv, scale, u);
   }
 }
 
@@ -286,6 +401,36 @@ static cudaError_t start(void (*kernel)(RowArgs), unsigned grid, unsigned thread
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+template <class T, RowOp kOp, bool kVec>
+static cudaError_t start_held(const RowArgs& a, cudaStream_t stream) {
+  const int kE = 16 / (int)sizeof(T), bytes = (a.cols + 2 * kE - 2) / kE * 16;
+  const int smem = 2 * bytes + (kVec ? 0 : (a.cols + 3) / 4 * 16);
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(rows_held_kernel<T, kOp, kVec>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldBytes);
+    if (e != cudaSuccess) return e;
+  }
+  const int units = kVec ? a.cols / kE : a.cols;
+  int threads = (units + 2) / 3;
+  threads = threads < 64 ? 64 : (threads > 512 ? 512 : (threads + 31) / 32 * 32);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)a.rows);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, rows_held_kernel<T, kOp, kVec>, a, bytes);
+}
+// Whether a row fits the shared memory that lets three blocks share an SM.
+template <class T>
+static bool held(const RowArgs& a, bool vec) {
+  const int64_t kE = 16 / (int)sizeof(T), bytes = (a.cols + 2 * kE - 2) / kE * 16;
+  return 2 * bytes + (vec ? 0 : (int64_t)(a.cols + 3) / 4 * 16) <= kHeldBytes;
 }
 
 static bool whole(const void* p, int64_t ld, int size, int bytes) {
@@ -304,18 +449,23 @@ static cudaError_t run(const RowArgs& a, cudaStream_t stream) {
   auto block = [](int64_t n, int v) { return (unsigned)(((n + v - 1) / v + 31) / 32 * 32); };  // threads for n units, v each
   if (vec) {
     const int64_t n = a.cols / kE;
-    // A warp with up to 4 vectors a lane, where the rows fill the GPU that way; a block with one vector a thread for few rows (the
-    // shortest chain), with up to 4 for many (fewer warps to wait at each row's end).
+    // A warp per row with up to 4 vectors a lane, where the rows fill the GPU that way; else a block, in registers with one vector a thread (two, of
+    // 32-bit values or for few rows); longer rows in shared memory. (4096 rows of 4096 bf16, the norm: one vector a thread 26 us, two 30,
+    // four 35; 4096 x 12288 f16, gated: four 85 us, three 74, read twice 69, in shared memory 56.)
     if (n <= 32) return start(rows_kernel<T, kOp, kE, 1, true>, (rows + 7) / 8, 256, a, stream);
+    if (n <= 64 && rows > 608) return start(rows_kernel<T, kOp, kE, 2, true>, (rows + 7) / 8, 256, a, stream);
     if (n <= 128 && rows > 608) return start(rows_kernel<T, kOp, kE, 4, true>, (rows + 7) / 8, 256, a, stream);
-    if (n <= 1024 && rows <= 304) return start(rows_kernel<T, kOp, kE, 1, false>, rows, block(n, 1), a, stream);
-    constexpr int kV = 32 / kE;
-    if (n <= 512 * kV) return start(rows_kernel<T, kOp, kE, kV, false>, rows, block(n, kV), a, stream);
+    if (n <= 1024) return start(rows_kernel<T, kOp, kE, 1, false>, rows, block(n, 1), a, stream);
+    if (n <= 2048 && (kE == 4 || rows <= 304)) return start(rows_kernel<T, kOp, kE, 2, false>, rows, block(n, 2), a, stream);
+    if (held<T>(a, true)) return start_held<T, kOp, true>(a, stream);
     return start(rows_long_kernel<T, kOp, kE>, rows, 512, a, stream);
   }
+  // Rows at any address: an element at a time, neighbours by neighbours. (3000 x 3333 f16, gated: eight a thread 48 us, in shared memory
+  // 32; 4096 x 1001 bf16, the norm: eight 14.2 us, in shared memory 29; 2000 x 7777: 68 and 55; 5000 x 777, gated: eight 15.5, four 11.7.)
   if (a.cols <= 256 && rows > 608) return start(rows_kernel<T, kOp, 1, 8, true>, (rows + 7) / 8, 256, a, stream);
-  if (a.cols <= 8192) return start(rows_kernel<T, kOp, 1, 8, false>, rows, block(a.cols, 8), a, stream);
-  if (a.cols <= 16384) return start(rows_kernel<T, kOp, 1, 32, false>, rows, block(a.cols, 32), a, stream);
+  if (a.cols <= (kOp == kRowGated ? 2048 : 768)) return start(rows_kernel<T, kOp, 1, 4, false>, rows, block(a.cols, 4), a, stream);
+  if (kOp != kRowGated && a.cols <= 6144) return start(rows_kernel<T, kOp, 1, 8, false>, rows, block(a.cols, 8), a, stream);
+  if (held<T>(a, false)) return start_held<T, kOp, false>(a, stream);
   return start(rows_long_kernel<T, kOp, 1>, rows, 512, a, stream);
 }
 template <class T>
