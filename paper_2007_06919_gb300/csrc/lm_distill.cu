@@ -13,6 +13,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <climits>
 #include <cstdint>
 
 #include "../../include/aqd.h"
@@ -106,25 +107,21 @@ struct Vec<__nv_bfloat16> {
   }
 };
 
-// Vector v of a row: elements [v kE - off, v kE - off + kE) of it, off the row's first element's place in its 16 bytes.
+// Vector v of a row is the 16 bytes v of the aligned memory that holds it: elements [v kE - off, v kE - off + kE) of the row, off its first
+// element's place in its 16 bytes. The row's first and last vectors may hold others' elements: these two are
+// read (others' as -infinity) and written element by element.
 template <class T>
-__device__ __forceinline__ uint4 load_vec(const T* x, int64_t first, int vocab) {
+__device__ __noinline__ uint4 load_edge(const T* x, int64_t first, int vocab) {
   constexpr int kE = Vec<T>::kE;
-  if (first >= 0 && first + kE <= vocab) return __ldcs(reinterpret_cast<const uint4*>(x + first));
   float f[kE];
 #pragma unroll
   for (int e = 0; e < kE; ++e) f[e] = first + e >= 0 && first + e < vocab ? load_f32(x + first + e) : -INFINITY;
   return Vec<T>::pack(f);
 }
 template <class T>
-__device__ __forceinline__ void store_vec(T* g, int64_t first, int vocab, bool whole, const float (&f)[Vec<T>::kE]) {
-  constexpr int kE = Vec<T>::kE;
-  if (whole && first >= 0 && first + kE <= vocab) {
-    __stcs(reinterpret_cast<uint4*>(g + first), Vec<T>::pack(f));
-    return;
-  }
+__device__ __forceinline__ void store_edge(T* g, int64_t first, int vocab, const float (&f)[Vec<T>::kE]) {
 #pragma unroll
-  for (int e = 0; e < kE; ++e)
+  for (int e = 0; e < Vec<T>::kE; ++e)
     if (first + e >= 0 && first + e < vocab) store_f32(g + first + e, f[e]);
 }
 
@@ -137,11 +134,15 @@ __device__ __forceinline__ Soft join(Soft a, Soft b) {
   if (m == -INFINITY) return {m, a.s + b.s};  // nothing yet (or NaN sums, which stay)
   return {m, a.s * ex2(a.m - m) + b.s * ex2(b.m - m)};
 }
-__device__ __forceinline__ Soft lanes_join(Soft v) {  // (a fixed order: every lane gets the same)
+// Two shares at once over a warp, so that one's chain hides the other's (a fixed order: every lane gets the same).
+__device__ __forceinline__ void lanes_join(Soft& a, Soft& b) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
-    v = join(v, Soft{__shfl_xor_sync(0xffffffffu, v.m, o), __shfl_xor_sync(0xffffffffu, v.s, o)});
-  return v;
+  for (int o = 16; o > 0; o >>= 1) {
+    const Soft x{__shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.s, o)};
+    const Soft y{__shfl_xor_sync(0xffffffffu, b.m, o), __shfl_xor_sync(0xffffffffu, b.s, o)};
+    a = join(a, x);
+    b = join(b, y);
+  }
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -168,16 +169,16 @@ __device__ __forceinline__ float terms(const uint4& v, float c, float zero) {
 
 // A token per cluster of `splits` blocks, each a range of its vectors. kStay: the range stays in shared memory.
 template <class T, bool kStay>
-__global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 5) distill_kernel(const DistillArgs p, const int splits) {
-  extern __shared__ __align__(16) uint8_t smem[];  // the kept places' logits, shares and indices, then the range
+__global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(const DistillArgs p, const int splits) {
+  extern __shared__ __align__(16) uint8_t smem[];  // the kept places' logits, teacher logits, indices and shares, then the range
   __shared__ Soft swt[kMaxWarps], sws[kMaxSplits * kMaxWarps];  // the warps' shares: of the kept places, of the logits (all blocks')
-  __shared__ float ssum[kMaxThreads / 32];
   constexpr int kE = Vec<T>::kE;
   const int threads = blockDim.x, tops = (p.top + 3) & ~3;
   float* slz = reinterpret_cast<float*>(smem);
   float* sp = slz + tops;
   int* sidx = reinterpret_cast<int*>(sp + tops);
-  const uint4* held = reinterpret_cast<const uint4*>(sidx + tops);
+  float* share = reinterpret_cast<float*>(sidx + tops);
+  const uint4* held = reinterpret_cast<const uint4*>(share + tops);
   const int64_t row = blockIdx.x / (unsigned)splits;
   const int rank = (int)(blockIdx.x - (unsigned)row * (unsigned)splits);
   if (splits > 1) cluster_arrive();  // (waited for before the first store into another block: all have started)
@@ -188,16 +189,17 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 5) distill_kernel(con
   const bool whole = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(g)) & 15) == 0;
   const int vecs = (int)(((int64_t)p.vocab + off + kE - 1) / kE), per = (vecs + splits - 1) / splits;
   const int v0 = rank * per, v1 = min(v0 + per, vecs);
+  const int in0 = off > 0, in1 = (int)(((int64_t)p.vocab + off) / kE);  // the vectors that the row fills
+  const uint4* xv = reinterpret_cast<const uint4*>(x - off);
   const float rt = 1.0f / p.tau, c = kLog2e * rt;
   const float w = p.row_weight ? p.row_weight[row] : 1.0f;
-  const bool sums = !p.lse_in && (w != 0.0f || p.lse);  // the normalizer is computed here
+  const bool sums = !p.lse_in && (p.lse || w != 0.0f);  // the normalizer is computed here
   if constexpr (kStay) {
     if (sums || (g && w != 0.0f)) {
-      for (int v = v0 + (int)threadIdx.x; v < v1; v += threads) {
-        const int64_t first = (int64_t)v * kE - off;
-        const uint32_t to = tc::smem_u32(held + (v - v0));
-        if (first >= 0 && first + kE <= p.vocab) tc::cp_async<16>(to, x + first, true);
-        else *const_cast<uint4*>(held + (v - v0)) = load_vec(x, first, p.vocab);
+      uint32_t to = tc::smem_u32(held + threadIdx.x);
+      for (int v = v0 + (int)threadIdx.x; v < v1; v += threads, to += threads * 16) {
+        if (v >= in0 && v < in1) tc::cp_async<16>(to, xv + v, true);
+        else const_cast<uint4*>(held)[v - v0] = load_edge(x, (int64_t)v * kE - off, p.vocab);
       }
     }
     tc::cp_async_commit();
@@ -227,7 +229,7 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 5) distill_kernel(con
         const int at = v + u * threads;
         if (at >= v1) raw[u] = make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
         else if (kStay) raw[u] = held[at - v0];
-        else raw[u] = load_vec(x, (int64_t)at * kE - off, p.vocab);
+        else raw[u] = at >= in0 && at < in1 ? __ldcs(xv + at) : load_edge(x, (int64_t)at * kE - off, p.vocab);
       }
       float top = -INFINITY;
 #pragma unroll
@@ -244,8 +246,7 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 5) distill_kernel(con
   // Every warp's share to every block of the cluster, then one barrier. (Also: no gradient is written in place before all
   // blocks have read their kept places' logits.)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = threads >> 5;
-  t = lanes_join(t);
-  s = lanes_join(s);
+  lanes_join(t, s);
   if (lane == 0) swt[warp] = t;
   if (splits > 1) {
     cluster_wait();
@@ -258,59 +259,55 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 5) distill_kernel(con
     if (lane == 0) sws[warp] = s;
     __syncthreads();
   }
-  t = lanes_join(lane < warps ? swt[lane] : Soft{-INFINITY, 0.0f});
-  s = Soft{-INFINITY, 0.0f};
-  if (sums) {
-    if (lane < splits * warps) s = sws[lane];
-    if (lane + 32 < splits * warps) s = join(s, sws[lane + 32]);
-    s = lanes_join(s);
-  }
+  t = lane < warps ? swt[lane] : Soft{-INFINITY, 0.0f};
+  s = lane < splits * warps ? sws[lane] : Soft{-INFINITY, 0.0f};
+  if (lane + 32 < splits * warps) s = join(s, sws[lane + 32]);
+  lanes_join(t, s);
   const bool live = w != 0.0f && (t.m != -INFINITY || t.s != 0.0f);
   if (sums) {
     lse2 = s.m == -INFINITY && s.s == 0.0f ? -INFINITY : s.m + log2f(s.s);
     if (p.lse && rank == 0 && threadIdx.x == 0) p.lse[row] = lse2 * kLn2;
   }
-  float f0 = 0.0f;
-  if (live) {
-    const float lt = t.m + log2f(t.s);
+  const float lt = t.m + log2f(t.s), f0 = w * rt;
+  if (p.loss && rank == 0 && warp == 0) {
     float loss = 0.0f;
-    for (int j = threadIdx.x; j < p.top; j += threads) {
-      const float lp = sp[j] - lt, pj = sidx[j] >= 0 ? exp2f(lp) : 0.0f;
-      if (pj != 0.0f) loss += pj * (lp - (slz[j] - lse2));
-      sp[j] = pj;
-    }
-    if (p.loss && rank == 0) {
-      for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
-      if ((threadIdx.x & 31) == 0) ssum[threadIdx.x >> 5] = loss;
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        loss = 0.0f;
-        for (int i = 0; i < threads / 32; ++i) loss += ssum[i];
-        p.loss[row] = w * (loss * kLn2);
+    if (live) {
+      for (int j = lane; j < p.top; j += 32) {
+        const float lp = sp[j] - lt, pj = sidx[j] >= 0 ? exp2f(lp) : 0.0f;
+        if (pj != 0.0f) loss += pj * (lp - (slz[j] - lse2));
       }
+      for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
+      loss = w * (loss * kLn2);
     }
-    f0 = w * rt;
-  } else if (p.loss && rank == 0 && threadIdx.x == 0) {
-    p.loss[row] = 0.0f;
+    if (lane == 0) p.loss[row] = loss;
   }
   if (!g) return;
+  for (int j = threadIdx.x; j < p.top; j += threads) share[j] = sidx[j] >= 0 ? exp2f(sp[j] - lt) : 0.0f;
+  const int stores = whole ? 0 : INT_MAX;  // vectors from here on are stored whole
+  uint4* gv = reinterpret_cast<uint4*>(g - off);
+#pragma unroll 2
   for (int v = v0 + (int)threadIdx.x; v < v1; v += threads) {
+    const bool inside = v >= in0 && v < in1;
     float f[kE];
-    const int64_t first = (int64_t)v * kE - off;
-    if (live) Vec<T>::unpack(kStay ? held[v - v0] : load_vec(x, first, p.vocab), f);
+    if (live) {
+      Vec<T>::unpack(kStay ? held[v - v0] : inside ? __ldcs(xv + v) : load_edge(x, (int64_t)v * kE - off, p.vocab), f);
 #pragma unroll
-    for (int e = 0; e < kE; ++e) f[e] = live ? f0 * ex2(fmaf(f[e], c, -lse2)) : 0.0f;
-    store_vec(g, first, p.vocab, whole, f);
+      for (int e = 0; e < kE; ++e) f[e] = f0 * ex2(fmaf(f[e], c, -lse2));
+    } else {
+#pragma unroll
+      for (int e = 0; e < kE; ++e) f[e] = 0.0f;
+    }
+    if (inside && v >= stores) __stcs(gv + v, Vec<T>::pack(f));
+    else store_edge(g, (int64_t)v * kE - off, p.vocab, f);
   }
   if (!live) return;
   __syncthreads();
   // the kept places of this block's range (one listed several times takes the sum of its shares, every time alike)
   for (int j = threadIdx.x; j < p.top; j += threads) {
-    const int i = sidx[j];
-    const int v = (int)(((int64_t)i + off) / kE);
+    const int i = sidx[j], v = (int)(((int64_t)i + off) / kE);
     if (i < 0 || v < v0 || v >= v1) continue;
     float pj = 0.0f;
-    for (int l = 0; l < p.top; ++l) pj += sidx[l] == i ? sp[l] : 0.0f;
+    for (int l = 0; l < p.top; ++l) pj += sidx[l] == i ? share[l] : 0.0f;
     store_f32(g + i, f0 * (ex2(slz[j] - lse2) - pj));
   }
 }
@@ -330,10 +327,10 @@ static cudaError_t run(const DistillArgs& a, cudaStream_t stream) {
   // about four vectors a thread where they are that few
   int64_t threads = (per + 3) / 4;
   threads = threads < 64 ? 64 : (threads > kMaxThreads ? kMaxThreads : (threads + 31) / 32 * 32);
-  const size_t smem = (size_t)((a.top + 3) / 4 * 4) * 12 + (stay ? (size_t)per * 16 : 0);
+  const size_t smem = (size_t)((a.top + 3) / 4 * 4) * 16 + (stay ? (size_t)per * 16 : 0);
   void (*kernel)(DistillArgs, int) = stay ? distill_kernel<T, true> : distill_kernel<T, false>;
   if (smem > 40 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlice + kMaxTop * 12);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlice + kMaxTop * 16);
     if (e != cudaSuccess) return e;
   }
   // (a grid holds 2^31 - 1 blocks: the tokens in pieces)
