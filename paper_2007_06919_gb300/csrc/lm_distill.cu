@@ -1,10 +1,12 @@
 // lm_distill.cu -- distillation from a teacher's top logits: the loss of each token, its normalizer, and the gradient.
 //
 // Bound by memory: the logits are read once and the gradient written once. Between the normalizer's sum and the gradient a token's
-// logits stay in shared memory, spread over the blocks of a cluster (about 32 KB each, so that several blocks share an SM and
+// logits stay in shared memory, spread over the blocks of a cluster (up to 48 KB each, so that several blocks share an SM and
 // one's copies overlap another's sums and barriers), which join their (maximum, sum) through distributed shared memory. Every thread
 // reads only what it copied itself (cp.async), so the copies need no barrier. Tokens of a larger vocabulary than eight blocks
-// hold (1.6 MB of logits) are read a second time for the gradient.
+// hold (1.6 MB of logits) are read a second time for the gradient. (2048 x 131072 bf16, loss and gradient: logits in registers 336 us,
+// in shared memory 230, 4.7 TB/s; a cluster for several tokens, the next one's copies under way: 358, the fewer blocks an SM
+// then holds have too few warps for the sums and exponentials, which take most of the issue slots.)
 //
 // Exponentials are taken to base 2 (one multiply-add and one ex2.approx, within 2 units of 2^-23 of its value): with c = log2(e) / tau,
 // q_v = 2^(x_v c - lse2). A row may start at any element: its first and last vectors are read and
@@ -26,7 +28,7 @@ namespace distill {
 
 constexpr int kMaxThreads = 256, kMaxTop = 1024, kMaxSplits = 8;
 constexpr int kMaxWarps = kMaxThreads / 32;
-constexpr int kSlice = 32 * 1024, kMaxSlice = 200 * 1024;  // bytes of a block's logits: wanted, at most
+constexpr int kSlice = 48 * 1024, kMaxSlice = 200 * 1024;  // bytes of a block's logits: wanted, at most
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float load_f32(const float* p) { return *p; }
@@ -134,15 +136,19 @@ __device__ __forceinline__ Soft join(Soft a, Soft b) {
   if (m == -INFINITY) return {m, a.s + b.s};  // nothing yet (or NaN sums, which stay)
   return {m, a.s * ex2(a.m - m) + b.s * ex2(b.m - m)};
 }
-// Two shares at once over a warp, so that one's chain hides the other's (a fixed order: every lane gets the same).
-__device__ __forceinline__ void lanes_join(Soft& a, Soft& b) {
+// Floats as integers of the same order, and back (a NaN above or below all).
+__device__ __forceinline__ int ordered(float f) {
+  const int i = __float_as_int(f);
+  return i ^ ((i >> 31) & 0x7fffffff);
+}
+// A warp's shares, every lane gets the same: the largest maximum, the sums scaled to it, then added in a fixed order.
+__device__ __forceinline__ Soft lanes_join(Soft v) {
+  const int top = __reduce_max_sync(0xffffffffu, ordered(v.m));
+  const float m = __int_as_float(top ^ ((top >> 31) & 0x7fffffff));
+  v.s *= ex2(v.m - (m == -INFINITY ? 0.0f : m));
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const Soft x{__shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.s, o)};
-    const Soft y{__shfl_xor_sync(0xffffffffu, b.m, o), __shfl_xor_sync(0xffffffffu, b.s, o)};
-    a = join(a, x);
-    b = join(b, y);
-  }
+  for (int o = 16; o > 0; o >>= 1) v.s += __shfl_xor_sync(0xffffffffu, v.s, o);
+  return {m, v.s};
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -169,7 +175,7 @@ __device__ __forceinline__ float terms(const uint4& v, float c, float zero) {
 
 // A token per cluster of `splits` blocks, each a range of its vectors. kStay: the range stays in shared memory.
 template <class T, bool kStay>
-__global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(const DistillArgs p, const int splits) {
+__global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(const DistillArgs p, const int splits, const int per) {
   extern __shared__ __align__(16) uint8_t smem[];  // the kept places' logits, teacher logits, indices and shares, then the range
   __shared__ Soft swt[kMaxWarps], sws[kMaxSplits * kMaxWarps];  // the warps' shares: of the kept places, of the logits (all blocks')
   constexpr int kE = Vec<T>::kE;
@@ -179,15 +185,15 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
   int* sidx = reinterpret_cast<int*>(sp + tops);
   float* share = reinterpret_cast<float*>(sidx + tops);
   const uint4* held = reinterpret_cast<const uint4*>(share + tops);
-  const int64_t row = blockIdx.x / (unsigned)splits;
-  const int rank = (int)(blockIdx.x - (unsigned)row * (unsigned)splits);
+  const int64_t row = blockIdx.y;
+  const int rank = (int)blockIdx.x;
   if (splits > 1) cluster_arrive();  // (waited for before the first store into another block: all have started)
   tc::grid_dep_wait();
   const T* x = static_cast<const T*>(p.logits) + row * p.ld_logits;
   T* g = p.grad ? static_cast<T*>(p.grad) + row * p.ld_grad : nullptr;
   const int off = (int)((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
   const bool whole = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(g)) & 15) == 0;
-  const int vecs = (int)(((int64_t)p.vocab + off + kE - 1) / kE), per = (vecs + splits - 1) / splits;
+  const int vecs = (int)(((int64_t)p.vocab + off + kE - 1) / kE);
   const int v0 = rank * per, v1 = min(v0 + per, vecs);
   const int in0 = off > 0, in1 = (int)(((int64_t)p.vocab + off) / kE);  // the vectors that the row fills
   const uint4* xv = reinterpret_cast<const uint4*>(x - off);
@@ -246,7 +252,8 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
   // Every warp's share to every block of the cluster, then one barrier. (Also: no gradient is written in place before all
   // blocks have read their kept places' logits.)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = threads >> 5;
-  lanes_join(t, s);
+  if (warp * 32 < p.top) t = lanes_join(t);
+  if (sums) s = lanes_join(s);
   if (lane == 0) swt[warp] = t;
   if (splits > 1) {
     cluster_wait();
@@ -259,10 +266,12 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
     if (lane == 0) sws[warp] = s;
     __syncthreads();
   }
-  t = lane < warps ? swt[lane] : Soft{-INFINITY, 0.0f};
-  s = lane < splits * warps ? sws[lane] : Soft{-INFINITY, 0.0f};
-  if (lane + 32 < splits * warps) s = join(s, sws[lane + 32]);
-  lanes_join(t, s);
+  t = lanes_join(lane < warps ? swt[lane] : Soft{-INFINITY, 0.0f});
+  if (sums) {
+    s = lane < splits * warps ? sws[lane] : Soft{-INFINITY, 0.0f};
+    if (lane + 32 < splits * warps) s = join(s, sws[lane + 32]);
+    s = lanes_join(s);
+  }
   const bool live = w != 0.0f && (t.m != -INFINITY || t.s != 0.0f);
   if (sums) {
     lse2 = s.m == -INFINITY && s.s == 0.0f ? -INFINITY : s.m + log2f(s.s);
@@ -315,7 +324,9 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
 template <class T>
 static cudaError_t run(const DistillArgs& a, cudaStream_t stream) {
   constexpr int kE = Vec<T>::kE;
-  const int64_t vecs = ((int64_t)a.vocab + 2 * kE - 2) / kE;  // at most
+  // a row's vectors, at most: one more where rows start between vectors
+  const bool aligned = (reinterpret_cast<uintptr_t>(a.logits) & 15) == 0 && a.ld_logits % kE == 0;
+  const int64_t vecs = ((int64_t)a.vocab + (aligned ? kE - 1 : 2 * kE - 2)) / kE;
   const int64_t bytes = vecs * 16;
   int64_t splits = (bytes + kSlice - 1) / kSlice;
   // few tokens: more blocks a token, down to a vector a thread
@@ -328,13 +339,12 @@ static cudaError_t run(const DistillArgs& a, cudaStream_t stream) {
   int64_t threads = (per + 3) / 4;
   threads = threads < 64 ? 64 : (threads > kMaxThreads ? kMaxThreads : (threads + 31) / 32 * 32);
   const size_t smem = (size_t)((a.top + 3) / 4 * 4) * 16 + (stay ? (size_t)per * 16 : 0);
-  void (*kernel)(DistillArgs, int) = stay ? distill_kernel<T, true> : distill_kernel<T, false>;
+  void (*kernel)(DistillArgs, int, int) = stay ? distill_kernel<T, true> : distill_kernel<T, false>;
   if (smem > 40 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlice + kMaxTop * 16);
     if (e != cudaSuccess) return e;
   }
-  // (a grid holds 2^31 - 1 blocks: the tokens in pieces)
-  const int64_t most = 2147483647LL / splits;
+  constexpr int64_t most = 65535;  // the grid's second dimension: the tokens in pieces
   for (int64_t m = 0; m < a.tokens; m += most) {
     DistillArgs p = a;
     p.tokens = a.tokens - m < most ? a.tokens - m : most;
@@ -347,7 +357,7 @@ static cudaError_t run(const DistillArgs& a, cudaStream_t stream) {
     if (p.lse) p.lse += m;
     if (p.lse_in) p.lse_in += m;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(p.tokens * splits));
+    cfg.gridDim = dim3((unsigned)splits, (unsigned)p.tokens);
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
@@ -360,7 +370,7 @@ static cudaError_t run(const DistillArgs& a, cudaStream_t stream) {
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = splits > 1 ? 2 : 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p, (int)splits);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p, (int)splits, (int)per);
     if (e != cudaSuccess) return e;
   }
   return cudaGetLastError();
