@@ -463,7 +463,8 @@ aqd_status aqd_linear_int8(const aqd_linear_args* args, const aqd_linear_weights
  * logit is -infinity; a token with none has loss 0 and gradient 0. A place listed twice counts twice.
  * A token of weight 0 has loss 0 and gradient 0 whatever its logits hold. A logit of -infinity has q = 0; where a
  * kept place of p > 0 has it, the loss is +infinity. A NaN or +infinity among a token's logits or kept
- * teacher logits makes its loss and gradient NaN, as do logits that are all -infinity. Statistics are
+ * teacher logits makes its loss and gradient NaN, as do logits that are all -infinity. logit / tau has to lie
+ * within float32's range; differences from a row's maximum count alone, so rows of the lowest value are even ones. Statistics are
  * float32; each thread sums a fixed share of a row and shares combine in a fixed order (deterministic).
  *   loss, lse: [tokens] float32 or NULL; lse = ln sum_v exp(logits[v] / tau), which the backward reads.
  *   grad: NULL (loss alone) or rows of the logits' type; it may be the logits themselves (same pointer and ld).
@@ -483,7 +484,8 @@ typedef struct {
 } aqd_distill_args;
 aqd_status aqd_distill_topk(const aqd_distill_args* args, float* loss, float* lse, aqd_stream_t stream);
 /* The gradient alone, from the lse that aqd_distill_topk wrote; row_weight is the factor of each token's gradient
- * (the weight times the gradient that arrives at its loss). */
+ * (the weight times the gradient that arrives at its loss). q carries the rounding of lse, |lse| 2^-24 of its value;
+ * aqd_distill_topk's own gradient does not. */
 aqd_status aqd_distill_topk_backward(const aqd_distill_args* args, const float* lse, aqd_stream_t stream);
 
 /* ---- elementwise ------------------------------------------------------------------ */

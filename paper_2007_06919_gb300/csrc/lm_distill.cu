@@ -8,9 +8,9 @@
 // in shared memory 230, 4.7 TB/s; a cluster for several tokens, the next one's copies under way: 358, the fewer blocks an SM
 // then holds have too few warps for the sums and exponentials, which take most of the issue slots.)
 //
-// Exponentials are taken to base 2 (one multiply-add and one ex2.approx, within 2 units of 2^-23 of its value): with c = log2(e) / tau,
-// q_v = 2^(x_v c - lse2). A row may start at any element: its first and last vectors are read and
-// written element by element where they hold others'.
+// q_v = exp(z_v - m) / s with z = x / tau: z_v - m is one multiply-add, rounded once, so that logits of any size
+// (a row of the type's lowest value too) keep their differences; then a multiplication by log2(e) and ex2.approx (within 2 units of 2^-23).
+// A row may start at any element: its first and last vectors are read and written element by element where they hold others'.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -29,7 +29,7 @@ namespace distill {
 constexpr int kMaxThreads = 256, kMaxTop = 1024, kMaxSplits = 8;
 constexpr int kMaxWarps = kMaxThreads / 32;
 constexpr int kSlice = 48 * 1024, kMaxSlice = 200 * 1024;  // bytes of a block's logits: wanted, at most
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float load_f32(const float* p) { return *p; }
 __device__ __forceinline__ float load_f32(const __half* p) { return __half2float(*p); }
@@ -37,9 +37,10 @@ __device__ __forceinline__ float load_f32(const __nv_bfloat16* p) { return __bfl
 __device__ __forceinline__ void store_f32(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_f32(__half* p, float v) { *p = __float2half_rn(v); }
 __device__ __forceinline__ void store_f32(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-__device__ __forceinline__ float ex2(float x) {
+// exp(x): 2^(x log2 e); the product's rounding, 2^-24 |x log2 e|, is relative to the result, so small where the result counts
+__device__ __forceinline__ float ex(float x) {
   float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * kLog2e));
   return y;
 }
 
@@ -127,14 +128,14 @@ __device__ __forceinline__ void store_edge(T* g, int64_t first, int vocab, const
     if (first + e >= 0 && first + e < vocab) store_f32(g + first + e, f[e]);
 }
 
-// The maximum m and the sum s of 2^(z - m) of a share of a softmax's terms; an empty share is (-inf, 0).
+// The maximum m and the sum s of exp(z - m) of a share of a softmax's terms; an empty share is (-inf, 0).
 struct alignas(8) Soft {
   float m, s;
 };
 __device__ __forceinline__ Soft join(Soft a, Soft b) {
   const float m = fmaxf(a.m, b.m);
   if (m == -INFINITY) return {m, a.s + b.s};  // nothing yet (or NaN sums, which stay)
-  return {m, a.s * ex2(a.m - m) + b.s * ex2(b.m - m)};
+  return {m, a.s * ex(a.m - m) + b.s * ex(b.m - m)};
 }
 // Floats as integers of the same order, and back (a NaN above or below all).
 __device__ __forceinline__ int ordered(float f) {
@@ -145,7 +146,7 @@ __device__ __forceinline__ int ordered(float f) {
 __device__ __forceinline__ Soft lanes_join(Soft v) {
   const int top = __reduce_max_sync(0xffffffffu, ordered(v.m));
   const float m = __int_as_float(top ^ ((top >> 31) & 0x7fffffff));
-  v.s *= ex2(v.m - (m == -INFINITY ? 0.0f : m));
+  v.s *= ex(v.m - (m == -INFINITY ? 0.0f : m));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v.s += __shfl_xor_sync(0xffffffffu, v.s, o);
   return {m, v.s};
@@ -156,16 +157,16 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 // A share and one more term z.
 __device__ __forceinline__ Soft add(Soft a, float z) {
   const float m = fmaxf(a.m, z), zero = m == -INFINITY ? 0.0f : m;
-  return {m, a.s * ex2(a.m - zero) + ex2(z - zero)};
+  return {m, a.s * ex(a.m - zero) + ex(z - zero)};
 }
-// sum 2^(x c - zero) over a vector
+// sum exp(x rt - zero) over a vector
 template <class T>
-__device__ __forceinline__ float terms(const uint4& v, float c, float zero) {
+__device__ __forceinline__ float terms(const uint4& v, float rt, float zero) {
   constexpr int kE = Vec<T>::kE;
   float f[kE];
   Vec<T>::unpack(v, f);
 #pragma unroll
-  for (int e = 0; e < kE; ++e) f[e] = ex2(fmaf(f[e], c, -zero));
+  for (int e = 0; e < kE; ++e) f[e] = ex(fmaf(f[e], rt, -zero));
 #pragma unroll
   for (int d = kE / 2; d > 0; d >>= 1)
 #pragma unroll
@@ -197,7 +198,7 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
   const int v0 = rank * per, v1 = min(v0 + per, vecs);
   const int in0 = off > 0, in1 = (int)(((int64_t)p.vocab + off) / kE);  // the vectors that the row fills
   const uint4* xv = reinterpret_cast<const uint4*>(x - off);
-  const float rt = 1.0f / p.tau, c = kLog2e * rt;
+  const float rt = 1.0f / p.tau;
   const float w = p.row_weight ? p.row_weight[row] : 1.0f;
   const bool sums = !p.lse_in && (p.lse || w != 0.0f);  // the normalizer is computed here
   if constexpr (kStay) {
@@ -210,19 +211,17 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
     }
     tc::cp_async_commit();
   }
-  // the kept places, in base 2; an empty one has index -1
+  // the kept places; an empty one has index -1
   Soft t{-INFINITY, 0.0f};
   for (int j = threadIdx.x; j < p.top; j += threads) {
     const int64_t i = p.index[row * p.top + j];
-    const float z = p.teacher[row * p.top + j] * c;
+    const float z = p.teacher[row * p.top + j] * rt;
     const bool in = i >= 0 && i < p.vocab && z != -INFINITY;
     sidx[j] = in ? (int)i : -1;
     sp[j] = z;
-    slz[j] = in ? load_f32(x + i) * c : 0.0f;
+    slz[j] = in ? load_f32(x + i) : 0.0f;
     if (in) t = add(t, z);
   }
-  float lse2 = 0.0f;
-  if (p.lse_in) lse2 = p.lse_in[row] * kLog2e;
   Soft s{-INFINITY, 0.0f};
   if constexpr (kStay) tc::cp_async_wait<0>();
   if (sums) {
@@ -240,12 +239,12 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
       float top = -INFINITY;
 #pragma unroll
       for (int u = 0; u < kU; ++u) top = Vec<T>::top(raw[u], top);
-      const float m = fmaxf(s.m, top * c), zero = m == -INFINITY ? 0.0f : m;  // (nothing but -inf so far: every term is 0)
-      s = Soft{m, s.s * ex2(s.m - zero)};
+      const float m = fmaxf(s.m, top * rt), zero = m == -INFINITY ? 0.0f : m;  // (nothing but -inf so far: every term is 0)
+      s = Soft{m, s.s * ex(s.m - zero)};
 #pragma unroll
       for (int u = 0; u < kU; ++u) {
         if (v + u * threads >= v1) break;
-        s.s += terms<T>(raw[u], c, zero);
+        s.s += terms<T>(raw[u], rt, zero);
       }
     }
   }
@@ -273,25 +272,25 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
     s = lanes_join(s);
   }
   const bool live = w != 0.0f && (t.m != -INFINITY || t.s != 0.0f);
-  if (sums) {
-    lse2 = s.m == -INFINITY && s.s == 0.0f ? -INFINITY : s.m + log2f(s.s);
-    if (p.lse && rank == 0 && threadIdx.x == 0) p.lse[row] = lse2 * kLn2;
-  }
-  const float lt = t.m + log2f(t.s), f0 = w * rt;
+  if (sums && p.lse && rank == 0 && threadIdx.x == 0) p.lse[row] = s.m == -INFINITY && s.s == 0.0f ? -INFINITY : s.m + logf(s.s);
+  if (p.lse_in) s = Soft{p.lse_in[row], 1.0f};
+  const float f0 = w * rt;
   if (p.loss && rank == 0 && warp == 0) {
     float loss = 0.0f;
     if (live) {
+      const float lt = logf(t.s), ls = logf(s.s);
       for (int j = lane; j < p.top; j += 32) {
-        const float lp = sp[j] - lt, pj = sidx[j] >= 0 ? exp2f(lp) : 0.0f;
-        if (pj != 0.0f) loss += pj * (lp - (slz[j] - lse2));
+        const float lp = (sp[j] - t.m) - lt, pj = sidx[j] >= 0 ? ex(sp[j] - t.m) / t.s : 0.0f;
+        if (pj != 0.0f) loss += pj * (lp - (fmaf(slz[j], rt, -s.m) - ls));
       }
       for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
-      loss = w * (loss * kLn2);
+      loss *= w;
     }
     if (lane == 0) p.loss[row] = loss;
   }
   if (!g) return;
-  for (int j = threadIdx.x; j < p.top; j += threads) share[j] = sidx[j] >= 0 ? exp2f(sp[j] - lt) : 0.0f;
+  for (int j = threadIdx.x; j < p.top; j += threads) share[j] = sidx[j] >= 0 ? ex(sp[j] - t.m) / t.s : 0.0f;
+  const float fs = f0 / s.s;
   const int stores = whole ? 0 : INT_MAX;  // vectors from here on are stored whole
   uint4* gv = reinterpret_cast<uint4*>(g - off);
 #pragma unroll 2
@@ -301,7 +300,7 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
     if (live) {
       Vec<T>::unpack(kStay ? held[v - v0] : inside ? __ldcs(xv + v) : load_edge(x, (int64_t)v * kE - off, p.vocab), f);
 #pragma unroll
-      for (int e = 0; e < kE; ++e) f[e] = f0 * ex2(fmaf(f[e], c, -lse2));
+      for (int e = 0; e < kE; ++e) f[e] = fs * ex(fmaf(f[e], rt, -s.m));
     } else {
 #pragma unroll
       for (int e = 0; e < kE; ++e) f[e] = 0.0f;
@@ -317,7 +316,7 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
     if (i < 0 || v < v0 || v >= v1) continue;
     float pj = 0.0f;
     for (int l = 0; l < p.top; ++l) pj += sidx[l] == i ? share[l] : 0.0f;
-    store_f32(g + i, f0 * (ex2(slz[j] - lse2) - pj));
+    store_f32(g + i, fs * ex(fmaf(slz[j], rt, -s.m)) - f0 * pj);
   }
 }
 

@@ -190,6 +190,27 @@ def test_weight_zero_and_non_finite_rows(vocab, dtype):
     assert out.loss[7].isfinite() and out.grad[7].isfinite().all()
 
 
+@pytest.mark.parametrize("vocab", [50, 5001, 140000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_of_the_lowest_value(vocab, dtype):
+    """Every z - m is 0 then, exactly: q is even, and what rounds are the sums, logarithms and exponentials."""
+    x, index, teacher, w = inputs(3, 3, vocab, 6, dtype)
+    w[:] = 1
+    x[0] = torch.finfo(dtype).min                    # no logit left by a mask
+    teacher[1] = torch.finfo(torch.float32).min      # the teacher's kept logits alike
+    x[2] = torch.finfo(dtype).min
+    teacher[2, 1:] = torch.finfo(torch.float32).min  # one kept logit
+    out = aqd.distill_topk(x, index, teacher, row_weight=w, grad=True)
+    # less each row's maximum, which changes neither loss nor gradient: ln V is lost beside 3e38 in 64 bits too
+    shifted = x.double() - x.double().amax(1, keepdim=True)
+    loss, _, _, _, _ = plain(shifted, index, teacher, w, 1.0)
+    grad, size = gradient(shifted, index, teacher, w, 1.0)
+    torch.cuda.synchronize()
+    wide = (20 + math.log(vocab) + 600) * E
+    assert ((out.loss.double() - loss).abs() <= 4 * wide).all()
+    assert ((out.grad.double() - grad).abs() <= 4 * wide * size + HALF[dtype] * grad.abs() * 1.01 + TINY[dtype]).all()
+
+
 def test_gradient_of_the_formula_and_differences():
     x, index, teacher, w = inputs(9, 4, 300, 10, torch.float32)
     index[0, 4] = index[0, 1]
