@@ -44,13 +44,12 @@ __device__ __forceinline__ float ex(float x) {
   return y;
 }
 
-// A 16-byte vector of T as float32 and back; -infinity in T's bits, in every place.
+// A 16-byte vector of T as float32 and back.
 template <class T>
 struct Vec;
 template <>
 struct Vec<float> {
   static constexpr int kE = 4;
-  static constexpr uint32_t kLow = 0xff800000u;
   static __device__ __forceinline__ void unpack(const uint4& v, float (&f)[4]) {
     f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
   }
@@ -64,7 +63,6 @@ struct Vec<float> {
 template <>
 struct Vec<__half> {
   static constexpr int kE = 8;
-  static constexpr uint32_t kLow = 0xfc00fc00u;
   static __device__ __forceinline__ void two(uint32_t w, float& a, float& b) {
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
     a = f.x; b = f.y;
@@ -89,7 +87,6 @@ struct Vec<__half> {
 template <>
 struct Vec<__nv_bfloat16> {
   static constexpr int kE = 8;
-  static constexpr uint32_t kLow = 0xff80ff80u;
   static __device__ __forceinline__ void two(uint32_t w, float& a, float& b) {
     a = __uint_as_float(w << 16); b = __uint_as_float(w & 0xffff0000u);
   }
@@ -204,10 +201,16 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
   if constexpr (kStay) {
     if (sums || (g && w != 0.0f)) {
       uint32_t to = tc::smem_u32(held + threadIdx.x);
-      for (int v = v0 + (int)threadIdx.x; v < v1; v += threads, to += threads * 16) {
-        if (v >= in0 && v < in1) tc::cp_async<16>(to, xv + v, true);
-        else const_cast<uint4*>(held)[v - v0] = load_edge(x, (int64_t)v * kE - off, p.vocab);
+      const uint4* from = xv + v0 + (int)threadIdx.x;
+      int v = v0 + (int)threadIdx.x;
+      if (v < in0 && v < v1) {
+        const_cast<uint4*>(held)[v - v0] = load_edge(x, (int64_t)v * kE - off, p.vocab);
+        v += threads, from += threads, to += threads * 16;
       }
+      const int end = min(v1, in1);
+#pragma unroll 4
+      for (; v < end; v += threads, from += threads, to += threads * 16) tc::cp_async<16>(to, from, true);
+      if (v < v1) const_cast<uint4*>(held)[v - v0] = load_edge(x, (int64_t)v * kE - off, p.vocab);
     }
     tc::cp_async_commit();
   }
@@ -226,26 +229,28 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
   if constexpr (kStay) tc::cp_async_wait<0>();
   if (sums) {
     // a few vectors at a time: their maximum, then their terms
-    constexpr int kU = kStay ? 2 : 4;
-    for (int v = v0 + (int)threadIdx.x; v < v1; v += kU * threads) {
+    constexpr int kU = 4;
+    auto read = [&](int v) -> uint4 {
+      if constexpr (kStay) return held[v - v0];
+      return v >= in0 && v < in1 ? __ldcs(xv + v) : load_edge(x, (int64_t)v * kE - off, p.vocab);
+    };
+    int v = v0 + (int)threadIdx.x;
+    for (; v + (kU - 1) * threads < v1; v += kU * threads) {
       uint4 raw[kU];
 #pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        const int at = v + u * threads;
-        if (at >= v1) raw[u] = make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
-        else if (kStay) raw[u] = held[at - v0];
-        else raw[u] = at >= in0 && at < in1 ? __ldcs(xv + at) : load_edge(x, (int64_t)at * kE - off, p.vocab);
-      }
+      for (int u = 0; u < kU; ++u) raw[u] = read(v + u * threads);
       float top = -INFINITY;
 #pragma unroll
       for (int u = 0; u < kU; ++u) top = Vec<T>::top(raw[u], top);
       const float m = fmaxf(s.m, top * rt), zero = m == -INFINITY ? 0.0f : m;  // (nothing but -inf so far: every term is 0)
       s = Soft{m, s.s * ex(s.m - zero)};
 #pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        if (v + u * threads >= v1) break;
-        s.s += terms<T>(raw[u], rt, zero);
-      }
+      for (int u = 0; u < kU; ++u) s.s += terms<T>(raw[u], rt, zero);
+    }
+    for (; v < v1; v += threads) {
+      const uint4 raw = read(v);
+      const float m = fmaxf(s.m, Vec<T>::top(raw, -INFINITY) * rt), zero = m == -INFINITY ? 0.0f : m;
+      s = Soft{m, s.s * ex(s.m - zero) + terms<T>(raw, rt, zero)};
     }
   }
   // Every warp's share to every block of the cluster, then one barrier. (Also: no gradient is written in place before all
