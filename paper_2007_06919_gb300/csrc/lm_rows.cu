@@ -99,6 +99,40 @@ __device__ __forceinline__ void store_vec_any(void* p, int64_t i, int dtype, con
   else store_vec<kE>(static_cast<__nv_bfloat16*>(p) + i, f);
 }
 
+// Vectors of rows that start `off` elements into one: vector v holds the row's elements from v kE - off on, whole ones inside the row
+// (for kShift false always), the first and last of them cut by its ends.
+template <int kE, bool kShift>
+__device__ __forceinline__ bool inside(int64_t k, int64_t cols) { return !kShift || (k >= 0 && k + kE <= cols); }
+template <int kE, class T>
+__device__ __forceinline__ void load_each(const T* p, int64_t k, int64_t cols, float (&f)[kE]) {
+#pragma unroll
+  for (int j = 0; j < kE; ++j) f[j] = k + j >= 0 && k + j < cols ? to_f32(p[k + j]) : 0.0f;
+}
+// the vector at p, element k of the row
+template <int kE, bool kShift, class T>
+__device__ __forceinline__ void load_at(const T* p, int k, int cols, float (&f)[kE]) {
+  if (inside<kE, kShift>(k, cols)) load_vec<kE>(p, f);
+  else load_each<kE>(p - k, k, cols, f);
+}
+// the norm's weights, which do not start where a row does: element by element for kShift. (Out of two aligned vectors, the words picked
+// by the distance: no faster, 4096 x 1001 bf16 12.3 us to 11.8.)
+template <int kE, bool kShift>
+__device__ __forceinline__ void load_weight(const RowArgs& p, int64_t k, float (&f)[kE]) {
+  if constexpr (!kShift) load_vec_any<kE>(p.weight, k, p.weight_dtype, f);
+  else if (p.weight_dtype == AQD_F32) load_each<kE>(static_cast<const float*>(p.weight), k, p.cols, f);
+  else if (p.weight_dtype == AQD_F16) load_each<kE>(static_cast<const __half*>(p.weight), k, p.cols, f);
+  else load_each<kE>(static_cast<const __nv_bfloat16*>(p.weight), k, p.cols, f);
+}
+template <int kE, bool kShift, class T>
+__device__ __forceinline__ void store_sum(const RowArgs& p, int64_t row, int k, const float (&f)[kE]) {
+  if (inside<kE, kShift>(k, p.cols)) store_vec<kE>(static_cast<T*>(p.sum) + row * p.ld_sum + k, f);
+  else {
+#pragma unroll
+    for (int j = 0; j < kE; ++j)
+      if (k + j >= 0 && k + j < p.cols) store_vec<1>(static_cast<T*>(p.sum) + row * p.ld_sum + k + j, reinterpret_cast<const float(&)[1]>(f[j]));
+  }
+}
+
 // Both activations are g times a logistic function: (1 + tanh z) / 2 = 1 / (1 + e^-2z), which loses nothing for z << 0 as 1 + tanh z
 // does. The exponential and the reciprocal are the fast hardware functions': together within 2^-21 of their size for |z| <= 8, far inside
 // half a code's step. (1 + e^-z infinite gives 0.)
@@ -122,7 +156,7 @@ __device__ __forceinline__ void row_scale(float a, float ss, float rrms, float& 
 }
 
 // The codes and values of kE adjacent u (which they replace), all finite or inv and u 0.
-template <int kE>
+template <int kE, bool kShift>
 __device__ __forceinline__ void write_codes(const RowArgs& p, int64_t row, int64_t k, float inv, float scale, float (&u)[kE]) {
   uint32_t q[kE];
 #pragma unroll
@@ -130,6 +164,15 @@ __device__ __forceinline__ void write_codes(const RowArgs& p, int64_t row, int64
     const float t = fmaf(u[j], inv, kRound);
     q[j] = __float_as_uint(t);
     u[j] = (t - kRound) * scale;
+  }
+  if (!inside<kE, kShift>(k, p.cols)) {
+#pragma unroll
+    for (int j = 0; j < kE; ++j) {
+      if (k + j < 0 || k + j >= p.cols) continue;
+      if (p.codes) p.codes[row * p.ld_codes + k + j] = (int8_t)q[j];
+      if (p.values) store_any(p.values, row * p.ld_values + k + j, p.values_dtype, u[j]);
+    }
+    return;
   }
   if (p.codes) {
     int8_t* c = p.codes + row * p.ld_codes + k;
@@ -164,29 +207,31 @@ __device__ __forceinline__ void block_stats(uint32_t& top, float& ss) {
 }
 
 // kWarpRow: a warp per row, else a block; kV vectors of kE elements a thread (32 values of 32 bits take a block of at most 512).
-template <class T, RowOp kOp, int kE, int kV, bool kWarpRow>
+// kShift: rows start inside a vector, at the same element of it in every tensor but the weights.
+template <class T, RowOp kOp, int kE, int kV, bool kWarpRow, bool kShift>
 __global__ void __launch_bounds__(kWarpRow ? 256 : (kV * kE >= 32 ? 512 : 1024)) rows_kernel(const RowArgs p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t row = kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + warp : (int64_t)blockIdx.x;
   if (kWarpRow && row >= p.rows) return;
-  const int first = (kWarpRow ? lane : (int)threadIdx.x) * kE, step = (kWarpRow ? 32 : (int)blockDim.x) * kE;
   const T* a = static_cast<const T*>(p.a) + row * p.lda;
   const T* b = static_cast<const T*>(p.b) + row * p.ldb;
+  const int thread = kWarpRow ? lane : (int)threadIdx.x, step = (kWarpRow ? 32 : (int)blockDim.x) * kE;
+  const int first = thread * kE - (kShift ? (int)((reinterpret_cast<uintptr_t>(a) & 15) / sizeof(T)) : 0);
   float u[kV][kE];
   float ss = 0.0f;
   uint32_t top = 0;  // |u| as its bits: they order as the magnitudes do, a NaN above all
   if constexpr (kOp == kRowPlain) {
 #pragma unroll
     for (int i = 0; i < kV; ++i)
-      if (first + i * step < p.cols) load_vec<kE>(a + first + i * step, u[i]);
+      if (first + i * step < p.cols) load_at<kE, kShift>(a + first + i * step, first + i * step, p.cols, u[i]);
   } else {
     float v[kV][kE];
 #pragma unroll
     for (int i = 0; i < kV; ++i)
       if (first + i * step < p.cols) {
-        load_vec<kE>(a + first + i * step, u[i]);
-        if (kOp == kRowGated || p.b) load_vec<kE>(b + first + i * step, v[i]);
+        load_at<kE, kShift>(a + first + i * step, first + i * step, p.cols, u[i]);
+        if (kOp == kRowGated || p.b) load_at<kE, kShift>(b + first + i * step, first + i * step, p.cols, v[i]);
       }
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
@@ -197,9 +242,9 @@ __global__ void __launch_bounds__(kWarpRow ? 256 : (kV * kE >= 32 ? 512 : 1024))
 #pragma unroll
           for (int j = 0; j < kE; ++j) u[i][j] += v[i][j];
         }
-        if (p.sum) store_vec<kE>(static_cast<T*>(p.sum) + row * p.ld_sum + k, u[i]);
+        if (p.sum) store_sum<kE, kShift, T>(p, row, k, u[i]);
         float w[kE];
-        load_vec_any<kE>(p.weight, k, p.weight_dtype, w);
+        load_weight<kE, kShift>(p, k, w);
 #pragma unroll
         for (int j = 0; j < kE; ++j) {
           ss = fmaf(u[i][j], u[i][j], ss);
@@ -226,7 +271,7 @@ __global__ void __launch_bounds__(kWarpRow ? 256 : (kV * kE >= 32 ? 512 : 1024))
   }
   float inv, scale;
   row_scale(__uint_as_float(top), ss, kOp == kRowNorm ? rsqrtf(ss / (float)p.cols + p.eps) : 1.0f, inv, scale);
-  if (first == 0) p.scales[row] = scale;
+  if ((kShift ? thread : first) == 0) p.scales[row] = scale;
   if (isnan(scale)) {
 #pragma unroll
     for (int i = 0; i < kV; ++i)
@@ -237,7 +282,7 @@ __global__ void __launch_bounds__(kWarpRow ? 256 : (kV * kE >= 32 ? 512 : 1024))
   for (int i = 0; i < kV; ++i) {
     const int k = first + i * step;
     if (k >= p.cols) break;
-    write_codes<kE>(p, row, k, inv, scale, u[i]);
+    write_codes<kE, kShift>(p, row, k, inv, scale, u[i]);
   }
 }
 
@@ -290,18 +335,23 @@ __global__ void __launch_bounds__(512) rows_long_kernel(const RowArgs p) {
 #pragma unroll
       for (int j = 0; j < kE; ++j) u[j] = 0.0f;
     }
-    write_codes<kE>(p, row, k, inv, scale, u);
+    write_codes<kE, false>(p, row, k, inv, scale, u);
   }
 }
 
-// One block per row, which waits in shared memory: all of it is on its way at once, and few registers let several blocks share an SM. kVec: a
+// How the rows lie for rows_held_kernel: whole vectors; whole but for their ends (they start at the same element of a vector
+// in every tensor but the weights); or anyhow.
+enum Lie { kWhole, kShifted, kAnyhow };
+
+// One block per row, which waits in shared memory: all of it is on its way at once, and few registers let several blocks share an SM. A
 // thread copies, and later reads, its own vectors, and u takes the place of the two inputs that it came from (a single
-// input of 16 bits is read twice instead). Else rows at any address: whole vectors of the aligned memory that holds them, their edges element by
+// input of 16 bits is read twice instead). kAnyhow: whole vectors of the aligned memory that holds the rows, their edges element by
 // element, and u in a place of its own; the threads then take the row's elements in turn.
-template <class T, RowOp kOp, bool kVec>
-__global__ void __launch_bounds__(512, 3) rows_held_kernel(const RowArgs p, const int bytes) {
-  extern __shared__ __align__(16) uint8_t smem[];  // a, then b (`bytes` each), then u (not kVec)
+template <class T, RowOp kOp, Lie kLie>
+__global__ void __launch_bounds__(512, kLie == kShifted && kOp == kRowNorm ? 2 : 3) rows_held_kernel(const RowArgs p, const int bytes) {
+  extern __shared__ __align__(16) uint8_t smem[];  // a, then b (`bytes` each), then u (kAnyhow)
   constexpr int kE = 16 / sizeof(T);
+  constexpr bool kVec = kLie != kAnyhow, kShift = kLie == kShifted;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int64_t row = blockIdx.x;
   const bool two = kOp == kRowGated || (kOp == kRowNorm && p.b);
@@ -312,16 +362,28 @@ __global__ void __launch_bounds__(512, 3) rows_held_kernel(const RowArgs p, cons
     if (i == 1 && !two) break;
     uint8_t* to = smem + i * bytes;
     int v0 = 0, v1 = p.cols / kE;
-    if constexpr (!kVec) {
+    if constexpr (kLie != kWhole) {
       off[i] = (int)((reinterpret_cast<uintptr_t>(ab[i]) & 15) / sizeof(T));
       v0 = off[i] > 0;
       v1 = (off[i] + p.cols) / kE;
+    }
+    if constexpr (kLie == kAnyhow) {
       // the edges, an element a thread: the first kE - off, and those from vector v1 on
       const int t = threadIdx.x, k = t < 32 ? t : v1 * kE - off[i] + t - 32;
       if (t < 32 ? v0 > 0 && k < kE - off[i] && k < p.cols : t < 32 + kE && k >= 0 && k < p.cols)
         reinterpret_cast<T*>(to)[off[i] + k] = ab[i][k];
+      for (int v = v0 + (int)threadIdx.x; v < v1; v += blockDim.x) tc::cp_async<16>(tc::smem_u32(to + v * 16), ab[i] + v * kE - off[i], true);
+    } else {
+      for (int v = threadIdx.x; v * kE - off[i] < p.cols; v += blockDim.x) {
+        if (!kShift || (v >= v0 && v < v1)) {
+          tc::cp_async<16>(tc::smem_u32(to + v * 16), ab[i] + v * kE - off[i], true);
+        } else {  // cut by the row's ends: what is not the row's is 0
+          float f[kE];
+          load_each<kE>(ab[i], v * kE - off[i], p.cols, f);
+          store_vec<kE>(reinterpret_cast<T*>(to) + v * kE, f);
+        }
+      }
     }
-    for (int v = v0 + (int)threadIdx.x; v < v1; v += blockDim.x) tc::cp_async<16>(tc::smem_u32(to + v * 16), ab[i] + v * kE - off[i], true);
   }
   tc::cp_async_commit();
   tc::cp_async_wait<0>();
@@ -342,7 +404,7 @@ __global__ void __launch_bounds__(512, 3) rows_held_kernel(const RowArgs p, cons
 #pragma unroll
           for (int j = 0; j < kU; ++j) u[j] += v[j];
         }
-        load_vec_any<kU>(p.weight, k, p.weight_dtype, v);
+        load_weight<kU, kShift>(p, k, v);
 #pragma unroll
         for (int j = 0; j < kU; ++j) { h[j] = u[j]; u[j] *= v[j]; }
       } else {
@@ -351,10 +413,11 @@ __global__ void __launch_bounds__(512, 3) rows_held_kernel(const RowArgs p, cons
       }
     }
   };
-  for (int k = (int)threadIdx.x * kU; k < p.cols; k += (int)blockDim.x * kU) {
+  const int first = (int)threadIdx.x * kU - (kShift ? off[0] : 0), step = (int)blockDim.x * kU;
+  for (int k = first; k < p.cols; k += step) {
     float u[kU], h[kU];
     units_of(k, u, h);
-    if (kOp == kRowNorm && p.sum) store_vec<kU>(static_cast<T*>(p.sum) + row * p.ld_sum + k, h);
+    if (kOp == kRowNorm && p.sum) store_sum<kU, kShift, T>(p, row, k, h);
 #pragma unroll
     for (int j = 0; j < kU; ++j) {
       if (kOp == kRowNorm) ss = fmaf(h[j], h[j], ss);
@@ -362,7 +425,7 @@ __global__ void __launch_bounds__(512, 3) rows_held_kernel(const RowArgs p, cons
     }
     if constexpr (!kVec) us[k] = u[0];
     else if (!again) {
-      uint4* at = reinterpret_cast<uint4*>(smem) + k / kE;
+      uint4* at = reinterpret_cast<uint4*>(smem) + (k + off[0]) / kE;
       at[0] = make_uint4(__float_as_uint(u[0]), __float_as_uint(u[1]), __float_as_uint(u[2]), __float_as_uint(u[3]));
       if constexpr (kE == 8)
         *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(at) + bytes) = make_uint4(__float_as_uint(u[4]), __float_as_uint(u[5]), __float_as_uint(u[6]), __float_as_uint(u[7]));
@@ -372,12 +435,12 @@ __global__ void __launch_bounds__(512, 3) rows_held_kernel(const RowArgs p, cons
   float inv, scale;
   row_scale(__uint_as_float(top), ss, kOp == kRowNorm ? rsqrtf(ss / (float)p.cols + p.eps) : 1.0f, inv, scale);
   if (threadIdx.x == 0) p.scales[row] = scale;
-  for (int k = (int)threadIdx.x * kU; k < p.cols; k += (int)blockDim.x * kU) {
+  for (int k = first; k < p.cols; k += step) {
     float u[kU], h[kU];
     if constexpr (!kVec) u[0] = us[k];
     else if (again) units_of(k, u, h);
     else {
-      const uint4* at = reinterpret_cast<const uint4*>(smem) + k / kE;
+      const uint4* at = reinterpret_cast<const uint4*>(smem) + (k + off[0]) / kE;
       load_vec<4>(reinterpret_cast<const float*>(at), *reinterpret_cast<float(*)[4]>(&u[0]));
       if constexpr (kE == 8)
         load_vec<4>(reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(at) + bytes), *reinterpret_cast<float(*)[4]>(&u[kE / 2]));
@@ -386,7 +449,7 @@ __global__ void __launch_bounds__(512, 3) rows_held_kernel(const RowArgs p, cons
 #pragma unroll
       for (int j = 0; j < kU; ++j) u[j] = 0.0f;
     }
-    write_codes<kU>(p, row, k, inv, scale, u);
+    write_codes<kU, kShift>(p, row, k, inv, scale, u);
   }
 }
 
@@ -403,15 +466,15 @@ static cudaError_t start(void (*kernel)(RowArgs), unsigned grid, unsigned thread
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-template <class T, RowOp kOp, bool kVec>
+template <class T, RowOp kOp, Lie kLie>
 static cudaError_t start_held(const RowArgs& a, cudaStream_t stream) {
   const int kE = 16 / (int)sizeof(T), bytes = (a.cols + 2 * kE - 2) / kE * 16;
-  const int smem = 2 * bytes + (kVec ? 0 : (a.cols + 3) / 4 * 16);
+  const int smem = 2 * bytes + (kLie != kAnyhow ? 0 : (a.cols + 3) / 4 * 16);
   if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(rows_held_kernel<T, kOp, kVec>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldBytes);
+    const cudaError_t e = cudaFuncSetAttribute(rows_held_kernel<T, kOp, kLie>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldBytes);
     if (e != cudaSuccess) return e;
   }
-  const int units = kVec ? a.cols / kE : a.cols;
+  const int units = kLie != kAnyhow ? bytes / 16 : a.cols;
   int threads = (units + 2) / 3;
   threads = threads < 64 ? 64 : (threads > 512 ? 512 : (threads + 31) / 32 * 32);
   cudaLaunchConfig_t cfg = {};
@@ -424,7 +487,7 @@ static cudaError_t start_held(const RowArgs& a, cudaStream_t stream) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, rows_held_kernel<T, kOp, kVec>, a, bytes);
+  return cudaLaunchKernelEx(&cfg, rows_held_kernel<T, kOp, kLie>, a, bytes);
 }
 // Whether a row fits the shared memory that lets three blocks share an SM.
 template <class T>
@@ -438,6 +501,30 @@ static bool whole(const void* p, int64_t ld, int size, int bytes) {
 }
 static int size_of(int dtype) { return dtype == AQD_F32 ? 4 : 2; }
 
+// Rows in vectors. A warp per row with up to 4 vectors a lane, where the rows fill the GPU that way; else a block, in registers with one
+// vector a thread (two, of 32-bit values or for few rows); longer rows in shared memory. (4096 rows of 4096 bf16, the norm: one
+// vector a thread 26 us, two 30, four 35; 4096 x 12288 f16, gated: four 85 us, three 74, read twice 69, in shared memory 56.)
+template <class T, RowOp kOp, bool kShift>
+static cudaError_t run_vectors(const RowArgs& a, cudaStream_t stream) {
+  constexpr int kE = 16 / sizeof(T);
+  const unsigned rows = (unsigned)a.rows;
+  auto block = [](int64_t n, int v) { return (unsigned)(((n + v - 1) / v + 31) / 32 * 32); };  // threads for n vectors, v each
+  if constexpr (kShift) {
+    // (4096 x 1001 bf16, the norm: 11.7 us, an element at a time 14.2; 500 x 5001 f16: in shared memory 7.5, in registers 8.8, an element
+    // at a time 11.2; 2000 x 7777 bf16: 43.8, 52.4, 55; 100 x 3001: in registers 3.3, in shared memory 4.4.)
+    const int64_t n = ((int64_t)a.cols + 2 * kE - 2) / kE;
+    if (n <= (rows > 304 ? 256 : 1024)) return start(rows_kernel<T, kOp, kE, 1, false, true>, rows, block(n, 1), a, stream);
+  } else {
+    const int64_t n = a.cols / kE;
+    if (n <= 32) return start(rows_kernel<T, kOp, kE, 1, true, false>, (rows + 7) / 8, 256, a, stream);
+    if (n <= 64 && rows > 608) return start(rows_kernel<T, kOp, kE, 2, true, false>, (rows + 7) / 8, 256, a, stream);
+    if (n <= 128 && rows > 608) return start(rows_kernel<T, kOp, kE, 4, true, false>, (rows + 7) / 8, 256, a, stream);
+    if (n <= 1024) return start(rows_kernel<T, kOp, kE, 1, false, false>, rows, block(n, 1), a, stream);
+    if (n <= 2048 && (kE == 4 || rows <= 304)) return start(rows_kernel<T, kOp, kE, 2, false, false>, rows, block(n, 2), a, stream);
+  }
+  return start_held<T, kOp, kShift ? kShifted : kWhole>(a, stream);
+}
+
 template <class T, RowOp kOp>
 static cudaError_t run(const RowArgs& a, cudaStream_t stream) {
   constexpr int kE = 16 / sizeof(T);
@@ -446,26 +533,25 @@ static cudaError_t run(const RowArgs& a, cudaStream_t stream) {
                    whole(a.codes, a.ld_codes, 1, kE) && whole(a.values, a.ld_values, vs, kE * vs > 16 ? 16 : kE * vs) &&
                    whole(a.weight, 0, 1, wbytes);
   const unsigned rows = (unsigned)a.rows;
-  auto block = [](int64_t n, int v) { return (unsigned)(((n + v - 1) / v + 31) / 32 * 32); };  // threads for n units, v each
+  auto block = [](int64_t n, int v) { return (unsigned)(((n + v - 1) / v + 31) / 32 * 32); };  // threads for n elements, v each
   if (vec) {
-    const int64_t n = a.cols / kE;
-    // A warp per row with up to 4 vectors a lane, where the rows fill the GPU that way; else a block, in registers with one vector a thread (two, of
-    // 32-bit values or for few rows); longer rows in shared memory. (4096 rows of 4096 bf16, the norm: one vector a thread 26 us, two 30,
-    // four 35; 4096 x 12288 f16, gated: four 85 us, three 74, read twice 69, in shared memory 56.)
-    if (n <= 32) return start(rows_kernel<T, kOp, kE, 1, true>, (rows + 7) / 8, 256, a, stream);
-    if (n <= 64 && rows > 608) return start(rows_kernel<T, kOp, kE, 2, true>, (rows + 7) / 8, 256, a, stream);
-    if (n <= 128 && rows > 608) return start(rows_kernel<T, kOp, kE, 4, true>, (rows + 7) / 8, 256, a, stream);
-    if (n <= 1024) return start(rows_kernel<T, kOp, kE, 1, false>, rows, block(n, 1), a, stream);
-    if (n <= 2048 && (kE == 4 || rows <= 304)) return start(rows_kernel<T, kOp, kE, 2, false>, rows, block(n, 2), a, stream);
-    if (held<T>(a, true)) return start_held<T, kOp, true>(a, stream);
+    if (a.cols <= 1024 * kE || held<T>(a, true)) return run_vectors<T, kOp, false>(a, stream);
     return start(rows_long_kernel<T, kOp, kE>, rows, 512, a, stream);
   }
+  // Whether every tensor's rows start at the same element of their vectors. (Up to 64 vectors the ends are too many of them: 4096 x 257
+  // bf16, the norm, 6.4 us, an element at a time 5.9; 4096 x 513 8.9 and 9.3.)
+  auto alike = [&](const void* p, int64_t ld, int size) {
+    return p == nullptr || ((reinterpret_cast<uintptr_t>(p) / size - reinterpret_cast<uintptr_t>(a.a) / ts) % kE == 0 && (ld - a.lda) % kE == 0);
+  };
+  if (alike(a.b, a.ldb, ts) && alike(a.sum, a.ld_sum, ts) && alike(a.codes, a.ld_codes, 1) && alike(a.values, a.ld_values, vs) &&
+      a.cols > 64 * kE && held<T>(a, true))
+    return run_vectors<T, kOp, true>(a, stream);
   // Rows at any address: an element at a time, neighbours by neighbours. (3000 x 3333 f16, gated: eight a thread 48 us, in shared memory
   // 32; 4096 x 1001 bf16, the norm: eight 14.2 us, in shared memory 29; 2000 x 7777: 68 and 55; 5000 x 777, gated: eight 15.5, four 11.7.)
-  if (a.cols <= 256 && rows > 608) return start(rows_kernel<T, kOp, 1, 8, true>, (rows + 7) / 8, 256, a, stream);
-  if (a.cols <= (kOp == kRowGated ? 2048 : 768)) return start(rows_kernel<T, kOp, 1, 4, false>, rows, block(a.cols, 4), a, stream);
-  if (kOp != kRowGated && a.cols <= 6144) return start(rows_kernel<T, kOp, 1, 8, false>, rows, block(a.cols, 8), a, stream);
-  if (held<T>(a, false)) return start_held<T, kOp, false>(a, stream);
+  if (a.cols <= 256 && rows > 608) return start(rows_kernel<T, kOp, 1, 8, true, false>, (rows + 7) / 8, 256, a, stream);
+  if (a.cols <= (kOp == kRowGated ? 2048 : 768)) return start(rows_kernel<T, kOp, 1, 4, false, false>, rows, block(a.cols, 4), a, stream);
+  if (kOp != kRowGated && a.cols <= 6144) return start(rows_kernel<T, kOp, 1, 8, false, false>, rows, block(a.cols, 8), a, stream);
+  if (held<T>(a, false)) return start_held<T, kOp, kAnyhow>(a, stream);
   return start(rows_long_kernel<T, kOp, 1>, rows, 512, a, stream);
 }
 template <class T>

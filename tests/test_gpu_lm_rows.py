@@ -123,6 +123,28 @@ def test_strides_and_addresses(cols, start, pad):
     check(g, act64(x.double(), "silu") * r.double(), None)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(700, 257), (700, 515), (310, 1537), (9, 1539), (400, 5003), (330, 8189), (5, 8189), (320, 9215), (3, 9213), (310, 18425)])
+def test_rows_that_start_inside_a_vector(rows, cols, dtype):
+    """Adjacent rows of odd widths: every tensor's rows start at the same place in their vectors, which is another for every row."""
+    x, r = normal(11, rows, cols).to(dtype), normal(12, rows, cols).to(dtype)
+    w = (1 + 0.3 * normal(13, cols)).to(dtype)
+    h = x.double() + r.double() if dtype != torch.float32 else (x + r).double()
+    q = aqd.rms_norm_quant(x, w, residual=r, values=True)
+    check(q, norm64(h, w, 1e-6), dtype)
+    assert torch.equal(q.summed, (x.float() + r.float()).to(dtype))
+    check(aqd.rms_norm_quant(x, w, values=torch.float32), norm64(x.double(), w, 1e-6), torch.float32)
+    check(aqd.quant_rows(x, values=torch.bfloat16), x.double(), torch.bfloat16)
+    x[:, 0], r[:, 0] = 3.0, 4.0
+    check(aqd.gated_act_quant(x, r, act="gelu_tanh", values=True), act64(x.double(), "gelu_tanh") * r.double(), dtype)
+    # whole vectors around the matrix stay as they are
+    room = torch.full((rows * cols + 64,), 7.0, dtype=dtype, device="cuda")
+    s = room[32:32 + rows * cols].view(rows, cols)
+    aqd.rms_norm_quant(x, w, residual=r, summed=s)
+    torch.cuda.synchronize()
+    assert torch.equal(s, (x.float() + r.float()).to(dtype)) and (room[:32] == 7).all() and (room[32 + rows * cols:] == 7).all()
+
+
 def test_leading_dimensions_and_broadcast_rows():
     x, w = normal(7, 2, 5, 3, 96).half(), torch.ones(96, device="cuda")
     check(aqd.rms_norm_quant(x, w), norm64(x.double(), w, 1e-6), None)
