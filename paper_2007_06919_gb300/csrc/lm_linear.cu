@@ -139,6 +139,19 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// Tokens' codes from rows at any address to rows that start on 16 bytes, 4 codes a thread.
+__global__ void __launch_bounds__(256) align_kernel(const int8_t* __restrict__ x, int64_t ldx, int32_t k, uint32_t* __restrict__ out, int64_t pitch) {
+  tc::grid_dep_wait();
+  const int i = (blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= k) return;
+  x += blockIdx.y * ldx + i;
+  uint32_t v = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (i + j < k) v |= (uint32_t)(uint8_t)x[j] << (8 * j);
+  out[(blockIdx.y * pitch + i) / 4] = v;
+}
+
 constexpr int kSmallWarps = 8;
 
 constexpr int small_bytes(int g, int r, int depth) {
@@ -155,7 +168,7 @@ constexpr int small_bytes(int g, int r, int depth) {
 // copies, the tokens' loads then waited for at each stage, 33; tokens as F16 once per block and K split
 // over a cluster, 20.)
 template <int kG, int kR, int kDepth, bool kLong>
-__global__ void __launch_bounds__(kSmallWarps * 32, 2) linear_ring_kernel(const LinArgs p) {
+__global__ void __launch_bounds__(kSmallWarps * 32, kG * kR == 16 ? 1 : 2) linear_ring_kernel(const LinArgs p) {
   extern __shared__ __align__(16) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int64_t pitch = ((int64_t)p.k + 127) / 128 * 128;
@@ -268,16 +281,23 @@ static cudaError_t run_ring(const LinArgs& a, cudaStream_t stream) {
   return cudaLaunchKernelEx(&cfg, linear_ring_kernel<kG, kR, kDepth, kLong>, a);
 }
 
-// Time of this kernel (us) for more than 16 tokens, fitted to n 1024 .. 16384, k 1024 .. 4096: throughput of a warp's pieces, or a warp's own chain.
-static float ring_estimate(const LinArgs& a) {
+// Time of this kernel (us) for more than 16 tokens, fitted to n 1024 .. 16384, k 1024 .. 12288: throughput of a warp's pieces, or a warp's own
+// chain. For more than 32 tokens, two row tiles a warp (and one block per SM) or one.
+static float pairs_of_rows(const LinArgs& a) {
+  const float blocks = (float)((a.n + 31) / 32) * (float)((a.m + 63) / 64);
+  return 3.0f + 0.164f * (float)((a.k + 63) / 64) * ceilf(blocks / 152.0f);
+}
+static float single_rows(const LinArgs& a) {
   const float k64 = (float)((a.k + 63) / 64), n = (float)a.n;
-  const float work = a.m <= 32 ? (n > 32 * 120 ? n / 32 * 0.62f : n / 16 * 0.5f) : n / 16 * 0.9f * (float)((a.m + 63) / 64);
+  if (a.m > 32) return 3.0f + 0.1f * k64 * ceilf((float)((a.n + 15) / 16) * (float)((a.m + 63) / 64) / 152.0f);
+  const float work = n > 32 * 120 ? n / 32 * 0.62f : n / 16 * 0.5f;
   return 3.0f + fmaxf(1e-3f * k64 * work, 0.05f * k64);
 }
+static float ring_estimate(const LinArgs& a) { return a.m <= 32 ? single_rows(a) : fminf(single_rows(a), pairs_of_rows(a)); }
 
 // Two row tiles a warp halve the work on the tokens' codes for each weight, and the blocks: they pay from about a block per SM on (16
-// tokens, K 4096: n 1024 2.7 us against 2.2, n 4096 6.5 against 6.8; 24 tokens, n 12288 18.2 against 22.4; one to eight tokens, n 12288 12.9
-// against 11.2: not there).
+// tokens, K 4096: n 1024 2.7 us against 2.2, n 4096 6.5 against 6.8; 24 tokens, n 12288 18.2 against 22.4; 64 tokens, n 4096 13.7 against 17.9,
+// n 2048 13.4 against 9.5; one to eight tokens, n 12288 12.9 against 11.2: not there).
 static int launch_ring(const LinArgs& a, cudaStream_t stream, std::string* err) {
   const bool longk = a.k > 16 * 64 * kSmallWarps, wide = a.n > 32 * 120;
   cudaError_t e;
@@ -286,6 +306,7 @@ static int launch_ring(const LinArgs& a, cudaStream_t stream, std::string* err) 
   else if (a.m <= 16) e = longk ? run_ring<2, 1, 4, true>(a, stream) : run_ring<2, 1, 4, false>(a, stream);
   else if (a.m <= 32 && wide && !longk) e = run_ring<4, 2, 3, false>(a, stream);  // (longk would spill)
   else if (a.m <= 32) e = longk ? run_ring<4, 1, 4, true>(a, stream) : run_ring<4, 1, 4, false>(a, stream);
+  else if (pairs_of_rows(a) < single_rows(a)) e = longk ? run_ring<8, 2, 3, true>(a, stream) : run_ring<8, 2, 3, false>(a, stream);
   else e = longk ? run_ring<8, 1, 3, true>(a, stream) : run_ring<8, 1, 3, false>(a, stream);
   if (e == cudaSuccess) e = cudaGetLastError();
   if (e != cudaSuccess) { *err = std::string("8-bit product launch: ") + cudaGetErrorString(e); return AQD_ERR_CUDA; }
@@ -311,10 +332,30 @@ int launch_linear_prepare(const int8_t* codes, int64_t ld, int32_t n, int32_t k,
 
 size_t linear_workspace_bytes(int64_t m, int32_t n, int32_t k) { return linear_tc_workspace_bytes(m, k); }
 
-int launch_linear(const LinArgs& a, cudaStream_t stream, std::string* err) {
-  const bool aligned = a.ldx % 16 == 0 && (reinterpret_cast<uintptr_t>(a.x) & 15) == 0;
+int launch_linear(const LinArgs& call, cudaStream_t stream, std::string* err) {
+  LinArgs a = call;
+  bool aligned = (a.m == 1 || a.ldx % 16 == 0) && (reinterpret_cast<uintptr_t>(a.x) & 15) == 0;
+  const float tc = a.m > 16 || !aligned ? linear_tc_estimate(a) : INFINITY;
+  // Few tokens at other addresses are copied to the workspace first (2 us; 16 tokens, n 4096, K 4100: the tensor cores, which take any address,
+  // 17.1 us; up to 16 aligned tokens never need these).
+  const int64_t pitch = ((int64_t)a.k + 15) / 16 * 16;
+  if (!aligned && a.m <= 64 && a.ws && a.ws_bytes >= (size_t)(a.m * pitch) && (a.m <= 16 || lin::ring_estimate(a) + 2.0f < tc)) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((a.k + 1023) / 1024), (unsigned)a.m);
+    cfg.blockDim = dim3(256);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, lin::align_kernel, a.x, a.ldx, a.k, reinterpret_cast<uint32_t*>(a.ws), pitch);
+    if (e != cudaSuccess) { *err = std::string("8-bit product launch: ") + cudaGetErrorString(e); return AQD_ERR_CUDA; }
+    a.x = reinterpret_cast<const int8_t*>(a.ws);
+    a.ldx = pitch;
+    return lin::launch_ring(a, stream, err);
+  }
   if (aligned && a.m <= 16) return lin::launch_ring(a, stream, err);
-  const float tc = linear_tc_estimate(a);
   if (tc < INFINITY && (!aligned || tc < lin::ring_estimate(a))) return launch_linear_tc(a, stream, err);
   // the tokens in pieces of the grid's second dimension
   const int64_t most = 65535LL * (aligned ? 64 : lin::kTM);
