@@ -1,12 +1,13 @@
 // lm_distill.cu -- distillation from a teacher's top logits: the loss of each token, its normalizer, and the gradient.
 //
-// Bound by memory: the logits are read once and the gradient written once. Between the normalizer's sum and the gradient a token's
+// The logits are read once and the gradient written once. Between the normalizer's sum and the gradient a token's
 // logits stay in shared memory, spread over the blocks of a cluster (up to 48 KB each, so that several blocks share an SM and
 // one's copies overlap another's sums and barriers), which join their (maximum, sum) through distributed shared memory. Every thread
 // reads only what it copied itself (cp.async), so the copies need no barrier. Tokens of a larger vocabulary than eight blocks
 // hold (1.6 MB of logits) are read a second time for the gradient. (2048 x 131072 bf16, loss and gradient: logits in registers 336 us,
-// in shared memory 230, 4.7 TB/s; a cluster for several tokens, the next one's copies under way: 358, the fewer blocks an SM
-// then holds have too few warps for the sums and exponentials, which take most of the issue slots.)
+// in shared memory 219, 4.9 TB/s; a cluster for several tokens, the next one's copies under way: 358, an SM
+// then holds too few warps for the sums and exponentials.) Bound by memory and, nearly as much, by the instructions of the two passes and of
+// each block's joins (70% of the issue slots): hence pairs of float32, and blocks that leave early where there is no gradient.
 //
 // q_v = exp(z_v - m) / s with z = x / tau: z_v - m is one multiply-add, rounded once, so that logits of any size
 // (a row of the type's lowest value too) keep their differences; then a multiplication by log2(e) and ex2.approx (within 2 units of 2^-23).
@@ -42,6 +43,36 @@ __device__ __forceinline__ float ex(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * kLog2e));
   return y;
+}
+
+// Two float32 at a time: half the instructions, which bound the passes over a row.
+__device__ __forceinline__ uint64_t two_of(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void one_each(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// exp(x rt - zero) of two values
+__device__ __forceinline__ uint64_t ex_two(float a, float b, float rt, float zero) {
+  one_each(mul2(fma2(two_of(a, b), two_of(rt, rt), two_of(-zero, -zero)), two_of(kLog2e, kLog2e)), a, b);
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+  return two_of(a, b);
 }
 
 // A 16-byte vector of T as float32 and back.
@@ -162,13 +193,15 @@ __device__ __forceinline__ float terms(const uint4& v, float rt, float zero) {
   constexpr int kE = Vec<T>::kE;
   float f[kE];
   Vec<T>::unpack(v, f);
+  uint64_t sum[kE / 2];
 #pragma unroll
-  for (int e = 0; e < kE; ++e) f[e] = ex(fmaf(f[e], rt, -zero));
+  for (int e = 0; e < kE / 2; ++e) sum[e] = ex_two(f[2 * e], f[2 * e + 1], rt, zero);
 #pragma unroll
-  for (int d = kE / 2; d > 0; d >>= 1)
+  for (int d = kE / 4; d > 0; d >>= 1)
 #pragma unroll
-    for (int e = 0; e < d; ++e) f[e] += f[e + d];
-  return f[0];
+    for (int e = 0; e < d; ++e) sum[e] = add2(sum[e], sum[e + d]);
+  one_each(sum[0], f[0], f[1]);
+  return f[0] + f[1];
 }
 
 // A token per cluster of `splits` blocks, each a range of its vectors. kStay: the range stays in shared memory.
@@ -216,7 +249,8 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
   }
   // the kept places; an empty one has index -1
   Soft t{-INFINITY, 0.0f};
-  for (int j = threadIdx.x; j < p.top; j += threads) {
+  const bool joins = g || rank == 0;  // (the loss alone: the first block of a cluster has it)
+  for (int j = threadIdx.x; joins && j < p.top; j += threads) {
     const int64_t i = p.index[row * p.top + j];
     const float z = p.teacher[row * p.top + j] * rt;
     const bool in = i >= 0 && i < p.vocab && z != -INFINITY;
@@ -256,20 +290,23 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
   // Every warp's share to every block of the cluster, then one barrier. (Also: no gradient is written in place before all
   // blocks have read their kept places' logits.)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = threads >> 5;
-  if (warp * 32 < p.top) t = lanes_join(t);
+  if (joins && warp * 32 < p.top) t = lanes_join(t);
   if (sums) s = lanes_join(s);
   if (lane == 0) swt[warp] = t;
   if (splits > 1) {
     cluster_wait();
-    if (lane < splits) {
+    if (lane < (g ? splits : 1)) {
       const uint32_t to = tc::mapa_shared(tc::smem_u32(&sws[rank * warps + warp]), (uint32_t)lane);
       asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(s.m), "f"(s.s) : "memory");
     }
-    tc::cluster_sync();
+    cluster_arrive();
+    if (!joins) return;
+    cluster_wait();
   } else {
     if (lane == 0) sws[warp] = s;
     __syncthreads();
   }
+  if (!g && warp != 0) return;
   t = lanes_join(lane < warps ? swt[lane] : Soft{-INFINITY, 0.0f});
   if (sums) {
     s = lane < splits * warps ? sws[lane] : Soft{-INFINITY, 0.0f};
@@ -296,21 +333,36 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
   if (!g) return;
   for (int j = threadIdx.x; j < p.top; j += threads) share[j] = sidx[j] >= 0 ? ex(sp[j] - t.m) / t.s : 0.0f;
   const float fs = f0 / s.s;
-  const int stores = whole ? 0 : INT_MAX;  // vectors from here on are stored whole
   uint4* gv = reinterpret_cast<uint4*>(g - off);
-#pragma unroll 2
-  for (int v = v0 + (int)threadIdx.x; v < v1; v += threads) {
-    const bool inside = v >= in0 && v < in1;
-    float f[kE];
-    if (live) {
-      Vec<T>::unpack(kStay ? held[v - v0] : inside ? __ldcs(xv + v) : load_edge(x, (int64_t)v * kE - off, p.vocab), f);
+  auto slopes = [&](int v, bool inside, float (&f)[kE]) {
+    Vec<T>::unpack(kStay ? held[v - v0] : inside ? __ldcs(xv + v) : load_edge(x, (int64_t)v * kE - off, p.vocab), f);
 #pragma unroll
-      for (int e = 0; e < kE; ++e) f[e] = fs * ex(fmaf(f[e], rt, -s.m));
-    } else {
+    for (int e = 0; e < kE; e += 2) one_each(mul2(ex_two(f[e], f[e + 1], rt, s.m), two_of(fs, fs)), f[e], f[e + 1]);
+  };
+  int v = v0 + (int)threadIdx.x;
+  if (live && whole) {
+    if (v < in0 && v < v1) {
+      float f[kE];
+      slopes(v, false, f);
+      store_edge(g, (int64_t)v * kE - off, p.vocab, f);
+      v += threads;
+    }
+    const int end = min(v1, in1);
+#pragma unroll 2
+    for (; v < end; v += threads) {
+      float f[kE];
+      slopes(v, true, f);
+      __stcs(gv + v, Vec<T>::pack(f));
+    }
+  }
+  for (; v < v1; v += threads) {  // the row's last vector; all, where the gradient lies otherwise than the logits, or is 0
+    float f[kE];
+    if (live) slopes(v, v >= in0 && v < in1, f);
+    else {
 #pragma unroll
       for (int e = 0; e < kE; ++e) f[e] = 0.0f;
     }
-    if (inside && v >= stores) __stcs(gv + v, Vec<T>::pack(f));
+    if (whole && v >= in0 && v < in1) __stcs(gv + v, Vec<T>::pack(f));
     else store_edge(g, (int64_t)v * kE - off, p.vocab, f);
   }
   if (!live) return;
