@@ -219,18 +219,34 @@ __global__ void __launch_bounds__(kSmallWarps * 32, kG * kR == 16 ? 1 : 2) linea
   for (int i = 0; i < mine; ++i) {
     tc::cp_async_wait<kDepth - 2>();
     const uint32_t from = ring + (uint32_t)(i % kDepth) * (kPieces * 512);
-    uint32_t wf[2 * kR][8];
+    if constexpr (kR < 3) {  // the weights wait in registers
+      uint32_t wf[2 * kR][8];
 #pragma unroll
-    for (int r = 0; r < 2 * kR; ++r) piece_to_f16(lds128(from + r * 512), 0u, wf[r]);
+      for (int r = 0; r < 2 * kR; ++r) piece_to_f16(lds128(from + r * 512), 0u, wf[r]);
 #pragma unroll
-    for (int j = 0; j < kG; ++j) {
-      uint32_t xf[8];
-      piece_to_f16(lds128(from + (2 * kR + j) * 512), 0x80808080u, xf);
+      for (int j = 0; j < kG; ++j) {
+        uint32_t xf[8];
+        piece_to_f16(lds128(from + (2 * kR + j) * 512), 0x80808080u, xf);
 #pragma unroll
-      for (int r = 0; r < kR; ++r)
+        for (int r = 0; r < kR; ++r)
+#pragma unroll
+          for (int q = 0; q < 8; q += 2)
+            mma_16816(d[r][j], wf[2 * r][q], wf[2 * r + 1][q], wf[2 * r][q + 1], wf[2 * r + 1][q + 1], xf[q], xf[q + 1]);
+      }
+    } else {  // the tokens do
+      uint32_t xf[kG][8];
+#pragma unroll
+      for (int j = 0; j < kG; ++j) piece_to_f16(lds128(from + (2 * kR + j) * 512), 0x80808080u, xf[j]);
+#pragma unroll
+      for (int r = 0; r < kR; ++r) {
+        uint32_t lo[8], hi[8];
+        piece_to_f16(lds128(from + 2 * r * 512), 0u, lo);
+        piece_to_f16(lds128(from + (2 * r + 1) * 512), 0u, hi);
 #pragma unroll
         for (int q = 0; q < 8; q += 2)
-          mma_16816(d[r][j], wf[2 * r][q], wf[2 * r + 1][q], wf[2 * r][q + 1], wf[2 * r + 1][q + 1], xf[q], xf[q + 1]);
+#pragma unroll
+          for (int j = 0; j < kG; ++j) mma_16816(d[r][j], lo[q], hi[q], lo[q + 1], hi[q + 1], xf[j][q], xf[j][q + 1]);
+      }
     }
     fetch(i + kDepth - 1);
     if (kLong && (i & 15) == 15) {
@@ -282,33 +298,43 @@ static cudaError_t run_ring(const LinArgs& a, cudaStream_t stream) {
   return cudaLaunchKernelEx(&cfg, linear_ring_kernel<kG, kR, kDepth, kLong>, a);
 }
 
-// Time of this kernel (us) for more than 16 tokens, fitted to n 1024 .. 16384, k 1024 .. 12288: throughput of a warp's pieces, or a warp's own
-// chain. For more than 32 tokens, two row tiles a warp (and one block per SM) or one.
-static float pairs_of_rows(const LinArgs& a) {
-  const float blocks = (float)((a.n + 31) / 32) * (float)((a.m + 63) / 64);
-  return 3.0f + 0.164f * (float)((a.k + 63) / 64) * ceilf(blocks / 152.0f);
+// Time of this kernel (us) with r row tiles a warp, for the launch that takes m tokens in groups of 8: a launch's fill and drain, and
+// blocks per SM times a block's share of an SM, most of which grows with K. Fitted to n 1024 .. 16384, K 1024 .. 12288. More row tiles halve, or
+// third, the work on the tokens' codes for each weight, and the blocks, so the best count follows from how the blocks fill the SMs (K 4096, 1, 2 and 3 row
+// tiles: 24 tokens, n 2048 5.6, 7.6 and 8.8 us; n 6144 11.2, 11.1, 9.4; n 8192 13.9, 11.4, 14.3; n 12288 19.4, 16.6, 14.8; 16 tokens, n 12288 15.1, 13.2,
+// 12.2; 64 tokens, n 2048 9.5 and 13.4, n 4096 17.9 and 13.6). 0: no such kernel (it would spill registers), or never the best (up to 8 tokens,
+// n 12288 11.5 and 10.9, n 16384 13.5 and 15.0).
+static int groups_of(int64_t m) { return m <= 8 ? 1 : m <= 16 ? 2 : m <= 24 ? 3 : m <= 32 ? 4 : 8; }
+static float ring_time(const LinArgs& a, int r) {
+  static constexpr float kTime[9][3][2] = {{}, {{3.1f, 1.45f}}, {{2.7f, 2.1f}, {2.2f, 3.65f}, {2.6f, 4.85f}}, {{2.6f, 2.85f}, {3.2f, 4.3f}, {2.9f, 5.8f}},
+                                           {{2.6f, 3.3f}, {3.3f, 4.95f}}, {}, {}, {}, {{0.9f, 8.5f}, {1.3f, 12.3f}}};
+  const int g = groups_of(a.m);
+  const float *t = kTime[g][r - 1], grows = g == 8 ? 0.75f : 0.9f;
+  if (t[1] == 0.0f || (a.k > 16 * 64 * kSmallWarps && (r == 3 || (r == 2 && (g == 3 || g == 4))))) return INFINITY;
+  const float blocks = (float)(((int64_t)a.n + 16 * r - 1) / (16 * r)) * (float)((a.m + 8 * g - 1) / (8 * g));
+  return t[0] + t[1] * ceilf(blocks / 152.0f) * (1.0f - grows + grows * (float)((a.k + 63) / 64) / 64.0f);
 }
-static float single_rows(const LinArgs& a) {
-  const float k64 = (float)((a.k + 63) / 64), n = (float)a.n;
-  if (a.m > 32) return 3.0f + 0.1f * k64 * ceilf((float)((a.n + 15) / 16) * (float)((a.m + 63) / 64) / 152.0f);
-  const float work = n > 32 * 120 ? n / 32 * 0.62f : n / 16 * 0.5f;
-  return 3.0f + fmaxf(1e-3f * k64 * work, 0.05f * k64);
+static int ring_tiles(const LinArgs& a) {  // the row tiles of the fastest
+  const float t[3] = {ring_time(a, 1), ring_time(a, 2), ring_time(a, 3)};
+  return t[2] < t[1] && t[2] < t[0] ? 3 : t[1] < t[0] ? 2 : 1;
 }
-static float ring_estimate(const LinArgs& a) { return a.m <= 32 ? single_rows(a) : fminf(single_rows(a), pairs_of_rows(a)); }
+static float ring_estimate(const LinArgs& a) { return ring_time(a, ring_tiles(a)); }
 
-// Two row tiles a warp halve the work on the tokens' codes for each weight, and the blocks: they pay from about a block per SM on (16
-// tokens, K 4096: n 1024 2.7 us against 2.2, n 4096 6.5 against 6.8; 24 tokens, n 12288 18.2 against 22.4; 64 tokens, n 4096 13.7 against 17.9,
-// n 2048 13.4 against 9.5; one to eight tokens, n 12288 12.9 against 11.2: not there).
 static int launch_ring(const LinArgs& a, cudaStream_t stream, std::string* err) {
-  const bool longk = a.k > 16 * 64 * kSmallWarps, wide = a.n > 32 * 120;
+  const bool longk = a.k > 16 * 64 * kSmallWarps;
+  const int g = groups_of(a.m), r = ring_tiles(a);
   cudaError_t e;
-  if (a.m <= 8) e = longk ? run_ring<1, 1, 4, true>(a, stream) : run_ring<1, 1, 4, false>(a, stream);
-  else if (a.m <= 16 && wide) e = longk ? run_ring<2, 2, 4, true>(a, stream) : run_ring<2, 2, 4, false>(a, stream);
-  else if (a.m <= 16) e = longk ? run_ring<2, 1, 4, true>(a, stream) : run_ring<2, 1, 4, false>(a, stream);
-  else if (a.m <= 32 && wide && !longk) e = run_ring<4, 2, 3, false>(a, stream);  // (longk would spill)
-  else if (a.m <= 32) e = longk ? run_ring<4, 1, 4, true>(a, stream) : run_ring<4, 1, 4, false>(a, stream);
-  else if (pairs_of_rows(a) < single_rows(a)) e = longk ? run_ring<8, 2, 3, true>(a, stream) : run_ring<8, 2, 3, false>(a, stream);
-  else e = longk ? run_ring<8, 1, 3, true>(a, stream) : run_ring<8, 1, 3, false>(a, stream);
+  if (g == 1) e = longk ? run_ring<1, 1, 4, true>(a, stream) : run_ring<1, 1, 4, false>(a, stream);
+  else if (g == 2 && r == 1) e = longk ? run_ring<2, 1, 4, true>(a, stream) : run_ring<2, 1, 4, false>(a, stream);
+  else if (g == 2 && r == 2) e = longk ? run_ring<2, 2, 4, true>(a, stream) : run_ring<2, 2, 4, false>(a, stream);
+  else if (g == 2) e = run_ring<2, 3, 3, false>(a, stream);
+  else if (g == 3 && r == 1) e = longk ? run_ring<3, 1, 4, true>(a, stream) : run_ring<3, 1, 4, false>(a, stream);
+  else if (g == 3 && r == 2) e = run_ring<3, 2, 3, false>(a, stream);
+  else if (g == 3) e = run_ring<3, 3, 3, false>(a, stream);
+  else if (g == 4 && r == 1) e = longk ? run_ring<4, 1, 4, true>(a, stream) : run_ring<4, 1, 4, false>(a, stream);
+  else if (g == 4) e = run_ring<4, 2, 3, false>(a, stream);
+  else if (r == 1) e = longk ? run_ring<8, 1, 3, true>(a, stream) : run_ring<8, 1, 3, false>(a, stream);
+  else e = longk ? run_ring<8, 2, 3, true>(a, stream) : run_ring<8, 2, 3, false>(a, stream);
   if (e == cudaSuccess) e = cudaGetLastError();
   if (e != cudaSuccess) { *err = std::string("8-bit product launch: ") + cudaGetErrorString(e); return AQD_ERR_CUDA; }
   return 0;
