@@ -25,7 +25,7 @@ namespace aqd {
 namespace rows {
 
 constexpr float kTiny = 7.52316385e-37f;  // 2^-120: 127 / a stays finite above it
-constexpr int kHeldBytes = 72 * 1024;
+constexpr int kHeldBytes = 72 * 1024;  // shared memory of a held row: three blocks share an SM
 constexpr float kRound = 12582912.0f;     // 1.5 * 2^23: x + kRound has x rounded to nearest even in its low bits, for |x| < 2^22
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
@@ -113,6 +113,27 @@ template <int kE, bool kShift, class T>
 __device__ __forceinline__ void load_at(const T* p, int k, int cols, float (&f)[kE]) {
   if (inside<kE, kShift>(k, cols)) load_vec<kE>(p, f);
   else load_each<kE>(p - k, k, cols, f);
+}
+// kE values from shared memory, element `at` of a vector that starts on 16 bytes: out of the two aligned vectors that hold them, the words
+// picked by the distance.
+template <int kE, class T>
+__device__ __forceinline__ void load_across(const T* from, int at, float (&f)[kE]) {
+  static_assert(kE * sizeof(T) == 16, "");
+  const int s = at % kE, q = s * (int)sizeof(T) / 4;  // elements, and words, into the first
+  const uint4* v = reinterpret_cast<const uint4*>(from) + at / kE;
+  const uint4 lo = v[0], hi = v[s ? 1 : 0];
+  uint32_t x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+  for (int i = 0; i < 6; ++i) x[i] = q & 2 ? x[i + 2] : x[i];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) x[i] = q & 1 ? x[i + 1] : x[i];
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(x[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2<T>(__funnelshift_r(x[i], x[i + 1], (s & 1) * 16), f[2 * i], f[2 * i + 1]);
+  }
 }
 // the norm's weights, which do not start where a row does: element by element for kShift. (Out of two aligned vectors, the words picked
 // by the distance: no faster, 4096 x 1001 bf16 12.3 us to 11.8.)
@@ -340,18 +361,18 @@ __global__ void __launch_bounds__(512) rows_long_kernel(const RowArgs p) {
 }
 
 // How the rows lie for rows_held_kernel: whole vectors; whole but for their ends (they start at the same element of a vector
-// in every tensor but the weights); or anyhow.
-enum Lie { kWhole, kShifted, kAnyhow };
+// in every tensor but the weights); so the outputs alone, and the inputs anyhow; or all anyhow.
+enum Lie { kWhole, kShifted, kLoose, kAnyhow };
 
 // One block per row, which waits in shared memory: all of it is on its way at once, and few registers let several blocks share an SM. A
 // thread copies, and later reads, its own vectors, and u takes the place of the two inputs that it came from (a single
-// input of 16 bits is read twice instead). kAnyhow: whole vectors of the aligned memory that holds the rows, their edges element by
-// element, and u in a place of its own; the threads then take the row's elements in turn.
+// input of 16 bits is read twice instead). kLoose, kAnyhow: whole vectors of the aligned memory that holds the rows, their edges element by
+// element, and u in a place of its own; the threads then take the outputs' vectors, or the row's elements, in turn.
 template <class T, RowOp kOp, Lie kLie>
-__global__ void __launch_bounds__(512, kLie == kShifted && kOp == kRowNorm ? 2 : 3) rows_held_kernel(const RowArgs p, const int bytes) {
-  extern __shared__ __align__(16) uint8_t smem[];  // a, then b (`bytes` each), then u (kAnyhow)
+__global__ void __launch_bounds__(512, (kLie == kShifted && kOp == kRowNorm) || kLie == kLoose ? 2 : 3) rows_held_kernel(const RowArgs p, const int bytes) {
+  extern __shared__ __align__(16) uint8_t smem[];  // a, then b (`bytes` each), then u (kLoose, kAnyhow)
   constexpr int kE = 16 / sizeof(T);
-  constexpr bool kVec = kLie != kAnyhow, kShift = kLie == kShifted;
+  constexpr bool kVec = kLie != kAnyhow, kOwn = kLie == kWhole || kLie == kShifted, kShift = kLie == kShifted || kLie == kLoose;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int64_t row = blockIdx.x;
   const bool two = kOp == kRowGated || (kOp == kRowNorm && p.b);
@@ -367,7 +388,7 @@ __global__ void __launch_bounds__(512, kLie == kShifted && kOp == kRowNorm ? 2 :
       v0 = off[i] > 0;
       v1 = (off[i] + p.cols) / kE;
     }
-    if constexpr (kLie == kAnyhow) {
+    if constexpr (!kOwn) {
       // the edges, an element a thread: the first kE - off, and those from vector v1 on
       const int t = threadIdx.x, k = t < 32 ? t : v1 * kE - off[i] + t - 32;
       if (t < 32 ? v0 > 0 && k < kE - off[i] && k < p.cols : t < 32 + kE && k >= 0 && k < p.cols)
@@ -387,18 +408,33 @@ __global__ void __launch_bounds__(512, kLie == kShifted && kOp == kRowNorm ? 2 :
   }
   tc::cp_async_commit();
   tc::cp_async_wait<0>();
-  if (!kVec) __syncthreads();
+  if (!kOwn) __syncthreads();
   float ss = 0.0f;
   uint32_t top = 0;
   constexpr int kU = kVec ? kE : 1;
-  const bool again = kVec && sizeof(T) == 2 && !two;  // u is computed twice
+  const bool again = kOwn && sizeof(T) == 2 && !two;  // u is computed twice
   float* us = reinterpret_cast<float*>(smem + 2 * bytes);
+  int out = kShift ? off[0] : 0;  // the outputs' first element's place in its vector
+  if constexpr (kLie == kLoose) {
+    if (p.codes) out = (int)(reinterpret_cast<uintptr_t>(p.codes + row * p.ld_codes) % kE);
+    else {
+      const int size = p.values_dtype == AQD_F32 ? 4 : 2;
+      out = (int)(((reinterpret_cast<uintptr_t>(p.values) / size) + row * p.ld_values) % kE);
+    }
+  }
+  // kU values from element k of an input on
+  auto input = [&](int i, int k, float (&f)[kU]) {
+    const T* from = reinterpret_cast<const T*>(smem + i * bytes);
+    if constexpr (kLie != kLoose) load_vec<kU>(from + off[i] + k, f);
+    else if (inside<kU, true>(k, p.cols)) load_across<kU>(from, off[i] + k, f);
+    else load_each<kU>(from + off[i], k, p.cols, f);
+  };
   // kU values from element k on: u and, under the norm, h
   auto units_of = [&](int k, float (&u)[kU], float (&h)[kU]) {
-    load_vec<kU>(reinterpret_cast<const T*>(smem) + off[0] + k, u);
+    input(0, k, u);
     if constexpr (kOp != kRowPlain) {
       float v[kU];
-      if (two) load_vec<kU>(reinterpret_cast<const T*>(smem + bytes) + off[1] + k, v);
+      if (two) input(1, k, v);
       if constexpr (kOp == kRowNorm) {
         if (two) {
 #pragma unroll
@@ -413,7 +449,7 @@ __global__ void __launch_bounds__(512, kLie == kShifted && kOp == kRowNorm ? 2 :
       }
     }
   };
-  const int first = (int)threadIdx.x * kU - (kShift ? off[0] : 0), step = (int)blockDim.x * kU;
+  const int first = (int)threadIdx.x * kU - out, step = (int)blockDim.x * kU;
   for (int k = first; k < p.cols; k += step) {
     float u[kU], h[kU];
     units_of(k, u, h);
@@ -423,9 +459,9 @@ __global__ void __launch_bounds__(512, kLie == kShifted && kOp == kRowNorm ? 2 :
       if (kOp == kRowNorm) ss = fmaf(h[j], h[j], ss);
       top = max(top, __float_as_uint(fabsf(u[j])));
     }
-    if constexpr (!kVec) us[k] = u[0];
+    if constexpr (!kOwn) store_vec<kU>(us + k + out, u);
     else if (!again) {
-      uint4* at = reinterpret_cast<uint4*>(smem) + (k + off[0]) / kE;
+      uint4* at = reinterpret_cast<uint4*>(smem) + (k + out) / kE;
       at[0] = make_uint4(__float_as_uint(u[0]), __float_as_uint(u[1]), __float_as_uint(u[2]), __float_as_uint(u[3]));
       if constexpr (kE == 8)
         *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(at) + bytes) = make_uint4(__float_as_uint(u[4]), __float_as_uint(u[5]), __float_as_uint(u[6]), __float_as_uint(u[7]));
@@ -437,10 +473,10 @@ __global__ void __launch_bounds__(512, kLie == kShifted && kOp == kRowNorm ? 2 :
   if (threadIdx.x == 0) p.scales[row] = scale;
   for (int k = first; k < p.cols; k += step) {
     float u[kU], h[kU];
-    if constexpr (!kVec) u[0] = us[k];
+    if constexpr (!kOwn) load_vec<kU>(us + k + out, u);
     else if (again) units_of(k, u, h);
     else {
-      const uint4* at = reinterpret_cast<const uint4*>(smem) + (k + off[0]) / kE;
+      const uint4* at = reinterpret_cast<const uint4*>(smem) + (k + out) / kE;
       load_vec<4>(reinterpret_cast<const float*>(at), *reinterpret_cast<float(*)[4]>(&u[0]));
       if constexpr (kE == 8)
         load_vec<4>(reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(at) + bytes), *reinterpret_cast<float(*)[4]>(&u[kE / 2]));
@@ -469,13 +505,14 @@ static cudaError_t start(void (*kernel)(RowArgs), unsigned grid, unsigned thread
 template <class T, RowOp kOp, Lie kLie>
 static cudaError_t start_held(const RowArgs& a, cudaStream_t stream) {
   const int kE = 16 / (int)sizeof(T), bytes = (a.cols + 2 * kE - 2) / kE * 16;
-  const int smem = 2 * bytes + (kLie != kAnyhow ? 0 : (a.cols + 3) / 4 * 16);
+  const int smem = 2 * bytes + (kLie < kLoose ? 0 : bytes / 16 * kE * 4);
   if (smem > 48 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(rows_held_kernel<T, kOp, kLie>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldBytes);
     if (e != cudaSuccess) return e;
   }
   const int units = kLie != kAnyhow ? bytes / 16 : a.cols;
-  int threads = (units + 2) / 3;
+  // (three vectors a thread; four of kLoose, whose registers are more: 3000 x 3333 f16, gated, 20.3 us, three 22.2, two 24.8)
+  int threads = kLie == kLoose ? (units + 3) / 4 : (units + 2) / 3;
   threads = threads < 64 ? 64 : (threads > 512 ? 512 : (threads + 31) / 32 * 32);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)a.rows);
@@ -489,11 +526,11 @@ static cudaError_t start_held(const RowArgs& a, cudaStream_t stream) {
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, rows_held_kernel<T, kOp, kLie>, a, bytes);
 }
-// Whether a row fits the shared memory that lets three blocks share an SM.
+// Whether a row fits its share of an SM's shared memory.
 template <class T>
-static bool held(const RowArgs& a, bool vec) {
-  const int64_t kE = 16 / (int)sizeof(T), bytes = (a.cols + 2 * kE - 2) / kE * 16;
-  return 2 * bytes + (vec ? 0 : (int64_t)(a.cols + 3) / 4 * 16) <= kHeldBytes;
+static bool held(const RowArgs& a, Lie lie) {
+  const int64_t kE = 16 / (int)sizeof(T), bytes = ((int64_t)a.cols + 2 * kE - 2) / kE * 16;
+  return 2 * bytes + (lie < kLoose ? 0 : bytes / 16 * kE * 4) <= kHeldBytes;
 }
 
 static bool whole(const void* p, int64_t ld, int size, int bytes) {
@@ -535,23 +572,29 @@ static cudaError_t run(const RowArgs& a, cudaStream_t stream) {
   const unsigned rows = (unsigned)a.rows;
   auto block = [](int64_t n, int v) { return (unsigned)(((n + v - 1) / v + 31) / 32 * 32); };  // threads for n elements, v each
   if (vec) {
-    if (a.cols <= 1024 * kE || held<T>(a, true)) return run_vectors<T, kOp, false>(a, stream);
+    if (a.cols <= 1024 * kE || held<T>(a, kWhole)) return run_vectors<T, kOp, false>(a, stream);
     return start(rows_long_kernel<T, kOp, kE>, rows, 512, a, stream);
   }
   // Whether every tensor's rows start at the same element of their vectors. (Up to 64 vectors the ends are too many of them: 4096 x 257
   // bf16, the norm, 6.4 us, an element at a time 5.9; 4096 x 513 8.9 and 9.3.)
-  auto alike = [&](const void* p, int64_t ld, int size) {
-    return p == nullptr || ((reinterpret_cast<uintptr_t>(p) / size - reinterpret_cast<uintptr_t>(a.a) / ts) % kE == 0 && (ld - a.lda) % kE == 0);
+  auto alike = [&](const void* p, int64_t ld, int size, const void* q, int64_t ldq, int sizeq) {
+    return p == nullptr || q == nullptr ||
+           ((reinterpret_cast<uintptr_t>(p) / size - reinterpret_cast<uintptr_t>(q) / sizeq) % kE == 0 && (ld - ldq) % kE == 0);
   };
-  if (alike(a.b, a.ldb, ts) && alike(a.sum, a.ld_sum, ts) && alike(a.codes, a.ld_codes, 1) && alike(a.values, a.ld_values, vs) &&
-      a.cols > 64 * kE && held<T>(a, true))
-    return run_vectors<T, kOp, true>(a, stream);
-  // Rows at any address: an element at a time, neighbours by neighbours. (3000 x 3333 f16, gated: eight a thread 48 us, in shared memory
-  // 32; 4096 x 1001 bf16, the norm: eight 14.2 us, in shared memory 29; 2000 x 7777: 68 and 55; 5000 x 777, gated: eight 15.5, four 11.7.)
+  const bool outputs = alike(a.sum, a.ld_sum, ts, a.codes, a.ld_codes, 1) && alike(a.values, a.ld_values, vs, a.codes, a.ld_codes, 1) &&
+                       alike(a.sum, a.ld_sum, ts, a.values, a.ld_values, vs);
+  const bool all = outputs && alike(a.b, a.ldb, ts, a.a, a.lda, ts) && alike(a.codes, a.ld_codes, 1, a.a, a.lda, ts) &&
+                   alike(a.values, a.ld_values, vs, a.a, a.lda, ts);
+  if (all && a.cols > 64 * kE && held<T>(a, kShifted)) return run_vectors<T, kOp, true>(a, stream);
+  // The outputs' rows alike, the inputs' not (the two halves of rows of an odd width): 3000 x 3333 f16, gated, 20.3 us, an element at a time 32;
+  // 1000 x 2049 bf16 6.8 and 11.5; 5000 x 777 13.6 and 11.6.
+  if (outputs && a.cols > 2048 && held<T>(a, kLoose)) return start_held<T, kOp, kLoose>(a, stream);
+  // Rows at any address: an element at a time, neighbours by neighbours. (4096 x 1001 bf16, the norm: eight 14.2 us, in shared memory
+  // 29; 2000 x 7777: 68 and 55; 5000 x 777, gated: eight 15.5, four 11.7.)
   if (a.cols <= 256 && rows > 608) return start(rows_kernel<T, kOp, 1, 8, true, false>, (rows + 7) / 8, 256, a, stream);
   if (a.cols <= (kOp == kRowGated ? 2048 : 768)) return start(rows_kernel<T, kOp, 1, 4, false, false>, rows, block(a.cols, 4), a, stream);
   if (kOp != kRowGated && a.cols <= 6144) return start(rows_kernel<T, kOp, 1, 8, false, false>, rows, block(a.cols, 8), a, stream);
-  if (held<T>(a, false)) return start_held<T, kOp, kAnyhow>(a, stream);
+  if (held<T>(a, kAnyhow)) return start_held<T, kOp, kAnyhow>(a, stream);
   return start(rows_long_kernel<T, kOp, 1>, rows, 512, a, stream);
 }
 template <class T>

@@ -145,6 +145,27 @@ def test_rows_that_start_inside_a_vector(rows, cols, dtype):
     assert torch.equal(s, (x.float() + r.float()).to(dtype)) and (room[:32] == 7).all() and (room[32 + rows * cols:] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [2049, 3335, 6001, 9001])
+def test_inputs_that_lie_otherwise_than_the_outputs(cols, dtype):
+    """The two halves of rows of an odd width, and of a wider matrix: the inputs start at other places in their vectors than the outputs."""
+    rows = 37
+    both = normal(14, rows, 2 * cols).to(dtype)
+    x, r = both.chunk(2, dim=1)
+    w = (1 + 0.3 * normal(15, cols)).to(dtype)
+    h = x.double() + r.double() if dtype != torch.float32 else (x + r).double()
+    q = aqd.rms_norm_quant(x, w, residual=r, values=True)
+    check(q, norm64(h, w, 1e-6), dtype)
+    assert torch.equal(q.summed, (x.float() + r.float()).to(dtype))
+    check(aqd.quant_rows(r, values=torch.float32), r.double(), torch.float32)
+    v = aqd.quant_rows(r, codes=False, values=torch.float16)
+    torch.cuda.synchronize()
+    assert torch.equal(v.values, aqd.quant_rows(r, values=torch.float16).values)
+    wide = normal(16, rows, cols + 5).to(dtype)[:, 3:3 + cols]
+    wide[:, 0], x[:, 0] = 3.0, 4.0
+    check(aqd.gated_act_quant(wide, x, values=True), act64(wide.double(), "silu") * x.double(), dtype)
+
+
 def test_leading_dimensions_and_broadcast_rows():
     x, w = normal(7, 2, 5, 3, 96).half(), torch.ones(96, device="cuda")
     check(aqd.rms_norm_quant(x, w), norm64(x.double(), w, 1e-6), None)
