@@ -6,8 +6,9 @@
 // over the row gives as sum h^2; the scale takes the factor.
 //
 // All three are bound by memory, and a row's codes need all of it: it waits on chip in between, so it is read once. Short rows
-// wait in registers (rows_kernel: a warp or a block each), longer ones in shared memory (rows_held_kernel), and rows longer
-// than that are read twice, the second time from L2 (rows_long_kernel). 16-byte accesses where all tensors allow them.
+// wait in registers (rows_kernel: a warp or a block each), longer ones in shared memory (rows_held_kernel), of a block or of a cluster's
+// blocks, and rows longer than that are read twice, the second time from L2 (rows_long_kernel). 16-byte accesses where the
+// tensors lie so that these are possible.
 // (4096 x 4096 bf16, the norm with its residual, codes and values: 26 us, 5.8 TB/s; 4096 x 12288 f16, gated: 56 us, 6.2 TB/s.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -368,13 +369,28 @@ enum Lie { kWhole, kShifted, kLoose, kAnyhow };
 // thread copies, and later reads, its own vectors, and u takes the place of the two inputs that it came from (a single
 // input of 16 bits is read twice instead). kLoose, kAnyhow: whole vectors of the aligned memory that holds the rows, their edges element by
 // element, and u in a place of its own; the threads then take the outputs' vectors, or the row's elements, in turn.
-template <class T, RowOp kOp, Lie kLie>
-__global__ void __launch_bounds__(512, (kLie == kShifted && kOp == kRowNorm) || kLie == kLoose ? 2 : 3) rows_held_kernel(const RowArgs p, const int bytes) {
-  extern __shared__ __align__(16) uint8_t smem[];  // a, then b (`bytes` each), then u (kLoose, kAnyhow)
+// kSplit (of kWhole): a cluster of `splits` blocks per row, `part` columns each, which join their statistics.
+template <class T, RowOp kOp, Lie kLie, bool kSplit>
+__global__ void __launch_bounds__(512, (kLie == kShifted && kOp == kRowNorm) || kLie == kLoose ? 2 : 3)
+rows_held_kernel(const RowArgs call, const int bytes, const int splits, const int part) {
+  extern __shared__ __align__(16) uint8_t smem[];  // a, then b where there are two (`bytes` each), then u (kLoose, kAnyhow)
   constexpr int kE = 16 / sizeof(T);
+  __shared__ uint2 joined[kSplit ? 8 : 1];  // every block's statistics
+  RowArgs p = call;
+  if constexpr (kSplit) {  // from here on a row is this block's part of it
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // (waited for before the first store into another block)
+    const int64_t k0 = (int64_t)blockIdx.x * part;
+    p.cols = min(part, call.cols - (int)k0);
+    p.a = static_cast<const T*>(p.a) + k0;
+    if (p.b) p.b = static_cast<const T*>(p.b) + k0;
+    if (p.sum) p.sum = static_cast<T*>(p.sum) + k0;
+    if (p.weight) p.weight = static_cast<const uint8_t*>(p.weight) + k0 * (p.weight_dtype == AQD_F32 ? 4 : 2);
+    if (p.codes) p.codes += k0;
+    if (p.values) p.values = static_cast<uint8_t*>(p.values) + k0 * (p.values_dtype == AQD_F32 ? 4 : 2);
+  }
   constexpr bool kVec = kLie != kAnyhow, kOwn = kLie == kWhole || kLie == kShifted, kShift = kLie == kShifted || kLie == kLoose;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int64_t row = blockIdx.x;
+  const int64_t row = kSplit ? blockIdx.y : blockIdx.x;
   const bool two = kOp == kRowGated || (kOp == kRowNorm && p.b);
   const T* ab[2] = {static_cast<const T*>(p.a) + row * p.lda, static_cast<const T*>(p.b) + row * p.ldb};
   int off[2] = {0, 0};
@@ -413,7 +429,7 @@ __global__ void __launch_bounds__(512, (kLie == kShifted && kOp == kRowNorm) || 
   uint32_t top = 0;
   constexpr int kU = kVec ? kE : 1;
   const bool again = kOwn && sizeof(T) == 2 && !two;  // u is computed twice
-  float* us = reinterpret_cast<float*>(smem + 2 * bytes);
+  float* us = reinterpret_cast<float*>(smem + (two ? 2 : 1) * bytes);
   int out = kShift ? off[0] : 0;  // the outputs' first element's place in its vector
   if constexpr (kLie == kLoose) {
     if (p.codes) out = (int)(reinterpret_cast<uintptr_t>(p.codes + row * p.ld_codes) % kE);
@@ -468,9 +484,22 @@ __global__ void __launch_bounds__(512, (kLie == kShifted && kOp == kRowNorm) || 
     }
   }
   block_stats<kOp == kRowNorm>(top, ss);
+  if constexpr (kSplit) {
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if ((int)threadIdx.x < splits) {
+      const uint32_t to = tc::mapa_shared(tc::smem_u32(&joined[blockIdx.x]), threadIdx.x);
+      asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(to), "r"(top), "r"(__float_as_uint(ss)) : "memory");
+    }
+    tc::cluster_sync();
+    ss = 0.0f;
+    for (int i = 0; i < splits; ++i) {  // in the blocks' order
+      top = max(top, joined[i].x);
+      ss += __uint_as_float(joined[i].y);
+    }
+  }
   float inv, scale;
-  row_scale(__uint_as_float(top), ss, kOp == kRowNorm ? rsqrtf(ss / (float)p.cols + p.eps) : 1.0f, inv, scale);
-  if (threadIdx.x == 0) p.scales[row] = scale;
+  row_scale(__uint_as_float(top), ss, kOp == kRowNorm ? rsqrtf(ss / (float)call.cols + p.eps) : 1.0f, inv, scale);
+  if (threadIdx.x == 0 && (!kSplit || blockIdx.x == 0)) p.scales[row] = scale;
   for (int k = first; k < p.cols; k += step) {
     float u[kU], h[kU];
     if constexpr (!kOwn) load_vec<kU>(us + k + out, u);
@@ -502,35 +531,63 @@ static cudaError_t start(void (*kernel)(RowArgs), unsigned grid, unsigned thread
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-template <class T, RowOp kOp, Lie kLie>
-static cudaError_t start_held(const RowArgs& a, cudaStream_t stream) {
-  const int kE = 16 / (int)sizeof(T), bytes = (a.cols + 2 * kE - 2) / kE * 16;
-  const int smem = 2 * bytes + (kLie < kLoose ? 0 : bytes / 16 * kE * 4);
+template <class T, RowOp kOp, Lie kLie, bool kSplit>
+static cudaError_t start_held(const RowArgs& a, cudaStream_t stream, int splits = 1) {
+  const int kE = 16 / (int)sizeof(T);
+  const int part = kSplit ? (a.cols / kE + splits - 1) / splits * kE : a.cols, bytes = (part + 2 * kE - 2) / kE * 16;
+  const int smem = (kOp == kRowGated || a.b ? 2 : 1) * bytes + (kLie < kLoose ? 0 : bytes / 16 * kE * 4);
+  void (*kernel)(RowArgs, int, int, int) = rows_held_kernel<T, kOp, kLie, kSplit>;
   if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(rows_held_kernel<T, kOp, kLie>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldBytes);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldBytes);
     if (e != cudaSuccess) return e;
   }
   const int units = kLie != kAnyhow ? bytes / 16 : a.cols;
-  // (three vectors a thread; four of kLoose, whose registers are more: 3000 x 3333 f16, gated, 20.3 us, three 22.2, two 24.8)
-  int threads = kLie == kLoose ? (units + 3) / 4 : (units + 2) / 3;
+  // Three vectors a thread; four or five where that lets more blocks share an SM: of kLoose, for its registers (3000 x 3333 f16, gated, four
+  // 20.3 us, three 22.2, two 24.8), and of a cluster, whose parts are shorter (3000 x 10240 f32, gated, five 60, four 65, three 77; 1000 x
+  // 16384 f32, the norm, five 54, four 51).
+  constexpr int kEach = kLie == kLoose ? 4 : !kSplit ? 3 : kOp == kRowGated ? 5 : 4;
+  int threads = (units + kEach - 1) / kEach;
   threads = threads < 64 ? 64 : (threads > 512 ? 512 : (threads + 31) / 32 * 32);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)a.rows);
   cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)splits;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, rows_held_kernel<T, kOp, kLie>, a, bytes);
+  if constexpr (!kSplit) {
+    cfg.gridDim = dim3((unsigned)a.rows);
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a, bytes, 1, part);
+  } else {
+    cfg.numAttrs = 2;
+    constexpr int64_t most = 65535;  // the grid's second dimension: the rows in pieces
+    for (int64_t m = 0; m < a.rows; m += most) {
+      RowArgs p = a;
+      p.rows = a.rows - m < most ? a.rows - m : most;
+      p.a = static_cast<const T*>(a.a) + m * a.lda;
+      if (p.b) p.b = static_cast<const T*>(a.b) + m * a.ldb;
+      if (p.sum) p.sum = static_cast<T*>(a.sum) + m * a.ld_sum;
+      if (p.codes) p.codes += m * a.ld_codes;
+      if (p.values) p.values = static_cast<uint8_t*>(a.values) + m * a.ld_values * (a.values_dtype == AQD_F32 ? 4 : 2);
+      p.scales += m;
+      cfg.gridDim = dim3((unsigned)splits, (unsigned)p.rows);
+      const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p, bytes, splits, part);
+      if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+  }
 }
 // Whether a row fits its share of an SM's shared memory.
 template <class T>
 static bool held(const RowArgs& a, Lie lie) {
   const int64_t kE = 16 / (int)sizeof(T), bytes = ((int64_t)a.cols + 2 * kE - 2) / kE * 16;
-  return 2 * bytes + (lie < kLoose ? 0 : bytes / 16 * kE * 4) <= kHeldBytes;
+  return (a.b ? 2 : 1) * bytes + (lie < kLoose ? 0 : bytes / 16 * kE * 4) <= kHeldBytes;
 }
 
 static bool whole(const void* p, int64_t ld, int size, int bytes) {
@@ -559,7 +616,7 @@ static cudaError_t run_vectors(const RowArgs& a, cudaStream_t stream) {
     if (n <= 1024) return start(rows_kernel<T, kOp, kE, 1, false, false>, rows, block(n, 1), a, stream);
     if (n <= 2048 && (kE == 4 || rows <= 304)) return start(rows_kernel<T, kOp, kE, 2, false, false>, rows, block(n, 2), a, stream);
   }
-  return start_held<T, kOp, kShift ? kShifted : kWhole>(a, stream);
+  return start_held<T, kOp, kShift ? kShifted : kWhole, false>(a, stream);
 }
 
 template <class T, RowOp kOp>
@@ -573,6 +630,14 @@ static cudaError_t run(const RowArgs& a, cudaStream_t stream) {
   auto block = [](int64_t n, int v) { return (unsigned)(((n + v - 1) / v + 31) / 32 * 32); };  // threads for n elements, v each
   if (vec) {
     if (a.cols <= 1024 * kE || held<T>(a, kWhole)) return run_vectors<T, kOp, false>(a, stream);
+    // Longer rows in the shared memory of a cluster; for few rows of more blocks than they need. (1500 x 32768 f32, gated: 101 us, read twice
+    // 139; 1000 x 131072 bf16 178 and 230; 300 x 131072 bf16, the norm, 71 and 100; one row of 32768 f32, gated, 3.3 and 11.4.)
+    const int64_t room = kHeldBytes / 16 / (a.b ? 2 : 1) - 2, n = a.cols / kE;
+    int64_t splits = (n + room - 1) / room;
+    if (splits <= 8) {
+      if (splits < 304 / rows) splits = 304 / rows < 8 ? 304 / rows : 8;
+      return start_held<T, kOp, kWhole, true>(a, stream, (int)splits);
+    }
     return start(rows_long_kernel<T, kOp, kE>, rows, 512, a, stream);
   }
   // Whether every tensor's rows start at the same element of their vectors. (Up to 64 vectors the ends are too many of them: 4096 x 257
@@ -588,13 +653,13 @@ static cudaError_t run(const RowArgs& a, cudaStream_t stream) {
   if (all && a.cols > 64 * kE && held<T>(a, kShifted)) return run_vectors<T, kOp, true>(a, stream);
   // The outputs' rows alike, the inputs' not (the two halves of rows of an odd width): 3000 x 3333 f16, gated, 20.3 us, an element at a time 32;
   // 1000 x 2049 bf16 6.8 and 11.5; 5000 x 777 13.6 and 11.6.
-  if (outputs && a.cols > 2048 && held<T>(a, kLoose)) return start_held<T, kOp, kLoose>(a, stream);
+  if (outputs && a.cols > 2048 && held<T>(a, kLoose)) return start_held<T, kOp, kLoose, false>(a, stream);
   // Rows at any address: an element at a time, neighbours by neighbours. (4096 x 1001 bf16, the norm: eight 14.2 us, in shared memory
   // 29; 2000 x 7777: 68 and 55; 5000 x 777, gated: eight 15.5, four 11.7.)
   if (a.cols <= 256 && rows > 608) return start(rows_kernel<T, kOp, 1, 8, true, false>, (rows + 7) / 8, 256, a, stream);
   if (a.cols <= (kOp == kRowGated ? 2048 : 768)) return start(rows_kernel<T, kOp, 1, 4, false, false>, rows, block(a.cols, 4), a, stream);
   if (kOp != kRowGated && a.cols <= 6144) return start(rows_kernel<T, kOp, 1, 8, false, false>, rows, block(a.cols, 8), a, stream);
-  if (held<T>(a, kAnyhow)) return start_held<T, kOp, kAnyhow>(a, stream);
+  if (held<T>(a, kAnyhow)) return start_held<T, kOp, kAnyhow, false>(a, stream);
   return start(rows_long_kernel<T, kOp, 1>, rows, 512, a, stream);
 }
 template <class T>

@@ -166,6 +166,39 @@ def test_inputs_that_lie_otherwise_than_the_outputs(cols, dtype):
     check(aqd.gated_act_quant(wide, x, values=True), act64(wide.double(), "silu") * x.double(), dtype)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 18440), (310, 24576), (7, 36872), (2, 73736), (320, 40960), (3, 147440), (1, 300000)])
+def test_rows_of_several_blocks(rows, cols, dtype):
+    x, r = normal(17, rows, cols).to(dtype), normal(18, rows, cols).to(dtype)
+    w = (1 + 0.3 * normal(19, cols)).to(dtype)
+    x[0, cols - 1] = 9.0  # the largest is in the last block's part
+    h = x.double() + r.double() if dtype != torch.float32 else (x + r).double()
+    q = aqd.rms_norm_quant(x, w, residual=r, values=True)
+    check(q, norm64(h, w, 1e-6), dtype)
+    assert torch.equal(q.summed, (x.float() + r.float()).to(dtype))
+    check(aqd.rms_norm_quant(x, w), norm64(x.double(), w, 1e-6), None)
+    check(aqd.quant_rows(x, values=torch.float32), x.double(), torch.float32)
+    again = aqd.rms_norm_quant(x, w, residual=r, values=True, summed=x)
+    torch.cuda.synchronize()
+    assert torch.equal(again.codes, q.codes) and torch.equal(again.scales, q.scales) and torch.equal(x, q.summed)
+    x[:, 0], r[:, 0] = 3.0, 4.0
+    check(aqd.gated_act_quant(x, r, values=True), act64(x.double(), "silu") * r.double(), dtype)
+    x[rows - 1, cols // 2] = math.nan
+    q = aqd.quant_rows(x)
+    torch.cuda.synchronize()
+    assert q.scales[rows - 1].isnan() and (q.codes[rows - 1] == 0).all() and q.scales[:rows - 1].isfinite().all()
+
+
+def test_more_long_rows_than_a_grid_has():
+    one = normal(20, 1, 40000).half()
+    q = aqd.quant_rows(one.expand(65539, 40000))
+    torch.cuda.synchronize()
+    check(aqd.RowCodes(q.codes[:1], q.scales[:1]), one.double(), None)
+    assert (q.scales == q.scales[0]).all()
+    for at in (0, 65534, 65535, 65538):
+        assert torch.equal(q.codes[at], q.codes[0])
+
+
 def test_leading_dimensions_and_broadcast_rows():
     x, w = normal(7, 2, 5, 3, 96).half(), torch.ones(96, device="cuda")
     check(aqd.rms_norm_quant(x, w), norm64(x.double(), w, 1e-6), None)
