@@ -371,7 +371,8 @@ typedef struct {
 } aqd_row_codes;
 
 /* How a row u of float32 values becomes codes: a = max |u_k|, scale = a / 127, code = u / scale
- * rounded to nearest, ties to even (computed as u * (127 / a)). A row with a < 2^-120 has scale 0 and codes 0. A row
+ * rounded to nearest, ties to even (computed as u * (127 / a)). A row with a < 2^-120 (under the norm: with every
+ * |h_k weight_k| below that) has scale 0 and codes 0. A row
  * that holds a NaN or an infinity (or, under the norm, whose sum of squares passes float32's range)
  * has scale NaN, codes 0 and values NaN, so the products that read it give NaN.
  * All pointers are device pointers aligned to their element; rows that start at 16-byte boundaries
@@ -436,8 +437,8 @@ aqd_status aqd_linear_prepare_weights(const int8_t* codes, int64_t ld, const aqd
  * NULL. With y_dtype AQD_I32, y receives the integer sums and x_scale, the weights' scales and bias are not read.
  * x: int8 codes, any ldx >= 0. workspace: aqd_linear_workspace_bytes(m, w) bytes or more, 256-byte aligned,
  * or NULL; its contents do not matter, and calls that share it must not overlap in time. Results are identical with
- * and without it: with more than 64 tokens, or rows of codes that are not 16-byte aligned, it holds the codes as the tensor cores read
- * them and the sums of tiles that several blocks share, and a call without it runs on slower kernels. */
+ * and without it: with more than 16 tokens, or rows of codes that are not 16-byte aligned, it may hold the codes as the kernels read
+ * them, and a call without it runs on slower ones. */
 typedef struct {
   int64_t m;
   const int8_t* x;
