@@ -36,7 +36,7 @@ namespace lintc {
 using namespace tc;
 
 constexpr int kKC = 128;           // K per stage
-constexpr int kRaw = 4;            // stages of the weights' bytes
+constexpr int kMinRaw = 4, kMaxRaw = 8;  // stages of the weights' bytes
 constexpr int kCvt = 4;            // stages of converted weights (TMEM: 64 columns each beside 256 accumulator columns)
 constexpr int kMaxX = 8;           // stages of the tokens
 // Warps: 8 read the accumulators and write outputs, 8 convert, in two sets that take stages in turn, and one thread each issues
@@ -47,7 +47,7 @@ constexpr int kWarpCvt = kEpi, kWarpTmaW = kWarpCvt + kSets * kSetWarps, kWarpTm
 constexpr int kThreads = (kWarpTmaW + 4) * 32;  // (an idle warp fills the issuing warps' warpgroup)
 constexpr int kRegsLaunch = 65536 / kThreads / 8 * 8, kRegsEpi = 176, kRegsCvt = 40, kRegsIssue = 48;
 static_assert(kEpi * kRegsEpi + kSets * kSetWarps * kRegsCvt + 4 * kRegsIssue <= kThreads / 32 * kRegsLaunch, "the launch's registers");
-static_assert(kCvt % kSets == 0 && kRaw % kSets == 0, "one set for each stage of the weights");
+static_assert(kCvt % kSets == 0 && kMinRaw % kSets == 0 && kMaxRaw % kSets == 0, "one set for each stage of the weights");
 constexpr int kEpiCols = kEpi / 4, kBlocks = 16 / kEpiCols;  // warps of a lane quarter; 16-token blocks of each
 constexpr int kTmemA = 256;        // first column of the converted weights
 constexpr int kRawW = 128 * kKC;   // bytes of a stage's weights
@@ -58,14 +58,14 @@ struct Params {
   int32_t nt, tok_tiles;           // tokens per tile (multiple of 16), token tiles
   int32_t chunks;                  // K in pieces of kKC
   int32_t tiles, pairs;            // pair j computes tiles j, j + pairs, ...
-  int32_t x_stages;
+  int32_t raw_stages, x_stages;    // (raw_stages: kMinRaw or kMaxRaw)
 };
 struct Maps {
   CUtensorMap w, x;
 };
 
 struct Barriers {
-  uint64_t raw_full[kRaw], raw_empty[kRaw], cv_full[kCvt], cv_empty[kCvt], x_full[kMaxX], x_empty[kMaxX], d_full, d_empty, done;
+  uint64_t raw_full[kMaxRaw], raw_empty[kMaxRaw], cv_full[kCvt], cv_empty[kCvt], x_full[kMaxX], x_empty[kMaxX], d_full, d_empty, done;
   uint32_t tmem, seg;
   int abort_flag;
   alignas(16) float scales[2][256];  // the tokens' scales of a tile, and of the next
@@ -143,13 +143,13 @@ linear_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Para
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x >> 1;
   const int rows_x = p.nt >> 1;                      // tokens of this CTA
-  const uint32_t raw0 = smem_u32(smem), x0 = raw0 + kRaw * kRawW;
+  const uint32_t raw0 = smem_u32(smem), x0 = raw0 + (uint32_t)p.raw_stages * kRawW;
   const uint32_t x_half = (uint32_t)rows_x * kKC, x_bytes = 2 * x_half;  // 64 K of F16 a row and half (whole kilobytes: rows_x is a multiple of 8)
-  Barriers& bar = *reinterpret_cast<Barriers*>(smem + kRaw * kRawW + p.x_stages * x_bytes);
+  Barriers& bar = *reinterpret_cast<Barriers*>(smem + p.raw_stages * kRawW + p.x_stages * x_bytes);
   volatile int* abort_flag = &bar.abort_flag;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kRaw; ++i) {
+    for (int i = 0; i < kMaxRaw; ++i) {
       mbar_init(smem_u32(&bar.raw_full[i]), 1);
       mbar_init(smem_u32(&bar.raw_empty[i]), kSetWarps);
     }
@@ -196,16 +196,16 @@ linear_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Para
           mbar_arrive_expect_tx(full, kRawW);
           tma_load_2d(raw0 + st * kRawW, &maps.w, c * kKC, yw, full);
           ++issued;
-          if (++st == kRaw) { st = 0; ph ^= 1; }
+          if (++st == (uint32_t)p.raw_stages) { st = 0; ph ^= 1; }
         }
       }
       if (!ok) {
         fail(abort_flag, p.a.status);
         // the copies in flight end before the block does (each of these waits is bounded too)
         int never = 0;
-        for (uint32_t i = 0; i < (issued < kRaw ? issued : kRaw); ++i) {
+        for (uint32_t i = 0; i < (issued < (uint32_t)p.raw_stages ? issued : (uint32_t)p.raw_stages); ++i) {
           const uint32_t q = issued - 1 - i;
-          mbar_wait(smem_u32(&bar.raw_full[q % kRaw]), (q / kRaw) & 1, &never);
+          mbar_wait(smem_u32(&bar.raw_full[q % p.raw_stages]), (q / p.raw_stages) & 1, &never);
         }
       }
     }
@@ -279,8 +279,9 @@ linear_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Para
     // a thread converts one row; piece c (16 codes) of a row lies at c ^ (row & 7) of its 128 bytes
     const uint32_t from = (uint32_t)row * 128 + (uint32_t)((row & 7) << 4);
     const int total = (p.tiles - pair + p.pairs - 1) / p.pairs * p.chunks;
+    uint32_t rst = (uint32_t)set, rph = 0;
     for (int i = set; i < total; i += kSets) {
-      const uint32_t rst = (uint32_t)i % kRaw, rph = ((uint32_t)i / kRaw) & 1, cst = (uint32_t)i % kCvt, cph = ((uint32_t)i / kCvt) & 1;
+      const uint32_t cst = (uint32_t)i % kCvt, cph = ((uint32_t)i / kCvt) & 1;
       bool ok = mbar_wait_inline(smem_u32(&bar.raw_full[rst]), rph, abort_flag) &&
                 mbar_wait_inline(smem_u32(&bar.cv_empty[cst]), cph ^ 1, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
@@ -305,6 +306,8 @@ linear_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Para
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bar.raw_empty[rst]));
+      rst += kSets;
+      if (rst >= (uint32_t)p.raw_stages) { rst -= (uint32_t)p.raw_stages; rph ^= 1; }
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
@@ -469,7 +472,7 @@ static float plan(const LinArgs& a, int pairs, Params* p) {
   int64_t width = 16;
   for (int nt = 16; nt <= 256; nt += 16) {
     const int64_t tm = (a.m + nt - 1) / nt, waves = (tn * tm + pairs - 1) / pairs;
-    const float t = (float)(waves * chunks) * fmaxf(0.42f, 0.00273f * nt) + 4.5f + 0.02f * nt;
+    const float t = (float)(waves * chunks) * fmaxf(0.38f, 0.00273f * nt) + 4.5f + 0.02f * nt;
     if (t < best) { best = t; width = nt; }
     if (tm == 1) break;
   }
@@ -502,9 +505,12 @@ int launch_linear_tc(const LinArgs& a, cudaStream_t stream, std::string* err) {
   Params p{};
   plan(a, sm_pairs(), &p);
   const int rows_x = p.nt / 2, xs = 2 * rows_x * kKC;
-  p.x_stages = (kSmemLimit - (int)sizeof(Barriers) - kRaw * kRawW) / xs;
+  // narrow tiles leave room for more of the weights on their way, which their short stages need (64 tokens, n 12288, K 4096 17.8 us; 19.4
+  // with kMinRaw); wide ones need it for the tokens
+  p.raw_stages = p.nt <= 128 ? kMaxRaw : kMinRaw;
+  p.x_stages = (kSmemLimit - (int)sizeof(Barriers) - p.raw_stages * kRawW) / xs;
   if (p.x_stages > kMaxX) p.x_stages = kMaxX;
-  const size_t smem = (size_t)kRaw * kRawW + (size_t)p.x_stages * xs + sizeof(Barriers);
+  const size_t smem = (size_t)p.raw_stages * kRawW + (size_t)p.x_stages * xs + sizeof(Barriers);
   const int64_t pitch = lin_pitch(a.k);
   Maps maps;
   if (!encode(&maps.w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.w + kLinHeader, pitch, a.n, pitch, 128) ||
