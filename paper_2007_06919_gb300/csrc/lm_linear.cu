@@ -165,9 +165,9 @@ constexpr int small_bytes(int g, int r, int depth) {
 // of a row are its fragments of four MMAs: each lane copies the bytes that it will itself multiply into its own places of a ring in
 // shared memory (kDepth pieces ahead, no barrier between lanes) and turns them into F16 in registers. Sums are exact in FP32 over
 // 1024 K, then add up in int32 (kLong: a warp has more than that), across warps in shared memory.
-// (Measured: 1 x 4096 x 4096 5.7 us, 1 x 12288 x 4096 11.2, 4.5 TB/s; loads straight into registers, a round of them at a time, 24 x 12288 x 4096 23.3 us against 18.2; weights by bulk
-// copies, the tokens' loads then waited for at each stage, 33; tokens as F16 once per block and K split
-// over a cluster, 20.)
+// (Measured: 1 x 4096 x 4096 5.7 us; 1 x 12288 x 4096 11.3, 4.4 TB/s; 24 x 12288 x 4096 14.8, 3.4 TB/s. At two row tiles and 18.2 us for that
+// one: loads straight into registers, a round of them at a time, 23.3; weights by bulk copies, the tokens' loads then waited for
+// at each stage, 33; tokens as F16 once per block and K split over a cluster, 20.)
 template <int kG, int kR, int kDepth, bool kLong>
 __global__ void __launch_bounds__(kSmallWarps * 32, kG * kR == 16 ? 1 : 2) linear_ring_kernel(const LinArgs p) {
   extern __shared__ __align__(16) uint8_t smem[];
