@@ -18,7 +18,9 @@ namespace lin {
 
 // Rows of k codes plus 128, as bytes (what the conversion to F16 starts from), padded with code 0 to whole chunks of
 // 128; and the header's first word, the most chunks in a row that any row of weights lets an FP32 accumulator sum exactly:
-// those of every window of that length have sum |w| * 128 <= 2^24. (8 chunks always do.) One warp per row.
+// those of every window of that length have sum |w| * 128 <= 2^24. (8 chunks always do.) One warp per row, eight chunks' loads at a
+// time, in words where all rows start on one.
+template <bool kWords>
 __global__ void __launch_bounds__(128) prepare_kernel(const int8_t* __restrict__ codes, int64_t ld, int32_t n, int32_t k,
                                                       int64_t pitch, uint8_t* __restrict__ out) {
   __shared__ uint16_t sums[4][1024];  // sum |w| of each chunk (at most 128 * 128)
@@ -26,18 +28,28 @@ __global__ void __launch_bounds__(128) prepare_kernel(const int8_t* __restrict__
   const int chunks = (int)(pitch / 128);
   int most = chunks;
   for (int64_t row = (int64_t)blockIdx.x * 4 + warp; row < n; row += (int64_t)gridDim.x * 4) {
-    for (int c = 0; c < chunks; ++c) {
-      uint32_t word = 0;
-      int s = 0;
-      for (int j = 0; j < 4; ++j) {
-        const int i = c * 128 + lane * 4 + j;
-        const int w = i < k ? codes[row * ld + i] : 0;
-        s += w < 0 ? -w : w;
-        word |= (uint32_t)(uint8_t)(w + 128) << (8 * j);
+    const int8_t* from = codes + row * ld;
+    uint32_t* to = reinterpret_cast<uint32_t*>(out + kLinHeader + row * pitch) + lane;
+    for (int c0 = 0; c0 < chunks; c0 += 8) {
+      uint32_t w[8];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const int i = (c0 + c) * 128 + lane * 4;
+        w[c] = 0;
+        if (kWords && i + 4 <= k) w[c] = __ldg(reinterpret_cast<const uint32_t*>(from + i));
+        else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (i + j < k) w[c] |= (uint32_t)(uint8_t)from[i + j] << (8 * j);
+        }
       }
-      *reinterpret_cast<uint32_t*>(out + kLinHeader + row * pitch + c * 128 + lane * 4) = word;
-      s = __reduce_add_sync(0xffffffffu, s);
-      if (lane == 0) sums[warp][c] = (uint16_t)s;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        if (c0 + c >= chunks) break;
+        to[(c0 + c) * 32] = w[c] ^ 0x80808080u;
+        const uint32_t s = __reduce_add_sync(0xffffffffu, __dp4a(__vabs4(w[c]), 0x01010101u, 0u));  // (|-128| is 128 there)
+        if (lane == 0) sums[warp][c0 + c] = (uint16_t)s;
+      }
     }
     __syncwarp();
     if (lane == 0) {  // windows (lo, hi]: each hi's longest with a sum in range; the shortest of those that could not grow
@@ -353,7 +365,9 @@ int launch_linear_prepare(const int8_t* codes, int64_t ld, int32_t n, int32_t k,
                           std::string* err) {
   const cudaError_t e = cudaMemsetAsync(out, 0x7f, 4, stream);
   if (e != cudaSuccess) { *err = std::string("weight preparation: ") + cudaGetErrorString(e); return AQD_ERR_CUDA; }
-  lin::prepare_kernel<<<n < 4864 ? (n + 3) / 4 : 1216, 128, 0, stream>>>(codes, ld, n, k, lin_pitch(k), out);
+  const bool words = ld % 4 == 0 && (reinterpret_cast<uintptr_t>(codes) & 3) == 0;
+  void (*kernel)(const int8_t*, int64_t, int32_t, int32_t, int64_t, uint8_t*) = words ? lin::prepare_kernel<true> : lin::prepare_kernel<false>;
+  kernel<<<n < 9728 ? (n + 3) / 4 : 2432, 128, 0, stream>>>(codes, ld, n, k, lin_pitch(k), out);
   return launched("weight preparation launch: ", err);
 }
 
