@@ -537,7 +537,8 @@ static cudaError_t start_held(const RowArgs& a, cudaStream_t stream, int splits 
   const int part = kSplit ? (a.cols / kE + splits - 1) / splits * kE : a.cols, bytes = (part + 2 * kE - 2) / kE * 16;
   const int smem = (kOp == kRowGated || a.b ? 2 : 1) * bytes + (kLie < kLoose ? 0 : bytes / 16 * kE * 4);
   void (*kernel)(RowArgs, int, int, int) = rows_held_kernel<T, kOp, kLie, kSplit>;
-  if (smem > 48 * 1024) {
+  // (a block has 48 KB without asking, the kernel's own arrays among them: 128 to 320 bytes)
+  if (smem > 40 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldBytes);
     if (e != cudaSuccess) return e;
   }
