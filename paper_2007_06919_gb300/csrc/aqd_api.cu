@@ -24,6 +24,8 @@ static int32_t g_forced_path = 0;
 __device__ uint32_t g_status_word;
 
 static aqd_status fail(aqd_status s, const std::string& msg) {
+  // CUDA keeps a refused call's error until it is read: the next launch, the caller's own too, would take it for its own
+  if (s == AQD_ERR_CUDA) cudaGetLastError();
   g_last_error = msg;
   return s;
 }
