@@ -790,14 +790,20 @@ class LinearWeights:
         return cls(q.codes, q.scales, stream=stream)
 
 
-def linear_workspace(m: int, w: LinearWeights) -> torch.Tensor | None:
-    """A workspace for linear_int8 with up to m tokens; None where it needs none."""
-    n = int(_calls().aqd_linear_workspace_bytes(m, w.desc))
+@functools.lru_cache(maxsize=4096)
+def _linear_workspace_bytes(m: int, n: int, k: int) -> int:
+    return int(_calls().aqd_linear_workspace_bytes(m, _LINEAR_W.pack(0, 0, n, k)))
+
+
+def linear_workspace(m: int, *w: LinearWeights, stream=None) -> torch.Tensor | None:
+    """A workspace for linear_int8 with up to m tokens, for one layer or for several whose calls follow one another on one stream; None where
+    they need none. It belongs to the stream: released after calls were made there, its memory goes to that stream's later work only."""
+    n = max(_linear_workspace_bytes(m, v.n, v.k) for v in w)
     if n == 0:
         return None
-    buf = torch.empty(n + 256, dtype=torch.uint8, device=w.device)
-    off = (-buf.data_ptr()) % 256
-    return buf[off:off + n]
+    buf = _new(n + 256, torch.uint8, w[0].device, stream)
+    off = -buf.data_ptr() % 256
+    return buf[off:off + n] if off else buf
 
 
 def linear_int8(x: torch.Tensor, x_scale: torch.Tensor | None, w: LinearWeights, *, bias: torch.Tensor | None = None,

@@ -18,9 +18,19 @@ import torch
 from . import aqd
 
 
+def _workspace(m: int, layers, stream):
+    """A workspace for one call of a model: of that call's stream alone, since calls on several streams may overlap, and as large as its own
+    tokens need. The layers' products follow one another, so they share it. None for codes that products read where they lie (up to 16 rows, each
+    on 16 bytes)."""
+    if m > 16 or (m > 1 and any(w.k % 16 for w in layers)):
+        return aqd.linear_workspace(m, *layers, stream=stream)
+    return None
+
+
 class FeedForward:
     """One block: norm weight [d], gate and up [hidden, d], down [d, hidden] in floating point; the products' weights
-    are quantized here. tokens: the most that a call brings (the workspaces' size)."""
+    are quantized here. Calls may bring any number of tokens, on several streams at a time. (tokens has no effect: a workspace is
+    taken for each call.)"""
 
     def __init__(self, norm: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, down: torch.Tensor, *, act: str = "silu",
                  eps: float = 1e-6, tokens: int = 1):
@@ -29,28 +39,31 @@ class FeedForward:
         self.norm, self.act, self.eps, self.tokens, self.hidden = norm, act, eps, tokens, gate.shape[0]
         self.both = aqd.LinearWeights.from_float(torch.cat([gate, up]))
         self.down = aqd.LinearWeights.from_float(down)
-        self._ws = aqd.linear_workspace(tokens, self.both), aqd.linear_workspace(tokens, self.down)
 
-    def __call__(self, x: torch.Tensor, residual: torch.Tensor | None = None, stream=None):
-        """(block's output, x + residual) of tokens x [..., d]: the two are the next norm's x and residual."""
+    def __call__(self, x: torch.Tensor, residual: torch.Tensor | None = None, stream=None, workspace=None):
+        """(block's output, x + residual) of tokens x [..., d]: the two are the next norm's x and residual. workspace: one for
+        these tokens and both layers (linear_workspace) that no call on another stream uses meanwhile; the call takes one where none is given."""
+        if workspace is None:
+            workspace = _workspace(x.numel() // self.both.k, (self.both, self.down), stream)
         q = aqd.rms_norm_quant(x, self.norm, eps=self.eps, residual=residual, stream=stream)
-        both = aqd.linear_int8(q.codes, q.scales, self.both, out_dtype=x.dtype, workspace=self._ws[0], stream=stream)
+        both = aqd.linear_int8(q.codes, q.scales, self.both, out_dtype=x.dtype, workspace=workspace, stream=stream)
         h = aqd.gated_act_quant(both[..., :self.hidden], both[..., self.hidden:], act=self.act, stream=stream)
-        y = aqd.linear_int8(h.codes, h.scales, self.down, out_dtype=x.dtype, workspace=self._ws[1], stream=stream)
+        y = aqd.linear_int8(h.codes, h.scales, self.down, out_dtype=x.dtype, workspace=workspace, stream=stream)
         return y, x if residual is None else q.summed
 
 
 class Head:
-    """Norm weight [d] and a projection [vocab, d] to logits."""
+    """Norm weight [d] and a projection [vocab, d] to logits; calls and tokens as a block's."""
 
     def __init__(self, norm: torch.Tensor, weight: torch.Tensor, *, eps: float = 1e-6, tokens: int = 1):
         self.norm, self.eps = norm, eps
         self.proj = aqd.LinearWeights.from_float(weight)
-        self._ws = aqd.linear_workspace(tokens, self.proj)
 
-    def __call__(self, x: torch.Tensor, residual: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    def __call__(self, x: torch.Tensor, residual: torch.Tensor | None = None, stream=None, workspace=None) -> torch.Tensor:
+        if workspace is None:
+            workspace = _workspace(x.numel() // self.proj.k, (self.proj,), stream)
         q = aqd.rms_norm_quant(x, self.norm, eps=self.eps, residual=residual, stream=stream)
-        return aqd.linear_int8(q.codes, q.scales, self.proj, out_dtype=x.dtype, workspace=self._ws, stream=stream)
+        return aqd.linear_int8(q.codes, q.scales, self.proj, out_dtype=x.dtype, workspace=workspace, stream=stream)
 
     def distill(self, logits: torch.Tensor, index: torch.Tensor, teacher: torch.Tensor, *, tau: float = 1.0,
                 row_weight: torch.Tensor | None = None, rate: float = 0.0):
@@ -72,10 +85,12 @@ class Decoder:
 
     def __call__(self, x: torch.Tensor, stream=None) -> torch.Tensor:
         """Logits [..., vocab] of tokens x [..., d]."""
+        layers = [w for block in self.blocks for w in (block.both, block.down)] + [self.head.proj]
+        ws = _workspace(x.numel() // layers[0].k, layers, stream)
         residual = None
         for block in self.blocks:
-            x, residual = block(x, residual, stream=stream)
-        return self.head(x, residual, stream=stream)
+            x, residual = block(x, residual, stream=stream, workspace=ws)
+        return self.head(x, residual, stream=stream, workspace=ws)
 
 
 def main():
