@@ -27,7 +27,25 @@ def _workspace(m: int, layers, stream):
     return None
 
 
-class FeedForward:
+class _Part:
+    """Weights that calls on any stream read, in the memory of the stream current at construction."""
+
+    def _keep(self, norm: torch.Tensor, *layers):
+        self._memory = [norm] + [t for w in layers for t in (w.prepared, w.scales)]
+        self._readers = {aqd._stream()}
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().synchronize()  # prepared before the first call, wherever that comes
+
+    def _read_on(self, stream):
+        """Keeps the weights' memory, once they are dropped, until this stream has finished with it."""
+        handle = aqd._stream(stream)
+        if handle not in self._readers:
+            for t in self._memory:
+                t.record_stream(torch.cuda.current_stream() if stream is None else stream)
+            self._readers.add(handle)
+
+
+class FeedForward(_Part):
     """One block: norm weight [d], gate and up [hidden, d], down [d, hidden] in floating point; the products' weights
     are quantized here. Calls may bring any number of tokens, on several streams at a time. (tokens has no effect: a workspace is
     taken for each call.)"""
@@ -39,10 +57,12 @@ class FeedForward:
         self.norm, self.act, self.eps, self.tokens, self.hidden = norm, act, eps, tokens, gate.shape[0]
         self.both = aqd.LinearWeights.from_float(torch.cat([gate, up]))
         self.down = aqd.LinearWeights.from_float(down)
+        self._keep(norm, self.both, self.down)
 
     def __call__(self, x: torch.Tensor, residual: torch.Tensor | None = None, stream=None, workspace=None):
         """(block's output, x + residual) of tokens x [..., d]: the two are the next norm's x and residual. workspace: one for
         these tokens and both layers (linear_workspace) that no call on another stream uses meanwhile; the call takes one where none is given."""
+        self._read_on(stream)
         if workspace is None:
             workspace = _workspace(x.numel() // self.both.k, (self.both, self.down), stream)
         q = aqd.rms_norm_quant(x, self.norm, eps=self.eps, residual=residual, stream=stream)
@@ -52,14 +72,16 @@ class FeedForward:
         return y, x if residual is None else q.summed
 
 
-class Head:
+class Head(_Part):
     """Norm weight [d] and a projection [vocab, d] to logits; calls and tokens as a block's."""
 
     def __init__(self, norm: torch.Tensor, weight: torch.Tensor, *, eps: float = 1e-6, tokens: int = 1):
         self.norm, self.eps = norm, eps
         self.proj = aqd.LinearWeights.from_float(weight)
+        self._keep(norm, self.proj)
 
     def __call__(self, x: torch.Tensor, residual: torch.Tensor | None = None, stream=None, workspace=None) -> torch.Tensor:
+        self._read_on(stream)
         if workspace is None:
             workspace = _workspace(x.numel() // self.proj.k, (self.proj,), stream)
         q = aqd.rms_norm_quant(x, self.norm, eps=self.eps, residual=residual, stream=stream)

@@ -16,6 +16,15 @@ class Stream:
         self.waited += 1
 
 
+class Kept:
+    """Memory of the model's own, and the streams that the allocator was told of."""
+    def __init__(self, *shape):
+        self.shape, self.streams = torch.Size(shape), []
+
+    def record_stream(self, s):
+        self.streams.append(s)
+
+
 @pytest.fixture
 def record(monkeypatch):
     """The products' (tokens, weights, workspace, stream) in turn; every workspace knows its size and stream, and stays alive."""
@@ -30,20 +39,21 @@ def record(monkeypatch):
 
     monkeypatch.setattr(feedforward, "aqd", SimpleNamespace(
         LinearWeights=SimpleNamespace(from_float=lambda w, stream=None: SimpleNamespace(
-            n=w.shape[0], k=w.shape[1], device=w.device, index=0, scales=torch.ones(w.shape[0]), prepared=torch.empty(0))),
+            n=w.shape[0], k=w.shape[1], device=w.device, index=0, scales=Kept(w.shape[0]), prepared=Kept(1))),
         linear_workspace=lambda m, *w, stream=None: SimpleNamespace(m=m, k=max(v.k for v in w), stream=stream),
         rms_norm_quant=lambda x, w, *, eps, residual=None, stream=None: codes(x.shape),
         gated_act_quant=lambda g, u, *, act, stream=None: codes(g.shape),
         linear_int8=linear, _stream=lambda s=None: (s or default).cuda_stream))
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: default)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     return SimpleNamespace(calls=calls, default=default)
 
 
 def decoder(tokens, d=32, hidden=48, vocab=70):
     def part(h, v):
         return torch.zeros(h, v)
-    blocks = [feedforward.FeedForward(torch.ones(d), part(hidden, d), part(hidden, d), part(d, hidden), tokens=tokens) for _ in range(2)]
-    return feedforward.Decoder(blocks, feedforward.Head(torch.ones(d), part(vocab, d), tokens=tokens))
+    blocks = [feedforward.FeedForward(Kept(d), part(hidden, d), part(hidden, d), part(d, hidden), tokens=tokens) for _ in range(2)]
+    return feedforward.Decoder(blocks, feedforward.Head(Kept(d), part(vocab, d), tokens=tokens))
 
 
 def test_no_workspace_is_shared_by_calls_on_several_streams(record):
@@ -75,6 +85,25 @@ def test_blocks_and_heads_alone(record, tokens):
         net.blocks[0](torch.zeros(tokens, 30), stream=s)
         net.head(torch.zeros(tokens, 30), stream=s)
     assert len(record.calls) == 6 and all(ws.m >= m and ws.k >= w.k and ws.stream is s for m, w, ws, s in record.calls)
+
+
+def test_the_weights_are_there_for_every_stream(record):
+    """Prepared on the stream current then, they are complete before a call may come on another."""
+    net = decoder(4)
+    assert record.default.waited >= len(net.blocks) + 1
+
+
+def test_memory_in_use_on_another_stream_is_not_given_away(record):
+    """A model that is dropped while another stream still reads its weights."""
+    net, s = decoder(4), Stream(5)
+    kept = [t for part in net.blocks + [net.head] for t in (part.norm, *(v for w in vars(part).values() if hasattr(w, "prepared")
+                                                                           for v in (w.prepared, w.scales)))]
+    assert len(kept) == 2 * 5 + 3
+    net(torch.zeros(4, 32))
+    assert not any(t.streams for t in kept)
+    for _ in range(3):
+        net(torch.zeros(4, 32), stream=s)
+    assert all(t.streams == [s] for t in kept)
 
 
 def test_few_tokens_of_odd_rows_have_a_workspace(record):

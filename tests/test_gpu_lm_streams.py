@@ -42,3 +42,32 @@ def test_more_tokens_than_stated(tokens):
     small, _, _, _ = model(12, 256, 512, 1000, 1, 1)
     assert torch.equal(net(x), small(x))
     torch.cuda.synchronize()
+
+
+def test_first_call_on_another_stream():
+    want = model(13, 512, 1024, 2000, 2, 40)[0]
+    x = torch.randn(40, 512, device="cuda").bfloat16()
+    want = want(x)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    torch.cuda._sleep(20_000_000)  # the weights are prepared behind this
+    net = model(13, 512, 1024, 2000, 2, 40)[0]
+    got = net(x, stream=s)
+    s.synchronize()
+    assert torch.equal(got, want)
+    torch.cuda.synchronize()
+
+
+def test_a_model_dropped_while_a_stream_still_reads_it():
+    net, _, _, x = model(14, 512, 1024, 2000, 2, 40)
+    want = net(x)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+    got = net(x, stream=s)
+    sizes = [t.numel() * t.element_size() for part in net.blocks + [net.head] for t in part._memory]
+    del net
+    taken = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(3)]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and len(taken) == 3 * len(sizes)
