@@ -836,7 +836,11 @@ def linear_int8(x: torch.Tensor, x_scale: torch.Tensor | None, w: LinearWeights,
         xs = _vector(x_scale, m, torch.float32, "x_scale", dev)
         if bias is not None:
             bp = _vector(bias, n, torch.float32, "bias", dev)
-    wsp, wsb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    wsp, wsb = None, 0
+    if workspace is not None:
+        if not workspace.is_cuda or workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous CUDA tensor on the call's device")
+        wsp, wsb = workspace.data_ptr(), workspace.nbytes
     _check(_calls().aqd_linear_int8(_LINEAR.pack(m, x.data_ptr(), ld, xs, bp, out.data_ptr(), ldy, yd), w.desc, wsp, wsb,
                                     _stream(stream)), "aqd_linear_int8")
     return out
