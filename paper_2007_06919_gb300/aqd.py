@@ -661,6 +661,14 @@ def _rows_of(t: torch.Tensor, name: str, device: int | None = None):
     return m, c, (ld if m > 1 else max(ld, c))
 
 
+def _runs_on(device: int, stream):
+    """ValueError unless kernels go where the call's tensors are: the current device, and the stream's."""
+    here = _raw_device() if _raw_device is not None else torch.cuda.current_device()
+    if device != here or (stream is not None and stream.device.index != here):
+        raise ValueError(f"the call's tensors are on device {device}, the current device is {here}"
+                         + ("" if stream is None else f", the stream's {stream.device}"))
+
+
 def _float_dtype(t: torch.Tensor, name: str) -> int:
     d = _DTYPE.get(t.dtype)
     if d is None:
@@ -712,6 +720,7 @@ def quant_rows(x: torch.Tensor, *, codes: bool = True, values=False, stream=None
     for the values that the codes stand for too."""
     m, c, ld = _rows_of(x, "x")
     d = _float_dtype(x, "x")
+    _runs_on(x.get_device(), stream)
     q, s, v, out = _row_codes_out(x, c, codes, values, stream)
     _check(_calls().aqd_quant_rows(m, c, x.data_ptr(), ld, d, out, _stream(stream)), "aqd_quant_rows")
     return RowCodes(q, s, v)
@@ -724,6 +733,7 @@ def rms_norm_quant(x: torch.Tensor, weight: torch.Tensor, *, eps: float = 1e-6, 
     m, c, ld = _rows_of(x, "x")
     d = _float_dtype(x, "x")
     dev = x.get_device()
+    _runs_on(dev, stream)
     rp = rl = sp = sl = 0
     if residual is not None:
         if residual.shape != x.shape or residual.dtype is not x.dtype:
@@ -753,7 +763,9 @@ def gated_act_quant(gate: torch.Tensor, up: torch.Tensor, *, act: str = "silu", 
     d = _float_dtype(gate, "gate")
     if up.shape != gate.shape or up.dtype is not gate.dtype:
         raise ValueError("up must have gate's shape and type")
-    lu = _rows_of(up, "up", gate.get_device())[2]
+    dev = gate.get_device()
+    _runs_on(dev, stream)
+    lu = _rows_of(up, "up", dev)[2]
     if act not in _ACT:
         raise ValueError(f"act must be one of {sorted(_ACT)}, got {act!r}")
     q, s, v, out = _row_codes_out(gate, c, codes, values, stream)
@@ -770,6 +782,7 @@ class LinearWeights:
         if codes.dim() != 2 or codes.dtype != torch.int8:
             raise ValueError("codes must be an int8 matrix [n, k]")
         n, k, ld = _rows_of(codes, "codes")
+        _runs_on(codes.get_device(), stream)
         sp = _vector(scales, n, torch.float32, "scales", codes.get_device())
         nbytes = int(_calls().aqd_linear_weights_bytes(n, k))
         if nbytes == 0:
@@ -816,6 +829,7 @@ def linear_int8(x: torch.Tensor, x_scale: torch.Tensor | None, w: LinearWeights,
         raise ValueError("x must hold int8 codes")
     dev = w.index
     m, k, ld = _rows_of(x, "x", dev)
+    _runs_on(dev, stream)
     n = w.n
     if k != w.k:
         raise ValueError(f"x has {k} columns, the weights {w.k}")
@@ -852,10 +866,11 @@ class DistillLoss(NamedTuple):
     grad: torch.Tensor | None = None
 
 
-def _distill_args(logits, index, teacher, row_weight, tau, grad):
+def _distill_args(logits, index, teacher, row_weight, tau, grad, stream):
     m, v, ld = _rows_of(logits, "logits")
     d = _float_dtype(logits, "logits")
     dev = logits.get_device()
+    _runs_on(dev, stream)
     top = teacher.shape[-1] if teacher.dim() else 0
     if index.shape != teacher.shape or index.shape[:-1] != logits.shape[:-1]:
         raise ValueError("index and teacher must have the logits' shape but for the last dimension")
@@ -877,7 +892,7 @@ def distill_topk(logits: torch.Tensor, index: torch.Tensor, teacher: torch.Tenso
     teacher float32 [..., top] at the vocabulary places index int64 [..., top]. grad: True, or a tensor (the logits
     themselves: in place), for the gradient of the losses' sum in the same pass."""
     g = _new(logits.shape, logits.dtype, logits.device, stream) if grad is True else None if grad is False else grad
-    _, args = _distill_args(logits, index, teacher, row_weight, tau, g)
+    _, args = _distill_args(logits, index, teacher, row_weight, tau, g, stream)
     loss = _new(logits.shape[:-1], torch.float32, logits.device, stream)
     lse = _new(logits.shape[:-1], torch.float32, logits.device, stream)
     _check(_calls().aqd_distill_topk(args, loss.data_ptr(), lse.data_ptr(), _stream(stream)), "aqd_distill_topk")
@@ -890,7 +905,7 @@ def distill_topk_backward(logits: torch.Tensor, index: torch.Tensor, teacher: to
     """The gradient of distill_topk's losses from the lse that it returned; row_weight: the factor of each token's
     gradient."""
     g = _new(logits.shape, logits.dtype, logits.device, stream) if grad is None else grad
-    m, args = _distill_args(logits, index, teacher, row_weight, tau, g)
+    m, args = _distill_args(logits, index, teacher, row_weight, tau, g, stream)
     lp = _vector(lse, m, torch.float32, "lse", logits.get_device())
     _check(_calls().aqd_distill_topk_backward(args, lp, _stream(stream)), "aqd_distill_topk_backward")
     return g

@@ -81,3 +81,35 @@ def test_a_workspace_of_any_type(made):
     for space in (Tensor((1 << 20,), torch.uint8), Tensor((64, 1 << 10), torch.float32), None):
         aqd.linear_int8(*codes(), layer(), workspace=space)
     assert made == ["aqd_linear_int8"] * 3
+
+
+def matrix(index=0, dtype=torch.float32, cols=128):
+    return Tensor((4, cols), dtype, index)
+
+
+def vector(n, index=0, dtype=torch.float32):
+    return Tensor((n,), dtype, index)
+
+
+CALLS = {
+    "quant_rows": lambda d, s: aqd.quant_rows(matrix(d), stream=s),
+    "rms_norm_quant": lambda d, s: aqd.rms_norm_quant(matrix(d), vector(128, d), residual=matrix(d), stream=s),
+    "gated_act_quant": lambda d, s: aqd.gated_act_quant(matrix(d), matrix(d), stream=s),
+    "LinearWeights": lambda d, s: aqd.LinearWeights(matrix(d, torch.int8), vector(4, d), stream=s),
+    "linear_int8": lambda d, s: aqd.linear_int8(*codes(d), layer(d), stream=s),
+    "distill_topk": lambda d, s: aqd.distill_topk(matrix(d), matrix(d, torch.int64, 8), matrix(d, cols=8), grad=True, stream=s),
+    "distill_topk_backward": lambda d, s: aqd.distill_topk_backward(matrix(d), matrix(d, torch.int64, 8), matrix(d, cols=8), vector(4, d), stream=s),
+}
+
+
+@pytest.mark.parametrize("call", list(CALLS))
+def test_tensors_and_streams_of_another_device_than_the_current_one(made, call):
+    """The kernels would run on the current device whatever the addresses are of."""
+    here, there = (SimpleNamespace(device=torch.device("cuda", i), cuda_stream=5) for i in (0, 1))
+    for d, s in ((1, None), (1, there), (0, there), (1, here)):
+        with pytest.raises(ValueError, match="device"):
+            CALLS[call](d, s)
+    assert [n for n in made if not n.endswith("_bytes")] == []
+    CALLS[call](0, None)
+    CALLS[call](0, here)
+    assert len([n for n in made if not n.endswith("_bytes")]) == 2
