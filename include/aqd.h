@@ -387,7 +387,8 @@ aqd_status aqd_quant_rows(int64_t rows, int32_t cols, const void* x, int64_t ldx
  *   u_k = h_k / sqrt(mean(h^2) + eps) * weight_k,
  * in float32 throughout; `sum` (NULL: not wanted) receives h rounded to `dtype`, the type of x, residual
  * and sum; the norm reads the unrounded h. sum may be x or residual itself (same pointer and ld): the residual
- * stream updated in place. weight: cols values of weight_dtype. eps >= 0. */
+ * stream updated in place. weight: cols values of weight_dtype. eps >= 0; with eps = 0 rows whose squares lie below
+ * float32's range are normalized like others. */
 typedef struct {
   int64_t rows;
   int32_t cols, dtype;

@@ -192,7 +192,7 @@ struct RowArgs {
   int64_t ld_values;
   int32_t values_dtype;
 };
-enum RowOp { kRowPlain = 0, kRowNorm = 1, kRowGated = 2 };
+enum RowOp { kRowPlain = 0, kRowNorm = 1, kRowGated = 2, kRowNormSmall = 3 };  // (the last: lm_rows.cu's own, the norm with an eps of nearly 0)
 int launch_rows(RowOp op, const RowArgs& a, cudaStream_t stream, std::string* err);
 
 // Prepared weights: a header (kLinHeader bytes), then n rows of lin_pitch(k) bytes, zero past k.

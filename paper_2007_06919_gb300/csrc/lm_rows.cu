@@ -26,6 +26,7 @@ namespace aqd {
 namespace rows {
 
 constexpr float kTiny = 7.52316385e-37f;  // 2^-120: 127 / a stays finite above it
+constexpr float kMinNormal = 1.17549435e-38f;  // 2^-126
 constexpr int kHeldBytes = 72 * 1024;  // shared memory of a held row: three blocks share an SM
 constexpr float kRound = 12582912.0f;     // 1.5 * 2^23: x + kRound has x rounded to nearest even in its low bits, for |x| < 2^22
 
@@ -166,14 +167,49 @@ __device__ __forceinline__ float activate(float g, int act) {
   return g * r;
 }
 
-// A row's codes: u * inv rounded; its scale. (rms: of the row, under the norm, else 1 / rms is 1)
-__device__ __forceinline__ void row_scale(float a, float ss, float rrms, float& inv, float& scale) {
+__host__ __device__ constexpr bool is_norm(RowOp op) { return op == kRowNorm || op == kRowNormSmall; }
+
+// The sum of a row's squares, under the norm. Squares are exact to 2^-150, so their mean plus eps is as good as float32's from 2^-126 on. Where
+// eps is below that (0, mostly; kRowNormSmall) the mean of a row of small values may be too, and `low` has the squares of 2^100 h, in
+// range for every row that small. (4096 x 4096 bf16 27.9 us, 25.7 without; 1000 x 32768 f32, over clusters of two blocks an SM instead of three, 111 and 93.
+// The two sums in one kernel for every eps would spill there; the second one in a pass ahead, read in a rare branch of these kernels: 8192 x 1024 bf16
+// 22.3 us for every eps, 13.4 now.)
+template <RowOp kOp>
+struct Squares {
+  float sum = 0.0f, low = 0.0f;
+  __device__ __forceinline__ void add(float h) {
+    if constexpr (is_norm(kOp)) sum = fmaf(h, h, sum);
+    if constexpr (kOp == kRowNormSmall) low = fmaf(h * 0x1p100f, h * 0x1p100f, low);
+  }
+  __device__ __forceinline__ void join(const Squares& o) {
+    if constexpr (is_norm(kOp)) sum += o.sum;
+    if constexpr (kOp == kRowNormSmall) low += o.low;
+  }
+  __device__ __forceinline__ void join_lanes() {
+    if constexpr (is_norm(kOp))
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if constexpr (kOp == kRowNormSmall)
+      for (int o = 16; o > 0; o >>= 1) low += __shfl_xor_sync(0xffffffffu, low, o);
+  }
+};
+
+// A row's codes: u * inv rounded; its scale, under the norm with the factor 1 / rms.
+template <RowOp kOp>
+__device__ __forceinline__ void row_scale(const RowArgs& p, int cols, float a, const Squares<kOp>& s, float& inv, float& scale) {
   inv = 0.0f;
   scale = 0.0f;
-  if (!(a < INFINITY) || !(ss < INFINITY)) scale = NAN;
+  float rrms = 1.0f, up = 1.0f;
+  if constexpr (is_norm(kOp)) rrms = rsqrtf(s.sum / (float)cols + p.eps);
+  if constexpr (kOp == kRowNormSmall) {
+    if (s.sum / (float)cols + p.eps < kMinNormal) {  // 2^100 / rms(2^100 h), the power in two parts that stay in range
+      rrms = rsqrtf(s.low / (float)cols + p.eps * 0x1p100f * 0x1p100f) * 0x1p60f;
+      up = 0x1p40f;
+    }
+  }
+  if (!(a < INFINITY) || !(s.sum < INFINITY)) scale = NAN;
   else if (a >= kTiny) {
     inv = 127.0f / a;
-    scale = a / 127.0f * rrms;
+    scale = a / 127.0f * rrms * up;
   }
 }
 
@@ -211,21 +247,23 @@ __device__ __forceinline__ void write_codes(const RowArgs& p, int64_t row, int64
 }
 
 // Statistics of a block's threads, in a fixed order: lanes, then warps.
-template <bool kSum>
-__device__ __forceinline__ void block_stats(uint32_t& top, float& ss) {
-  __shared__ float ssum[32];
+template <RowOp kOp>
+__device__ __forceinline__ void block_stats(uint32_t& top, Squares<kOp>& ss) {
+  __shared__ float ssum[32], slow[32];
   __shared__ uint32_t smax[32];
   const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   top = __reduce_max_sync(0xffffffffu, top);
-  if (kSum)
-    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-  if (lane == 0) { ssum[threadIdx.x >> 5] = ss; smax[threadIdx.x >> 5] = top; }
+  ss.join_lanes();
+  if (lane == 0) {
+    if constexpr (is_norm(kOp)) ssum[threadIdx.x >> 5] = ss.sum;
+    if constexpr (kOp == kRowNormSmall) slow[threadIdx.x >> 5] = ss.low;
+    smax[threadIdx.x >> 5] = top;
+  }
   __syncthreads();
   top = __reduce_max_sync(0xffffffffu, lane < warps ? smax[lane] : 0u);
-  if (kSum) {
-    ss = lane < warps ? ssum[lane] : 0.0f;
-    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-  }
+  if constexpr (is_norm(kOp)) ss.sum = lane < warps ? ssum[lane] : 0.0f;
+  if constexpr (kOp == kRowNormSmall) ss.low = lane < warps ? slow[lane] : 0.0f;
+  ss.join_lanes();
 }
 
 // kWarpRow: a warp per row, else a block; kV vectors of kE elements a thread (32 values of 32 bits take a block of at most 512).
@@ -241,7 +279,7 @@ __global__ void __launch_bounds__(kWarpRow ? 256 : (kV * kE >= 32 ? 512 : 1024))
   const int thread = kWarpRow ? lane : (int)threadIdx.x, step = (kWarpRow ? 32 : (int)blockDim.x) * kE;
   const int first = thread * kE - (kShift ? (int)((reinterpret_cast<uintptr_t>(a) & 15) / sizeof(T)) : 0);
   float u[kV][kE];
-  float ss = 0.0f;
+  Squares<kOp> ss;
   uint32_t top = 0;  // |u| as its bits: they order as the magnitudes do, a NaN above all
   if constexpr (kOp == kRowPlain) {
 #pragma unroll
@@ -259,7 +297,7 @@ __global__ void __launch_bounds__(kWarpRow ? 256 : (kV * kE >= 32 ? 512 : 1024))
     for (int i = 0; i < kV; ++i) {
       const int k = first + i * step;
       if (k >= p.cols) break;
-      if constexpr (kOp == kRowNorm) {
+      if constexpr (is_norm(kOp)) {
         if (p.b) {
 #pragma unroll
           for (int j = 0; j < kE; ++j) u[i][j] += v[i][j];
@@ -269,7 +307,7 @@ __global__ void __launch_bounds__(kWarpRow ? 256 : (kV * kE >= 32 ? 512 : 1024))
         load_weight<kE, kShift>(p, k, w);
 #pragma unroll
         for (int j = 0; j < kE; ++j) {
-          ss = fmaf(u[i][j], u[i][j], ss);
+          ss.add(u[i][j]);
           u[i][j] *= w[j];
         }
       } else {
@@ -286,13 +324,12 @@ __global__ void __launch_bounds__(kWarpRow ? 256 : (kV * kE >= 32 ? 512 : 1024))
   }
   if constexpr (kWarpRow) {
     top = __reduce_max_sync(0xffffffffu, top);
-    if (kOp == kRowNorm)
-      for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    ss.join_lanes();
   } else {
-    block_stats<kOp == kRowNorm>(top, ss);
+    block_stats(top, ss);
   }
   float inv, scale;
-  row_scale(__uint_as_float(top), ss, kOp == kRowNorm ? rsqrtf(ss / (float)p.cols + p.eps) : 1.0f, inv, scale);
+  row_scale(p, p.cols, __uint_as_float(top), ss, inv, scale);
   if ((kShift ? thread : first) == 0) p.scales[row] = scale;
   if (isnan(scale)) {
 #pragma unroll
@@ -315,7 +352,7 @@ __device__ __forceinline__ void units(const RowArgs& p, int64_t row, int64_t k, 
   if constexpr (kOp != kRowPlain) {
     float v[kE];
     if (kOp == kRowGated || p.b) load_vec<kE>(static_cast<const T*>(p.b) + row * p.ldb + k, v);
-    if constexpr (kOp == kRowNorm) {
+    if constexpr (is_norm(kOp)) {
       if (p.b) {
 #pragma unroll
         for (int j = 0; j < kE; ++j) u[j] += v[j];
@@ -336,23 +373,24 @@ template <class T, RowOp kOp, int kE>
 __global__ void __launch_bounds__(512) rows_long_kernel(const RowArgs p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int64_t row = blockIdx.x;
-  float ss = 0.0f, u[kE], h[kE];
+  Squares<kOp> ss;
+  float u[kE], h[kE];
   uint32_t top = 0;
   for (int64_t k = (int64_t)threadIdx.x * kE; k < p.cols; k += 512 * kE) {
     units<T, kOp, kE>(p, row, k, u, h);
 #pragma unroll
     for (int j = 0; j < kE; ++j) {
-      if (kOp == kRowNorm) ss = fmaf(h[j], h[j], ss);
+      if constexpr (is_norm(kOp)) ss.add(h[j]);
       top = max(top, __float_as_uint(fabsf(u[j])));
     }
   }
-  block_stats<kOp == kRowNorm>(top, ss);
+  block_stats(top, ss);
   float inv, scale;
-  row_scale(__uint_as_float(top), ss, kOp == kRowNorm ? rsqrtf(ss / (float)p.cols + p.eps) : 1.0f, inv, scale);
+  row_scale(p, p.cols, __uint_as_float(top), ss, inv, scale);
   if (threadIdx.x == 0) p.scales[row] = scale;
   for (int64_t k = (int64_t)threadIdx.x * kE; k < p.cols; k += 512 * kE) {
     units<T, kOp, kE>(p, row, k, u, h);
-    if (kOp == kRowNorm && p.sum) store_vec<kE>(static_cast<T*>(p.sum) + row * p.ld_sum + k, h);
+    if (is_norm(kOp) && p.sum) store_vec<kE>(static_cast<T*>(p.sum) + row * p.ld_sum + k, h);
     if (isnan(scale)) {
 #pragma unroll
       for (int j = 0; j < kE; ++j) u[j] = 0.0f;
@@ -371,11 +409,11 @@ enum Lie { kWhole, kShifted, kLoose, kAnyhow };
 // element, and u in a place of its own; the threads then take the outputs' vectors, or the row's elements, in turn.
 // kSplit (of kWhole): a cluster of `splits` blocks per row, `part` columns each, which join their statistics.
 template <class T, RowOp kOp, Lie kLie, bool kSplit>
-__global__ void __launch_bounds__(512, (kLie == kShifted && kOp == kRowNorm) || kLie == kLoose ? 2 : 3)
+__global__ void __launch_bounds__(512, (kLie == kShifted && is_norm(kOp)) || kLie == kLoose || (kSplit && kOp == kRowNormSmall) ? 2 : 3)
 rows_held_kernel(const RowArgs call, const int bytes, const int splits, const int part) {
   extern __shared__ __align__(16) uint8_t smem[];  // a, then b where there are two (`bytes` each), then u (kLoose, kAnyhow)
   constexpr int kE = 16 / sizeof(T);
-  __shared__ uint2 joined[kSplit ? 8 : 1];  // every block's statistics
+  __shared__ uint4 joined[kSplit ? 8 : 1];  // every block's maximum and squares
   RowArgs p = call;
   if constexpr (kSplit) {  // from here on a row is this block's part of it
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // (waited for before the first store into another block)
@@ -391,7 +429,7 @@ rows_held_kernel(const RowArgs call, const int bytes, const int splits, const in
   constexpr bool kVec = kLie != kAnyhow, kOwn = kLie == kWhole || kLie == kShifted, kShift = kLie == kShifted || kLie == kLoose;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int64_t row = kSplit ? blockIdx.y : blockIdx.x;
-  const bool two = kOp == kRowGated || (kOp == kRowNorm && p.b);
+  const bool two = kOp == kRowGated || (is_norm(kOp) && p.b);
   const T* ab[2] = {static_cast<const T*>(p.a) + row * p.lda, static_cast<const T*>(p.b) + row * p.ldb};
   int off[2] = {0, 0};
 #pragma unroll
@@ -425,7 +463,7 @@ rows_held_kernel(const RowArgs call, const int bytes, const int splits, const in
   tc::cp_async_commit();
   tc::cp_async_wait<0>();
   if (!kOwn) __syncthreads();
-  float ss = 0.0f;
+  Squares<kOp> ss;
   uint32_t top = 0;
   constexpr int kU = kVec ? kE : 1;
   const bool again = kOwn && sizeof(T) == 2 && !two;  // u is computed twice
@@ -451,7 +489,7 @@ rows_held_kernel(const RowArgs call, const int bytes, const int splits, const in
     if constexpr (kOp != kRowPlain) {
       float v[kU];
       if (two) input(1, k, v);
-      if constexpr (kOp == kRowNorm) {
+      if constexpr (is_norm(kOp)) {
         if (two) {
 #pragma unroll
           for (int j = 0; j < kU; ++j) u[j] += v[j];
@@ -469,10 +507,10 @@ rows_held_kernel(const RowArgs call, const int bytes, const int splits, const in
   for (int k = first; k < p.cols; k += step) {
     float u[kU], h[kU];
     units_of(k, u, h);
-    if (kOp == kRowNorm && p.sum) store_sum<kU, kShift, T>(p, row, k, h);
+    if (is_norm(kOp) && p.sum) store_sum<kU, kShift, T>(p, row, k, h);
 #pragma unroll
     for (int j = 0; j < kU; ++j) {
-      if (kOp == kRowNorm) ss = fmaf(h[j], h[j], ss);
+      if constexpr (is_norm(kOp)) ss.add(h[j]);
       top = max(top, __float_as_uint(fabsf(u[j])));
     }
     if constexpr (!kOwn) store_vec<kU>(us + k + out, u);
@@ -483,22 +521,26 @@ rows_held_kernel(const RowArgs call, const int bytes, const int splits, const in
         *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(at) + bytes) = make_uint4(__float_as_uint(u[4]), __float_as_uint(u[5]), __float_as_uint(u[6]), __float_as_uint(u[7]));
     }
   }
-  block_stats<kOp == kRowNorm>(top, ss);
+  block_stats(top, ss);
   if constexpr (kSplit) {
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if ((int)threadIdx.x < splits) {
       const uint32_t to = tc::mapa_shared(tc::smem_u32(&joined[blockIdx.x]), threadIdx.x);
-      asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(to), "r"(top), "r"(__float_as_uint(ss)) : "memory");
+      asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(to), "r"(top), "r"(__float_as_uint(ss.sum)) : "memory");
+      if constexpr (kOp == kRowNormSmall) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to + 8), "r"(__float_as_uint(ss.low)) : "memory");
     }
     tc::cluster_sync();
-    ss = 0.0f;
+    ss = Squares<kOp>();
     for (int i = 0; i < splits; ++i) {  // in the blocks' order
       top = max(top, joined[i].x);
-      ss += __uint_as_float(joined[i].y);
+      Squares<kOp> other;
+      other.sum = __uint_as_float(joined[i].y);
+      if constexpr (kOp == kRowNormSmall) other.low = __uint_as_float(joined[i].z);
+      ss.join(other);
     }
   }
   float inv, scale;
-  row_scale(__uint_as_float(top), ss, kOp == kRowNorm ? rsqrtf(ss / (float)call.cols + p.eps) : 1.0f, inv, scale);
+  row_scale(p, call.cols, __uint_as_float(top), ss, inv, scale);
   if (threadIdx.x == 0 && (!kSplit || blockIdx.x == 0)) p.scales[row] = scale;
   for (int k = first; k < p.cols; k += step) {
     float u[kU], h[kU];
@@ -666,6 +708,9 @@ static cudaError_t run(const RowArgs& a, cudaStream_t stream) {
 template <class T>
 static cudaError_t run_op(RowOp op, const RowArgs& a, cudaStream_t stream) {
   if (op == kRowPlain) return run<T, kRowPlain>(a, stream);
+  if constexpr (!std::is_same<T, __half>::value) {  // (no square of a binary16 value or sum is that small)
+    if (op == kRowNorm && a.eps < kMinNormal) return run<T, kRowNormSmall>(a, stream);
+  }
   if (op == kRowNorm) return run<T, kRowNorm>(a, stream);
   return run<T, kRowGated>(a, stream);
 }
