@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(kMaxThreads, kStay ? 6 : 4) distill_kernel(con
   }
   if (!g) return;
   for (int j = threadIdx.x; j < p.top; j += threads) share[j] = sidx[j] >= 0 ? ex(sp[j] - t.m) / t.s : 0.0f;
-  const float fs = f0 / s.s;
+  const float fs = isnan(t.s) ? NAN : f0 / s.s;  // (p a NaN: its sum, which q is multiplied by, is one too)
   uint4* gv = reinterpret_cast<uint4*>(g - off);
   auto slopes = [&](int v, bool inside, float (&f)[kE]) {
     Vec<T>::unpack(kStay ? held[v - v0] : inside ? __ldcs(xv + v) : load_edge(x, (int64_t)v * kE - off, p.vocab), f);
