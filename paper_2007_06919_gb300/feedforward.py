@@ -93,7 +93,9 @@ class Head(_Part):
         rate > 0: a gradient step on these. On the current stream."""
         out = aqd.distill_topk(logits, index, teacher, tau=tau, row_weight=row_weight, grad=True)
         vocab = logits.shape[-1]
-        slope = (out.grad.view(-1, vocab).float() * logits.reshape(-1, vocab).float()).sum(0)
+        grad = out.grad.view(-1, vocab)
+        # a gradient of 0 adds nothing, whatever the logit: of a token of weight 0 it may be a NaN, of a place that a mask rules out -infinity
+        slope = (grad.float() * logits.reshape(-1, vocab).float()).masked_fill_(grad == 0, 0.0).sum(0)
         if rate:
             self.proj.scales.mul_(torch.exp(-rate * slope))
         return out.loss, slope
