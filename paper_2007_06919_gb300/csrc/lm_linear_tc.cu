@@ -9,7 +9,8 @@
 // warp's store of one token's outputs is contiguous, and a channel's scale is one register). The tokens' codes, which every channel tile
 // reads again, become F16 once per call, in the workspace (expand_kernel), and TMA brings them as the B operand. One thread of the pair issues
 // the MMAs (cta_group::2).
-// (Measured at 8192 tokens, n 12288, K 4096: 435 to 473 us, 1740 to 1890 TFLOP/s, a library bf16 product's rate; both operands converted
+// (Measured at 8192 tokens, n 12288, K 4096, with expand_kernel: 445 to 460 us for the first launches after a pause, 1790 to 1850 TFLOP/s; 490 us, 1680 TFLOP/s,
+// from 50 ms on, when the power limit lowers the clock. A library bf16 product of that size 412 to 433 and 470. Both operands converted
 // in the kernel 578 us at best, bound by the converting warps' issue slots and their stages' shared memory.)
 //
 // A pair computes whole tiles, in turn. The tiles' width in tokens follows the problem (plan): narrow tiles give few tokens to every pair, where

@@ -171,7 +171,7 @@ __host__ __device__ constexpr bool is_norm(RowOp op) { return op == kRowNorm || 
 
 // The sum of a row's squares, under the norm. Squares are exact to 2^-150, so their mean plus eps is as good as float32's from 2^-126 on. Where
 // eps is below that (0, mostly; kRowNormSmall) the mean of a row of small values may be too, and `low` has the squares of 2^100 h, in
-// range for every row that small. (4096 x 4096 bf16 27.9 us, 25.7 without; 1000 x 32768 f32, over clusters of two blocks an SM instead of three, 111 and 93.
+// range for every row that small. (4096 x 4096 bf16 27.9 us, 25.7 without; 1000 x 32768 f32, over clusters of two blocks an SM instead of three, 111 and 94.
 // The two sums in one kernel for every eps would spill there; the second one in a pass ahead, read in a rare branch of these kernels: 8192 x 1024 bf16
 // 22.3 us for every eps, 13.4 now.)
 template <RowOp kOp>
@@ -586,8 +586,8 @@ static cudaError_t start_held(const RowArgs& a, cudaStream_t stream, int splits 
   }
   const int units = kLie != kAnyhow ? bytes / 16 : a.cols;
   // Three vectors a thread; four or five where that lets more blocks share an SM: of kLoose, for its registers (3000 x 3333 f16, gated, four
-  // 20.3 us, three 22.2, two 24.8), and of a cluster, whose parts are shorter (3000 x 10240 f32, gated, five 60, four 65, three 77; 1000 x
-  // 16384 f32, the norm, five 54, four 51).
+  // 20.3 us, three 22.2, two 24.8), and of a cluster, whose parts are shorter (3000 x 10240 f32, gated, five 58, four 63, three 74; 1000 x
+  // 16384 f32, the norm, five 51, four 48).
   constexpr int kEach = kLie == kLoose ? 4 : !kSplit ? 3 : kOp == kRowGated ? 5 : 4;
   int threads = (units + kEach - 1) / kEach;
   threads = threads < 64 ? 64 : (threads > 512 ? 512 : (threads + 31) / 32 * 32);
@@ -673,8 +673,8 @@ static cudaError_t run(const RowArgs& a, cudaStream_t stream) {
   auto block = [](int64_t n, int v) { return (unsigned)(((n + v - 1) / v + 31) / 32 * 32); };  // threads for n elements, v each
   if (vec) {
     if (a.cols <= 1024 * kE || held<T>(a, kWhole)) return run_vectors<T, kOp, false>(a, stream);
-    // Longer rows in the shared memory of a cluster; for few rows of more blocks than they need. (1500 x 32768 f32, gated: 101 us, read twice
-    // 139; 1000 x 131072 bf16 178 and 230; 300 x 131072 bf16, the norm, 71 and 100; one row of 32768 f32, gated, 3.3 and 11.4.)
+    // Longer rows in the shared memory of a cluster; for few rows of more blocks than they need. (1500 x 32768 f32, gated: 97 us, read twice
+    // 138; 1000 x 131072 bf16, gated, 171 and 229; 300 x 131072 bf16, the norm, 69 and 102; one row of 32768 f32, gated, 3.3 and 11.8.)
     const int64_t room = kHeldBytes / 16 / (a.b ? 2 : 1) - 2, n = a.cols / kE;
     int64_t splits = (n + room - 1) / room;
     if (splits <= 8) {
