@@ -454,6 +454,131 @@ size_t aqd_linear_workspace_bytes(int64_t m, const aqd_linear_weights* w);
 aqd_status aqd_linear_int8(const aqd_linear_args* args, const aqd_linear_weights* w, void* workspace, size_t ws_bytes,
                            aqd_stream_t stream);
 
+/* ---- attention of an 8-bit decoder ------------------------------------------------------ */
+
+/* What lies between a decoder's 8-bit query-key-value product and its 8-bit output product: norms of queries and keys with
+ * the position rotation, a cache of keys and values in 4 bits (Eq. 1's uniform quantizer, its interval taken from each row as above),
+ * attention over that cache, and attention over whole prompts.
+ *
+ * Tensors of heads are [tokens][heads][head_dim] with strides in elements: ld from a token to the next, ldh from a head to the
+ * next, both >= 0 and any for an input; the values of a head are adjacent. kv_heads divides heads: query head h reads key and value
+ * head h / (heads / kv_heads). Outputs do not overlap inputs or each other, except where said. */
+
+/* A cache of `pages` pages; a page holds page_size places (a power of two, 16..1024) of every key-value head. Place p of page g is
+ * slot g * page_size + p. A place holds, of each head, a key row and a value row: head_dim (64, 128, 192 or 256) codes of 4 bits,
+ * the row's lowest value and its step, both bfloat16:
+ *   low = the largest bfloat16 <= min_k x_k,  step = the least bfloat16 >= (max_k x_k - low) / 15 (at least 2^-126, but 0 where max = low),
+ *   code_k = (x_k - low) / step to the nearest, ties to even (0 where step = 0);  value = low + step * code.
+ * So a value is off by half a step at most. Rows that hold a NaN or an infinity, or whose values span more than float32's range, read back
+ * as NaN. The layout within a page is the library's own. */
+typedef struct {
+  void* data; /* aqd_kv_cache_bytes(...) bytes (device), 256-byte aligned; its first contents do not matter */
+  int64_t pages;
+  int32_t page_size, kv_heads, head_dim;
+} aqd_kv_cache;
+/* 0 for sizes that are not supported (pages < 1, kv_heads outside 1..65535, over 2^40 bytes, and as above). */
+size_t aqd_kv_cache_bytes(int64_t pages, int32_t page_size, int32_t kv_heads, int32_t head_dim);
+
+/* Queries and keys before attention, per token and head, in float32, rounded once to `dtype` (AQD_F32, AQD_F16, AQD_BF16, of all tensors here but
+ * the weights and tables):
+ *   u_k = x_k / sqrt(mean(x^2) + eps) * weight_k  (weight NULL: u = x, for queries and keys each; head_dim values of weight_dtype),
+ *   then pair f of the first rot_dim places turns by the angle a = positions[token] * inv_freq[f], f < rot_dim / 2:
+ *   (u_i, u_j) -> (u_i cos a - u_j sin a, u_j cos a + u_i sin a), with i = f, j = f + rot_dim / 2, or, if interleaved, i = 2 f, j = 2 f + 1.
+ * The angle is exact to 2^-24 of a turn while |position| < 2^38 and |position * inv_freq| < 2^28 (it is reduced in fixed point). rot_dim: even, 0..head_dim.
+ * head_dim: even, 2..512 (with a cache: its own). q_out may be q, and k_out k (same pointer and strides).
+ * heads may be 0 (keys alone). cache NULL: v and slots are not read. With a cache, each token's keys (rotated and rounded to `dtype`) and
+ * values v are written to place slots[token] too, the bytes that aqd_cache_write would write; k_out may then be NULL. A slot outside the cache is
+ * skipped. The slots inside it are distinct; of one listed twice a row may mix both tokens'. */
+typedef struct {
+  int64_t tokens;
+  int32_t heads, kv_heads, head_dim, dtype;
+  const void* q;
+  int64_t ldq, ldqh;
+  const void* k;
+  int64_t ldk, ldkh;
+  const void* v;
+  int64_t ldv, ldvh;
+  void* q_out;
+  int64_t ldq_out, ldqh_out;
+  void* k_out;
+  int64_t ldk_out, ldkh_out;
+  const void* q_weight;
+  const void* k_weight;
+  int32_t weight_dtype;
+  float eps;
+  const int64_t* positions;
+  const float* inv_freq;
+  int32_t rot_dim, interleaved;
+  const int64_t* slots;
+} aqd_qk_rope_args;
+aqd_status aqd_qk_norm_rope(const aqd_qk_rope_args* args, const aqd_kv_cache* cache, aqd_stream_t stream);
+
+/* Rows of keys and values (k, v: [tokens][kv_heads][head_dim] of dtype) to places slots[token], and the values that the places hold back from there
+ * (a slot outside the cache: skipped by the write, zeros from the read). Reading, k or v may be NULL. Slots as above; a read may list one twice. */
+typedef struct {
+  int64_t tokens;
+  int32_t dtype;
+  void* k;
+  int64_t ldk, ldkh;
+  void* v;
+  int64_t ldv, ldvh;
+  const int64_t* slots;
+} aqd_cache_rows;
+aqd_status aqd_cache_write(const aqd_cache_rows* rows, const aqd_kv_cache* cache, aqd_stream_t stream);
+aqd_status aqd_cache_read(const aqd_cache_rows* rows, const aqd_kv_cache* cache, aqd_stream_t stream);
+
+/* Attention of each sequence's last tokens over the cache. Sequence s has lengths[s] places, place t in page pages[s][t / page_size] (a row of
+ * `columns` entries of the table; longer lengths are cut to columns * page_size, negative ones are 0), and the queries of tokens starts[s] .. starts[s+1] - 1
+ * (starts NULL: token s alone; tokens = seqs then). Query j of its n sees the places t < lengths[s] - n + j + 1: its own token's and those before.
+ *   o = sum_t p_t v_t,  p = softmax over the places seen of scale * q . k_t,  lse = ln sum_t exp(scale * q . k_t).
+ * k_t and v_t are the cache's values. A query that sees no place gets o = 0 and lse = -infinity. Places in a page outside [0, pages) are not there.
+ * Rows of out behind the last sequence are left as they were. dtype (q and out): AQD_F16 or AQD_BF16. starts[0] >= 0, not falling, at most tokens.
+ * scale > 0, finite. q takes part as float16 after a power-of-two factor per row (values below 2^-29 of the row's largest lose bits); scores,
+ * statistics and sums are float32, p times the value's step is float16 with the largest step's power in front.
+ * Work is split over places by the lengths at hand; parts join in a fixed order. workspace: aqd_cache_attention_workspace_bytes(...) bytes,
+ * 256-byte aligned; its contents do not matter, and calls that share it must not overlap in time. */
+typedef struct {
+  int64_t tokens;
+  int32_t seqs, heads, dtype;
+  float scale;
+  const void* q;
+  int64_t ldq, ldqh;
+  void* out;
+  int64_t ldo, ldoh;
+  float* lse;               /* [tokens][heads] or NULL */
+  const int32_t* starts;    /* [seqs + 1] or NULL */
+  const int32_t* lengths;   /* [seqs] */
+  const int32_t* page_table; /* [seqs][ld_table], `columns` of them used */
+  int64_t ld_table;
+  int32_t columns;
+} aqd_cache_attention_args;
+size_t aqd_cache_attention_workspace_bytes(int64_t tokens, int32_t seqs, int32_t heads, const aqd_kv_cache* cache);
+aqd_status aqd_cache_attention(const aqd_cache_attention_args* args, const aqd_kv_cache* cache, void* workspace, size_t ws_bytes, aqd_stream_t stream);
+
+/* Attention over whole sequences, packed one after another: sequence s has the queries starts[s] .. starts[s+1] - 1 and the keys and values
+ * kv_starts[s] .. kv_starts[s+1] - 1 (kv_starts NULL: the same). causal: query j of n sees the first m - n + j + 1 of its sequence's m keys; else all.
+ * o and lse as above; a query that sees nothing gets 0 and -infinity; rows behind the last sequence are left as they were. dtype (q, k, v, out): AQD_F16 or
+ * AQD_BF16; head_dim 64, 128, 192 or 256; every pointer of them 16-byte aligned, every stride a multiple of 8 elements. Scores, statistics and sums
+ * are float32; p is rounded to dtype before it meets v. Within a sequence, a NaN or infinity in a value row may reach queries up to 255 places before
+ * it; other sequences' rows are never read into a result. tokens and kv_tokens: rows of q and of k. */
+typedef struct {
+  int64_t tokens, kv_tokens;
+  int32_t seqs, heads, kv_heads, head_dim, dtype, causal;
+  float scale;
+  const void* q;
+  int64_t ldq, ldqh;
+  const void* k;
+  int64_t ldk, ldkh;
+  const void* v;
+  int64_t ldv, ldvh;
+  void* out;
+  int64_t ldo, ldoh;
+  float* lse;               /* [tokens][heads] or NULL */
+  const int32_t* starts;    /* [seqs + 1] */
+  const int32_t* kv_starts; /* [seqs + 1] or NULL */
+} aqd_prompt_attention_args;
+aqd_status aqd_prompt_attention(const aqd_prompt_attention_args* args, aqd_stream_t stream);
+
 /* ---- distillation from a teacher's top logits ----------------------------------------- */
 
 /* The loss that trains a low-bit student from a float teacher of which only the `top` largest logits of each

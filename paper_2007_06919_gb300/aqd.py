@@ -65,7 +65,9 @@ EXPORTS = ["aqd_row_bytes", "aqd_quantize_multiplier", "aqd_status_string", "aqd
            "aqd_fake_quant_backward_workspace_bytes", "aqd_fake_quant_backward",
            "aqd_bn_level_stats_workspace_bytes", "aqd_bn_level_stats", "aqd_quant_rows", "aqd_rms_norm_quant",
            "aqd_gated_act_quant", "aqd_linear_weights_bytes", "aqd_linear_prepare_weights",
-           "aqd_linear_workspace_bytes", "aqd_linear_int8", "aqd_distill_topk", "aqd_distill_topk_backward"]
+           "aqd_linear_workspace_bytes", "aqd_linear_int8", "aqd_distill_topk", "aqd_distill_topk_backward",
+           "aqd_kv_cache_bytes", "aqd_qk_norm_rope", "aqd_cache_write", "aqd_cache_read", "aqd_cache_attention_workspace_bytes",
+           "aqd_cache_attention", "aqd_prompt_attention"]
 
 _lib = None
 _hot = None  # the same library for the calls below that pass their structs as packed bytes
@@ -188,7 +190,14 @@ def load(build_if_missing: bool = True):
                        ("aqd_linear_workspace_bytes", [i64, vp]),
                        ("aqd_linear_int8", [vp, vp, vp, sz, vp]),
                        ("aqd_distill_topk", [vp, vp, vp, vp]),
-                       ("aqd_distill_topk_backward", [vp, vp, vp])):
+                       ("aqd_distill_topk_backward", [vp, vp, vp]),
+                       ("aqd_kv_cache_bytes", [i64, i32, i32, i32]),
+                       ("aqd_qk_norm_rope", [vp, vp, vp]),
+                       ("aqd_cache_write", [vp, vp, vp]),
+                       ("aqd_cache_read", [vp, vp, vp]),
+                       ("aqd_cache_attention_workspace_bytes", [i64, i32, i32, vp]),
+                       ("aqd_cache_attention", [vp, vp, vp, sz, vp]),
+                       ("aqd_prompt_attention", [vp, vp])):
         fn = getattr(hot, name)
         fn.argtypes = args
         fn.restype = sz if name.endswith("_bytes") else c_int
@@ -620,6 +629,11 @@ _GATED_ACT = struct.Struct("=qiiQqQqi4x")           # aqd_gated_act_args
 _LINEAR_W = struct.Struct("=QQii")                 # aqd_linear_weights
 _LINEAR = struct.Struct("=qQqQQQqi4x")             # aqd_linear_args
 _DISTILL = struct.Struct("=qiiQqQQifQQq")          # aqd_distill_args
+_KV_CACHE = struct.Struct("=Qqiii4x")              # aqd_kv_cache
+_QK_ROPE = struct.Struct("=qiiiiQqqQqqQqqQqqQqqQQifQQiiQ")  # aqd_qk_rope_args
+_CACHE_ROWS = struct.Struct("=qi4xQqqQqqQ")        # aqd_cache_rows
+_CACHE_ATTENTION = struct.Struct("=qiiifQqqQqqQQQQqi4x")  # aqd_cache_attention_args
+_PROMPT = struct.Struct("=qqiiiiiif4xQqqQqqQqqQqqQQQ")  # aqd_prompt_attention_args
 
 
 class RowCodes(NamedTuple):
@@ -858,6 +872,227 @@ def linear_int8(x: torch.Tensor, x_scale: torch.Tensor | None, w: LinearWeights,
     _check(_calls().aqd_linear_int8(_LINEAR.pack(m, x.data_ptr(), ld, xs, bp, out.data_ptr(), ldy, yd), w.desc, wsp, wsb,
                                     _stream(stream)), "aqd_linear_int8")
     return out
+
+
+# ------------------------------------------------------------------ attention of an 8-bit decoder
+
+
+def _heads(t: torch.Tensor, name: str, device: int | None = None):
+    """(tokens, heads, head_dim, stride of a token, of a head) of a CUDA tensor [tokens, heads, head_dim]; ValueError where the
+    values of a head are not adjacent. device: the index of the call's device."""
+    if not t.is_cuda or (device is not None and t.get_device() != device):
+        raise ValueError(f"{name} must be a CUDA tensor on the call's device")
+    if len(t.shape) != 3:
+        raise ValueError(f"{name} must be [tokens, heads, head_dim]")
+    n, h, d = t.shape
+    ld, ldh, last = t.stride()
+    if last != 1 and d > 1:
+        raise ValueError(f"the values of a head of {name} must be adjacent")
+    return n, h, d, ld, ldh
+
+
+def _out_heads(out: torch.Tensor | None, like: torch.Tensor, name: str, stream):
+    """The tensor for an output of like's shape and type (a new one where out is None), and its two strides."""
+    if out is None:
+        n, h, d = like.shape
+        return _new((n, h, d), like.dtype, like.device, stream), h * d, d
+    if out.shape != like.shape or out.dtype is not like.dtype:
+        raise ValueError(f"{name} must have its input's shape and type")
+    _, _, _, ld, ldh = _heads(out, name, like.get_device())
+    return out, ld, ldh
+
+
+class KVCache:
+    """A 4-bit cache of keys and values (aqd_kv_cache): `pages` pages of page_size places (a power of two, 16..1024), each
+    place a key and a value row of every head. Its memory belongs to the stream current at construction, or to `stream`."""
+
+    def __init__(self, pages: int, page_size: int, kv_heads: int, head_dim: int, device="cuda", stream=None):
+        nbytes = int(_calls().aqd_kv_cache_bytes(pages, page_size, kv_heads, head_dim))
+        if nbytes == 0:
+            raise ValueError(f"unsupported cache shape: {pages} pages of {page_size}, {kv_heads} heads of {head_dim}")
+        buf = _new(nbytes + 256, torch.uint8, device, stream)
+        off = -buf.data_ptr() % 256
+        self.data = buf[off:off + nbytes]
+        self.pages, self.page_size, self.kv_heads, self.head_dim = pages, page_size, kv_heads, head_dim
+        self.device, self.index = buf.device, buf.get_device()
+        self.desc = _KV_CACHE.pack(self.data.data_ptr(), pages, page_size, kv_heads, head_dim)
+
+
+class Rotated(NamedTuple):
+    q: torch.Tensor
+    k: torch.Tensor | None
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | None, inv_freq: torch.Tensor | None, *,
+                 q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6,
+                 interleaved: bool = False, q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None,
+                 v: torch.Tensor | None = None, cache: KVCache | None = None, slots: torch.Tensor | None = None,
+                 stream=None) -> Rotated:
+    """Queries [tokens, heads, head_dim] and keys [tokens, kv_heads, head_dim] normed for each head (where a weight is given) and
+    turned by their position (aqd_qk_norm_rope): positions int64 [tokens], inv_freq float32, one for each turned pair. q_out, k_out: q and
+    k themselves, in place. With a cache, keys and values v go to its places slots (int64 [tokens]) in the same pass, and k comes back only
+    where k_out is given."""
+    n, h, d, lq, lqh = _heads(q, "q")
+    dt = _float_dtype(q, "q")
+    dev = q.get_device()
+    _runs_on(dev, stream)
+    nk, hk, dk, lk, lkh = _heads(k, "k", dev)
+    if nk != n or dk != d or k.dtype is not q.dtype:
+        raise ValueError("k must have q's tokens, head_dim and type")
+    rot, pp, fp = 0, 0, 0
+    if inv_freq is not None and inv_freq.numel() > 0:
+        rot = 2 * inv_freq.numel()
+        if positions is None:
+            raise ValueError("positions are required")
+        fp = _vector(inv_freq, rot // 2, torch.float32, "inv_freq", dev)
+        pp = _vector(positions, n, torch.int64, "positions", dev)
+    wd, wq, wk = 0, 0, 0
+    if q_weight is not None:
+        wd = _float_dtype(q_weight, "q_weight")
+        wq = _vector(q_weight, d, q_weight.dtype, "q_weight", dev)
+    if k_weight is not None:
+        if q_weight is not None and k_weight.dtype is not q_weight.dtype:
+            raise ValueError("the weights must have one type")
+        wd = _float_dtype(k_weight, "k_weight")
+        wk = _vector(k_weight, d, k_weight.dtype, "k_weight", dev)
+    vp = lv = lvh = sp = 0
+    desc = None
+    if cache is not None:
+        if v is None or slots is None:
+            raise ValueError("v and slots are required with a cache")
+        nv, hv, dv, lv, lvh = _heads(v, "v", dev)
+        if (nv, hv, dv) != (n, hk, d) or v.dtype is not q.dtype:
+            raise ValueError("v must have k's shape and type")
+        if cache.index != dev:
+            raise ValueError("the cache must be on the call's device")
+        vp, sp, desc = v.data_ptr(), _vector(slots, n, torch.int64, "slots", dev), cache.desc
+    qo, lqo, lqoh = _out_heads(q_out, q, "q_out", stream)
+    kp = lko = lkoh = 0
+    if k_out is not None or cache is None:
+        k_out, lko, lkoh = _out_heads(k_out, k, "k_out", stream)
+        kp = k_out.data_ptr()
+    args = _QK_ROPE.pack(n, h, hk, d, dt, q.data_ptr(), lq, lqh, k.data_ptr(), lk, lkh, vp, lv, lvh, qo.data_ptr(), lqo, lqoh,
+                         kp, lko, lkoh, wq, wk, wd, eps, pp, fp, rot, 1 if interleaved else 0, sp)
+    _check(_calls().aqd_qk_norm_rope(args, desc, _stream(stream)), "aqd_qk_norm_rope")
+    return Rotated(qo, k_out)
+
+
+def cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, *, stream=None) -> None:
+    """Rows of keys and values [tokens, kv_heads, head_dim] in 4 bits to the cache's places slots, int64 [tokens]
+    (aqd_cache_write); a token whose slot lies outside the cache is skipped."""
+    n, h, d, lk, lkh = _heads(k, "k", cache.index)
+    dt = _float_dtype(k, "k")
+    _runs_on(cache.index, stream)
+    _, _, _, lv, lvh = _heads(v, "v", cache.index)
+    if v.shape != k.shape or v.dtype is not k.dtype:
+        raise ValueError("v must have k's shape and type")
+    if h != cache.kv_heads or d != cache.head_dim:
+        raise ValueError("k and v must have the cache's heads")
+    sp = _vector(slots, n, torch.int64, "slots", cache.index)
+    _check(_calls().aqd_cache_write(_CACHE_ROWS.pack(n, dt, k.data_ptr(), lk, lkh, v.data_ptr(), lv, lvh, sp), cache.desc,
+                                    _stream(stream)), "aqd_cache_write")
+
+
+def cache_read(cache: KVCache, slots: torch.Tensor, *, dtype=torch.bfloat16, stream=None):
+    """(keys, values), [tokens, kv_heads, head_dim] of dtype: what the cache's places slots hold (aqd_cache_read); zeros for
+    a slot outside the cache. A prompt that goes on from cached places reads them so for prompt_attention."""
+    d = _DTYPE.get(dtype)
+    if d is None:
+        raise ValueError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
+    _runs_on(cache.index, stream)
+    n, h, w = slots.numel(), cache.kv_heads, cache.head_dim
+    sp = _vector(slots, n, torch.int64, "slots", cache.index)
+    k, v = _new((n, h, w), dtype, cache.device, stream), _new((n, h, w), dtype, cache.device, stream)
+    _check(_calls().aqd_cache_read(_CACHE_ROWS.pack(n, d, k.data_ptr(), h * w, w, v.data_ptr(), h * w, w, sp), cache.desc,
+                                   _stream(stream)), "aqd_cache_read")
+    return k, v
+
+
+@functools.lru_cache(maxsize=4096)
+def _cache_attention_bytes(tokens: int, seqs: int, heads: int, page_size: int, kv_heads: int, head_dim: int) -> int:
+    return int(_calls().aqd_cache_attention_workspace_bytes(tokens, seqs, heads, _KV_CACHE.pack(0, 1, page_size, kv_heads, head_dim)))
+
+
+def cache_attention_workspace(q: torch.Tensor, cache: KVCache, seqs: int, *, stream=None) -> torch.Tensor:
+    """A workspace for cache_attention with queries of q's shape and that many sequences, for calls that follow one another on
+    one stream."""
+    n = _cache_attention_bytes(q.shape[0], seqs, q.shape[1], cache.page_size, cache.kv_heads, cache.head_dim)
+    if n == 0:
+        raise ValueError("heads must be a multiple of the cache's")
+    buf = _new(n + 256, torch.uint8, cache.device, stream)
+    off = -buf.data_ptr() % 256
+    return buf[off:off + n] if off else buf
+
+
+def cache_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, lengths: torch.Tensor, *,
+                    starts: torch.Tensor | None = None, scale: float | None = None, out: torch.Tensor | None = None,
+                    lse: bool | torch.Tensor = False, workspace: torch.Tensor | None = None, stream=None):
+    """Attention of each sequence's last tokens over the cache (aqd_cache_attention): q [tokens, heads, head_dim], page_table int32
+    [seqs, columns], lengths int32 [seqs] (places of each sequence, its queries' own among them), starts int32 [seqs + 1] for several
+    queries a sequence. scale: 1 / sqrt(head_dim) where not given. Returns the output, or (output, lse [tokens, heads]) where lse is wanted.
+    workspace: cache_attention_workspace(q, cache, seqs), which calls that may overlap in time must not share."""
+    dev = cache.index
+    n, h, d, lq, lqh = _heads(q, "q", dev)
+    dt = _float_dtype(q, "q")
+    _runs_on(dev, stream)
+    if d != cache.head_dim:
+        raise ValueError("q must have the cache's head_dim")
+    if page_table.dtype is not torch.int32 or page_table.dim() != 2 or not page_table.is_cuda or page_table.get_device() != dev:
+        raise ValueError("page_table must be an int32 matrix on the call's device")
+    seqs, cols = page_table.shape
+    lt, last = page_table.stride()
+    if last != 1 and cols > 1:
+        raise ValueError("the entries of a row of page_table must be adjacent")
+    lp = _vector(lengths, seqs, torch.int32, "lengths", dev)
+    stp = 0 if starts is None else _vector(starts, seqs + 1, torch.int32, "starts", dev)
+    o, lo, loh = _out_heads(out, q, "out", stream)
+    ep, e = 0, None
+    if lse is not False:
+        e = _new((n, h), torch.float32, cache.device, stream) if lse is True else lse
+        ep = _vector(e, n * h, torch.float32, "lse", dev)
+    if workspace is None:
+        workspace = cache_attention_workspace(q, cache, seqs, stream=stream)
+    elif not workspace.is_cuda or workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor on the call's device")
+    args = _CACHE_ATTENTION.pack(n, seqs, h, dt, d ** -0.5 if scale is None else scale, q.data_ptr(), lq, lqh, o.data_ptr(), lo, loh, ep,
+                                 stp, lp, page_table.data_ptr(), max(lt, cols), cols)
+    _check(_calls().aqd_cache_attention(args, cache.desc, workspace.data_ptr(), workspace.nbytes, _stream(stream)),
+           "aqd_cache_attention")
+    return o if e is None else (o, e)
+
+
+def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, *,
+                     kv_starts: torch.Tensor | None = None, causal: bool = True, scale: float | None = None,
+                     out: torch.Tensor | None = None, lse: bool | torch.Tensor = False, stream=None):
+    """Attention over whole sequences packed one after another (aqd_prompt_attention): q [tokens, heads, head_dim], k and v
+    [kv_tokens, kv_heads, head_dim], starts int32 [seqs + 1], kv_starts where a sequence has other keys than queries (causal: its queries are
+    then the last ones). scale: 1 / sqrt(head_dim) where not given. Returns the output, or (output, lse [tokens, heads]) where lse is wanted."""
+    n, h, d, lq, lqh = _heads(q, "q")
+    dt = _float_dtype(q, "q")
+    dev = q.get_device()
+    _runs_on(dev, stream)
+    nk, hk, dk, lk, lkh = _heads(k, "k", dev)
+    _, _, _, lv, lvh = _heads(v, "v", dev)
+    if dk != d or v.shape != k.shape or k.dtype is not q.dtype or v.dtype is not q.dtype:
+        raise ValueError("k and v must have one shape, and q's head_dim and type")
+    seqs = starts.numel() - 1
+    if seqs < 0:
+        raise ValueError("starts must hold seqs + 1 numbers")
+    stp = _vector(starts, seqs + 1, torch.int32, "starts", dev)
+    ksp = 0
+    if kv_starts is not None:
+        ksp = _vector(kv_starts, seqs + 1, torch.int32, "kv_starts", dev)
+    elif nk != n:
+        raise ValueError("kv_starts is required where keys and queries differ in number")
+    o, lo, loh = _out_heads(out, q, "out", stream)
+    ep, e = 0, None
+    if lse is not False:
+        e = _new((n, h), torch.float32, q.device, stream) if lse is True else lse
+        ep = _vector(e, n * h, torch.float32, "lse", dev)
+    args = _PROMPT.pack(n, nk, seqs, h, hk, d, dt, 1 if causal else 0, d ** -0.5 if scale is None else scale, q.data_ptr(), lq, lqh,
+                        k.data_ptr(), lk, lkh, v.data_ptr(), lv, lvh, o.data_ptr(), lo, loh, ep, stp, ksp)
+    _check(_calls().aqd_prompt_attention(args, _stream(stream)), "aqd_prompt_attention")
+    return o if e is None else (o, e)
 
 
 class DistillLoss(NamedTuple):

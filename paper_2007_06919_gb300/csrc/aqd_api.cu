@@ -1038,6 +1038,223 @@ aqd_status aqd_linear_int8(const aqd_linear_args* l, const aqd_linear_weights* w
   return st ? fail((aqd_status)st, err) : AQD_OK;
 }
 
+// ---------------------------------------------------------------- attention of an 8-bit decoder
+
+static bool cache_shape(int32_t page_size, int32_t kv_heads, int32_t dim) {
+  return page_size >= 16 && page_size <= 1024 && (page_size & (page_size - 1)) == 0 && kv_heads >= 1 && kv_heads <= 65535 &&
+         (dim == 64 || dim == 128 || dim == 192 || dim == 256);
+}
+
+size_t aqd_kv_cache_bytes(int64_t pages, int32_t page_size, int32_t kv_heads, int32_t head_dim) {
+  if (!cache_shape(page_size, kv_heads, head_dim) || pages < 1 || pages > INT_MAX) return 0;
+  const double bytes = (double)pages * (page_size / 16) * kv_heads * cache_block_bytes(head_dim);
+  return bytes <= 1099511627776.0 ? (size_t)pages * (page_size / 16) * kv_heads * cache_block_bytes(head_dim) : 0;
+}
+
+// What is wrong with a cache, or NULL; fills g.
+static const char* cache_fault(const aqd_kv_cache* c, CacheGeom* g) {
+  if (!c) return "cache is NULL";
+  if (aqd_kv_cache_bytes(c->pages, c->page_size, c->kv_heads, c->head_dim) == 0) return "unsupported cache shape";
+  if (!c->data || misaligned(c->data, 256)) return "cache data must be a 256-byte aligned device pointer";
+  g->data = static_cast<uint8_t*>(c->data);
+  g->pages = c->pages; g->kv_heads = c->kv_heads; g->dim = c->head_dim;
+  g->page_shift = 0;
+  while ((1 << g->page_shift) < c->page_size) ++g->page_shift;
+  return nullptr;
+}
+// A tensor of heads that is read.
+static const char* heads_fault(const void* p, int64_t ld, int64_t ldh, int bytes) {
+  if (!p) return "a tensor of heads is NULL";
+  if (ld < 0 || ldh < 0) return "a stride of heads is negative";
+  if (misaligned(p, bytes)) return "a tensor of heads is not aligned to its type";
+  return nullptr;
+}
+// One that is written: no two of its rows share memory.
+static const char* heads_out_fault(const void* p, int64_t ld, int64_t ldh, int bytes, int64_t tokens, int64_t heads, int64_t dim) {
+  if (const char* f = heads_fault(p, ld, ldh, bytes)) return f;
+  const __int128 head_span = (__int128)(heads - 1) * ldh + dim, token_span = (__int128)(tokens - 1) * ld + dim;
+  const bool heads_inside = (heads == 1 || ldh >= dim) && (tokens == 1 || ld >= head_span);
+  const bool tokens_inside = (tokens == 1 || ld >= dim) && (heads == 1 || ldh >= token_span);
+  return heads_inside || tokens_inside ? nullptr : "rows of an output overlap";
+}
+static bool same_place(const void* a, int64_t la, int64_t ha, const void* b, int64_t lb, int64_t hb) { return a != b || (la == lb && ha == hb); }
+
+aqd_status aqd_qk_norm_rope(const aqd_qk_rope_args* n, const aqd_kv_cache* cache, aqd_stream_t stream) {
+  if (!n) return fail(AQD_ERR_INVALID, "args is NULL");
+  QkArgs a{};
+  const char* f = nullptr;
+  const int b = float_bytes(n->dtype);
+  if (n->tokens < 0 || n->tokens > INT_MAX) f = "tokens must be in [0, 2^31)";
+  else if (b == 0) f = "dtype must be AQD_F32, AQD_F16 or AQD_BF16";
+  else if (n->heads < 0 || n->heads > 65535 || n->kv_heads < 1 || n->kv_heads > 65535) f = "heads must be in 0..65535, kv_heads in 1..65535";
+  else if (n->head_dim < 2 || n->head_dim > 512 || n->head_dim % 2) f = "head_dim must be even, 2..512";
+  else if (n->rot_dim < 0 || n->rot_dim > n->head_dim || n->rot_dim % 2) f = "rot_dim must be even, 0..head_dim";
+  else if (!(n->eps >= 0.0f && std::isfinite(n->eps))) f = "eps must be finite and >= 0";
+  else if ((n->q_weight || n->k_weight) && float_bytes(n->weight_dtype) == 0) f = "weight_dtype must be AQD_F32, AQD_F16 or AQD_BF16";
+  else if ((n->q_weight && misaligned(n->q_weight, float_bytes(n->weight_dtype))) || (n->k_weight && misaligned(n->k_weight, float_bytes(n->weight_dtype))))
+    f = "weights must be aligned to their type";
+  if (!f && cache) {
+    f = cache_fault(cache, &a.cache);
+    if (!f && (cache->kv_heads != n->kv_heads || cache->head_dim != n->head_dim)) f = "the cache has other heads";
+  }
+  if (!f && n->tokens > 0) {
+    if (n->heads > 0) {
+      f = heads_fault(n->q, n->ldq, n->ldqh, b);
+      if (!f) f = heads_out_fault(n->q_out, n->ldq_out, n->ldqh_out, b, n->tokens, n->heads, n->head_dim);
+      if (!f && !same_place(n->q, n->ldq, n->ldqh, n->q_out, n->ldq_out, n->ldqh_out)) f = "q_out in place needs q's strides";
+    }
+    if (!f) f = heads_fault(n->k, n->ldk, n->ldkh, b);
+    if (!f && (n->k_out || !cache)) f = heads_out_fault(n->k_out, n->ldk_out, n->ldkh_out, b, n->tokens, n->kv_heads, n->head_dim);
+    if (!f && !same_place(n->k, n->ldk, n->ldkh, n->k_out, n->ldk_out, n->ldkh_out)) f = "k_out in place needs k's strides";
+    if (!f && cache) f = heads_fault(n->v, n->ldv, n->ldvh, b);
+    if (!f && cache && (!n->slots || misaligned(n->slots, 8))) f = "slots must be an 8-byte aligned device pointer";
+    if (!f && n->rot_dim > 0 && (!n->positions || !n->inv_freq)) f = "positions and inv_freq are required";
+    if (!f && n->rot_dim > 0 && (misaligned(n->positions, 8) || misaligned(n->inv_freq, 4))) f = "positions and inv_freq must be aligned to their types";
+  }
+  if (f) return fail(AQD_ERR_INVALID, f);
+  if (n->tokens == 0) return AQD_OK;
+  a.tokens = n->tokens; a.heads = n->heads; a.kv_heads = n->kv_heads; a.dim = n->head_dim; a.dtype = n->dtype;
+  a.q = n->q; a.ldq = n->ldq; a.ldqh = n->ldqh;
+  a.k = n->k; a.ldk = n->ldk; a.ldkh = n->ldkh;
+  a.v = n->v; a.ldv = n->ldv; a.ldvh = n->ldvh;
+  a.q_out = n->q_out; a.ldqo = n->ldq_out; a.ldqoh = n->ldqh_out;
+  a.k_out = n->k_out; a.ldko = n->ldk_out; a.ldkoh = n->ldkh_out;
+  a.q_weight = n->q_weight; a.k_weight = n->k_weight; a.weight_dtype = n->weight_dtype; a.eps = n->eps;
+  a.positions = n->positions; a.inv_freq = n->inv_freq; a.rot = n->rot_dim; a.interleaved = n->interleaved != 0;
+  a.slots = n->slots;
+  std::string err;
+  const int st = launch_heads(a, static_cast<cudaStream_t>(stream), &err);
+  return st ? fail((aqd_status)st, err) : AQD_OK;
+}
+
+// What is wrong with rows for the cache, or NULL.
+static const char* cache_rows_fault(const aqd_cache_rows* r, bool write, const aqd_kv_cache* cache, CacheGeom* g) {
+  if (!r) return "rows is NULL";
+  if (const char* f = cache_fault(cache, g)) return f;
+  const int b = float_bytes(r->dtype);
+  if (r->tokens < 0 || r->tokens > INT_MAX) return "tokens must be in [0, 2^31)";
+  if (b == 0) return "dtype must be AQD_F32, AQD_F16 or AQD_BF16";
+  if (r->tokens == 0) return nullptr;
+  if (!r->slots || misaligned(r->slots, 8)) return "slots must be an 8-byte aligned device pointer";
+  if (write) {
+    if (const char* f = heads_fault(r->k, r->ldk, r->ldkh, b)) return f;
+    return heads_fault(r->v, r->ldv, r->ldvh, b);
+  }
+  if (!r->k && !r->v) return "at least one of k and v is required";
+  if (r->k)
+    if (const char* f = heads_out_fault(r->k, r->ldk, r->ldkh, b, r->tokens, g->kv_heads, g->dim)) return f;
+  return r->v ? heads_out_fault(r->v, r->ldv, r->ldvh, b, r->tokens, g->kv_heads, g->dim) : nullptr;
+}
+
+aqd_status aqd_cache_write(const aqd_cache_rows* r, const aqd_kv_cache* cache, aqd_stream_t stream) {
+  QkArgs a{};
+  if (const char* f = cache_rows_fault(r, true, cache, &a.cache)) return fail(AQD_ERR_INVALID, f);
+  if (r->tokens == 0) return AQD_OK;
+  // rows of keys without a norm or a turn
+  a.tokens = r->tokens; a.kv_heads = a.cache.kv_heads; a.dim = a.cache.dim; a.dtype = r->dtype;
+  a.k = r->k; a.ldk = r->ldk; a.ldkh = r->ldkh;
+  a.v = r->v; a.ldv = r->ldv; a.ldvh = r->ldvh;
+  a.slots = r->slots;
+  std::string err;
+  const int st = launch_heads(a, static_cast<cudaStream_t>(stream), &err);
+  return st ? fail((aqd_status)st, err) : AQD_OK;
+}
+
+aqd_status aqd_cache_read(const aqd_cache_rows* r, const aqd_kv_cache* cache, aqd_stream_t stream) {
+  CacheReadArgs a{};
+  if (const char* f = cache_rows_fault(r, false, cache, &a.cache)) return fail(AQD_ERR_INVALID, f);
+  if (r->tokens == 0) return AQD_OK;
+  a.tokens = r->tokens; a.dtype = r->dtype;
+  a.k = r->k; a.ldk = r->ldk; a.ldkh = r->ldkh;
+  a.v = r->v; a.ldv = r->ldv; a.ldvh = r->ldvh;
+  a.slots = r->slots;
+  std::string err;
+  const int st = launch_cache_read(a, static_cast<cudaStream_t>(stream), &err);
+  return st ? fail((aqd_status)st, err) : AQD_OK;
+}
+
+static const char* attention_sizes_fault(int64_t tokens, int32_t seqs, int32_t heads, int32_t kv_heads) {
+  if (tokens < 0 || seqs < 0 || seqs > (1 << 24)) return "tokens must be >= 0, seqs in 0..2^24";
+  if (heads < 1 || heads > 65535 || kv_heads < 1 || kv_heads > 65535 || heads % kv_heads) return "heads must be in 1..65535, a multiple of kv_heads";
+  if (tokens * heads > INT_MAX / 2) return "tokens * heads must be below 2^30";
+  return nullptr;
+}
+
+size_t aqd_cache_attention_workspace_bytes(int64_t tokens, int32_t seqs, int32_t heads, const aqd_kv_cache* cache) {
+  if (!cache || !cache_shape(cache->page_size, cache->kv_heads, cache->head_dim)) return 0;
+  if (tokens > INT_MAX || attention_sizes_fault(tokens, seqs, heads, cache->kv_heads)) return 0;
+  return cache_attention_workspace_bytes(tokens, seqs, heads, cache->kv_heads, cache->head_dim);
+}
+
+aqd_status aqd_cache_attention(const aqd_cache_attention_args* n, const aqd_kv_cache* cache, void* workspace, size_t ws_bytes, aqd_stream_t stream) {
+  CacheAttnArgs a{};
+  const char* f = n ? cache_fault(cache, &a.cache) : "args is NULL";
+  if (!f && n->tokens > INT_MAX) f = "tokens must be in [0, 2^31)";
+  if (!f) f = attention_sizes_fault(n->tokens, n->seqs, n->heads, cache->kv_heads);
+  if (!f && n->dtype != AQD_F16 && n->dtype != AQD_BF16) f = "dtype must be AQD_F16 or AQD_BF16";
+  if (!f && !(n->scale > 0.0f && std::isfinite(n->scale))) f = "scale must be positive and finite";
+  if (!f && !n->starts && n->tokens != n->seqs) f = "without starts there is one token for each sequence";
+  if (!f && (n->columns < 0 || n->ld_table < n->columns || (int64_t)n->columns * cache->page_size > INT_MAX - 1024))
+    f = "columns must be >= 0, at most ld_table, and its places below 2^31 - 1024";
+  if (!f && n->tokens > 0 && n->seqs > 0) {
+    f = heads_fault(n->q, n->ldq, n->ldqh, 2);
+    if (!f) f = heads_out_fault(n->out, n->ldo, n->ldoh, 2, n->tokens, n->heads, cache->head_dim);
+    if (!f && (!n->lengths || (n->columns > 0 && !n->page_table))) f = "lengths and page_table are required";
+    if (!f && (misaligned(n->lengths, 4) || misaligned(n->page_table, 4) || misaligned(n->starts, 4) || misaligned(n->lse, 4)))
+      f = "lengths, page_table, starts and lse must be 4-byte aligned";
+    if (!f && (!workspace || misaligned(workspace, 256))) f = "workspace must be a 256-byte aligned device pointer";
+    if (!f && ws_bytes < cache_attention_workspace_bytes(n->tokens, n->seqs, n->heads, cache->kv_heads, cache->head_dim))
+      f = "workspace: aqd_cache_attention_workspace_bytes(...) bytes";
+  }
+  if (f) return fail(AQD_ERR_INVALID, f);
+  if (n->tokens == 0 || n->seqs == 0) return AQD_OK;
+  a.tokens = n->tokens; a.seqs = n->seqs; a.heads = n->heads; a.dtype = n->dtype; a.scale = n->scale;
+  a.q = n->q; a.ldq = n->ldq; a.ldqh = n->ldqh;
+  a.out = n->out; a.ldo = n->ldo; a.ldoh = n->ldoh;
+  a.lse = n->lse; a.starts = n->starts; a.lengths = n->lengths;
+  a.table = n->page_table; a.ld_table = n->ld_table; a.columns = n->columns;
+  a.ws = static_cast<uint8_t*>(workspace);
+  std::string err;
+  a.status = status_ptr(&err);
+  if (!a.status) return fail(AQD_ERR_CUDA, err);
+  const int st = launch_cache_attention(a, static_cast<cudaStream_t>(stream), &err);
+  return st ? fail((aqd_status)st, err) : AQD_OK;
+}
+
+aqd_status aqd_prompt_attention(const aqd_prompt_attention_args* n, aqd_stream_t stream) {
+  if (!n) return fail(AQD_ERR_INVALID, "args is NULL");
+  const char* f = nullptr;
+  if (n->tokens > INT_MAX || n->kv_tokens < 0 || n->kv_tokens > INT_MAX) f = "tokens and kv_tokens must be in [0, 2^31)";
+  if (!f) f = attention_sizes_fault(n->tokens, n->seqs, n->heads, n->kv_heads);
+  if (!f && n->head_dim != 64 && n->head_dim != 128 && n->head_dim != 192 && n->head_dim != 256) f = "head_dim must be 64, 128, 192 or 256";
+  if (!f && n->dtype != AQD_F16 && n->dtype != AQD_BF16) f = "dtype must be AQD_F16 or AQD_BF16";
+  if (!f && !(n->scale > 0.0f && std::isfinite(n->scale))) f = "scale must be positive and finite";
+  if (!f && n->tokens > 0 && n->seqs > 0) {
+    f = heads_fault(n->q, n->ldq, n->ldqh, 16);
+    if (!f) f = heads_out_fault(n->out, n->ldo, n->ldoh, 16, n->tokens, n->heads, n->head_dim);
+    if (!f && n->kv_tokens > 0) f = heads_fault(n->k, n->ldk, n->ldkh, 16);
+    if (!f && n->kv_tokens > 0) f = heads_fault(n->v, n->ldv, n->ldvh, 16);
+    if (!f && ((n->ldq | n->ldqh | n->ldk | n->ldkh | n->ldv | n->ldvh | n->ldo | n->ldoh) % 8)) f = "strides must be multiples of 8 elements";
+    if (!f && (!n->starts || misaligned(n->starts, 4) || misaligned(n->kv_starts, 4) || misaligned(n->lse, 4)))
+      f = "starts is required; starts, kv_starts and lse must be 4-byte aligned";
+  }
+  if (f) return fail(AQD_ERR_INVALID, f);
+  if (n->tokens == 0 || n->seqs == 0) return AQD_OK;
+  PromptArgs a{};
+  a.tokens = n->tokens; a.kv_tokens = n->kv_tokens; a.seqs = n->seqs; a.heads = n->heads; a.kv_heads = n->kv_heads; a.dim = n->head_dim;
+  a.dtype = n->dtype; a.causal = n->causal != 0; a.scale = n->scale;
+  a.q = n->q; a.ldq = n->ldq; a.ldqh = n->ldqh;
+  a.k = n->k; a.ldk = n->ldk; a.ldkh = n->ldkh;
+  a.v = n->v; a.ldv = n->ldv; a.ldvh = n->ldvh;
+  a.out = n->out; a.ldo = n->ldo; a.ldoh = n->ldoh;
+  a.lse = n->lse; a.starts = n->starts; a.kv_starts = n->kv_starts;
+  std::string err;
+  a.status = status_ptr(&err);
+  if (!a.status) return fail(AQD_ERR_CUDA, err);
+  const int st = launch_prompt(a, static_cast<cudaStream_t>(stream), &err);
+  return st ? fail((aqd_status)st, err) : AQD_OK;
+}
+
 // What is wrong with a distillation call, or NULL; fills a.
 static const char* distill_fault(const aqd_distill_args* d, DistillArgs* a) {
   if (!d) return "args is NULL";

@@ -223,6 +223,73 @@ float linear_tc_estimate(const LinArgs& a);
 size_t linear_tc_workspace_bytes(int64_t m, int32_t k);
 int launch_linear_tc(const LinArgs& a, cudaStream_t stream, std::string* err);
 
+// attention of an 8-bit decoder (lm_heads.cu, lm_cache_attention.cu, lm_prompt.cu)
+// The cache: a page holds, per head, page_size / 16 blocks of 16 places; a block is 16 key rows of dim / 2 bytes, 16 value rows, then a
+// (lowest value, step) pair of bfloat16 (low and high half of a word) for each of the 16 keys and each of the 16 values.
+struct CacheGeom {
+  uint8_t* data;
+  int64_t pages;
+  int32_t page_shift, kv_heads, dim;
+};
+inline int64_t cache_block_bytes(int32_t dim) { return 16 * ((int64_t)dim + 8); }
+struct QkArgs {
+  int64_t tokens;
+  int32_t heads, kv_heads, dim, dtype;
+  const void *q, *k, *v;
+  int64_t ldq, ldqh, ldk, ldkh, ldv, ldvh;
+  void *q_out, *k_out;
+  int64_t ldqo, ldqoh, ldko, ldkoh;
+  const void *q_weight, *k_weight;
+  int32_t weight_dtype;
+  float eps;
+  const int64_t* positions;
+  const float* inv_freq;
+  int32_t rot, interleaved;
+  CacheGeom cache;        // data NULL: none
+  const int64_t* slots;
+};
+int launch_heads(const QkArgs& a, cudaStream_t stream, std::string* err);
+struct CacheReadArgs {
+  int64_t tokens;
+  int32_t dtype;
+  void *k, *v;
+  int64_t ldk, ldkh, ldv, ldvh;
+  const int64_t* slots;
+  CacheGeom cache;
+};
+int launch_cache_read(const CacheReadArgs& a, cudaStream_t stream, std::string* err);
+struct CacheAttnArgs {
+  int64_t tokens;
+  int32_t seqs, heads, dtype;
+  float scale;
+  const void* q;
+  int64_t ldq, ldqh;
+  void* out;
+  int64_t ldo, ldoh;
+  float* lse;
+  const int32_t *starts, *lengths, *table;
+  int64_t ld_table;
+  int32_t columns;
+  CacheGeom cache;
+  uint8_t* ws;
+  uint32_t* status;
+};
+size_t cache_attention_workspace_bytes(int64_t tokens, int32_t seqs, int32_t heads, int32_t kv_heads, int32_t dim);
+int launch_cache_attention(const CacheAttnArgs& a, cudaStream_t stream, std::string* err);
+struct PromptArgs {
+  int64_t tokens, kv_tokens;
+  int32_t seqs, heads, kv_heads, dim, dtype, causal;
+  float scale;
+  const void *q, *k, *v;
+  int64_t ldq, ldqh, ldk, ldkh, ldv, ldvh;
+  void* out;
+  int64_t ldo, ldoh;
+  float* lse;
+  const int32_t *starts, *kv_starts;
+  uint32_t* status;
+};
+int launch_prompt(const PromptArgs& a, cudaStream_t stream, std::string* err);
+
 struct DistillArgs {
   int64_t tokens;
   int32_t vocab, dtype, top;
