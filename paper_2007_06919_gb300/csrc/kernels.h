@@ -289,6 +289,9 @@ struct PromptArgs {
   uint32_t* status;
 };
 int launch_prompt(const PromptArgs& a, cudaStream_t stream, std::string* err);
+// the tcgen05 kernel (lm_prompt_tc.cu): whether it takes the call, its launch
+bool prompt_tc_takes(const PromptArgs& a);
+int launch_prompt_tc(const PromptArgs& a, cudaStream_t stream, std::string* err);
 
 struct DistillArgs {
   int64_t tokens;

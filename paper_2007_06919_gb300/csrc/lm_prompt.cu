@@ -15,7 +15,7 @@
 #include "../../include/aqd.h"
 #include "common.cuh"
 #include "kernels.h"
-#include "lm_seq.cuh"
+#include "lm_prompt.cuh"
 #include "tc_ptx.cuh"
 
 namespace aqd {
@@ -26,21 +26,6 @@ using namespace tc;
 constexpr int kWarps = 4, kThreads = kWarps * 32, kRows = 64;
 // keys of a tile: 64 of a head's 256 values would spill
 __host__ __device__ constexpr int keys_of(int dim) { return dim == 256 ? 32 : 64; }
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack(float a, float b, __half*) {
-  const __half2 h = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ uint32_t pack(float a, float b, __nv_bfloat16*) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 template <class T>
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if constexpr (std::is_same<T, __half>::value)
@@ -60,39 +45,6 @@ __device__ __forceinline__ void ldsm_t(uint32_t (&r)[4], uint32_t addr) {
 template <int D>
 __device__ __forceinline__ uint32_t at(uint32_t base, int r, int c) {
   return base + r * (D * 2) + ((c & ~7) | ((c ^ r) & 7)) * 16;
-}
-
-struct Job {
-  int32_t found, start, queries, kv_start, keys, tile;
-};
-__device__ __forceinline__ int clamp_at(int64_t v, int64_t most) { return (int)(v < 0 ? 0 : v > most ? most : v); }
-
-// Unit `unit`'s sequence and tile of `rows` queries, the last tiles of a sequence (which see the most keys) first.
-__device__ bool find_job(const PromptArgs& p, int rows, int unit, Job* job, uint64_t* red) {
-  if (threadIdx.x == 0) job->found = 0;
-  uint64_t base = 0;
-  for (int b = 0; b < p.seqs; b += blockDim.x) {
-    const int s = b + threadIdx.x;
-    int start = 0, queries = 0, tiles = 0;
-    if (s < p.seqs) {
-      start = clamp_at(p.starts[s], p.tokens);
-      const int end = clamp_at(p.starts[s + 1], p.tokens);
-      queries = end > start ? end - start : 0;
-      tiles = (queries + rows - 1) / rows;
-    }
-    uint64_t before;
-    const uint64_t total = seq::block_scan((uint64_t)tiles, red, before);
-    const int64_t first = (int64_t)(base + before);
-    if (unit >= first && unit < first + tiles) {
-      const int32_t* ks = p.kv_starts ? p.kv_starts : p.starts;
-      const int k0 = clamp_at(ks[s], p.kv_tokens), k1 = clamp_at(ks[s + 1], p.kv_tokens);
-      *job = {1, start, queries, k0, k1 > k0 ? k1 - k0 : 0, tiles - 1 - (int)(unit - first)};
-    }
-    base += total;
-    if ((uint64_t)unit < base) break;
-  }
-  __syncthreads();
-  return job->found != 0;
 }
 
 template <class T, int D>
@@ -258,6 +210,7 @@ static cudaError_t run_type(const PromptArgs& a, cudaStream_t stream) {
 }  // namespace prompt
 
 int launch_prompt(const PromptArgs& a, cudaStream_t stream, std::string* err) {
+  if (prompt_tc_takes(a)) return launch_prompt_tc(a, stream, err);
   const cudaError_t e = a.dtype == AQD_F16 ? prompt::run_type<__half>(a, stream) : prompt::run_type<__nv_bfloat16>(a, stream);
   if (e == cudaSuccess) return 0;
   *err = std::string("prompt attention: ") + cudaGetErrorString(e);
