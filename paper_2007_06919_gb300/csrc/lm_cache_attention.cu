@@ -12,9 +12,11 @@
 // query rows as its columns: a group's heads fill them, where the usual form would pad them to 16, and codes go from shared memory into operand
 // registers with no exchange between lanes. (tcgen05 would want the expanded codes in shared memory or TMEM first, and its 128 rows mostly empty.)
 //
-// A block takes one key-value head, 8 or 16 rows (queries x heads of the group) and a run of places; its 8 warps take steps of 32 places in turn,
-// each with its own ring of bulk copies (a step is one or two runs of bytes in the cache), and join at the end. The run's length follows from all
-// sequences' lengths, so the blocks are even however these differ; parts of one sequence are joined by combine_kernel.
+// The unit of work is a warp's: one key-value head, 8 or 16 rows (queries x heads of the group) and a run of steps of 32 places, through the warp's own
+// ring of bulk copies (a step is one or two runs of bytes in the cache). The runs' length follows from all sequences' lengths, so that they fill
+// the GPU once and are even however the lengths differ; a block's 8 warps take runs that follow one another, of one sequence or of several, and join
+// what belongs together; combine_kernel joins what lies in several blocks. (64 sequences of 1 to 8192 places: blocks of one sequence each, of which the short ones
+// left most warps idle, 47 us.) Tables of few places give each sequence and head a block, and need no second kernel.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -24,7 +26,6 @@
 #include "../../include/aqd.h"
 #include "common.cuh"
 #include "kernels.h"
-#include "lm_seq.cuh"
 #include "tc_ptx.cuh"
 
 namespace aqd {
@@ -34,6 +35,7 @@ using namespace tc;
 
 constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr int kStep = 32;                 // places of a step
+constexpr float kGrowth = 4.0f;           // powers of two that a maximum may grow by before sums are brought to it
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __host__ __device__ constexpr int stage_bytes(int dim) { return 2 * 16 * (dim + 8); }
@@ -41,13 +43,17 @@ __host__ __device__ constexpr int stages(int dim) { return dim == 64 ? 6 : dim =
 __host__ __device__ constexpr int row_tiles(int dim) { return dim <= 128 ? 2 : 1; }  // most tiles of 8 rows a block
 
 struct Split {
-  int32_t units;        // blocks of a key-value head that fill the GPU
-  int32_t tiles;        // bound of the row tiles of all sequences
+  int32_t warps;        // tasks that fill the GPU
+  int32_t whole;        // a block for each sequence, tile and head
   int32_t group;        // query heads of a key-value head
   uint64_t group_magic;
   int32_t q_vec;        // rows of q on 16 bytes
-  int32_t* meta;        // [1 + 8 * tiles]
-  float* part;          // [unit][kv head][row]: dim sums, then maximum, sum, factor
+  int32_t* meta;        // [block][8]: Span
+  float* part;          // [block][2][row]: dim sums, then maximum, sum, factor
+};
+// What a block leaves to combine_kernel: the group of runs that begins in it and goes on in blocks up to `last` (0: none).
+struct Span {
+  int32_t last, start, queries, tile, head, pad[3];
 };
 
 __device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
@@ -72,18 +78,26 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-// nibble j of each 16-bit half, as the float16 numbers 64 + n
-template <int j>
-__device__ __forceinline__ uint32_t nibbles(uint32_t w) {
-  const uint32_t x = j == 0 ? w << 4 : j == 1 ? w : j == 2 ? w >> 4 : w >> 8;
-  return (x & 0x00f000f0u) | 0x54005400u;
-}
-// the same less 8, exactly: n - 8
-template <int j>
-__device__ __forceinline__ uint32_t centred(uint32_t w) {
+__device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
   uint32_t y;
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(nibbles<j>(w)), "r"(0x54805480u));
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
   return y;
+}
+// Nibbles of each 16-bit half of w as float16 numbers: under the exponent of 1024 the lowest four bits are 1024 + n, under that of 64 the next four are
+// 64 + n; a byte's shift brings the other two there. Keys: n and 64 + n (of the odd nibbles, which -64 sum(q) makes good), values: n - 8.
+__device__ __forceinline__ void key_codes(uint32_t w, uint32_t (&h)[4]) {
+  const uint32_t v = w >> 8;
+  h[0] = sub2((w & 0x000f000fu) | 0x64006400u, 0x64006400u);
+  h[1] = (w & 0x00f000f0u) | 0x54005400u;
+  h[2] = sub2((v & 0x000f000fu) | 0x64006400u, 0x64006400u);
+  h[3] = (v & 0x00f000f0u) | 0x54005400u;
+}
+__device__ __forceinline__ void value_codes(uint32_t w, uint32_t (&h)[4]) {
+  const uint32_t v = w >> 8;
+  h[0] = sub2((w & 0x000f000fu) | 0x64006400u, 0x64086408u);
+  h[1] = sub2((w & 0x00f000f0u) | 0x54005400u, 0x54805480u);
+  h[2] = sub2((v & 0x000f000fu) | 0x64006400u, 0x64086408u);
+  h[3] = sub2((v & 0x00f000f0u) | 0x54005400u, 0x54805480u);
 }
 template <int kWords>
 __device__ __forceinline__ void lds(uint32_t addr, uint32_t (&w)[kWords]) {
@@ -102,8 +116,9 @@ __device__ __forceinline__ void lds(uint32_t addr, uint32_t (&w)[kWords]) {
 __device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float step_of(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
+// A warp's task: run `run` of `runs`, `steps` steps each, of a sequence's tile of rows and a head; seq -1: none.
 struct Job {
-  int32_t seq, tile, chunk, chunks, first_unit, ordinal, start, queries, len, steps;  // steps: of a chunk
+  int32_t seq, tile, head, run, runs, steps, start, queries, len;
 };
 
 // A sequence's queries, first token and length, within what the caller's tensors hold.
@@ -121,45 +136,101 @@ __device__ __forceinline__ void sequence(const CacheAttnArgs& p, int s, int& sta
   len = n < 0 ? 0 : n > most ? (int)most : n;
 }
 
-// The unit of this block: its sequence, row tile and run of places. False where there are fewer units.
-__device__ bool find_job(const CacheAttnArgs& p, const Split& sp, int rows, int unit, Job* job, uint64_t* red) {
-  // steps of all tiles, and from them the steps of a run: whole rounds of the warps
-  uint64_t work = 0, before;
-  for (int b = 0; b < p.seqs; b += kThreads) {
-    uint64_t v = 0;
-    if (b + (int)threadIdx.x < p.seqs) {
-      int start, n, len;
-      sequence(p, b + threadIdx.x, start, n, len);
-      v = (uint64_t)((n * (int64_t)sp.group + rows - 1) / rows) * (uint64_t)((len + kStep - 1) / kStep);
+// The tasks of this block's warps. (Counts are 32 bits wide: the host refuses more. Starts that fall may make more; every job is one of its
+// sequence's all the same.)
+template <int kRows>
+__device__ __forceinline__ void find_jobs(const CacheAttnArgs& p, const Split& sp, Job* jobs, uint64_t* red) {
+  const int kv = p.cache.kv_heads, first_task = blockIdx.x * kWarps, lane = threadIdx.x & 31;
+  if (threadIdx.x < kWarps) jobs[threadIdx.x].seq = -1;
+  const int s0 = threadIdx.x;
+  int start = 0, n = 0, len = 0;
+  if (s0 < p.seqs) sequence(p, s0, start, n, len);
+  int steps = 1;
+  if (!sp.whole) {
+    // all tiles, and the steps of all tiles: runs fill the GPU once (or, beside many tiles, half of it)
+    uint64_t all = 0, tiles = 0;
+    for (int s = s0; s < p.seqs; s += kThreads) {
+      int st = start, ns = n, ls = len;
+      if (s != s0) sequence(p, s, st, ns, ls);
+      const uint32_t t = (uint32_t)(((int64_t)ns * sp.group + kRows - 1) / kRows);
+      tiles += t;
+      all += (uint64_t)t * (uint32_t)((ls + kStep - 1) / kStep);
     }
-    work += seq::block_scan(v, red, before);
+    for (int o = 16; o > 0; o >>= 1) {
+      all += __shfl_xor_sync(0xffffffffu, all, o);
+      tiles += __shfl_xor_sync(0xffffffffu, tiles, o);
+    }
+    if (lane == 0) { red[2 * (threadIdx.x >> 5)] = all; red[2 * (threadIdx.x >> 5) + 1] = tiles; }
+    __syncthreads();
+    all = tiles = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) { all += red[2 * w]; tiles += red[2 * w + 1]; }
+    all *= kv;
+    tiles *= kv;
+    const uint32_t most = tiles < (uint64_t)(sp.warps / 2) ? sp.warps - (uint32_t)tiles : sp.warps / 2;
+    const uint64_t per = all < (1u << 31) ? ((uint32_t)all + most - 1) / most : (all + most - 1) / most;
+    steps = per < 1 ? 1 : per > 0x3fffffff ? 0x3fffffff : (int)per;
   }
-  const int64_t per = (int64_t)((work + sp.units - 1) / sp.units);
-  const int steps = (int)((per < 1 ? 1 : per) + kWarps - 1) / kWarps * kWarps;
-  if (threadIdx.x == 0) job->chunks = 0;
-  uint64_t base = 0;
+  uint32_t base = 0;
   for (int b = 0; b < p.seqs; b += kThreads) {
-    uint64_t v = 0;
-    int start = 0, n = 0, len = 0, tiles = 0, chunks = 1;
-    if (b + (int)threadIdx.x < p.seqs) {
-      sequence(p, b + threadIdx.x, start, n, len);
-      tiles = (int)((n * (int64_t)sp.group + rows - 1) / rows);
-      chunks = (int)(((len + kStep - 1) / kStep + (int64_t)steps - 1) / steps);
-      if (chunks < 1) chunks = 1;
-      v = (uint64_t)tiles << 32 | (uint32_t)(tiles * chunks);
+    int runs = 1, each = steps;
+    uint32_t count = 0;
+    if (b > 0) {
+      start = n = len = 0;
+      if (b + s0 < p.seqs) sequence(p, b + s0, start, n, len);
     }
-    const uint64_t total = seq::block_scan(v, red, before);
-    const int first = (int)(uint32_t)(base + before), ordinal = (int)((base + before) >> 32);
-    if (unit >= first && unit < first + tiles * chunks && ordinal + (unit - first) / chunks < sp.tiles) {
-      const int tile = (unit - first) / chunks;
-      *job = {b + (int)threadIdx.x, tile, unit - first - tile * chunks, chunks, first + tile * chunks, ordinal + tile, start, n, len, steps};
+    if (b + s0 < p.seqs) {
+      const uint32_t all = (uint32_t)(len + kStep - 1) / kStep;
+      if (sp.whole) {
+        runs = kWarps;
+        each = (int)(all + kWarps - 1) / kWarps;
+      } else {
+        runs = (int)((all + each - 1) / (uint32_t)each);
+        if (runs < 1) runs = 1;
+      }
+      count = (uint32_t)(((int64_t)n * sp.group + kRows - 1) / kRows) * (uint32_t)(kv * runs);
+    }
+    // counts before this thread's
+    uint32_t before = count;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t u = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += u;
+    }
+    uint32_t* sums = reinterpret_cast<uint32_t*>(red + 2 * kWarps);
+    __syncthreads();  // (sums may still be read from the last 256 sequences)
+    if (lane == 31) sums[threadIdx.x >> 5] = before;
+    __syncthreads();
+    uint32_t total = 0;
+    before -= count;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const uint32_t u = sums[w];
+      if (w < (int)(threadIdx.x >> 5)) before += u;
+      total += u;
+    }
+    const int first = (int)(base + before);
+    if (first < first_task + kWarps && first + (int)count > first_task) {
+      const int lo = first > first_task ? first : first_task;
+      int run = lo - first, group = run / runs, tile = group / kv, head = group - tile * kv;
+      run -= group * runs;
+      for (int at = lo; at < first_task + kWarps && at < first + (int)count; ++at) {
+        jobs[at - first_task] = {b + s0, tile, head, run, runs, each, start, n, len};
+        if (++run == runs) {
+          run = 0;
+          if (++head == kv) { head = 0; ++tile; }
+        }
+      }
     }
     base += total;
+    if ((int)base >= first_task + kWarps) break;
   }
-  // (starts that fall make more units than there are blocks: nothing is joined then)
-  if (unit == 0 && blockIdx.y == 0 && threadIdx.x == 0) sp.meta[0] = (uint32_t)base <= gridDim.x && (base >> 32) <= (uint64_t)sp.tiles ? (int)(base >> 32) : 0;
   __syncthreads();
-  return job->chunks > 0;
+}
+
+// Places that row r of a tile sees.
+__device__ __forceinline__ int lim_of(const Job& jb, const Split& sp, int rows, int r, int last_row) {
+  return r < last_row ? jb.len - jb.queries + fast_div(jb.tile * rows + r, sp.group_magic) + 1 : 0;
 }
 
 template <class T, int D, int NT>
@@ -168,44 +239,74 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
   constexpr int kStages = stages(D), kStage = stage_bytes(D), kBlock = kStage / 2, kRows = 8 * NT;
   constexpr int KW = D / 32, VW = D / 64;  // words of a key row, and of a value row, that a lane reads
   extern __shared__ __align__(128) uint8_t smem[];  // [warp][stage]; at the end the warps' sums
-  __shared__ uint64_t bars[kWarps * kStages], red[kWarps];
-  __shared__ Job job;
+  __shared__ uint64_t bars[kWarps * kStages], red[2 * kWarps + kWarps / 2];
+  __shared__ Job jobs[kWarps];
   __shared__ int abort_word;
-  __shared__ float wm[kWarps][kRows], wl[kWarps][kRows], wc[kRows];  // maxima, sums; rows' factors of scores
+  __shared__ float wm[kWarps][kRows], wl[kWarps][kRows], wc[kWarps][kRows];  // rows' maxima, sums, factors of scores
   volatile int* abort_flag = &abort_word;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   if (threadIdx.x < kWarps * kStages) mbar_init(smem_u32(&bars[threadIdx.x]), 1);
-  if (threadIdx.x == 0) {
-    abort_word = 0;
-    fence_barrier_init();
-  }
+  if (threadIdx.x == 0) abort_word = 0;
+  fence_barrier_init();
   grid_dep_wait();
-  if (!find_job(p, sp, kRows, blockIdx.x, &job, red)) return;
-  const int head = blockIdx.y;
-  const Job jb = job;
-  if (jb.chunk == 0 && head == 0 && threadIdx.x == 0) {
-    int* m = sp.meta + 4 + 4 * jb.ordinal;
-    m[0] = jb.first_unit; m[1] = jb.chunks; m[2] = jb.start; m[3] = jb.tile;
-    sp.meta[4 + 4 * sp.tiles + jb.ordinal] = jb.queries;
+  find_jobs<kRows>(p, sp, jobs, red);
+  grid_dep_launch();
+  const Job jb = jobs[warp];
+  const int head = jb.head;
+  const bool idle = jb.seq < 0;
+  const int last_row = idle ? 0 : jb.queries * sp.group - jb.tile * kRows;  // rows of this tile and behind it
+  int lim_all = 0, lim_any = 0;  // places that the tile's first row sees, and its last
+  if (!idle) {
+    const int top = last_row < kRows ? last_row : kRows;
+    lim_all = jb.len - jb.queries + fast_div(jb.tile * kRows, sp.group_magic) + 1;
+    lim_any = jb.len - jb.queries + fast_div(jb.tile * kRows + top - 1, sp.group_magic) + 1;
   }
+
+  // the steps of the run that lie before the last place that a row sees
+  const int step0 = idle ? 0 : jb.run * jb.steps;
+  int end = (lim_any + kStep - 1) / kStep;  // (lim_any <= 0: none)
+  end = idle ? 0 : end < step0 + jb.steps ? end : step0 + jb.steps;
+  const int mine = end > step0 ? end - step0 : 0;
+  const int blocks_of_page = 1 << (p.cache.page_shift - 4);
+  const int32_t* table = p.table + (idle ? 0 : (int64_t)jb.seq * p.ld_table);
+  const uint32_t ring = smem_u32(smem) + warp * (kStages * kStage), bar0 = smem_u32(&bars[warp * kStages]);
+  int page0 = -1, page1 = -1;  // of step `lane` of the batch of 32 steps that is being issued
+  uint32_t there = 0;          // two bits a stage: its blocks were copied
+
+  auto issue = [&](int i) {
+    const int st = i % kStages;
+    if ((i & 31) == 0) {
+      const int place = (step0 + i + lane) * kStep;
+      page0 = i + lane < mine ? table[place >> p.cache.page_shift] : -1;
+      page1 = i + lane < mine && place + 16 < lim_any ? table[(place + 16) >> p.cache.page_shift] : -1;
+      if (page0 < 0 || page0 >= p.cache.pages) page0 = -1;
+      if (page1 < 0 || page1 >= p.cache.pages) page1 = -1;
+    }
+    const int a = __shfl_sync(0xffffffffu, page0, i & 31), b = __shfl_sync(0xffffffffu, page1, i & 31);
+    there = (there & ~(3u << (2 * st))) | (uint32_t)((a >= 0 ? 1 : 0) | (b >= 0 ? 2 : 0)) << (2 * st);
+    if (lane == 0) {
+      const int blk = (step0 + i) * 2;
+      const uint32_t dst = ring + st * kStage, bar = bar0 + 8 * st;
+      const bool one = a == b && blocks_of_page > 1;  // adjacent blocks of a page
+      mbar_arrive_expect_tx(bar, (uint32_t)((a >= 0) + (b >= 0)) * kBlock);
+      if (a >= 0)
+        bulk_load(dst, p.cache.data + (((int64_t)a * p.cache.kv_heads + head) * blocks_of_page + (blk & (blocks_of_page - 1))) * kBlock, one ? kStage : kBlock, bar);
+      if (b >= 0 && !one)
+        bulk_load(dst + kBlock, p.cache.data + (((int64_t)b * p.cache.kv_heads + head) * blocks_of_page + ((blk + 1) & (blocks_of_page - 1))) * kBlock, kBlock, bar);
+    }
+  };
+  // (the barriers were set up before find_jobs's barriers of the block)
+  for (int i = 0; i < kStages - 1 && i < mine; ++i) issue(i);
 
   // this lane's query rows (column g of each tile) as float16 with a power of two in front; the sums and factors of columns 2q, 2q + 1
   uint32_t qf[NT][KW][4];
-  float qs[NT][2], c2[NT][2];
-  int lim[NT][2], lim_all = 0, lim_any = 0;  // places that a column sees; the least of the tile's rows, the most
-  const int last_row = jb.queries * sp.group - jb.tile * kRows;  // rows of this tile and behind it
-  {
-    const int j0 = fast_div(jb.tile * kRows, sp.group_magic);
-    const int top = last_row < kRows ? last_row : kRows, j1 = fast_div(jb.tile * kRows + top - 1, sp.group_magic);
-    lim_all = jb.len - jb.queries + j0 + 1;
-    lim_any = jb.len - jb.queries + j1 + 1;
-  }
+  float qs[NT][2], qb[NT][2], c2[NT][2];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int r = t * 8 + g;
-    float f[KW][8], top = 0.0f, sum = 0.0f;
+    float f[KW][8], top = 0.0f, sum = 0.0f, odd = 0.0f;
     const bool live = r < last_row;
-    const int j = fast_div(jb.tile * kRows + r, sp.group_magic), h = jb.tile * kRows + r - j * sp.group;
+    const int j = live ? fast_div(jb.tile * kRows + r, sp.group_magic) : 0, h = jb.tile * kRows + r - j * sp.group;
     const T* x = static_cast<const T*>(p.q) + (live ? (int64_t)(jb.start + j) * p.ldq + (int64_t)(head * sp.group + h) * p.ldqh : 0) + q * (D / 4);
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
@@ -233,61 +334,26 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
       for (int i = 0; i < 4; ++i) {
         const __half2 h2 = __floats2half2_rn(f[w][i] * up, f[w][i + 4] * up);
         qf[t][w][i] = *reinterpret_cast<const uint32_t*>(&h2);
-        sum += __low2float(h2) + __high2float(h2);
+        const float both = __low2float(h2) + __high2float(h2);
+        sum += both;
+        if (i & 1) odd += both;
       }
     }
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    odd += __shfl_xor_sync(0xffffffffu, odd, 1);
+    odd += __shfl_xor_sync(0xffffffffu, odd, 2);
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       qs[t][c] = __shfl_sync(0xffffffffu, sum, (2 * q + c) * 4);
+      qb[t][c] = -64.0f * __shfl_sync(0xffffffffu, odd, (2 * q + c) * 4);
       c2[t][c] = fmaxf(__shfl_sync(0xffffffffu, down, (2 * q + c) * 4), 1.4e-45f);
-      const int rr = jb.tile * kRows + t * 8 + 2 * q + c;
-      lim[t][c] = t * 8 + 2 * q + c < last_row ? jb.len - jb.queries + fast_div(rr, sp.group_magic) + 1 : 0;
     }
   }
 
-  // this warp's steps of the run: step0 + warp, step0 + warp + kWarps, ... while before the last place that a row sees
-  const int step0 = jb.chunk * jb.steps;
-  int end = (lim_any + kStep - 1) / kStep;  // (lim_any <= 0: none)
-  end = end < step0 + jb.steps ? end : step0 + jb.steps;
-  const int mine = end > step0 + warp ? (end - step0 - warp + kWarps - 1) / kWarps : 0;
-  const int blocks_of_page = 1 << (p.cache.page_shift - 4);
-  const int32_t* table = p.table + (int64_t)jb.seq * p.ld_table;
-  const uint32_t ring = smem_u32(smem) + warp * (kStages * kStage), bar0 = smem_u32(&bars[warp * kStages]);
-  int page0 = -1, page1 = -1;  // of step `lane` of the batch of 32 steps that is being issued
-  uint32_t there = 0;          // two bits a stage: its blocks were copied
-  __syncwarp();
-
-  auto issue = [&](int i) {
-    const int st = i % kStages;
-    if ((i & 31) == 0) {
-      const int place = (step0 + warp + kWarps * (i + lane)) * kStep;
-      page0 = i + lane < mine ? table[place >> p.cache.page_shift] : -1;
-      page1 = i + lane < mine && place + 16 < lim_any ? table[(place + 16) >> p.cache.page_shift] : -1;
-      if (page0 < 0 || page0 >= p.cache.pages) page0 = -1;
-      if (page1 < 0 || page1 >= p.cache.pages) page1 = -1;
-    }
-    const int a = __shfl_sync(0xffffffffu, page0, i & 31), b = __shfl_sync(0xffffffffu, page1, i & 31);
-    there = (there & ~(3u << (2 * st))) | (uint32_t)((a >= 0 ? 1 : 0) | (b >= 0 ? 2 : 0)) << (2 * st);
-    if (lane == 0) {
-      const int blk = (step0 + warp + kWarps * i) * 2;
-      const uint32_t dst = ring + st * kStage, bar = bar0 + 8 * st;
-      mbar_arrive_expect_tx(bar, (uint32_t)((a >= 0) + (b >= 0)) * kBlock);
-      if (a >= 0) {
-        const uint8_t* src = p.cache.data + (((int64_t)a * p.cache.kv_heads + head) * blocks_of_page + (blk & (blocks_of_page - 1))) * kBlock;
-        bulk_load(dst, src, a == b && blocks_of_page > 1 ? kStage : kBlock, bar);
-      }
-      if (b >= 0 && !(a == b && blocks_of_page > 1)) {
-        const uint8_t* src = p.cache.data + (((int64_t)b * p.cache.kv_heads + head) * blocks_of_page + ((blk + 1) & (blocks_of_page - 1))) * kBlock;
-        bulk_load(dst + kBlock, src, kBlock, bar);
-      }
-    }
-  };
-
   float o[NT][D / 16][4], m[NT][2], l[NT][2], zs[NT][2];
-  // the value steps' power of two: weights p s reach float16 times `up_v`, so that the largest step lies in [2^14, 2^15); an exponent
-  // field, which only falls (0: no step so far)
+  // the value steps' power of two: weights p s reach float16 times `up_v`, so that the largest step lies in [2^10, 2^11) (and p may be 2^kGrowth); an
+  // exponent field, which only falls (0: no step so far)
   int up_v = 0;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -298,8 +364,6 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
 #pragma unroll
     for (int c = 0; c < 2; ++c) { m[t][c] = -INFINITY; l[t][c] = 0.0f; zs[t][c] = 0.0f; }
   }
-  __syncthreads();  // barriers are set up
-  for (int i = 0; i < kStages - 1 && i < mine; ++i) issue(i);
   int done = 0;
   bool ok = true;
   for (; done < mine; ++done) {
@@ -307,12 +371,10 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
     if (i + kStages - 1 < mine) issue(i + kStages - 1);  // (the stage that the last step freed: every lane has read it)
     if (!mbar_wait(bar0 + 8 * st, (uint32_t)(i / kStages) & 1, abort_flag)) { ok = false; break; }
     const uint32_t base = ring + st * kStage;
-    const int place = (step0 + warp + kWarps * i) * kStep;
+    const int place = (step0 + i) * kStep;
     const uint32_t here = there >> (2 * st) & 3u;
-    const bool edge = place + kStep > lim_all || here != 3u;
     float x[2][NT][4];
     uint32_t vz[2][2];
-    float steps_top = 0.0f;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const uint32_t blk = base + b * kBlock;
@@ -326,27 +388,27 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
       float acc[NT][4];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        acc[t][0] = acc[t][2] = -64.0f * qs[t][0];
-        acc[t][1] = acc[t][3] = -64.0f * qs[t][1];
+        acc[t][0] = acc[t][2] = qb[t][0];
+        acc[t][1] = acc[t][3] = qb[t][1];
       }
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
-        {
-          const uint32_t a0 = nibbles<0>(k0[w]), a1 = nibbles<0>(k1[w]), a2 = nibbles<1>(k0[w]), a3 = nibbles<1>(k1[w]);
+        uint32_t a[4], c[4];
+        key_codes(k0[w], a);
+        key_codes(k1[w], c);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) mma(acc[t], a0, a1, a2, a3, qf[t][w][0], qf[t][w][1]);
-        }
-        {
-          const uint32_t a0 = nibbles<2>(k0[w]), a1 = nibbles<2>(k1[w]), a2 = nibbles<3>(k0[w]), a3 = nibbles<3>(k1[w]);
+        for (int t = 0; t < NT; ++t) mma(acc[t], a[0], c[0], a[1], c[1], qf[t][w][0], qf[t][w][1]);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) mma(acc[t], a0, a1, a2, a3, qf[t][w][2], qf[t][w][3]);
-        }
+        for (int t = 0; t < NT; ++t) mma(acc[t], a[2], c[2], a[3], c[3], qf[t][w][2], qf[t][w][3]);
       }
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int c = 0; c < 4; ++c) x[b][t][c] = fmaf(acc[t][c], step_of(kz[c >> 1]), low_of(kz[c >> 1]) * qs[t][c & 1]);
-      if (edge) {
+    }
+    if (place + kStep > lim_all || here != 3u) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int at = place + 16 * b + 8 * h + g;
@@ -355,19 +417,23 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-              if (gone || at >= lim[t][c]) x[b][t][2 * h + c] = -INFINITY;
+            for (int c = 0; c < 2; ++c) {
+              const int lim = lim_of(jb, sp, kRows, t * 8 + 2 * q + c, last_row);
+              if (gone || at >= lim) x[b][t][2 * h + c] = -INFINITY;
+            }
         }
-      }
+    }
+    // Maxima so far, of each column's scores and of the value steps. What was summed is brought to a new maximum only where it grew by 2^kGrowth.
+    uint32_t tops = 0;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float s = step_of(vz[b][h]);
-        if (s < INFINITY) steps_top = fmaxf(steps_top, s);
+        const uint32_t e = vz[b][h] & 0x7f800000u;
+        if (e != 0x7f800000u) tops = max(tops, e);
       }
-    }
-    // new maxima, of each column's scores and of the value steps; what was summed so far is brought to them
-    const int top_e = (int)(__reduce_max_sync(0xffffffffu, __float_as_uint(steps_top)) >> 23);
-    const int up_new = top_e == 0 ? up_v : top_e < 15 ? 253 : 268 - top_e;
+    const int top_e = (int)(__reduce_max_sync(0xffffffffu, tops) >> 23);
+    const int up_new = top_e == 0 ? up_v : top_e < 11 ? 253 : 264 - top_e;
     float mx[NT][2];
     bool grew = up_new < up_v || up_v == 0;
 #pragma unroll
@@ -375,11 +441,8 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         float v = fmaxf(fmaxf(x[0][t][c], x[0][t][c + 2]), fmaxf(x[1][t][c], x[1][t][c + 2]));
-        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
-        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
-        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
-        mx[t][c] = fmaxf(m[t][c], v);
-        grew = grew || mx[t][c] > m[t][c];
+        mx[t][c] = v;
+        grew = grew || (v - m[t][c]) * c2[t][c] > kGrowth;
       }
     if (__any_sync(0xffffffffu, grew)) {
       float fs = 1.0f;
@@ -392,8 +455,13 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
         float f[2];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          f[c] = mx[t][c] == -INFINITY ? 1.0f : ex2((m[t][c] - mx[t][c]) * c2[t][c]);
-          m[t][c] = mx[t][c];
+          float v = mx[t][c];
+          v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+          v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+          v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+          v = fmaxf(v, m[t][c]);
+          f[c] = v == -INFINITY ? 1.0f : ex2((m[t][c] - v) * c2[t][c]);
+          m[t][c] = v;
           l[t][c] *= f[c];
           zs[t][c] *= f[c];
           f[c] *= fs;
@@ -404,33 +472,37 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
           for (int c = 0; c < 4; ++c) o[t][i2][c] *= f[c & 1];
       }
     }
-    float mu[NT][2];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) mu[t][c] = m[t][c] == -INFINITY ? 0.0f : m[t][c];
+    uint32_t pw[2][NT][2];
+    const float fv = __uint_as_float((uint32_t)up_v << 23);
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const uint32_t blk = base + b * kBlock + 8 * D;
-      uint32_t p0[NT], p1[NT];
-      const float f = __uint_as_float((uint32_t)up_v << 23), s0 = step_of(vz[b][0]) * f, s1 = step_of(vz[b][1]) * f;
+      const float s0 = step_of(vz[b][0]) * fv, s1 = step_of(vz[b][1]) * fv;
       const float z0 = fmaf(8.0f, step_of(vz[b][0]), low_of(vz[b][0])), z1 = fmaf(8.0f, step_of(vz[b][1]), low_of(vz[b][1]));
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        float w[4];
+        float w[4], z[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const float pr = ex2((x[b][t][c] - mu[t][c & 1]) * c2[t][c & 1]);
+          const float pr = ex2((x[b][t][c] - (m[t][c & 1] == -INFINITY ? 0.0f : m[t][c & 1])) * c2[t][c & 1]);
           l[t][c & 1] += pr;
           w[c] = pr * (c < 2 ? s0 : s1);
-          float z = pr * (c < 2 ? z0 : z1);
-          if (edge && x[b][t][c] == -INFINITY) w[c] = z = 0.0f;  // (a place that only later queries see may hold a NaN)
-          zs[t][c & 1] += z;
+          z[c] = pr * (c < 2 ? z0 : z1);
         }
+        if (place + kStep > lim_all || here != 3u) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (x[b][t][c] == -INFINITY) w[c] = z[c] = 0.0f;  // (a place that only later queries see may hold a NaN)
+        }
+        zs[t][0] += z[0] + z[2];
+        zs[t][1] += z[1] + z[3];
         const __half2 h0 = __floats2half2_rn(w[0], w[1]), h1 = __floats2half2_rn(w[2], w[3]);
-        p0[t] = transposed(*reinterpret_cast<const uint32_t*>(&h0));
-        p1[t] = transposed(*reinterpret_cast<const uint32_t*>(&h1));
+        pw[b][t][0] = transposed(*reinterpret_cast<const uint32_t*>(&h0));
+        pw[b][t][1] = transposed(*reinterpret_cast<const uint32_t*>(&h1));
       }
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const uint32_t blk = base + b * kBlock + 8 * D;
       uint32_t v[4][VW];
       lds<VW>(blk + (2 * q) * (D / 2) + g * (D / 16), v[0]);
       lds<VW>(blk + (2 * q + 1) * (D / 2) + g * (D / 16), v[1]);
@@ -438,15 +510,15 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
       lds<VW>(blk + (2 * q + 9) * (D / 2) + g * (D / 16), v[3]);
 #pragma unroll
       for (int u = 0; u < VW; ++u) {
-        const uint32_t e0 = __byte_perm(v[0][u], v[1][u], 0x5410), e1 = __byte_perm(v[0][u], v[1][u], 0x7632);
-        const uint32_t e2 = __byte_perm(v[2][u], v[3][u], 0x5410), e3 = __byte_perm(v[2][u], v[3][u], 0x7632);
+        uint32_t a0[4], a1[4], a2[4], a3[4];
+        value_codes(__byte_perm(v[0][u], v[1][u], 0x5410), a0);
+        value_codes(__byte_perm(v[0][u], v[1][u], 0x7632), a1);
+        value_codes(__byte_perm(v[2][u], v[3][u], 0x5410), a2);
+        value_codes(__byte_perm(v[2][u], v[3][u], 0x7632), a3);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          mma(o[t][4 * u + 0], centred<0>(e0), centred<0>(e1), centred<0>(e2), centred<0>(e3), p0[t], p1[t]);
-          mma(o[t][4 * u + 1], centred<1>(e0), centred<1>(e1), centred<1>(e2), centred<1>(e3), p0[t], p1[t]);
-          mma(o[t][4 * u + 2], centred<2>(e0), centred<2>(e1), centred<2>(e2), centred<2>(e3), p0[t], p1[t]);
-          mma(o[t][4 * u + 3], centred<3>(e0), centred<3>(e1), centred<3>(e2), centred<3>(e3), p0[t], p1[t]);
-        }
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int t = 0; t < NT; ++t) mma(o[t][4 * u + j], a0[j], a1[j], a2[j], a3[j], pw[b][t][0], pw[b][t][1]);
       }
     }
     __syncwarp();
@@ -456,11 +528,11 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
     int never = 0;
     for (int i = done; i < mine && i < done + kStages; ++i) mbar_wait(bar0 + 8 * (i % kStages), (uint32_t)(i / kStages) & 1, &never);
   }
-  grid_dep_launch();
   __syncthreads();  // every warp is through with the rings
 
-  // sums of this warp, at its own maxima: [row][channel]
-  float* mineo = reinterpret_cast<float*>(smem) + warp * kRows * D;
+  // sums of this warp, at its own maxima: [row][channel], rows kPitch apart (columns 2q, 2q + 1 of eight lanes at a time: other banks)
+  constexpr int kPitch = D + 4;
+  float* mineo = reinterpret_cast<float*>(smem) + warp * kRows * kPitch;
   const float back = up_v == 0 ? 0.0f : __uint_as_float((uint32_t)(254 - up_v) << 23);
 #pragma unroll
   for (int t = 0; t < NT; ++t)
@@ -473,137 +545,169 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
         s += __shfl_xor_sync(0xffffffffu, s, k);
       }
       const int row = t * 8 + 2 * q + c;
-      if (g == 0) { wm[warp][row] = m[t][c]; wl[warp][row] = s; }
-      if (g == 0 && warp == 0) wc[row] = c2[t][c];
-      float* y = mineo + row * D + g * (8 * VW);
+      if (g == 0) { wm[warp][row] = m[t][c]; wl[warp][row] = s; wc[warp][row] = c2[t][c]; }
+      float4* y = reinterpret_cast<float4*>(mineo + row * kPitch + g * (8 * VW));
 #pragma unroll
       for (int u = 0; u < VW; ++u)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          y[8 * u + j] = fmaf(o[t][4 * u + j][c], back, z);
-          y[8 * u + 4 + j] = fmaf(o[t][4 * u + j][c + 2], back, z);
-        }
+        for (int h = 0; h < 2; ++h)
+          y[2 * u + h] = make_float4(fmaf(o[t][4 * u][c + 2 * h], back, z), fmaf(o[t][4 * u + 1][c + 2 * h], back, z), fmaf(o[t][4 * u + 2][c + 2 * h], back, z),
+                                     fmaf(o[t][4 * u + 3][c + 2 * h], back, z));
     }
   __syncthreads();
-  const int rows = last_row < kRows ? last_row : kRows;
-  for (int i = threadIdx.x; i < rows * D; i += kThreads) {
-    const int row = i / D, ch = i - row * D;
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, wm[w][row]);
-    const float ref = top == -INFINITY ? 0.0f : top, cs = wc[row];
-    float sum = 0.0f, all = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float f = ex2((wm[w][row] - ref) * cs);
-      all = fmaf(wl[w][row], f, all);
-      sum = fmaf(reinterpret_cast<const float*>(smem)[(w * kRows + row) * D + ch], f, sum);
+  // groups of runs that belong together, the block's warps from `w0` to `w1`
+  Span* span = reinterpret_cast<Span*>(sp.meta) + blockIdx.x;
+  int goes_on = 0;
+  for (int w0 = 0, w1; w0 < kWarps && jobs[w0].seq >= 0; w0 = w1) {
+    const Job j0 = jobs[w0];
+    w1 = w0 + j0.runs - j0.run < kWarps ? w0 + j0.runs - j0.run : kWarps;
+    const bool whole = j0.run == 0 && w0 + j0.runs == w1;
+    const int behind = j0.queries * sp.group - j0.tile * kRows, rows = behind < kRows ? behind : kRows;
+    if (j0.run == 0 && !whole) {
+      goes_on = 1;
+      if (threadIdx.x == 0) *span = {(int)((blockIdx.x * kWarps + w0 + j0.runs - 1) / kWarps), j0.start, j0.queries, j0.tile, j0.head, {0, 0, 0}};
     }
-    if (jb.chunks == 1) {
-      const int rr = jb.tile * kRows + row, j = fast_div(rr, sp.group_magic), h = head * sp.group + rr - j * sp.group;
-      const int64_t token = jb.start + j;
-      put(static_cast<T*>(p.out) + token * p.ldo + (int64_t)h * p.ldoh + ch, top == -INFINITY && all == 0.0f ? 0.0f : sum / all);
-      if (p.lse && ch == 0) p.lse[token * p.heads + h] = fmaf(top, cs, log2f(all)) * kLn2;
-    } else {
-      float* part = sp.part + (((int64_t)blockIdx.x * gridDim.y + head) * kRows + row) * (D + 4);
-      part[ch] = sum;
-      if (ch == 0) { part[D] = top; part[D + 1] = all; part[D + 2] = cs; }
+    for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
+      const int row = i / (D / 4), ch = (i - row * (D / 4)) * 4;
+      float top = -INFINITY;
+      for (int w = w0; w < w1; ++w) top = fmaxf(top, wm[w][row]);
+      const float ref = top == -INFINITY ? 0.0f : top, cs = wc[w0][row];
+      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      float all = 0.0f;
+      for (int w = w0; w < w1; ++w) {
+        const float f = ex2((wm[w][row] - ref) * cs);
+        const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem) + (w * kRows + row) * kPitch + ch);
+        all = fmaf(wl[w][row], f, all);
+        sum.x = fmaf(v.x, f, sum.x); sum.y = fmaf(v.y, f, sum.y); sum.z = fmaf(v.z, f, sum.z); sum.w = fmaf(v.w, f, sum.w);
+      }
+      if (whole) {
+        const int rr = j0.tile * kRows + row, j = fast_div(rr, sp.group_magic), h = j0.head * sp.group + rr - j * sp.group;
+        const int64_t token = j0.start + j;
+        const float inv = top == -INFINITY && all == 0.0f ? 0.0f : 1.0f / all;
+        T* y = static_cast<T*>(p.out) + token * p.ldo + (int64_t)h * p.ldoh + ch;
+        put(y, sum.x * inv); put(y + 1, sum.y * inv); put(y + 2, sum.z * inv); put(y + 3, sum.w * inv);
+        if (p.lse && ch == 0) p.lse[token * p.heads + h] = fmaf(top, cs, log2f(all)) * kLn2;
+      } else {
+        float* part = sp.part + (((int64_t)blockIdx.x * 2 + (j0.run == 0 ? 1 : 0)) * kRows + row) * (D + 4);
+        *reinterpret_cast<float4*>(part + ch) = sum;
+        if (ch == 0) *reinterpret_cast<float4*>(part + D) = make_float4(top, all, cs, 0.0f);
+      }
     }
   }
+  if (!goes_on && threadIdx.x == 0) span->last = 0;
 }
 
-// One block for a row tile's row of a key-value head: the parts of its sequence, in a fixed order.
+// A block for a row of the group of runs that begins in block blockIdx.x and goes on: its parts, in a fixed order.
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_constant__ Split sp, const int rows) {
-  __shared__ float so[kWarps][D], sm[kWarps], sl[kWarps];
+  constexpr int kMost = 152 * 2 + 4;  // parts: a group has at most as many runs as fill the GPU
+  __shared__ float weight[kMost], so[kWarps][D], red[kWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   grid_dep_wait();
-  if ((int)blockIdx.x >= sp.meta[0]) return;
-  const int* meta = sp.meta + 4 + 4 * blockIdx.x;
-  const int first = meta[0], chunks = meta[1], start = meta[2], tile = meta[3], queries = sp.meta[4 + 4 * sp.tiles + blockIdx.x];
-  const int row = blockIdx.z, rr = tile * rows + row;
-  if (chunks == 1 || rr >= queries * sp.group) return;
-  float o[D / 32], m = -INFINITY, l = 0.0f;
+  const Span span = reinterpret_cast<const Span*>(sp.meta)[blockIdx.x];
+  const int row = blockIdx.y, rr = span.tile * rows + row, first = blockIdx.x;
+  const int parts = span.last - first + 1;
+  // (starts that fall make more tasks than there are blocks: such groups are left)
+  if (span.last <= first || span.last >= (int)gridDim.x || parts > kMost || rr >= span.queries * sp.group) return;
+  // (what a block goes on with comes first among its two parts, what it begins second)
+  const float* part = sp.part + ((int64_t)first * 2 * rows + row) * (D + 4);
+  const int64_t pitch = (int64_t)2 * rows * (D + 4), begin = rows * (D + 4);
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, cs = part[begin + D + 2], top = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int c = threadIdx.x + k * kThreads;
+    if (c < parts) {
+      const float4 v = *reinterpret_cast<const float4*>(part + c * pitch + (c == 0 ? begin : 0) + D);
+      m[k] = v.x; l[k] = v.y;
+      top = fmaxf(top, v.x);
+    }
+  }
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (lane == 0) red[warp] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) top = fmaxf(top, red[w]);
+  const float ref = top == -INFINITY ? 0.0f : top;
+  float all = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int c = threadIdx.x + k * kThreads;
+    const float f = ex2((m[k] - ref) * cs);
+    if (c < parts) weight[c] = f;
+    all = fmaf(l[k], f, all);
+  }
+  for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+  __syncthreads();
+  if (lane == 0) red[warp] = all;
+  float o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = 0.0f;
-  const int64_t pitch = (int64_t)gridDim.y * rows * (D + 4);
-  const float* part = sp.part + (((int64_t)first * gridDim.y + blockIdx.y) * rows + row) * (D + 4);
-  const float cs = part[D + 2];
-  for (int c = warp; c < chunks; c += kWarps) {
-    const float* x = part + c * pitch;
-    const float mc = x[D], lc = x[D + 1];
-    float v[D / 32];
+#pragma unroll 8
+  for (int c = warp; c < parts; c += kWarps) {
+    const float f = weight[c];
+    const float* x = part + c * pitch + (c == 0 ? begin : 0) + lane;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) v[i] = x[lane + 32 * i];
-    const float top = fmaxf(m, mc), ref = top == -INFINITY ? 0.0f : top;
-    const float fa = ex2((m - ref) * cs), fb = ex2((mc - ref) * cs);
-    m = top;
-    l = l * fa + lc * fb;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) o[i] = o[i] * fa + v[i] * fb;
+    for (int i = 0; i < D / 32; ++i) o[i] = fmaf(x[32 * i], f, o[i]);
   }
-  if (lane == 0) { sm[warp] = m; sl[warp] = l; }
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) so[warp][lane + 32 * i] = o[i];
   __syncthreads();
+  all = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) all += red[w];
   for (int ch = threadIdx.x; ch < D; ch += kThreads) {
-    float top = -INFINITY;
+    float sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sm[w]);
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, all = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float f = ex2((sm[w] - ref) * cs);
-      all = fmaf(sl[w], f, all);
-      sum = fmaf(so[w][ch], f, sum);
-    }
-    const int j = fast_div(rr, sp.group_magic), h = blockIdx.y * sp.group + rr - j * sp.group;
-    const int64_t token = start + j;
+    for (int w = 0; w < kWarps; ++w) sum += so[w][ch];
+    const int j = fast_div(rr, sp.group_magic), h = span.head * sp.group + rr - j * sp.group;
+    const int64_t token = span.start + j;
     put(static_cast<T*>(p.out) + token * p.ldo + (int64_t)h * p.ldoh + ch, top == -INFINITY && all == 0.0f ? 0.0f : sum / all);
     if (p.lse && ch == 0) p.lse[token * p.heads + h] = fmaf(top, cs, log2f(all)) * kLn2;
   }
 }
 
 struct Sizes {
-  int rows;             // of a block
-  int64_t tiles, units; // bounds: row tiles; units of a key-value head
-  int per_head;         // units that fill the GPU
+  int rows;             // of a tile
+  int warps;            // tasks that fill the GPU
+  int64_t tiles, blocks; // bounds: row tiles; blocks
   size_t part_off, bytes;
 };
 static Sizes sizes(int64_t tokens, int32_t seqs, int32_t heads, int32_t kv_heads, int32_t dim) {
   Sizes s{};
   const int64_t group = heads / kv_heads;
-  // 16 rows a block where most sequences have them: the codes' unpacking serves twice as many
+  // 16 rows a task where most sequences have them: the codes' unpacking serves twice as many
   const bool two = row_tiles(dim) > 1 && tokens * group > 8 * (int64_t)seqs;
   s.rows = two ? 16 : 8;
   s.tiles = tokens == seqs ? seqs * ((group + s.rows - 1) / s.rows) : tokens * group / s.rows + seqs;
   // (tokens == seqs with starts: each of n > 0 queries has at most ceil(n group / rows) <= n ceil(group / rows) tiles)
-  s.per_head = (int)((two || dim > 128 ? 152 : 304) / kv_heads);
-  if (s.per_head < 1) s.per_head = 1;
-  s.units = s.per_head + s.tiles;
-  s.part_off = ((size_t)(4 + 5 * s.tiles) * 4 + 255) / 256 * 256;
-  s.bytes = s.part_off + (size_t)s.units * kv_heads * s.rows * (dim + 4) * 4;
+  s.warps = 152 * (two || dim > 128 ? 1 : 2) * kWarps;
+  // tasks: a run each for `warps` of them at most (twice as many beside many tiles), and one more for each tile and head; or a block for each
+  s.blocks = (s.warps + kWarps - 1) / kWarps + s.tiles * kv_heads;
+  s.part_off = ((size_t)s.blocks * sizeof(Span) + 255) / 256 * 256;
+  s.bytes = s.part_off + (size_t)s.blocks * 2 * s.rows * (dim + 4) * 4;
   return s;
 }
 
 template <class T, int D, int NT>
 static cudaError_t run(const CacheAttnArgs& a, const Sizes& s, cudaStream_t stream) {
   Split sp{};
-  sp.units = s.per_head;
-  sp.tiles = (int32_t)s.tiles;
+  sp.warps = s.warps;
+  // up to four steps a warp: a second kernel's launch costs more than a finer split gives
+  sp.whole = ((int64_t)a.columns << a.cache.page_shift) <= 4 * kWarps * kStep;
   sp.group = a.heads / a.cache.kv_heads;
   sp.group_magic = div_magic(sp.group);
   sp.q_vec = (reinterpret_cast<uintptr_t>(a.q) & 15) == 0 && (a.ldq | a.ldqh) % 8 == 0;
   sp.meta = reinterpret_cast<int32_t*>(a.ws);
   sp.part = reinterpret_cast<float*>(a.ws + s.part_off);
-  constexpr int ring = kWarps * stages(D) * stage_bytes(D), join = kWarps * 8 * NT * D * 4;
+  constexpr int ring = kWarps * stages(D) * stage_bytes(D), join = kWarps * 8 * NT * (D + 4) * 4;
   constexpr int smem = ring > join ? ring : join;
   static_assert(smem <= 227 * 1024 - 4096, "");
   cudaError_t e = cudaFuncSetAttribute(cache_attention_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
+  const int64_t heads_tiles = s.tiles * a.cache.kv_heads;
+  const int64_t blocks = sp.whole ? heads_tiles : (s.warps + heads_tiles + kWarps - 1) / kWarps;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)s.units, (unsigned)a.cache.kv_heads);
+  cfg.gridDim = dim3((unsigned)blocks);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
@@ -613,10 +717,8 @@ static cudaError_t run(const CacheAttnArgs& a, const Sizes& s, cudaStream_t stre
   cfg.attrs = at;
   cfg.numAttrs = 1;
   e = cudaLaunchKernelEx(&cfg, cache_attention_kernel<T, D, NT>, a, sp);
-  if (e != cudaSuccess) return e;
-  // a table of no more than one run's places has no parts to join
-  if (((int64_t)a.columns << a.cache.page_shift) <= kWarps * kStep) return cudaSuccess;
-  cfg.gridDim = dim3((unsigned)s.tiles, (unsigned)a.cache.kv_heads, (unsigned)s.rows);
+  if (e != cudaSuccess || sp.whole) return e;
+  cfg.gridDim = dim3((unsigned)blocks, (unsigned)s.rows);
   cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, combine_kernel<T, D>, a, sp, s.rows);
 }
@@ -639,7 +741,7 @@ size_t cache_attention_workspace_bytes(int64_t tokens, int32_t seqs, int32_t hea
 
 int launch_cache_attention(const CacheAttnArgs& a, cudaStream_t stream, std::string* err) {
   const cacheattn::Sizes s = cacheattn::sizes(a.tokens, a.seqs, a.heads, a.cache.kv_heads, a.cache.dim);
-  if (s.units > 0x7fffffff || s.tiles > (1 << 26)) {
+  if (s.blocks > (1 << 27)) {  // (tasks are counted in 32 bits)
     *err = "too many tokens in one call";
     return 2;
   }
