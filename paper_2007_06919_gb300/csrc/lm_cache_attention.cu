@@ -66,8 +66,8 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   uint32_t y;
@@ -83,21 +83,27 @@ __device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
   return y;
 }
+// (w & mask) | exponent in one operation
+__device__ __forceinline__ uint32_t under(uint32_t w, uint32_t mask, uint32_t exponent) {
+  uint32_t y;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(w), "r"(mask), "r"(exponent));
+  return y;
+}
 // Nibbles of each 16-bit half of w as float16 numbers: under the exponent of 1024 the lowest four bits are 1024 + n, under that of 64 the next four are
 // 64 + n; a byte's shift brings the other two there. Keys: n and 64 + n (of the odd nibbles, which -64 sum(q) makes good), values: n - 8.
 __device__ __forceinline__ void key_codes(uint32_t w, uint32_t (&h)[4]) {
   const uint32_t v = w >> 8;
-  h[0] = sub2((w & 0x000f000fu) | 0x64006400u, 0x64006400u);
-  h[1] = (w & 0x00f000f0u) | 0x54005400u;
-  h[2] = sub2((v & 0x000f000fu) | 0x64006400u, 0x64006400u);
-  h[3] = (v & 0x00f000f0u) | 0x54005400u;
+  h[0] = sub2(under(w, 0x000f000fu, 0x64006400u), 0x64006400u);
+  h[1] = under(w, 0x00f000f0u, 0x54005400u);
+  h[2] = sub2(under(v, 0x000f000fu, 0x64006400u), 0x64006400u);
+  h[3] = under(v, 0x00f000f0u, 0x54005400u);
 }
 __device__ __forceinline__ void value_codes(uint32_t w, uint32_t (&h)[4]) {
   const uint32_t v = w >> 8;
-  h[0] = sub2((w & 0x000f000fu) | 0x64006400u, 0x64086408u);
-  h[1] = sub2((w & 0x00f000f0u) | 0x54005400u, 0x54805480u);
-  h[2] = sub2((v & 0x000f000fu) | 0x64006400u, 0x64086408u);
-  h[3] = sub2((v & 0x00f000f0u) | 0x54005400u, 0x54805480u);
+  h[0] = sub2(under(w, 0x000f000fu, 0x64006400u), 0x64086408u);
+  h[1] = sub2(under(w, 0x00f000f0u, 0x54005400u), 0x54805480u);
+  h[2] = sub2(under(v, 0x000f000fu, 0x64006400u), 0x64086408u);
+  h[3] = sub2(under(v, 0x00f000f0u, 0x54005400u), 0x54805480u);
 }
 template <int kWords>
 __device__ __forceinline__ void lds(uint32_t addr, uint32_t (&w)[kWords]) {
@@ -273,8 +279,12 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
   int page0 = -1, page1 = -1;  // of step `lane` of the batch of 32 steps that is being issued
   uint32_t there = 0;          // two bits a stage: its blocks were copied
 
+  const uint8_t* mine_data = p.cache.data + (int64_t)head * blocks_of_page * kBlock;  // this head's part of page 0
+  const uint32_t page_bytes = (uint32_t)p.cache.kv_heads * (uint32_t)blocks_of_page * kBlock;
+  int blk = idle ? 0 : (step0 * 2) & (blocks_of_page - 1);  // the next step's first block within its page
+  int ist = 0;                                              // its stage
+
   auto issue = [&](int i) {
-    const int st = i % kStages;
     if ((i & 31) == 0) {
       const int place = (step0 + i + lane) * kStep;
       page0 = i + lane < mine ? table[place >> p.cache.page_shift] : -1;
@@ -283,17 +293,22 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
       if (page1 < 0 || page1 >= p.cache.pages) page1 = -1;
     }
     const int a = __shfl_sync(0xffffffffu, page0, i & 31), b = __shfl_sync(0xffffffffu, page1, i & 31);
-    there = (there & ~(3u << (2 * st))) | (uint32_t)((a >= 0 ? 1 : 0) | (b >= 0 ? 2 : 0)) << (2 * st);
+    const uint32_t copied = (a >= 0 ? 1u : 0u) | (b >= 0 ? 2u : 0u);
+    there = (there & ~(3u << (2 * ist))) | copied << (2 * ist);
     if (lane == 0) {
-      const int blk = (step0 + i) * 2;
-      const uint32_t dst = ring + st * kStage, bar = bar0 + 8 * st;
-      const bool one = a == b && blocks_of_page > 1;  // adjacent blocks of a page
-      mbar_arrive_expect_tx(bar, (uint32_t)((a >= 0) + (b >= 0)) * kBlock);
-      if (a >= 0)
-        bulk_load(dst, p.cache.data + (((int64_t)a * p.cache.kv_heads + head) * blocks_of_page + (blk & (blocks_of_page - 1))) * kBlock, one ? kStage : kBlock, bar);
-      if (b >= 0 && !one)
-        bulk_load(dst + kBlock, p.cache.data + (((int64_t)b * p.cache.kv_heads + head) * blocks_of_page + ((blk + 1) & (blocks_of_page - 1))) * kBlock, kBlock, bar);
+      const uint32_t dst = ring + ist * kStage, bar = bar0 + 8 * ist;
+      const uint8_t* src = mine_data + (uint64_t)(uint32_t)a * page_bytes + (uint32_t)blk * kBlock;
+      if (copied == 3u && blocks_of_page > 1) {  // adjacent blocks of a page
+        mbar_arrive_expect_tx(bar, kStage);
+        bulk_load(dst, src, kStage, bar);
+      } else {
+        mbar_arrive_expect_tx(bar, (uint32_t)__popc(copied) * kBlock);
+        if (a >= 0) bulk_load(dst, src, kBlock, bar);
+        if (b >= 0) bulk_load(dst + kBlock, mine_data + (uint64_t)(uint32_t)b * page_bytes + (uint32_t)((blk + 1) & (blocks_of_page - 1)) * kBlock, kBlock, bar);
+      }
     }
+    blk = (blk + 2) & (blocks_of_page - 1);
+    ist = ist == kStages - 1 ? 0 : ist + 1;
   };
   // (the barriers were set up before find_jobs's barriers of the block)
   for (int i = 0; i < kStages - 1 && i < mine; ++i) issue(i);
@@ -364,14 +379,14 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
 #pragma unroll
     for (int c = 0; c < 2; ++c) { m[t][c] = -INFINITY; l[t][c] = 0.0f; zs[t][c] = 0.0f; }
   }
-  int done = 0;
+  int done = 0, st = 0;
+  uint32_t phase = 0;
   bool ok = true;
   for (; done < mine; ++done) {
-    const int i = done, st = i % kStages;
-    if (i + kStages - 1 < mine) issue(i + kStages - 1);  // (the stage that the last step freed: every lane has read it)
-    if (!mbar_wait(bar0 + 8 * st, (uint32_t)(i / kStages) & 1, abort_flag)) { ok = false; break; }
+    if (done + kStages - 1 < mine) issue(done + kStages - 1);  // (the stage that the last step freed: every lane has read it)
+    if (!mbar_wait(bar0 + 8 * st, phase, abort_flag)) { ok = false; break; }
     const uint32_t base = ring + st * kStage;
-    const int place = (step0 + i) * kStep;
+    const int place = (step0 + done) * kStep;
     const uint32_t here = there >> (2 * st) & 3u;
     float x[2][NT][4];
     uint32_t vz[2][2];
@@ -521,6 +536,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
           for (int t = 0; t < NT; ++t) mma(o[t][4 * u + j], a0[j], a1[j], a2[j], a3[j], pw[b][t][0], pw[b][t][1]);
       }
     }
+    if (++st == kStages) { st = 0; phase ^= 1; }
     __syncwarp();
   }
   if (!ok) {  // the copies in flight end before the block does (each wait is bounded)
