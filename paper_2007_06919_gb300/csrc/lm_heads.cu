@@ -3,16 +3,21 @@
 //
 // A row is one token's vector of one head. Some lanes of a warp hold it in registers, each with two vectors that the rotation pairs (i and
 // i + rot / 2), or that hold its pairs themselves (interleaved), so norm, rotation and codes take one read and one write, and what crosses
-// lanes is a sum of squares and a row's lowest and highest value. Bound by memory.
+// lanes is a sum of squares and a row's lowest and highest value. Bound by memory, if the instructions for a value stay below about eight: a
+// warp takes a token's heads in turn (rows_kernel), its lanes keep their places in the row, and with them the products of weights, cosines and sines;
+// float32 goes in pairs; 16-bit minima and maxima stay packed; codes come out of the bits of one multiply-add. (A row at a time with indexes, weights and turns
+// looked up for each: 8192 tokens of 40 heads of 128 in bfloat16 47 us, 16,384 tokens' 16 rows to codes 46 and back 34.)
+// Rows at any address, and rotations of any even length, take heads_kernel, a value at a time.
 //
-// The angle of position p at frequency f is p f / 2 pi turns, of which the whole ones do not count: with u = frac(f / 2 pi) 2^64 rounded to
-// an integer, p u mod 2^64 is the fraction, exact but for |p| 2^-64 of a turn (and the 2^-53 of u's own product), whatever the position. A block's
-// sines and cosines are computed once, for all heads.
+// The angle of position p at frequency f is p f / 2 pi turns, of which the whole ones do not count: with u = frac(f / 2 pi) 2^64 cut to
+// an integer, p u mod 2^64 is the fraction, exact but for |p| (1 + |f|) 2^-64 of a turn, whatever the position. A block's sines and cosines are computed
+// once, for all heads.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "../../include/aqd.h"
 #include "common.cuh"
@@ -79,37 +84,58 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
+// The quotient a / b from inv, 1 / b to about a step: what a first one leaves over corrects it. Exact where the quotient is a float32 (16-bit rows meet
+// codes exactly halfway between two often, and those have to stay there).
+__device__ __forceinline__ float quotient(float a, float b, float inv) {
+  const float q = __fmul_rn(a, inv);
+  return __fmaf_rn(__fmaf_rn(-q, b, a), inv, q);
+}
 // A row's lowest value and step, as the cache keeps them; NaN for both where a value is none or the span is out of range.
 struct RowStep {
   float low, step, inv;
   uint32_t word;
   __device__ __forceinline__ RowStep(float lo, float hi) {
-    const __nv_bfloat16 l = __float2bfloat16_rd(lo);
-    low = __bfloat162float(l);
-    __nv_bfloat16 s = __float2bfloat16_ru(__fdiv_rn(__fsub_rn(hi, low), 15.0f));
-    step = __bfloat162float(s);
-    if (hi == low) s = __float2bfloat16_rn(0.0f);
-    else if (step < 0x1p-126f) s = __float2bfloat16_rn(0x1p-126f);
-    step = __bfloat162float(s);
-    const bool fine = fabsf(low) < INFINITY && step < INFINITY;
-    inv = fine && step > 0.0f ? __frcp_rn(step) : 0.0f;
-    word = fine ? (uint32_t)__bfloat16_as_ushort(l) | (uint32_t)__bfloat16_as_ushort(s) << 16 : 0x7fc07fc0u;
-    if (!fine) low = step = 0.0f;
+    // bfloat16 is a float32's upper half: cut towards zero, or with the magnitude raised to the next
+    const uint32_t b = __float_as_uint(lo);
+    const uint32_t l = (b + (uint32_t)((int32_t)b >> 31 & 0xffff)) & 0xffff0000u;
+    low = __uint_as_float(l);
+    const float span = __fsub_rn(hi, low);
+    uint32_t s = __float_as_uint(quotient(span, 15.0f, 1.0f / 15.0f)) + 0xffffu & 0xffff0000u;
+    s = hi == low ? 0u : s < 0x00800000u ? 0x00800000u : s;
+    const bool fine = fabsf(low) < INFINITY && span < INFINITY;
+    word = fine ? l >> 16 | s : 0x7fc07fc0u;
+    step = fine ? __uint_as_float(s) : 0.0f;
+    if (!fine) low = 0.0f;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(step));
+    if (step == 0.0f) inv = 0.0f;
   }
-  // (x - low) / step to the nearest, ties to even. d * inv is off by 2^-23 of it, so only its integer can be wrong, by one, next to a tie;
-  // what is left of d under it decides, exactly (16-bit values meet exact ties often).
+  // (x - low) / step to the nearest, ties to even: the low bits under 1.5 2^23
   __device__ __forceinline__ uint32_t code(float x) const {
-    const float d = __fsub_rn(x, low);
-    float n = __fadd_rn(__fmaf_rn(d, inv, 12582912.0f), -12582912.0f);
-    const float r = __fmaf_rn(-n, step, d), h = 0.5f * step;
-    if (fabsf(r) >= h) {
-      const bool odd = ((int)n & 1) != 0;
-      if (r > h || (r == h && odd)) n += 1.0f;
-      else if (r < -h || (r == -h && odd)) n -= 1.0f;
-    }
-    return inv > 0.0f ? (uint32_t)(int)n & 15u : 0u;
+    return inv > 0.0f ? __float_as_uint(__fadd_rn(quotient(__fsub_rn(x, low), step, inv), 12582912.0f)) & 15u : 0u;
   }
 };
+
+// frac(f / 2 pi) 2^64: f is an integer of 24 bits times a power of two, so it is that integer times 2^64 / 2 pi, shifted (whole turns fall out at
+// the top; what is cut at the bottom, and of the constant, is below (1 + |f|) 2^-64 of a turn).
+__device__ __forceinline__ uint64_t turn_rate(float f) {
+  constexpr uint64_t kPerTurn = 0x28be60db9391054aull;  // floor(2^64 / 2 pi)
+  const uint32_t b = __float_as_uint(f), exponent = b >> 23 & 255u;
+  const uint64_t m = (b & 0x7fffffu) | (exponent ? 0x800000u : 0u);
+  const int e = (int)(exponent ? exponent : 1u) - 150;
+  const uint64_t lo = m * kPerTurn, hi = __umul64hi(m, kPerTurn);
+  uint64_t u;
+  if (e >= 0) u = e < 64 ? lo << e : 0;
+  else if (e > -64) u = lo >> -e | hi << (64 + e);
+  else u = e > -128 ? hi >> (-64 - e) : 0;
+  return b >> 31 ? 0 - u : u;
+}
+// Cosine and sine of position p at that rate: whole turns leave the product by themselves.
+__device__ __forceinline__ float2 turn_of(uint64_t rate, int64_t p) {
+  const uint64_t frac = (uint64_t)p * rate;
+  float s, c;
+  sincospif((float)(int32_t)(uint32_t)((frac + 0x80000000ull) >> 32) * 0x1p-31f, &s, &c);
+  return make_float2(c, s);
+}
 
 // The block of 16 places of a slot, and the slot's row in it.
 __device__ __forceinline__ uint8_t* place(const CacheGeom& c, int64_t slot, int head, int& row) {
@@ -120,225 +146,474 @@ __device__ __forceinline__ uint8_t* place(const CacheGeom& c, int64_t slot, int 
 }
 __device__ __forceinline__ bool in_cache(const CacheGeom& c, int64_t slot) { return slot >= 0 && (slot >> c.page_shift) < c.pages; }
 
-// V: elements of a vector (8 of 16 bits, 4 of 32; 1 for rows at any address or with any rot), kC: pairs of vectors a lane. lanes: those of a
-// row, a power of two, 32 for V = 1. A block takes `per` tokens, all rows of them.
-template <class T, int V, int kC, bool kCache>
-__global__ void __launch_bounds__(kThreads) heads_kernel(const QkArgs p, const int per, const int lanes, const uint64_t rows_magic) {
+// A warp per row, a value at a time: kC pairs of values a lane (rows of up to 64 kC values). A block takes `per` tokens, all rows of them.
+template <class T, bool kCache>
+__global__ void __launch_bounds__(kThreads) heads_kernel(const QkArgs p, const int per, const uint64_t rows_magic) {
+  constexpr int kC = 8;
   extern __shared__ float2 turns[];  // [per][rot / 2]: cosine, sine
-  __shared__ uint8_t bytes[V == 1 && kCache ? kThreads / 32 * 256 : 1];
+  __shared__ uint8_t bytes[kCache ? kThreads / 32 * 256 : 1];
   tc::grid_dep_wait();
   const int64_t t0 = (int64_t)blockIdx.x * per;
   const int here = (int)(p.tokens - t0 < per ? p.tokens - t0 : per), half = p.rot >> 1;
   for (int i = threadIdx.x; i < here * half; i += kThreads) {
-    const int t = half == 0 ? 0 : i / half, f = i - t * half;
-    double turn = (double)p.inv_freq[f] * 0.15915494309189535;
-    turn -= floor(turn);
-    const uint64_t u = __double2ull_rn(turn * 18446744073709551616.0);  // (a turn rounded up to 1 wraps in the product alike)
-    const uint64_t frac = (uint64_t)p.positions[t0 + t] * u;
-    float s, c;
-    sincospif((float)(int32_t)(uint32_t)((frac + 0x80000000ull) >> 32) * 0x1p-31f, &s, &c);
-    turns[i] = make_float2(c, s);
+    const int t = i / half, f = i - t * half;
+    turns[i] = turn_of(turn_rate(p.inv_freq[f]), p.positions[t0 + t]);
   }
   __syncthreads();
   const int each = p.heads + p.kv_heads * (kCache ? 2 : 1), rows = here * each;  // rows of a token: queries, keys, values
-  const int lane = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = kThreads / lanes;
-  for (int r0 = 0; r0 < rows; r0 += groups) {
-    const int r = r0 + group;
-    const bool live = r < rows;
-    const int t = fast_div(live ? r : 0, rows_magic), h = (live ? r : 0) - t * each;
+  const int lane = threadIdx.x & 31;
+  for (int r = threadIdx.x >> 5; r < rows; r += kThreads / 32) {
+    const int t = fast_div(r, rows_magic), h = r - t * each;
     const int64_t token = t0 + t;
     const bool is_q = h < p.heads, is_v = kCache && h >= p.heads + p.kv_heads;
     const int kh = is_v ? h - p.heads - p.kv_heads : h - p.heads;
     const T* x = is_q ? static_cast<const T*>(p.q) + token * p.ldq + h * p.ldqh
                : is_v ? static_cast<const T*>(p.v) + token * p.ldv + kh * p.ldvh
                       : static_cast<const T*>(p.k) + token * p.ldk + kh * p.ldkh;
-    float a[kC][V], b[kC][V];
+    float a[kC], b[kC];
     int ia[kC], ib[kC];
     float ss = 0.0f;
 #pragma unroll
     for (int c = 0; c < kC; ++c) {
-      const int i = lane + c * 32;  // (lanes is 32 where there are several)
-      if (p.interleaved || i * V >= half) {
-        ia[c] = 2 * i * V;
-        ib[c] = ia[c] + V;
-      } else {
-        ia[c] = i * V;
-        ib[c] = ia[c] + half;
-      }
-      const bool in = live && 2 * i * V < p.dim;
-#pragma unroll
-      for (int j = 0; j < V; ++j) a[c][j] = b[c][j] = 0.0f;
-      if (in) {
-        load<V>(x + ia[c], a[c]);
-        load<V>(x + ib[c], b[c]);
+      const int i = lane + c * 32;
+      const bool between = !p.interleaved && i < half;
+      ia[c] = between ? i : 2 * i;
+      ib[c] = between ? i + half : 2 * i + 1;
+      a[c] = b[c] = 0.0f;
+      if (2 * i < p.dim) {
+        a[c] = to_f32(x[ia[c]]);
+        b[c] = to_f32(x[ib[c]]);
       } else {
         ia[c] = -1;
       }
-#pragma unroll
-      for (int j = 0; j < V; ++j) ss = fmaf(a[c][j], a[c][j], fmaf(b[c][j], b[c][j], ss));
+      ss = fmaf(a[c], a[c], fmaf(b[c], b[c], ss));
     }
     const void* w = is_v ? nullptr : is_q ? p.q_weight : p.k_weight;
-    for (int o = lanes >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
     if (w) {
+      for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
       const float rms = rsqrtf(ss / (float)p.dim + p.eps);
 #pragma unroll
       for (int c = 0; c < kC; ++c) {
         if (ia[c] < 0) continue;
-        float wa[V], wb[V];
-        load_weight<V>(w, ia[c], p.weight_dtype, wa);
-        load_weight<V>(w, ib[c], p.weight_dtype, wb);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          a[c][j] = a[c][j] * rms * wa[j];
-          b[c][j] = b[c][j] * rms * wb[j];
-        }
+        float wa[1], wb[1];
+        load_weight<1>(w, ia[c], p.weight_dtype, wa);
+        load_weight<1>(w, ib[c], p.weight_dtype, wb);
+        a[c] = a[c] * rms * wa[0];
+        b[c] = b[c] * rms * wb[0];
       }
     }
     if (!is_v) {
-      const float2* turn = turns + t * half;
+      T* y = is_q ? static_cast<T*>(p.q_out) + token * p.ldqo + h * p.ldqoh
+                  : (p.k_out ? static_cast<T*>(p.k_out) + token * p.ldko + kh * p.ldkoh : nullptr);
 #pragma unroll
       for (int c = 0; c < kC; ++c) {
         if (ia[c] < 0) continue;
-        if (V > 1 && p.interleaved) {  // pairs within each vector
-#pragma unroll
-          for (int j = 0; j + 1 < V; j += 2) {
-            if (ia[c] < p.rot) {
-              const float2 cs = turn[(ia[c] + j) >> 1];
-              const float u = a[c][j], v = a[c][j + 1];
-              a[c][j] = u * cs.x - v * cs.y;
-              a[c][j + 1] = v * cs.x + u * cs.y;
-            }
-            if (ib[c] < p.rot) {
-              const float2 cs = turn[(ib[c] + j) >> 1];
-              const float u = b[c][j], v = b[c][j + 1];
-              b[c][j] = u * cs.x - v * cs.y;
-              b[c][j + 1] = v * cs.x + u * cs.y;
-            }
-          }
-        } else {
-          const int f = (lane + c * 32) * V;  // pairs between the two
-          if (f < half) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-              const float2 cs = turn[f + j];
-              const float u = a[c][j], v = b[c][j];
-              a[c][j] = u * cs.x - v * cs.y;
-              b[c][j] = v * cs.x + u * cs.y;
-            }
-          }
+        const int f = lane + c * 32;
+        if (f < half) {
+          const float2 cs = turns[t * half + f];
+          const float u = a[c], v = b[c];
+          a[c] = u * cs.x - v * cs.y;
+          b[c] = v * cs.x + u * cs.y;
         }
-      }
-      T* y = is_q ? static_cast<T*>(p.q_out) + token * p.ldqo + h * p.ldqoh
-                  : (p.k_out ? static_cast<T*>(p.k_out) + token * p.ldko + kh * p.ldkoh : nullptr);
-      if (y) {
-#pragma unroll
-        for (int c = 0; c < kC; ++c) {
-          if (ia[c] < 0) continue;
-          store<V>(y + ia[c], a[c]);
-          store<V>(y + ib[c], b[c]);
+        if (y) {
+          y[ia[c]] = from_f32<T>(a[c]);
+          y[ib[c]] = from_f32<T>(b[c]);
         }
       }
     }
     if constexpr (kCache) {
+      if (is_q) continue;
       float lo = INFINITY, hi = -INFINITY;
 #pragma unroll
       for (int c = 0; c < kC; ++c) {
         if (ia[c] < 0) continue;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          a[c][j] = to_f32(from_f32<T>(a[c][j]));  // codes are of the rounded values, whether these are stored or not
-          b[c][j] = to_f32(from_f32<T>(b[c][j]));
-          lo = min_nan(lo, min_nan(a[c][j], b[c][j]));
-          hi = max_nan(hi, max_nan(a[c][j], b[c][j]));
-        }
+        a[c] = to_f32(from_f32<T>(a[c]));  // codes are of the rounded values, whether these are stored or not
+        b[c] = to_f32(from_f32<T>(b[c]));
+        lo = min_nan(lo, min_nan(a[c], b[c]));
+        hi = max_nan(hi, max_nan(a[c], b[c]));
       }
-      for (int o = lanes >> 1; o > 0; o >>= 1) {
+      for (int o = 16; o > 0; o >>= 1) {
         lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
         hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
       }
-      const int64_t slot = live && !is_q ? p.slots[token] : -1;
-      const bool kept = in_cache(p.cache, slot);
+      const int64_t slot = p.slots[token];
+      if (!in_cache(p.cache, slot)) continue;
       const RowStep rs(lo, hi);
-      int row = 0;
-      uint8_t* blk = kept ? place(p.cache, slot, kh, row) : nullptr;
-      uint8_t* codes = kept ? blk + (is_v ? 8 * p.dim : 0) + row * (p.dim >> 1) : nullptr;
-      if (kept && lane == 0) *reinterpret_cast<uint32_t*>(blk + 16 * p.dim + (is_v ? 64 : 0) + 4 * row) = rs.word;
-      if constexpr (V > 1) {
-        if (kept && ia[0] >= 0) {
-          uint32_t wa = 0, wb = 0;
+      int row;
+      uint8_t* blk = place(p.cache, slot, kh, row);
+      if (lane == 0) *reinterpret_cast<uint32_t*>(blk + 16 * p.dim + (is_v ? 64 : 0) + 4 * row) = rs.word;
+      // codes meet their neighbours in shared memory
+      uint8_t* line = bytes + (threadIdx.x >> 5) * 256;
+      __syncwarp();
 #pragma unroll
-          for (int j = 0; j < V; ++j) {
-            wa |= rs.code(a[0][j]) << (4 * j);
-            wb |= rs.code(b[0][j]) << (4 * j);
-          }
-          if constexpr (V == 8) {
-            *reinterpret_cast<uint32_t*>(codes + (ia[0] >> 1)) = wa;
-            *reinterpret_cast<uint32_t*>(codes + (ib[0] >> 1)) = wb;
-          } else {
-            *reinterpret_cast<uint16_t*>(codes + (ia[0] >> 1)) = (uint16_t)wa;
-            *reinterpret_cast<uint16_t*>(codes + (ib[0] >> 1)) = (uint16_t)wb;
-          }
-        }
-      } else {  // a warp per row: codes meet their neighbours in shared memory
-        uint8_t* line = bytes + (threadIdx.x >> 5) * 256;
-        __syncwarp();
+      for (int c = 0; c < kC; ++c) {
+        if (ia[c] < 0) continue;
+        line[ia[c]] = (uint8_t)rs.code(a[c]);
+        line[ib[c]] = (uint8_t)rs.code(b[c]);
+      }
+      __syncwarp();
+      if (lane * 8 < p.dim) {
+        uint32_t w8 = 0;
 #pragma unroll
-        for (int c = 0; c < kC; ++c) {
-          if (ia[c] < 0) continue;
-          line[ia[c]] = (uint8_t)rs.code(a[c][0]);
-          line[ib[c]] = (uint8_t)rs.code(b[c][0]);
-        }
-        __syncwarp();
-        if (kept && lane * 8 < p.dim) {
-          uint32_t w8 = 0;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) w8 |= (uint32_t)line[lane * 8 + j] << (4 * j);
-          *reinterpret_cast<uint32_t*>(codes + 4 * lane) = w8;
-        }
+        for (int j = 0; j < 8; ++j) w8 |= (uint32_t)line[lane * 8 + j] << (4 * j);
+        *reinterpret_cast<uint32_t*>(blk + (is_v ? 8 * p.dim : 0) + row * (p.dim >> 1) + 4 * lane) = w8;
       }
     }
   }
 }
 
-// A lane per word of 8 codes; `lanes` (a power of two, at least dim / 8) to a row. Rows: [token][key or value][head].
-template <class T, bool kVec>
-__global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheReadArgs p, const int lanes, const uint64_t rows_magic) {
+// ---------------------------------------------------------------- rows at 16-byte addresses
+
+__device__ __forceinline__ uint64_t two_of(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void one_each(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// 16 bytes of a row as pairs of float32, and back
+template <class T> __device__ __forceinline__ void to_pairs(const uint4& v, uint64_t (&x)[8 / sizeof(T)]);
+template <> __device__ __forceinline__ void to_pairs<float>(const uint4& v, uint64_t (&x)[2]) {
+  x[0] = two_of(__uint_as_float(v.x), __uint_as_float(v.y));
+  x[1] = two_of(__uint_as_float(v.z), __uint_as_float(v.w));
+}
+__device__ __forceinline__ uint64_t half_pair(uint32_t w) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+  return two_of(f.x, f.y);
+}
+__device__ __forceinline__ uint64_t bfloat_pair(uint32_t w) { return two_of(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+template <> __device__ __forceinline__ void to_pairs<__half>(const uint4& v, uint64_t (&x)[4]) {
+  x[0] = half_pair(v.x); x[1] = half_pair(v.y); x[2] = half_pair(v.z); x[3] = half_pair(v.w);
+}
+template <> __device__ __forceinline__ void to_pairs<__nv_bfloat16>(const uint4& v, uint64_t (&x)[4]) {
+  x[0] = bfloat_pair(v.x); x[1] = bfloat_pair(v.y); x[2] = bfloat_pair(v.z); x[3] = bfloat_pair(v.w);
+}
+template <class T> __device__ __forceinline__ uint32_t word_of(uint64_t p);
+template <> __device__ __forceinline__ uint32_t word_of<__half>(uint64_t p) {
+  float a, b;
+  one_each(p, a, b);
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <> __device__ __forceinline__ uint32_t word_of<__nv_bfloat16>(uint64_t p) {
+  float a, b;
+  one_each(p, a, b);
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <class T>
+__device__ __forceinline__ uint4 from_pairs(const uint64_t (&x)[8 / sizeof(T)]) {
+  if constexpr (sizeof(T) == 4) {
+    float a, b, c, d;
+    one_each(x[0], a, b);
+    one_each(x[1], c, d);
+    return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+  } else {
+    return make_uint4(word_of<T>(x[0]), word_of<T>(x[1]), word_of<T>(x[2]), word_of<T>(x[3]));
+  }
+}
+
+// Lowest and highest value of a row, of which each of `lanes` lanes has two vectors; a NaN wins.
+template <class T>
+__device__ __forceinline__ void extremes(const uint4& a, const uint4& b, int lanes, bool in, float& lo, float& hi) {
+  if constexpr (sizeof(T) == 4) {
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    lo = in ? __uint_as_float(w[0]) : INFINITY;
+    hi = in ? __uint_as_float(w[0]) : -INFINITY;
+    if (in) {
+#pragma unroll
+      for (int i = 1; i < 8; ++i) {
+        lo = min_nan(lo, __uint_as_float(w[i]));
+        hi = max_nan(hi, __uint_as_float(w[i]));
+      }
+    }
+    for (int o = lanes >> 1; o > 0; o >>= 1) {
+      lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+      hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    }
+  } else {
+    using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+    auto as2 = [](uint32_t w) { return *reinterpret_cast<T2*>(&w); };
+    auto bits = [](T2 h) { return *reinterpret_cast<uint32_t*>(&h); };
+    const T2 l2 = __hmin2_nan(__hmin2_nan(__hmin2_nan(as2(a.x), as2(a.y)), __hmin2_nan(as2(a.z), as2(a.w))),
+                              __hmin2_nan(__hmin2_nan(as2(b.x), as2(b.y)), __hmin2_nan(as2(b.z), as2(b.w))));
+    const T2 h2 = __hmax2_nan(__hmax2_nan(__hmax2_nan(as2(a.x), as2(a.y)), __hmax2_nan(as2(a.z), as2(a.w))),
+                              __hmax2_nan(__hmax2_nan(as2(b.x), as2(b.y)), __hmax2_nan(as2(b.z), as2(b.w))));
+    // the lowest in the low half, the highest with its sign turned in the high half: one minimum for both
+    const uint32_t lw = bits(l2), hw = bits(h2);
+    T2 both = __hmin2_nan(as2(__byte_perm(lw, hw, 0x5410) ^ 0x80000000u), as2(__byte_perm(lw, hw, 0x7632) ^ 0x80000000u));
+    constexpr uint32_t inf = std::is_same<T, __half>::value ? 0x7c007c00u : 0x7f807f80u;
+    if (!in) both = as2(inf);
+    for (int o = lanes >> 1; o > 0; o >>= 1) both = __hmin2_nan(both, as2(__shfl_xor_sync(0xffffffffu, bits(both), o)));
+    lo = to_f32(both.x);
+    hi = -to_f32(both.y);
+  }
+}
+
+// Codes of the kN values of 16 bytes, the first in the lowest bits.
+template <class T>
+__device__ __forceinline__ uint32_t codes_of(const RowStep& rs, const uint4& v) {
+  constexpr int kPairs = 8 / sizeof(T);
+  uint64_t x[kPairs];
+  to_pairs<T>(v, x);
+  const uint64_t low = two_of(-rs.low, -rs.low), inv = two_of(rs.inv, rs.inv), magic = two_of(12582912.0f, 12582912.0f), step = two_of(-rs.step, -rs.step);
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) {
+    const uint64_t d = add2(x[i], low), q = mul2(d, inv), t = add2(fma2(fma2(q, step, d), inv, q), magic);
+    float ta, tb;
+    one_each(t, ta, tb);
+    w += __float_as_uint(ta) * (1u << (8 * i)) + __float_as_uint(tb) * (16u << (8 * i));  // (what is not the code adds up to a constant)
+  }
+  constexpr uint32_t kRest = 0x4b400000u + (0x4b400000u << 4) + (0x4b400000u << 8);
+  return rs.inv > 0.0f ? w - kRest : 0u;
+}
+
+// A warp, or several, to a token: the lanes of a row keep their places in it while the warp goes through the heads. lanes: a power of two, those past the
+// row's end idle. `share` warps (1, 2, 4 or 8) take a token's rows in turn. kPlain: keys and values to the cache as they are.
+template <class T, bool kCache, bool kInter, bool kPlain>
+__global__ void __launch_bounds__(kThreads, kPlain ? 4 : kCache ? 2 : 3) rows_kernel(const QkArgs p, const int share, const int lanes, const int lanes_log2) {
+  constexpr int V = 16 / sizeof(T), kPairs = V / 2;
+  extern __shared__ float2 turns[];  // [tokens of the block][rot / 2]: cosine, sine
   tc::grid_dep_wait();
-  const CacheGeom& g = p.cache;
-  const int lane = threadIdx.x & (lanes - 1), groups = kThreads / lanes, each = 2 * g.kv_heads;
-  const int64_t rows = p.tokens * each;
-  if (lane * 8 >= g.dim) return;
-  for (int64_t r = (int64_t)blockIdx.x * groups + threadIdx.x / lanes; r < rows; r += (int64_t)gridDim.x * groups) {
-    const int64_t token = rows < (1ll << 31) ? fast_div((int)r, rows_magic) : r / each;
-    int h = (int)(r - token * each);
-    const bool is_v = h >= g.kv_heads;
-    if (is_v) h -= g.kv_heads;
+  const int per = kThreads / 32 / share, warp = threadIdx.x >> 5, half = p.rot >> 1;
+  const int64_t t0 = (int64_t)blockIdx.x * per;
+  const int here = (int)(p.tokens - t0 < per ? p.tokens - t0 : per);
+  if constexpr (!kPlain) {
+    if (half > 0) {
+      // a thread keeps to one frequency, where there are as many threads
+      const int wide = half < kThreads ? half : kThreads, f0 = threadIdx.x % wide, step = kThreads / wide;
+      for (int f = f0; f < half; f += wide) {
+        const uint64_t rate = turn_rate(p.inv_freq[f]);
+        for (int t = threadIdx.x / wide; t < here && (int)threadIdx.x < wide * step; t += step) turns[t * half + f] = turn_of(rate, p.positions[t0 + t]);
+      }
+    }
+    __syncthreads();
+  }
+  const int t = warp / share;
+  if (t >= here) return;
+  const int64_t token = t0 + t;
+  const int lane = threadIdx.x & (lanes - 1), group = (threadIdx.x & 31) >> lanes_log2, groups = 32 >> lanes_log2;
+  const int first = (warp % share) * groups, step = share * groups;
+  // this lane's two vectors
+  const bool in = 2 * lane * V < p.dim, between = !kInter && lane * V < half;  // (pairs between the two)
+  const int ia = between ? lane * V : 2 * lane * V, ib = between ? ia + half : ia + V;
+  const bool turn_a = kInter ? ia < p.rot : between, turn_b = kInter ? ib < p.rot : between;
+  const int64_t slot = kCache ? p.slots[token] : -1;
+  const bool kept = kCache && in_cache(p.cache, slot);
+  int row = 0;
+  uint8_t* blk = kept ? place(p.cache, slot, 0, row) : nullptr;
+  const int64_t head_bytes = ((int64_t)1 << (p.cache.page_shift - 4)) * 16 * (p.cache.dim + 8);
+
+  auto to_cache = [&](int head, bool live, bool values, const uint4& a, const uint4& b) {
+    float lo, hi;
+    extremes<T>(a, b, lanes, in, lo, hi);
+    if (!kept || !live) return;
+    const RowStep rs(lo, hi);
+    uint8_t* y = blk + head * head_bytes;
+    if (lane == 0) *reinterpret_cast<uint32_t*>(y + 16 * p.dim + (values ? 64 : 0) + 4 * row) = rs.word;
+    if (!in) return;
+    y += (values ? 8 * p.dim : 0) + row * (p.dim >> 1);
+    const uint32_t wa = codes_of<T>(rs, a), wb = codes_of<T>(rs, b);
+    if constexpr (V == 8) {
+      *reinterpret_cast<uint32_t*>(y + (ia >> 1)) = wa;
+      *reinterpret_cast<uint32_t*>(y + (ib >> 1)) = wb;
+    } else {
+      *reinterpret_cast<uint16_t*>(y + (ia >> 1)) = (uint16_t)wa;
+      *reinterpret_cast<uint16_t*>(y + (ib >> 1)) = (uint16_t)wb;
+    }
+  };
+  // two rows' vectors at once: their loads are on the way together
+  auto fetch = [&](const T* x, int64_t ldh, int h, int n, uint4 (&a)[2], uint4 (&b)[2]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      a[k] = b[k] = make_uint4(0, 0, 0, 0);
+      if (in && h + k * step < n) {
+        const T* y = x + (int64_t)(h + k * step) * ldh;
+        a[k] = *reinterpret_cast<const uint4*>(y + ia);
+        b[k] = *reinterpret_cast<const uint4*>(y + ib);
+      }
+    }
+  };
+  const float per_value = 1.0f / (float)p.dim;
+  // rows of queries or keys: norm, turn, out, and keys to the cache
+  auto run = [&](const T* x, int64_t ldh, int n, const void* weight, T* y, int64_t ldyh, bool keys) {
+    // out = in * own + partner * other, and times 1 / rms at the end
+    uint64_t own_a[kPairs], own_b[kPairs], other_a[kPairs], other_b[kPairs];
+    const bool plain = kPlain || (!weight && half == 0);
+    if (!plain && in) {
+      float wa[V], wb[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) wa[j] = wb[j] = 1.0f;
+      if (weight) {
+        load_weight<V>(weight, ia, p.weight_dtype, wa);
+        load_weight<V>(weight, ib, p.weight_dtype, wb);
+      }
+      const float2* tt = turns + t * half;
+#pragma unroll
+      for (int j = 0; j < V; j += 2) {
+        float2 c0 = make_float2(1.0f, 0.0f), c1 = c0, d0 = c0, d1 = c0;
+        if constexpr (kInter) {
+          if (turn_a) c0 = c1 = tt[(ia + j) >> 1];
+          if (turn_b) d0 = d1 = tt[(ib + j) >> 1];
+          other_a[j / 2] = two_of(-wa[j + 1] * c0.y, wa[j] * c0.y);
+          other_b[j / 2] = two_of(-wb[j + 1] * d0.y, wb[j] * d0.y);
+        } else {
+          if (between) {
+            c0 = d0 = tt[ia + j];
+            c1 = d1 = tt[ia + j + 1];
+          }
+          other_a[j / 2] = two_of(-wb[j] * c0.y, -wb[j + 1] * c1.y);
+          other_b[j / 2] = two_of(wa[j] * c0.y, wa[j + 1] * c1.y);
+        }
+        own_a[j / 2] = two_of(wa[j] * c0.x, wa[j + 1] * c1.x);
+        own_b[j / 2] = two_of(wb[j] * d0.x, wb[j + 1] * d1.x);
+      }
+    }
+    for (int h0 = first; h0 < n; h0 += 2 * step) {
+      uint4 va[2], vb[2];
+      fetch(x, ldh, h0 + group, n, va, vb);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (h0 + k * step >= n) break;
+        const int h = h0 + group + k * step;
+        uint4 a = va[k], b = vb[k];
+        if (!plain) {
+          uint64_t u[kPairs], v[kPairs];
+          to_pairs<T>(a, u);
+          to_pairs<T>(b, v);
+          uint64_t f = two_of(1.0f, 1.0f);
+          if (weight) {
+            uint64_t s0 = 0, s1 = 0;
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+              s0 = fma2(u[i], u[i], s0);
+              s1 = fma2(v[i], v[i], s1);
+            }
+            float ss, s2;
+            one_each(add2(s0, s1), ss, s2);
+            ss += s2;
+            for (int o = lanes >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            const float rms = rsqrtf(fmaf(ss, per_value, p.eps));
+            f = two_of(rms, rms);
+          }
+          uint64_t ya[kPairs], yb[kPairs];
+#pragma unroll
+          for (int i = 0; i < kPairs; ++i) {
+            ya[i] = mul2(u[i], own_a[i]);
+            yb[i] = mul2(v[i], own_b[i]);
+            // (a place that does not turn has no partner, whose infinity would reach it)
+            if constexpr (kInter) {
+              float c, d;
+              one_each(u[i], c, d);
+              if (turn_a) ya[i] = fma2(two_of(d, c), other_a[i], ya[i]);
+              one_each(v[i], c, d);
+              if (turn_b) yb[i] = fma2(two_of(d, c), other_b[i], yb[i]);
+            } else if (between) {
+              ya[i] = fma2(v[i], other_a[i], ya[i]);
+              yb[i] = fma2(u[i], other_b[i], yb[i]);
+            }
+            ya[i] = mul2(ya[i], f);
+            yb[i] = mul2(yb[i], f);
+          }
+          a = from_pairs<T>(ya);
+          b = from_pairs<T>(yb);
+        }
+        if (y && in && h < n) {
+          T* z = y + (int64_t)h * ldyh;
+          *reinterpret_cast<uint4*>(z + ia) = a;
+          *reinterpret_cast<uint4*>(z + ib) = b;
+        }
+        if constexpr (kCache) {
+          if (keys) to_cache(h, h < n, false, a, b);  // codes are of the rounded values, whether these are stored or not
+        }
+      }
+    }
+  };
+  if (!kPlain && p.heads > 0) run(static_cast<const T*>(p.q) + token * p.ldq, p.ldqh, p.heads, p.q_weight, static_cast<T*>(p.q_out) + token * p.ldqo, p.ldqoh, false);
+  run(static_cast<const T*>(p.k) + token * p.ldk, p.ldkh, p.kv_heads, p.k_weight, p.k_out ? static_cast<T*>(p.k_out) + token * p.ldko : nullptr, p.ldkoh, true);
+  if constexpr (kCache) {
+    const T* x = static_cast<const T*>(p.v) + token * p.ldv;
+    for (int h0 = first; h0 < p.kv_heads; h0 += 2 * step) {
+      uint4 a[2], b[2];
+      fetch(x, p.ldvh, h0 + group, p.kv_heads, a, b);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (h0 + k * step >= p.kv_heads) break;
+        const int h = h0 + group + k * step;
+        to_cache(h, h < p.kv_heads, true, a[k], b[k]);
+      }
+    }
+  }
+}
+
+// A warp, or several, to a token, as above; a lane takes 16 codes (8 bytes) of a row, `lanes` lanes a row, keys' rows and then values'.
+template <class T, bool kVec>
+__global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheReadArgs p, const int share, const int lanes, const int lanes_log2) {
+  tc::grid_dep_wait();
+  const CacheGeom& c = p.cache;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & (lanes - 1), groups = 32 >> lanes_log2;
+  const int64_t token = ((int64_t)blockIdx.x * (kThreads / 32) + warp) / share;
+  if (token >= p.tokens || lane * 16 >= c.dim) return;
+  const int64_t slot = p.slots[token];
+  const bool kept = in_cache(c, slot);
+  int row = 0;
+  const uint8_t* blk = kept ? place(c, slot, 0, row) : nullptr;
+  const int64_t head_bytes = ((int64_t)1 << (c.page_shift - 4)) * 16 * (c.dim + 8);
+#pragma unroll 4
+  for (int r = (warp % share) * groups + ((threadIdx.x & 31) >> lanes_log2); r < 2 * c.kv_heads; r += share * groups) {
+    const bool is_v = r >= c.kv_heads;
+    const int h = is_v ? r - c.kv_heads : r;
     T* y = is_v ? static_cast<T*>(p.v) : static_cast<T*>(p.k);
     if (!y) continue;
-    y += token * (is_v ? p.ldv : p.ldk) + h * (is_v ? p.ldvh : p.ldkh) + lane * 8;
-    const int64_t slot = p.slots[token];
-    uint32_t w = 0, ls = 0;
-    if (in_cache(g, slot)) {
-      int row;
-      const uint8_t* blk = place(g, slot, h, row);
-      w = *reinterpret_cast<const uint32_t*>(blk + (is_v ? 8 * g.dim : 0) + row * (g.dim >> 1) + 4 * lane);
-      ls = *reinterpret_cast<const uint32_t*>(blk + 16 * g.dim + (is_v ? 64 : 0) + 4 * row);
+    y += token * (is_v ? p.ldv : p.ldk) + h * (is_v ? p.ldvh : p.ldkh) + lane * 16;
+    uint2 w = make_uint2(0, 0);
+    uint32_t ls = 0;
+    if (kept) {
+      const uint8_t* x = blk + h * head_bytes;
+      w = *reinterpret_cast<const uint2*>(x + (is_v ? 8 * c.dim : 0) + row * (c.dim >> 1) + 8 * lane);
+      ls = *reinterpret_cast<const uint32_t*>(x + 16 * c.dim + (is_v ? 64 : 0) + 4 * row);
     }
     const float low = __uint_as_float(ls << 16), step = __uint_as_float(ls & 0xffff0000u);
-    float f[8];
+    const uint64_t low2 = two_of(low, low), step2 = two_of(step, step), less = two_of(-8388608.0f, -8388608.0f);
+    uint64_t f[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = fmaf((float)(w >> (4 * j) & 15u), step, low);
+    for (int j = 0; j < 8; ++j) {  // (a code under the exponent of 2^23 is 2^23 + n)
+      const uint32_t u = (j < 4 ? w.x : w.y) >> (8 * (j & 3));
+      f[j] = fma2(add2(two_of(__uint_as_float((u & 15u) | 0x4b000000u), __uint_as_float((u >> 4 & 15u) | 0x4b000000u)), less), step2, low2);
+    }
     if constexpr (kVec) {
-      if constexpr (sizeof(T) == 4) {
-        const float lo4[4] = {f[0], f[1], f[2], f[3]}, hi4[4] = {f[4], f[5], f[6], f[7]};
-        store<4>(y, lo4);
-        store<4>(y + 4, hi4);
-      } else {
-        store<8>(y, f);
+      constexpr int kPairs = 8 / sizeof(T);
+#pragma unroll
+      for (int i = 0; i < 8; i += kPairs) {
+        uint64_t v[kPairs];
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) v[k] = f[i + k];
+        *reinterpret_cast<uint4*>(y + 2 * i) = from_pairs<T>(v);
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = from_f32<T>(f[j]);
+      for (int j = 0; j < 8; ++j) {
+        float a, b;
+        one_each(f[j], a, b);
+        y[2 * j] = from_f32<T>(a);
+        y[2 * j + 1] = from_f32<T>(b);
+      }
     }
   }
 }
@@ -350,28 +625,21 @@ static int pow2_at_least(int n) {
   return v;
 }
 
-template <class T, int V, int kC>
-static cudaError_t run_heads(const QkArgs& a, cudaStream_t stream) {
-  const int each = a.heads + a.kv_heads * (a.cache.data ? 2 : 1);
-  const int lanes = V == 1 ? 32 : pow2_at_least(a.dim / (2 * V)), groups = kThreads / lanes;
-  // tokens of a block: one while that leaves SMs without a block; else enough for four rows to a group of lanes, of which the table of
-  // turns takes 16 KB at most
-  int per = 1;
-  while (per * 2 * each <= 8 * groups && a.tokens / (per * 2) >= 4 * 152 && per * 2 * (a.rot / 2) * 8 <= 16384) per *= 2;
-  const int64_t blocks = (a.tokens + per - 1) / per;
-  cudaLaunchConfig_t cfg{};
+static void config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* at, int64_t blocks, size_t smem, cudaStream_t stream) {
   cfg.gridDim = dim3((unsigned)blocks);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = (size_t)per * (a.rot / 2) * sizeof(float2);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
-  cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  const uint64_t magic = div_magic(each);
-  if (a.cache.data) return cudaLaunchKernelEx(&cfg, heads_kernel<T, V, kC, true>, a, per, lanes, magic);
-  return cudaLaunchKernelEx(&cfg, heads_kernel<T, V, kC, false>, a, per, lanes, magic);
+}
+// Warps to a token: more while there are SMs to fill and rows for them. (`rows` of a warp's groups of lanes)
+static int share_of(int64_t tokens, int rows, int groups) {
+  int share = 1;
+  while (share < 8 && tokens * share < 152 * 32 && share * groups < rows) share *= 2;
+  return share;
 }
 
 template <class T>
@@ -382,27 +650,39 @@ static cudaError_t run_heads_type(const QkArgs& a, cudaStream_t stream) {
   vec = vec && on16(a.k) && (a.ldk | a.ldkh) % V == 0 && on16(a.q_weight) && on16(a.k_weight);
   if (a.k_out) vec = vec && on16(a.k_out) && (a.ldko | a.ldkoh) % V == 0;
   if (a.cache.data) vec = vec && on16(a.v) && (a.ldv | a.ldvh) % V == 0;
-  return vec ? run_heads<T, V, 1>(a, stream) : run_heads<T, 1, 8>(a, stream);
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute at[1];
+  if (vec) {
+    const int lanes = pow2_at_least(a.dim / (2 * V)), log2 = __builtin_ctz(lanes);
+    const int share = share_of(a.tokens, a.heads > a.kv_heads ? a.heads : a.kv_heads, 32 / lanes), per = kThreads / 32 / share;
+    config(cfg, at, (a.tokens + per - 1) / per, (size_t)per * (a.rot / 2) * sizeof(float2), stream);
+    if (a.cache.data && a.heads == 0 && !a.k_weight && a.rot == 0 && !a.k_out) return cudaLaunchKernelEx(&cfg, rows_kernel<T, true, false, true>, a, share, lanes, log2);
+    if (a.cache.data)
+      return a.interleaved ? cudaLaunchKernelEx(&cfg, rows_kernel<T, true, true, false>, a, share, lanes, log2)
+                           : cudaLaunchKernelEx(&cfg, rows_kernel<T, true, false, false>, a, share, lanes, log2);
+    return a.interleaved ? cudaLaunchKernelEx(&cfg, rows_kernel<T, false, true, false>, a, share, lanes, log2)
+                         : cudaLaunchKernelEx(&cfg, rows_kernel<T, false, false, false>, a, share, lanes, log2);
+  }
+  // a block's tokens: one while that leaves SMs without a block, else enough for four rows a warp
+  const int each = a.heads + a.kv_heads * (a.cache.data ? 2 : 1);
+  int per = 1;
+  while (per * 2 * each <= 32 && a.tokens / (per * 2) >= 4 * 152) per *= 2;
+  config(cfg, at, (a.tokens + per - 1) / per, (size_t)per * (a.rot / 2) * sizeof(float2), stream);
+  if (a.cache.data) return cudaLaunchKernelEx(&cfg, heads_kernel<T, true>, a, per, div_magic(each));
+  return cudaLaunchKernelEx(&cfg, heads_kernel<T, false>, a, per, div_magic(each));
 }
 
 template <class T>
 static cudaError_t run_read(const CacheReadArgs& a, cudaStream_t stream) {
   constexpr int V = 16 / sizeof(T);
   const bool vec = on16(a.k) && on16(a.v) && (a.ldk | a.ldkh | a.ldv | a.ldvh) % V == 0;
-  const int lanes = pow2_at_least(a.cache.dim / 8), groups = kThreads / lanes;
-  const int64_t rows = a.tokens * 2 * a.cache.kv_heads, blocks = (rows + groups - 1) / groups;
+  const int lanes = pow2_at_least(a.cache.dim / 16), log2 = __builtin_ctz(lanes);
+  const int share = share_of(a.tokens, 2 * a.cache.kv_heads, 32 / lanes);
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(blocks < (1 << 30) ? blocks : (1 << 30)));
-  cfg.blockDim = dim3(kThreads);
-  cfg.stream = stream;
   cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  const uint64_t magic = div_magic(2 * a.cache.kv_heads);
-  if (vec) return cudaLaunchKernelEx(&cfg, cache_read_kernel<T, true>, a, lanes, magic);
-  return cudaLaunchKernelEx(&cfg, cache_read_kernel<T, false>, a, lanes, magic);
+  config(cfg, at, (a.tokens * share + kThreads / 32 - 1) / (kThreads / 32), 0, stream);
+  if (vec) return cudaLaunchKernelEx(&cfg, cache_read_kernel<T, true>, a, share, lanes, log2);
+  return cudaLaunchKernelEx(&cfg, cache_read_kernel<T, false>, a, share, lanes, log2);
 }
 
 }  // namespace headrows
