@@ -575,20 +575,30 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheReadArg
   int row = 0;
   const uint8_t* blk = kept ? place(c, slot, 0, row) : nullptr;
   const int64_t head_bytes = ((int64_t)1 << (c.page_shift - 4)) * 16 * (c.dim + 8);
-#pragma unroll 4
-  for (int r = (warp % share) * groups + ((threadIdx.x & 31) >> lanes_log2); r < 2 * c.kv_heads; r += share * groups) {
-    const bool is_v = r >= c.kv_heads;
-    const int h = is_v ? r - c.kv_heads : r;
-    T* y = is_v ? static_cast<T*>(p.v) : static_cast<T*>(p.k);
-    if (!y) continue;
-    y += token * (is_v ? p.ldv : p.ldk) + h * (is_v ? p.ldvh : p.ldkh) + lane * 16;
-    uint2 w = make_uint2(0, 0);
-    uint32_t ls = 0;
-    if (kept) {
-      const uint8_t* x = blk + h * head_bytes;
-      w = *reinterpret_cast<const uint2*>(x + (is_v ? 8 * c.dim : 0) + row * (c.dim >> 1) + 8 * lane);
-      ls = *reinterpret_cast<const uint32_t*>(x + 16 * c.dim + (is_v ? 64 : 0) + 4 * row);
+  // four rows at a time: their loads are on the way together
+  for (int r0 = (warp % share) * groups + ((threadIdx.x & 31) >> lanes_log2); r0 < 2 * c.kv_heads; r0 += 4 * share * groups) {
+    uint2 words[4];
+    uint32_t steps[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r = r0 + k * share * groups, h = r >= c.kv_heads ? r - c.kv_heads : r;
+      words[k] = make_uint2(0, 0);
+      steps[k] = 0;
+      if (kept && r < 2 * c.kv_heads) {
+        const uint8_t* x = blk + h * head_bytes;
+        words[k] = *reinterpret_cast<const uint2*>(x + (r >= c.kv_heads ? 8 * c.dim : 0) + row * (c.dim >> 1) + 8 * lane);
+        steps[k] = *reinterpret_cast<const uint32_t*>(x + 16 * c.dim + (r >= c.kv_heads ? 64 : 0) + 4 * row);
+      }
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+    const int r = r0 + k * share * groups;
+    const bool is_v = r >= c.kv_heads;
+    T* y = is_v ? static_cast<T*>(p.v) : static_cast<T*>(p.k);
+    if (r >= 2 * c.kv_heads || !y) continue;
+    y += token * (is_v ? p.ldv : p.ldk) + (is_v ? r - c.kv_heads : r) * (is_v ? p.ldvh : p.ldkh) + lane * 16;
+    const uint2 w = words[k];
+    const uint32_t ls = steps[k];
     const float low = __uint_as_float(ls << 16), step = __uint_as_float(ls & 0xffff0000u);
     const uint64_t low2 = two_of(low, low), step2 = two_of(step, step), less = two_of(-8388608.0f, -8388608.0f);
     uint64_t f[8];
@@ -603,7 +613,7 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheReadArg
       for (int i = 0; i < 8; i += kPairs) {
         uint64_t v[kPairs];
 #pragma unroll
-        for (int k = 0; k < kPairs; ++k) v[k] = f[i + k];
+        for (int e = 0; e < kPairs; ++e) v[e] = f[i + e];
         *reinterpret_cast<uint4*>(y + 2 * i) = from_pairs<T>(v);
       }
     } else {
@@ -614,6 +624,7 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheReadArg
         y[2 * j] = from_f32<T>(a);
         y[2 * j + 1] = from_f32<T>(b);
       }
+    }
     }
   }
 }
