@@ -1,13 +1,18 @@
 // lm_prompt_tc.cu -- attention over packed prompts on the fifth-generation tensor cores, for heads of 64 and 128.
 //
-// A block takes 256 query rows of one head as two tiles of 128, and keys 128 at a time. Scores S = Q K^T and the outputs O of both tiles
+// A job is 256 query rows of one head, as two tiles of 128, and keys 128 at a time. Scores S = Q K^T and the outputs O of both tiles
 // live in TMEM; a thread per row reads its scores from there, subtracts the running maximum, takes exponentials, and writes the weights over the
 // scores as 16-bit numbers, from where they are the A operand of O += P V (V as it lies: its rows are K of that product). While one
-// tile's rows are at their exponentials, the tensor cores have the other tile's two products, so a step of both takes the longer of four
-// products of 128 x 128 x D (4 x 512 cycles for D = 128) and two passes over 128 scores a thread.
+// tile's rows are at their exponentials, the tensor cores have the other tile's two products. For heads of 128, whose outputs and scores fill TMEM, a step of
+// both takes four products of 128 x 128 x 128 (4 x 512 cycles); for heads of 64 the exponentials bound it (2 x 128 x 128 at 32 a cycle, 1024), and a third score
+// buffer has the next scores ready when a row is through.
 //
 // The outputs are brought to a new maximum only where it grew by more than a factor of 2^8 since the last time: weights stay below that, sums are
 // float32, and the division at the end is exact in it. So after the first few tiles of keys no row touches its outputs before the end.
+//
+// Blocks stay and take over the jobs of blocks that have not begun (clusterlaunchcontrol), one warp asking and looking up the sequence ahead of the
+// others: a job's first copies and scores run beside the last one's end. (With a block for each job, whose start and end cost 6 to 7 us: 13 prompts of up to
+// 2500 tokens, 28 heads of 64, 84 us.)
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -34,7 +39,10 @@ using prompt::kLog2e;
 using prompt::pack;
 
 constexpr int kTile = 128;                  // rows of a query tile, keys of a step
-constexpr int kSoftWarps = 8, kWarpTma = 8, kWarpMma = 9, kWarpFix = 10, kThreads = 384;
+constexpr int kSoftWarps = 8, kWarpTma = 8, kWarpMma = 9, kWarpFix = 10, kWarpJobs = 11, kThreads = 384;
+constexpr int kSlots = 4;                   // jobs known at a time
+constexpr int kAhead = 6;                   // steps before its end at which a job's block asks for the next one: late, so that blocks end evenly
+constexpr int kReaders = kSoftWarps + 3;    // arrivals that free a slot: each softmax warp, and the warps of copies, products and ends
 // registers: a row's 128 scores stay in its thread's
 constexpr int kRegsLaunch = 168, kRegsSoft = 200, kRegsIssue = 104;
 static_assert(kSoftWarps * kRegsSoft + 4 * kRegsIssue <= kThreads / 32 * kRegsLaunch, "the launch's registers");
@@ -44,10 +52,18 @@ constexpr float kGrowth = 8.0f;             // powers of two that a maximum may 
 __host__ __device__ constexpr int tile_bytes(int dim) { return kTile * dim * 2; }
 __host__ __device__ constexpr int ring(int dim) { return dim == 128 ? 5 : 8; }
 
-struct Barriers {
-  uint64_t q_full, full[8], empty[8], s_full[2], p_full[2], o_done[2], last_v, fixed;
-  uint64_t red[kThreads / 32];
+__host__ __device__ constexpr int bufs(int dim) { return dim == 128 ? 2 : 3; }  // score buffers
+
+struct Slot {
   Job job;
+  int32_t head, valid, n0, n1;  // n: steps of the two tiles
+};
+// Whoever waits on a barrier meets every one of its phases, and none of them runs two ahead of it: so scores have as many barriers for each tile as
+// there are buffers (they may be that many steps ahead), and a row waits for its last products before it hands its next weights over.
+struct Barriers {
+  uint64_t q_full, q_empty, full[8], empty[8], s_full[2][3], p_full[3], o_done[2], o_free[2], last_v, fixed, job_full[kSlots], job_empty[kSlots], want, answer;
+  alignas(16) uint4 response;
+  Slot slots[kSlots];
   uint32_t tmem;
   int abort_flag;
 };
@@ -119,20 +135,28 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   return r;
 }
 
-// The job's tiles of keys that query tile t sees.
+// Steps of query tile t of a job: tiles of keys that its rows see.
 __device__ __forceinline__ int steps_of(const Job& jb, int t, int causal) {
-  const int row0 = jb.tile * 2 * kTile + t * kTile;
-  const int rows = jb.queries - row0 < kTile ? jb.queries - row0 : kTile;
-  if (rows <= 0) return 0;
+  const int row0 = jb.tile * 2 * kTile + t * kTile, behind = jb.queries - row0, rows = behind < kTile ? behind : kTile;
   int64_t see = causal ? (int64_t)row0 + rows + (jb.keys - jb.queries) : jb.keys;
   see = see < 0 ? 0 : see > jb.keys ? jb.keys : see;
-  return (int)((see + kTile - 1) / kTile);
+  return rows > 0 ? (int)((see + kTile - 1) / kTile) : 0;
+}
+
+// Bounded like mbar_wait, but for as long as a job may take (64 times over), while no other role gave up.
+__device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  for (int i = 0; i < 64; ++i) {
+    if (mbar_wait_inline(bar, parity, abort_flag)) return true;
+    if (*abort_flag) return false;
+  }
+  return false;
 }
 
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ PromptArgs p) {
-  constexpr int kBytes = tile_bytes(D), kRing = ring(D), kBoxes = D / 64, kBox = kTile * 128;
-  constexpr uint32_t kO = 256;  // TMEM: scores of the tiles from columns 0 and 128 on (weights over them), outputs from 256 and 256 + D on
+  constexpr int kBytes = tile_bytes(D), kRing = ring(D), kBoxes = D / 64, kBox = kTile * 128, kBufs = bufs(D);
+  constexpr uint32_t kO = kBufs * kTile;  // TMEM: score buffers (weights over them) from column 0 on, then the outputs of both tiles
+  static_assert(kO + 2 * D <= 512, "");
   extern __shared__ __align__(1024) uint8_t smem[];  // queries of both tiles, the ring of keys and values, Barriers
   Barriers& bar = *reinterpret_cast<Barriers*>(smem + (2 + kRing) * kBytes);
   volatile int* abort_flag = &bar.abort_flag;
@@ -141,240 +165,444 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
 
   if (threadIdx.x == 0) {
     mbar_init(smem_u32(&bar.q_full), 1);
+    mbar_init(smem_u32(&bar.q_empty), 1);
     for (int i = 0; i < kRing; ++i) {
       mbar_init(smem_u32(&bar.full[i]), 1);
       mbar_init(smem_u32(&bar.empty[i]), 1);
     }
+    for (int i = 0; i < kBufs; ++i) mbar_init(smem_u32(&bar.p_full[i]), 4);
     for (int t = 0; t < 2; ++t) {
-      mbar_init(smem_u32(&bar.s_full[t]), 1);
-      mbar_init(smem_u32(&bar.p_full[t]), 4);
+      for (int i = 0; i < kBufs; ++i) mbar_init(smem_u32(&bar.s_full[t][i]), 1);
       mbar_init(smem_u32(&bar.o_done[t]), 1);
+      mbar_init(smem_u32(&bar.o_free[t]), 4);
+    }
+    for (int i = 0; i < kSlots; ++i) {
+      mbar_init(smem_u32(&bar.job_full[i]), 1);
+      mbar_init(smem_u32(&bar.job_empty[i]), kReaders);
     }
     mbar_init(smem_u32(&bar.last_v), 1);
     mbar_init(smem_u32(&bar.fixed), 1);
+    mbar_init(smem_u32(&bar.want), 1);
+    mbar_init(smem_u32(&bar.answer), 1);
     bar.abort_flag = 0;
     fence_barrier_init();
   }
-  grid_dep_wait();
-  if (!prompt::find_job(p, 2 * kTile, blockIdx.y, &bar.job, bar.red)) return;
-  const Job jb = bar.job;
   if (warp == kWarpMma) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bar.tmem)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  grid_dep_wait();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *const_cast<volatile uint32_t*>(&bar.tmem);
-  const int head = blockIdx.x, kvh = head / (p.heads / p.kv_heads);
-  const int n0 = steps_of(jb, 0, p.causal), n1 = steps_of(jb, 1, p.causal), n = n0 > n1 ? n0 : n1;
-  const int rows = jb.queries - jb.tile * 2 * kTile;  // of both tiles, and behind them
-  const bool cut = n * kTile > jb.keys;               // the last step's tile ends behind the sequence
+  const int group = p.heads / p.kv_heads;
 
   if (warp >= kSoftWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
-    if (warp == kWarpTma && elect_one() && n > 0) {
-      const uint32_t qf = smem_u32(&bar.q_full);
-      const int qrow = jb.start + jb.tile * 2 * kTile;
-      mbar_arrive_expect_tx(qf, rows > kTile ? 2 * kBytes : kBytes);
+    if (warp == kWarpJobs) {
+      // this block's own job first, then others'
+      int x = blockIdx.x, y = blockIdx.y, i = 0;
+      int seq0 = 0, base = 0, start = 0, queries = 0, tiles = 0, upto = 0;  // 32 sequences, a lane each: tiles of them, and up to the lane's end
+      auto load = [&] {
+        const int q = seq0 + lane;
+        start = queries = 0;
+        if (q < p.seqs) {
+          start = prompt::clamp_at(p.starts[q], p.tokens);
+          const int end = prompt::clamp_at(p.starts[q + 1], p.tokens);
+          queries = end > start ? end - start : 0;
+        }
+        tiles = (queries + 2 * kTile - 1) / (2 * kTile);
+        upto = tiles;
 #pragma unroll
-      for (int b = 0; b < kBoxes; ++b) tma_load_3d(sq + b * kBox, &maps.q, b * 64, head, qrow, qf);
-      if (rows > kTile) {
-#pragma unroll
-        for (int b = 0; b < kBoxes; ++b) tma_load_3d(sq + kBytes + b * kBox, &maps.q, b * 64, head, qrow + kTile, qf);
+        for (int o = 1; o < 32; o <<= 1) {
+          const int u = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += u;
+        }
+        upto += base;
+      };
+      load();
+      bool ok = true;
+      for (uint32_t asked = 0;; ++asked) {
+        // the sequence of unit y, and its tile: the last tiles of a sequence, which see the most keys, first
+        if (y < base) { seq0 = base = 0; load(); }
+        int end;
+        while (y >= (end = __shfl_sync(0xffffffffu, upto, 31)) && seq0 + 32 < p.seqs) {
+          base = end;
+          seq0 += 32;
+          load();
+        }
+        if (y < end) {
+          const int slot = i % kSlots;
+          if (!wait_long(smem_u32(&bar.job_empty[slot]), (uint32_t)(i / kSlots & 1) ^ 1, abort_flag)) ok = false;
+          if (ok && y >= upto - tiles && y < upto) {
+            const int q = seq0 + lane;
+            const int32_t* ks = p.kv_starts ? p.kv_starts : p.starts;
+            const int k0 = prompt::clamp_at(ks[q], p.kv_tokens), k1 = prompt::clamp_at(ks[q + 1], p.kv_tokens);
+            const Job jb{1, start, queries, k0, k1 > k0 ? k1 - k0 : 0, upto - 1 - y};
+            bar.slots[slot] = {jb, x, 1, steps_of(jb, 0, p.causal), steps_of(jb, 1, p.causal)};
+            mbar_arrive(smem_u32(&bar.job_full[slot]));
+          }
+          if (!ok || !wait_long(smem_u32(&bar.want), (uint32_t)i & 1, abort_flag)) { ok = false; break; }
+          ++i;
+        }
+        if (lane == 0) {
+          fence_proxy_async();  // (the last answer has been read)
+          mbar_arrive_expect_tx(smem_u32(&bar.answer), 16);
+          asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+                       ::"r"(smem_u32(&bar.response)), "r"(smem_u32(&bar.answer)) : "memory");
+        }
+        if (!mbar_wait_inline(smem_u32(&bar.answer), asked & 1, abort_flag)) {
+          int never = 0;
+          if (!mbar_wait_inline(smem_u32(&bar.answer), asked & 1, &never)) ok = false;
+        }
+        uint32_t taken, nx, ny;
+        asm volatile(
+            "{\n\t.reg .b128 r;\n\t.reg .pred p;\n\t.reg .b32 z, u;\n\t"
+            "ld.shared.b128 r, [%3];\n\t"
+            "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t"
+            "mov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\t"
+            "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, %2, z, u}, r;\n\t}"
+            : "=r"(taken), "=r"(nx), "=r"(ny) : "r"(smem_u32(&bar.response)) : "memory");
+        __syncwarp();
+        if (!taken || !ok) break;
+        x = (int)nx;
+        y = (int)ny;
       }
-      uint32_t st = 0, ph = 0;
+      const int slot = i % kSlots;
+      if (ok && !wait_long(smem_u32(&bar.job_empty[slot]), (uint32_t)(i / kSlots & 1) ^ 1, abort_flag)) ok = false;
+      if (!ok) fail(abort_flag, p.status);
+      __syncwarp();
+      if (lane == 0) {
+        bar.slots[slot].valid = 0;
+        mbar_arrive(smem_u32(&bar.job_full[slot]));
+      }
+    }
+    if (warp == kWarpTma && elect_one()) {
+      const uint32_t qf = smem_u32(&bar.q_full);
+      uint32_t st = 0, ph = 0, jobs = 0;
       int issued = 0;
-      auto load = [&](const CUtensorMap* map, int key) {
+      bool ok = true;
+      auto load = [&](const CUtensorMap* map, int head, int key) {
         if (!mbar_wait(smem_u32(&bar.empty[st]), ph ^ 1, abort_flag)) return false;
         const uint32_t full = smem_u32(&bar.full[st]);
         mbar_arrive_expect_tx(full, kBytes);
 #pragma unroll
-        for (int b = 0; b < kBoxes; ++b) tma_load_3d(ring0 + st * kBytes + b * kBox, map, b * 64, kvh, key, full);
+        for (int b = 0; b < kBoxes; ++b) tma_load_3d(ring0 + st * kBytes + b * kBox, map, b * 64, head, key, full);
         ++issued;
         if (++st == (uint32_t)kRing) { st = 0; ph ^= 1; }
         return true;
       };
-      bool ok = true;
-      for (int j = 0; ok && j < n; ++j) {
-        const int key = jb.kv_start + j * kTile;
-        ok = load(&maps.k, key) && load(&maps.v, key);
+      for (int i = 0; ok; ++i) {
+        const int slot = i % kSlots;
+        if (!wait_long(smem_u32(&bar.job_full[slot]), (uint32_t)(i / kSlots) & 1, abort_flag)) { ok = false; break; }
+        const Slot sl = bar.slots[slot];
+        mbar_arrive(smem_u32(&bar.job_empty[slot]));
+        if (!sl.valid) break;
+        const int keys = sl.n0 > sl.n1 ? sl.n0 : sl.n1;
+        if (keys == 0) continue;
+        if (!mbar_wait(smem_u32(&bar.q_empty), (jobs & 1) ^ 1, abort_flag)) { ok = false; break; }
+        ++jobs;
+        const int qrow = sl.job.start + sl.job.tile * 2 * kTile;
+        const bool two = sl.job.queries - sl.job.tile * 2 * kTile > kTile;
+        mbar_arrive_expect_tx(qf, two ? 2 * kBytes : kBytes);
+#pragma unroll
+        for (int b = 0; b < kBoxes; ++b) tma_load_3d(sq + b * kBox, &maps.q, b * 64, sl.head, qrow, qf);
+        if (two) {
+#pragma unroll
+          for (int b = 0; b < kBoxes; ++b) tma_load_3d(sq + kBytes + b * kBox, &maps.q, b * 64, sl.head, qrow + kTile, qf);
+        }
+        const int kvh = sl.head / group;
+        for (int j = 0; ok && j < keys; ++j) {
+          const int key = sl.job.kv_start + j * kTile;
+          ok = load(&maps.k, kvh, key) && load(&maps.v, kvh, key);
+        }
       }
       if (!ok) {
         fail(abort_flag, p.status);
         int never = 0;  // the copies in flight end before the block does (each of these waits is bounded too)
-        mbar_wait(qf, 0, &never);
+        if (jobs > 0) mbar_wait(qf, (jobs - 1) & 1, &never);
         for (int i = issued > kRing ? issued - kRing : 0; i < issued; ++i) mbar_wait(smem_u32(&bar.full[i % kRing]), (uint32_t)(i / kRing) & 1, &never);
       }
     }
-    if (warp == kWarpMma && elect_one() && n > 0) {
+    if (warp == kWarpMma && elect_one()) {
       constexpr uint32_t type = std::is_same<T, __half>::value ? 0u : (1u << 7) | (1u << 10);
       const uint32_t id_s = idesc_e4m3(kTile) | type, id_o = idesc_e4m3(D) | type | 1u << 16;  // (bit 16: B's rows are K)
-      auto scores = [&](int t, uint32_t k) {
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s)
-          mma_f16(tmem + t * kTile, sdesc_sw128(sq + t * kBytes + (s >> 2) * kBox + (s & 3) * 32), sdesc_sw128(k + (s >> 2) * kBox + (s & 3) * 32), id_s, s > 0);
-        mma_commit(smem_u32(&bar.s_full[t]));
-      };
-      bool ok = mbar_poll(smem_u32(&bar.q_full), 0, abort_flag) && mbar_poll(smem_u32(&bar.full[0]), 0, abort_flag);
-      if (ok) {
-        tc_fence_after();
-        if (n0 > 0) scores(0, ring0);
-        if (n1 > 0) scores(1, ring0);
-        mma_commit(smem_u32(&bar.empty[0]));
-      }
-      for (int j = 0; ok && j < n; ++j) {
-        const int iv = 2 * j + 1, ik = 2 * j + 2;  // places in the ring's order
-        const uint32_t v = ring0 + iv % kRing * kBytes, k = ring0 + ik % kRing * kBytes;
-        if (!mbar_poll(smem_u32(&bar.full[iv % kRing]), (uint32_t)(iv / kRing) & 1, abort_flag)) { ok = false; break; }
-        if (j == n - 1 && cut) {
-          mbar_arrive(smem_u32(&bar.last_v));
-          if (!mbar_poll(smem_u32(&bar.fixed), 0, abort_flag)) { ok = false; break; }
+      // Scores run up to kBufs steps ahead of the weights' products, into the next jobs where there are some: two places in the sequence of all
+      // steps. (This thread's own instructions, at about ten cycles each beside the rows' warps, could bound a step: places move by additions, descriptors
+      // by their low words.)
+      struct Cursor {
+        int slot, used;              // the next job's slot, and the parity of its use
+        int j, t, n0, n1;            // step of the job
+        uint32_t stage, phase, buf;  // of its tile of keys (or values) in the ring; its score buffer
+        __device__ __forceinline__ bool end() const { return j >= n0 && j >= n1; }
+        __device__ __forceinline__ bool first_use() const { return t == 0 || j >= n0; }  // of the tile of keys
+        __device__ __forceinline__ bool last_use() const { return t == 1 || j >= n1; }
+        __device__ __forceinline__ void advance() {
+          if (t == 0 && j < n1) {
+            t = 1;
+          } else {
+            ++j;
+            t = j < n0 ? 0 : 1;
+            stage += 2;
+            if (stage >= (uint32_t)kRing) { stage -= kRing; phase ^= 1; }
+          }
+          if (++buf == (uint32_t)kBufs) buf = 0;
         }
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const int nt = t ? n1 : n0;
-          if (j >= nt) continue;
-          if (!mbar_poll(smem_u32(&bar.p_full[t]), (uint32_t)j & 1, abort_flag)) { ok = false; break; }
-          tc_fence_after();
-#pragma unroll
-          for (int s = 0; s < kTile / 16; ++s)
-            mma_f16_ta(tmem + kO + t * D, tmem + t * kTile + s * 8, sdesc_sw128_mn(v + s * 2048, kBox), id_o, j > 0 || s > 0);
-          if (j + 1 == nt) mma_commit(smem_u32(&bar.o_done[t]));
-          if (j + 1 < nt) {
-            if (!mbar_poll(smem_u32(&bar.full[ik % kRing]), (uint32_t)(ik / kRing) & 1, abort_flag)) { ok = false; break; }
-            tc_fence_after();
-            scores(t, k);
+        __device__ __forceinline__ void take(const Slot& sl) {
+          n0 = sl.n0; n1 = sl.n1;
+          j = 0;
+          t = n0 > 0 ? 0 : 1;
+          if (++slot == kSlots) { slot = 0; used ^= 1; }
+        }
+      };
+      Cursor a{0, 0, 0, 0, 0, 0, 0, 0, 0}, c{0, 0, 0, 0, 0, 0, 1, 0, 0};
+      int ahead = 0, behind = 0;  // steps, and jobs, by which products are behind scores
+      uint32_t q_phase = 0, fix_phase = 0, p_phase = 0, s_buf[2] = {0, 0}, o_phase = 3;
+      int want = 0;
+      bool ok = true, more = true, cut = false;
+      const uint64_t dq = sdesc_sw128(sq), dk = sdesc_sw128(ring0), dv = sdesc_sw128_mn(ring0, kBox);
+      auto scores = [&] {
+        while (a.end()) {
+          const uint32_t bar_job = smem_u32(&bar.job_full[a.slot]);
+          if (!mbar_test(bar_job, a.used)) return false;  // not known yet
+          const Slot& sl = bar.slots[a.slot];
+          if (!sl.valid) {
+            more = false;
+            return false;
+          }
+          a.take(sl);
+          ++behind;
+          if (!a.end()) {
+            if (!mbar_poll(smem_u32(&bar.q_full), q_phase, abort_flag)) { ok = false; return false; }
+            q_phase ^= 1;
           }
         }
+        if (a.first_use() && !mbar_poll(smem_u32(&bar.full[a.stage]), a.phase, abort_flag)) { ok = false; return false; }
+        tc_fence_after();
+        const uint64_t q = dq + (uint32_t)a.t * (kBytes >> 4), k = dk + a.stage * (kBytes >> 4);
+        const uint32_t d = tmem + a.buf * kTile;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) mma_f16(d, q + ((s >> 2) * kBox + (s & 3) * 32 >> 4), k + ((s >> 2) * kBox + (s & 3) * 32 >> 4), id_s, s > 0);
+        const uint32_t n = a.t ? s_buf[1] : s_buf[0];
+        mma_commit(smem_u32(&bar.s_full[a.t][n]));
+        if (a.t) s_buf[1] = n + 1 == kBufs ? 0 : n + 1;
+        else s_buf[0] = n + 1 == kBufs ? 0 : n + 1;
+        if (a.last_use()) mma_commit(smem_u32(&bar.empty[a.stage]));
+        a.advance();
+        if (a.end()) mma_commit(smem_u32(&bar.q_empty));
+        ++ahead;
+        return true;
+      };
+      while (ok && more && ahead < kBufs && scores()) {}
+      while (ok) {
+        if (c.end()) {  // the next job
+          if (!wait_long(smem_u32(&bar.job_full[c.slot]), c.used, abort_flag)) { ok = false; break; }
+          const Slot& sl = bar.slots[c.slot];
+          if (!sl.valid) break;
+          const int slot = c.slot, keys = sl.n0 > sl.n1 ? sl.n0 : sl.n1;
+          cut = keys * kTile > sl.job.keys;
+          want = keys > kAhead / 2 ? keys - kAhead / 2 : 0;
+          c.take(sl);
+          --behind;
+          if (c.end() && behind < 0) {  // a job without steps: its slot may be another's by the time that scores come to it
+            a.take(sl);
+            ++behind;
+          }
+          mbar_arrive(smem_u32(&bar.job_empty[slot]));
+          if (c.end()) mbar_arrive(smem_u32(&bar.want));
+          continue;
+        }
+        if (c.j == want) {
+          mbar_arrive(smem_u32(&bar.want));
+          want = -1;
+        }
+        while (ok && ahead == 0) scores();  // (this step's own: its job is known)
+        // (a buffer is free for new scores once the products of its weights are issued: the tensor cores take them in order)
+        while (ok && more && ahead < kBufs && scores()) {}
         if (!ok) break;
-        mma_commit(smem_u32(&bar.empty[iv % kRing]));
-        if (j + 1 < n) mma_commit(smem_u32(&bar.empty[ik % kRing]));
+        if (c.first_use() && !mbar_poll(smem_u32(&bar.full[c.stage]), c.phase, abort_flag)) { ok = false; break; }
+        if (cut && c.first_use() && c.j + 1 >= c.n0 && c.j + 1 >= c.n1) {
+          mbar_arrive(smem_u32(&bar.last_v));
+          if (!mbar_poll(smem_u32(&bar.fixed), fix_phase, abort_flag)) { ok = false; break; }
+          fix_phase ^= 1;
+        }
+        if (c.j == 0) {  // the last job's outputs have been read
+          if (!mbar_poll(smem_u32(&bar.o_free[c.t]), o_phase >> c.t & 1, abort_flag)) { ok = false; break; }
+          o_phase ^= 1u << c.t;
+        }
+        if (!mbar_poll(smem_u32(&bar.p_full[c.buf]), p_phase >> c.buf & 1, abort_flag)) { ok = false; break; }
+        p_phase ^= 1u << c.buf;
+        tc_fence_after();
+        const uint64_t v = dv + c.stage * (kBytes >> 4);
+        const uint32_t o = tmem + kO + c.t * D, w = tmem + c.buf * kTile;
+#pragma unroll
+        for (int s = 0; s < kTile / 16; ++s) mma_f16_ta(o, w + s * 8, v + (s * 2048 >> 4), id_o, c.j > 0 || s > 0);
+        mma_commit(smem_u32(&bar.o_done[c.t]));
+        if (c.last_use()) mma_commit(smem_u32(&bar.empty[c.stage]));
+        c.advance();
+        --ahead;
       }
       if (!ok) fail(abort_flag, p.status);
     }
-    if (warp == kWarpFix && cut && n > 0) {
-      // the last tile's value rows behind the sequence's end are another's: 0 instead, so that weights of 0 meet no NaN
-      const int iv = 2 * (n - 1) + 1, first = jb.keys - (n - 1) * kTile;
-      if (mbar_wait(smem_u32(&bar.last_v), 0, abort_flag)) {
-        uint8_t* v = smem + (2 + iv % kRing) * kBytes;
-        for (int i = first * 8 + lane; i < kTile * 8; i += 32)
-          for (int b = 0; b < kBoxes; ++b) reinterpret_cast<uint4*>(v + b * kBox)[i] = make_uint4(0, 0, 0, 0);
+    if (warp == kWarpFix) {
+      uint32_t ring_at = 0, ends = 0;
+      for (int i = 0;; ++i) {
+        const int slot = i % kSlots;
+        if (!wait_long(smem_u32(&bar.job_full[slot]), (uint32_t)(i / kSlots) & 1, abort_flag)) break;
+        const Slot sl = bar.slots[slot];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bar.job_empty[slot]));
+        if (!sl.valid) break;
+        const int keys = sl.n0 > sl.n1 ? sl.n0 : sl.n1;
+        ring_at += 2 * keys;
+        if (keys * kTile <= sl.job.keys) continue;
+        // the last tile's value rows behind the sequence's end are another's: 0 instead, so that weights of 0 meet no NaN
+        if (!wait_long(smem_u32(&bar.last_v), ends & 1, abort_flag)) break;
+        ++ends;
+        uint8_t* v = smem + (2 + (ring_at - 1) % kRing) * kBytes;
+        for (int r = (sl.job.keys - (keys - 1) * kTile) * 8 + lane; r < kTile * 8; r += 32)
+          for (int b = 0; b < kBoxes; ++b) reinterpret_cast<uint4*>(v + b * kBox)[r] = make_uint4(0, 0, 0, 0);
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bar.fixed));
-      } else {
-        fail(abort_flag, p.status);
       }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
     const int t = warp >> 2, row = (warp & 3) * 32 + lane;  // (a warp reads the quarter of TMEM's lanes that its number gives)
-    const int nt = t ? n1 : n0, at = jb.tile * 2 * kTile + t * kTile + row;  // this thread's row of the sequence
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tmem + t * kTile + lanes, to = tmem + kO + t * D + lanes;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, to = tmem + kO + t * D + lanes;
     const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f), grow = kGrowth / c2;
-    int64_t see = p.causal ? (int64_t)at + (jb.keys - jb.queries) + 1 : jb.keys;
-    const int lim = (int)(see < 0 ? 0 : see > jb.keys ? jb.keys : see);
-    float m = -INFINITY, l = 0.0f;
+    uint32_t first = 0, sums = 0;  // steps of all jobs so far, and this tile's
     bool ok = true;
-    for (int j = 0; j < nt; ++j) {
-      if (!mbar_wait_inline(smem_u32(&bar.s_full[t]), (uint32_t)j & 1, abort_flag)) { ok = false; break; }
-      tc_fence_after();
-      float s[kTile];
+    for (int i = 0; ok; ++i) {
+      const int slot = i % kSlots;
+      if (!wait_long(smem_u32(&bar.job_full[slot]), (uint32_t)(i / kSlots) & 1, abort_flag)) { ok = false; break; }
+      const Job jb = bar.slots[slot].job;
+      const int head = bar.slots[slot].head, valid = bar.slots[slot].valid, n0 = bar.slots[slot].n0, n1 = bar.slots[slot].n1;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bar.job_empty[slot]));
+      if (!valid) break;
+      // both tiles' steps in turn while both have one, then the rest of the longer one's
+      const int nt = t ? n1 : n0, both = n0 < n1 ? n0 : n1, at = jb.tile * 2 * kTile + t * kTile + row;  // this thread's row of the sequence
+      int64_t see = p.causal ? (int64_t)at + (jb.keys - jb.queries) + 1 : jb.keys;
+      const int lim = (int)(see < 0 ? 0 : see > jb.keys ? jb.keys : see);
+      float m = -INFINITY, l = 0.0f;
+      for (int j = 0; j < nt; ++j) {
+        const uint32_t place = first + (j < both ? 2 * j + t : j + both), buf = place % kBufs, ts = tmem + buf * kTile + lanes;
+        const uint32_t mine = sums + j;  // this tile's steps
+        bool last_done = j == 0;         // whether the last step's products are known to be done
+        if (!mbar_wait_inline(smem_u32(&bar.s_full[t][mine % kBufs]), mine / kBufs & 1, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        float s[kTile];
 #pragma unroll
-      for (int i = 0; i < kTile; i += 32) tmem_ld32(ts + i, s + i);
-      tmem_wait_ld();
+        for (int i2 = 0; i2 < kTile; i2 += 32) tmem_ld32(ts + i2, s + i2);
+        tmem_wait_ld();
 #pragma unroll
-      for (int i = 0; i < kTile; i += 32) settle(s + i);
-      const int here = lim - j * kTile;  // places of this tile that the row sees
-      if (__any_sync(0xffffffffu, here < kTile)) {
+        for (int i2 = 0; i2 < kTile; i2 += 32) settle(s + i2);
+        const int here = lim - j * kTile;  // places of this tile that the row sees
+        if (__any_sync(0xffffffffu, here < kTile)) {
 #pragma unroll
-        for (int i = 0; i < kTile; ++i)
-          if (i >= here) s[i] = -INFINITY;
-      }
-      float a[4] = {s[0], s[1], s[2], s[3]};
+          for (int i2 = 0; i2 < kTile; ++i2)
+            if (i2 >= here) s[i2] = -INFINITY;
+        }
+        float a[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-      for (int i = 4; i < kTile; i += 4)
+        for (int i2 = 4; i2 < kTile; i2 += 4)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) a[c] = fmaxf(a[c], s[i + c]);
-      const float top = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
-      const bool grew = top > m + grow;  // (from -infinity: any score)
-      if (__any_sync(0xffffffffu, grew)) {
-        const float f = grew ? ex2((m - top) * c2) : 1.0f;
-        if (grew) m = top;
-        l *= f;
-        if (j > 0) {
-          // (the last step's products are done: this step's scores were issued behind them and have arrived)
+          for (int c = 0; c < 4; ++c) a[c] = fmaxf(a[c], s[i2 + c]);
+        const float top = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
+        const bool grew = top > m + grow;  // (from -infinity: any score)
+        if (__any_sync(0xffffffffu, grew)) {
+          const float f = grew ? ex2((m - top) * c2) : 1.0f;
+          if (grew) m = top;
+          l *= f;
+          if (j > 0) {
+            if (!mbar_wait_inline(smem_u32(&bar.o_done[t]), mine - 1 & 1, abort_flag)) { ok = false; break; }
+            last_done = true;
+            tc_fence_after();
 #pragma unroll
-          for (int i = 0; i < D; i += 16) {
-            uint32_t o[16];
-            tmem_ld16(to + i, o);
-            tmem_wait_ld();
-            reg_fence16(o);
+            for (int i2 = 0; i2 < D; i2 += 16) {
+              uint32_t o[16];
+              tmem_ld16(to + i2, o);
+              tmem_wait_ld();
+              reg_fence16(o);
 #pragma unroll
-            for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
-            tmem_st16(to + i, o);
+              for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
+              tmem_st16(to + i2, o);
+            }
           }
         }
-      }
-      float ref = m == -INFINITY ? 0.0f : m;
-      // the factor goes into one multiply-add with the maximum, but where scores are so large that its rounding shows
-      if (__any_sync(0xffffffffu, fabsf(ref * c2) > 1e5f)) {
+        float ref = m == -INFINITY ? 0.0f : m;
+        // the factor goes into one multiply-add with the maximum, but where scores are so large that its rounding shows
+        if (__any_sync(0xffffffffu, fabsf(ref * c2) > 1e5f)) {
 #pragma unroll
-        for (int i = 0; i < kTile; ++i) s[i] -= ref;
-        ref = 0.0f;
-      }
-      const uint64_t c22 = two_of(c2, c2), r22 = two_of(-ref * c2, -ref * c2);
-      uint64_t sum[2] = {0, 0};
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        uint32_t w[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float x, y;
-          one_each(fma2(two_of(s[32 * h + 2 * i], s[32 * h + 2 * i + 1]), c22, r22), x, y);
-          x = ex2(x);
-          y = ex2(y);
-          sum[i & 1] = add2(sum[i & 1], two_of(x, y));
-          w[i] = pack(x, y, (T*)nullptr);
+          for (int i2 = 0; i2 < kTile; ++i2) s[i2] -= ref;
+          ref = 0.0f;
         }
-        tmem_st16(ts + 16 * h, w);
+        const uint64_t c22 = two_of(c2, c2), r22 = two_of(-ref * c2, -ref * c2);
+        uint64_t sum[2] = {0, 0};
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          uint32_t w[16];
+#pragma unroll
+          for (int i2 = 0; i2 < 16; ++i2) {
+            float x, y;
+            one_each(fma2(two_of(s[32 * h + 2 * i2], s[32 * h + 2 * i2 + 1]), c22, r22), x, y);
+            x = ex2(x);
+            y = ex2(y);
+            sum[i2 & 1] = add2(sum[i2 & 1], two_of(x, y));
+            w[i2] = pack(x, y, (T*)nullptr);
+          }
+          tmem_st16(ts + 16 * h, w);
+        }
+        float u, v;
+        one_each(add2(sum[0], sum[1]), u, v);
+        l += u + v;
+        tmem_wait_st();
+        if (!last_done && !mbar_wait_inline(smem_u32(&bar.o_done[t]), mine - 1 & 1, abort_flag)) { ok = false; break; }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bar.p_full[buf]));
       }
-      float u, v;
-      one_each(add2(sum[0], sum[1]), u, v);
-      l += u + v;
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bar.p_full[t]));
+      if (ok && nt > 0 && !mbar_wait_inline(smem_u32(&bar.o_done[t]), sums + nt - 1 & 1, abort_flag)) ok = false;
+      if (!ok) break;
+      first += n0 + n1;
+      sums += nt;
+      tc_fence_after();
+      const int behind = jb.queries - jb.tile * 2 * kTile - t * kTile;
+      const bool live = row < behind;
+      const float inv = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
+      T* y = static_cast<T*>(p.out) + (int64_t)(jb.start + at) * p.ldo + (int64_t)head * p.ldoh;
+      if (behind > 0) {
+#pragma unroll
+        for (int i2 = 0; i2 < D; i2 += 32) {
+          float o[32];
+          if (nt > 0) {
+            tmem_ld32(to + i2, o);
+            tmem_wait_ld();
+            settle(o);
+          } else {
+#pragma unroll
+            for (int c = 0; c < 32; ++c) o[c] = 0.0f;
+          }
+          if (i2 + 32 == D && nt > 0) {  // read: the next job's products may come
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bar.o_free[t]));
+          }
+          if (live) {
+#pragma unroll
+            for (int c = 0; c < 32; c += 8)
+              *reinterpret_cast<uint4*>(y + i2 + c) = make_uint4(pack(o[c] * inv, o[c + 1] * inv, (T*)nullptr), pack(o[c + 2] * inv, o[c + 3] * inv, (T*)nullptr),
+                                                                 pack(o[c + 4] * inv, o[c + 5] * inv, (T*)nullptr), pack(o[c + 6] * inv, o[c + 7] * inv, (T*)nullptr));
+          }
+        }
+        if (live && p.lse) p.lse[(int64_t)(jb.start + at) * p.heads + head] = fmaf(m, c2, log2f(l)) * kLn2;
+      }
     }
-    if (ok && nt > 0 && !mbar_wait_inline(smem_u32(&bar.o_done[t]), 0, abort_flag)) ok = false;
     if (!ok) fail(abort_flag, p.status);
-    tc_fence_after();
-    const bool live = t * kTile + row < rows;
-    const float inv = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
-    T* y = static_cast<T*>(p.out) + (int64_t)(jb.start + at) * p.ldo + (int64_t)head * p.ldoh;
-    if (t * kTile < rows) {
-#pragma unroll
-      for (int i = 0; i < D; i += 32) {
-        float o[32];
-        if (nt > 0) {
-          tmem_ld32(to + i, o);
-          tmem_wait_ld();
-          settle(o);
-        } else {
-#pragma unroll
-          for (int c = 0; c < 32; ++c) o[c] = 0.0f;
-        }
-        if (live && ok) {
-#pragma unroll
-          for (int c = 0; c < 32; c += 8)
-            *reinterpret_cast<uint4*>(y + i + c) = make_uint4(pack(o[c] * inv, o[c + 1] * inv, (T*)nullptr), pack(o[c + 2] * inv, o[c + 3] * inv, (T*)nullptr),
-                                                              pack(o[c + 4] * inv, o[c + 5] * inv, (T*)nullptr), pack(o[c + 6] * inv, o[c + 7] * inv, (T*)nullptr));
-        }
-      }
-      if (live && ok && p.lse) p.lse[(int64_t)(jb.start + at) * p.heads + head] = fmaf(m, c2, log2f(l)) * kLn2;
-    }
     tc_fence_before();
   }
   __syncthreads();
