@@ -3,9 +3,9 @@
 // A job is 256 query rows of one head, as two tiles of 128, and keys 128 at a time. Scores S = Q K^T and the outputs O of both tiles
 // live in TMEM; a thread per row reads its scores from there, subtracts the running maximum, takes exponentials, and writes the weights over the
 // scores as 16-bit numbers, from where they are the A operand of O += P V (V as it lies: its rows are K of that product). While one
-// tile's rows are at their exponentials, the tensor cores have the other tile's two products. For heads of 128, whose outputs and scores fill TMEM, a step of
-// both takes four products of 128 x 128 x 128 (4 x 512 cycles); for heads of 64 the exponentials bound it (2 x 128 x 128 at 32 a cycle, 1024), and a third score
-// buffer has the next scores ready when a row is through.
+// tile's rows are at their exponentials, the tensor cores have the other tile's two products. For heads of 128 a step of
+// both takes four products of 128 x 128 x 128 (4 x 512 cycles); for heads of 64 the exponentials bound it (2 x 128 x 128 at 32 a cycle, 1024). (A third score
+// buffer there, which has the next scores ready when a row is through, gave nothing.)
 //
 // The outputs are brought to a new maximum only where it grew by more than a factor of 2^8 since the last time: weights stay below that, sums are
 // float32, and the division at the end is exact in it. So after the first few tiles of keys no row touches its outputs before the end.
@@ -40,8 +40,8 @@ using prompt::pack;
 
 constexpr int kTile = 128;                  // rows of a query tile, keys of a step
 constexpr int kSoftWarps = 8, kWarpTma = 8, kWarpMma = 9, kWarpFix = 10, kWarpJobs = 11, kThreads = 384;
-constexpr int kSlots = 4;                   // jobs known at a time
-constexpr int kAhead = 6;                   // steps before its end at which a job's block asks for the next one: late, so that blocks end evenly
+constexpr int kSlots = 3;                   // jobs known at a time
+constexpr int kAhead = 3;                   // tiles of keys before its end at which a job's block asks for the next one: late, so that blocks end evenly
 constexpr int kReaders = kSoftWarps + 3;    // arrivals that free a slot: each softmax warp, and the warps of copies, products and ends
 // registers: a row's 128 scores stay in its thread's
 constexpr int kRegsLaunch = 168, kRegsSoft = 200, kRegsIssue = 104;
@@ -52,16 +52,13 @@ constexpr float kGrowth = 8.0f;             // powers of two that a maximum may 
 __host__ __device__ constexpr int tile_bytes(int dim) { return kTile * dim * 2; }
 __host__ __device__ constexpr int ring(int dim) { return dim == 128 ? 5 : 8; }
 
-__host__ __device__ constexpr int bufs(int dim) { return dim == 128 ? 2 : 3; }  // score buffers
-
 struct Slot {
   Job job;
   int32_t head, valid, n0, n1;  // n: steps of the two tiles
 };
-// Whoever waits on a barrier meets every one of its phases, and none of them runs two ahead of it: so scores have as many barriers for each tile as
-// there are buffers (they may be that many steps ahead), and a row waits for its last products before it hands its next weights over.
+// Whoever waits on a barrier meets every one of its phases, and none of them runs two ahead of it.
 struct Barriers {
-  uint64_t q_full, q_empty, full[8], empty[8], s_full[2][3], p_full[3], o_done[2], o_free[2], last_v, fixed, job_full[kSlots], job_empty[kSlots], want, answer;
+  uint64_t q_full[2], q_empty[2], full[8], empty[8], s_full[2], p_full[2], o_done[2], o_free[2], last_v, fixed, job_full[kSlots], job_empty[kSlots], want, answer;
   alignas(16) uint4 response;
   Slot slots[kSlots];
   uint32_t tmem;
@@ -77,23 +74,27 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
       " [%0], [%1, {%2, %3, %4}], [%5];"
       ::"r"(dst), "l"((uint64_t)map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
-// D (+)= A B with A in TMEM (a lane per row, two 16-bit numbers a column)
-__device__ __forceinline__ void mma_f16_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+// Shared-memory descriptors, 128-byte swizzle: the upper word is the same for all here (1024 bytes from 8 rows to the next, version 1, the swizzle), the
+// lower one has the address and the leading offset: of operands whose rows are M or N (K adjacent), unused; of the one whose rows are K, blocks of 64 columns x 8
+// rows, the bytes from 64 columns to the next.
+constexpr uint32_t kDescHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t desc_low(uint32_t saddr, uint32_t leading) { return (saddr & 0x3FFFFu) >> 4 | (leading >> 4) << 16; }
+// D (+)= A B, both in shared memory; and with A in TMEM (a lane per row, two 16-bit numbers a column)
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+      "mov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "n"(kDescHigh) : "memory");
 }
-// 128-byte-swizzled descriptor of an operand whose rows are K: blocks of 64 columns x 8 rows of K, 1024 bytes from 8 rows to the next (stride offset),
-// `block` bytes from 64 columns to the next (leading offset)
-__device__ __forceinline__ uint64_t sdesc_sw128_mn(uint32_t saddr, uint32_t block) {
-  uint64_t d = (uint64_t)((saddr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)(block >> 4) << 16;
-  d |= (uint64_t)(1024 >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "mov.b64 y, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "n"(kDescHigh) : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* f) {
   uint32_t r[32];
@@ -152,11 +153,22 @@ __device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity, volatil
   return false;
 }
 
+// The same for warps that wait most of a job: asleep in between, since a warp that keeps asking takes issue slots from the rows' warps beside it
+// (8192 tokens, 32 heads of 64: 3% with two such warps asking).
+__device__ __forceinline__ bool wait_asleep(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (mbar_test(bar, parity)) return true;
+  const uint64_t deadline = globaltimer() + 64 * kTimeoutNs;
+  for (;;) {
+    __nanosleep(256);
+    if (mbar_test(bar, parity)) return true;
+    if (*abort_flag || globaltimer() > deadline) return false;
+  }
+}
+
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ PromptArgs p) {
-  constexpr int kBytes = tile_bytes(D), kRing = ring(D), kBoxes = D / 64, kBox = kTile * 128, kBufs = bufs(D);
-  constexpr uint32_t kO = kBufs * kTile;  // TMEM: score buffers (weights over them) from column 0 on, then the outputs of both tiles
-  static_assert(kO + 2 * D <= 512, "");
+  constexpr int kBytes = tile_bytes(D), kRing = ring(D), kBoxes = D / 64, kBox = kTile * 128;
+  constexpr uint32_t kO = 2 * kTile;  // TMEM: scores of the tiles from columns 0 and 128 on (weights over them), then their outputs
   extern __shared__ __align__(1024) uint8_t smem[];  // queries of both tiles, the ring of keys and values, Barriers
   Barriers& bar = *reinterpret_cast<Barriers*>(smem + (2 + kRing) * kBytes);
   volatile int* abort_flag = &bar.abort_flag;
@@ -164,15 +176,15 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
   const uint32_t sq = smem_u32(smem), ring0 = sq + 2 * kBytes;
 
   if (threadIdx.x == 0) {
-    mbar_init(smem_u32(&bar.q_full), 1);
-    mbar_init(smem_u32(&bar.q_empty), 1);
     for (int i = 0; i < kRing; ++i) {
       mbar_init(smem_u32(&bar.full[i]), 1);
       mbar_init(smem_u32(&bar.empty[i]), 1);
     }
-    for (int i = 0; i < kBufs; ++i) mbar_init(smem_u32(&bar.p_full[i]), 4);
     for (int t = 0; t < 2; ++t) {
-      for (int i = 0; i < kBufs; ++i) mbar_init(smem_u32(&bar.s_full[t][i]), 1);
+      mbar_init(smem_u32(&bar.q_full[t]), 1);
+      mbar_init(smem_u32(&bar.q_empty[t]), 1);
+      mbar_init(smem_u32(&bar.s_full[t]), 1);
+      mbar_init(smem_u32(&bar.p_full[t]), 4);
       mbar_init(smem_u32(&bar.o_done[t]), 1);
       mbar_init(smem_u32(&bar.o_free[t]), 4);
     }
@@ -234,7 +246,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
         }
         if (y < end) {
           const int slot = i % kSlots;
-          if (!wait_long(smem_u32(&bar.job_empty[slot]), (uint32_t)(i / kSlots & 1) ^ 1, abort_flag)) ok = false;
+          if (!wait_asleep(smem_u32(&bar.job_empty[slot]), (uint32_t)(i / kSlots & 1) ^ 1, abort_flag)) ok = false;
           if (ok && y >= upto - tiles && y < upto) {
             const int q = seq0 + lane;
             const int32_t* ks = p.kv_starts ? p.kv_starts : p.starts;
@@ -243,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
             bar.slots[slot] = {jb, x, 1, steps_of(jb, 0, p.causal), steps_of(jb, 1, p.causal)};
             mbar_arrive(smem_u32(&bar.job_full[slot]));
           }
-          if (!ok || !wait_long(smem_u32(&bar.want), (uint32_t)i & 1, abort_flag)) { ok = false; break; }
+          if (!ok || !wait_asleep(smem_u32(&bar.want), (uint32_t)i & 1, abort_flag)) { ok = false; break; }
           ++i;
         }
         if (lane == 0) {
@@ -271,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
         y = (int)ny;
       }
       const int slot = i % kSlots;
-      if (ok && !wait_long(smem_u32(&bar.job_empty[slot]), (uint32_t)(i / kSlots & 1) ^ 1, abort_flag)) ok = false;
+      if (ok && !wait_asleep(smem_u32(&bar.job_empty[slot]), (uint32_t)(i / kSlots & 1) ^ 1, abort_flag)) ok = false;
       if (!ok) fail(abort_flag, p.status);
       __syncwarp();
       if (lane == 0) {
@@ -280,9 +292,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
       }
     }
     if (warp == kWarpTma && elect_one()) {
-      const uint32_t qf = smem_u32(&bar.q_full);
-      uint32_t st = 0, ph = 0, jobs = 0;
-      int issued = 0;
+      uint32_t st = 0, ph = 0, q_phase = 3;  // (q_phase: a bit for each tile, the parity that its next wait has)
+      int issued = 0, q_issued[2] = {0, 0};
       bool ok = true;
       auto load = [&](const CUtensorMap* map, int head, int key) {
         if (!mbar_wait(smem_u32(&bar.empty[st]), ph ^ 1, abort_flag)) return false;
@@ -296,153 +307,138 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
       };
       for (int i = 0; ok; ++i) {
         const int slot = i % kSlots;
-        if (!wait_long(smem_u32(&bar.job_full[slot]), (uint32_t)(i / kSlots) & 1, abort_flag)) { ok = false; break; }
+        if (!wait_asleep(smem_u32(&bar.job_full[slot]), (uint32_t)(i / kSlots) & 1, abort_flag)) { ok = false; break; }
         const Slot sl = bar.slots[slot];
         mbar_arrive(smem_u32(&bar.job_empty[slot]));
         if (!sl.valid) break;
-        const int keys = sl.n0 > sl.n1 ? sl.n0 : sl.n1;
-        if (keys == 0) continue;
-        if (!mbar_wait(smem_u32(&bar.q_empty), (jobs & 1) ^ 1, abort_flag)) { ok = false; break; }
-        ++jobs;
-        const int qrow = sl.job.start + sl.job.tile * 2 * kTile;
-        const bool two = sl.job.queries - sl.job.tile * 2 * kTile > kTile;
-        mbar_arrive_expect_tx(qf, two ? 2 * kBytes : kBytes);
+        const int keys = sl.n0 > sl.n1 ? sl.n0 : sl.n1, kvh = sl.head / group;
+        // queries of tile 0, the first keys, queries of tile 1: in the order in which their places come free
 #pragma unroll
-        for (int b = 0; b < kBoxes; ++b) tma_load_3d(sq + b * kBox, &maps.q, b * 64, sl.head, qrow, qf);
-        if (two) {
+        for (int t = 0; t < 2; ++t) {
+          if (ok && (t ? sl.n1 : sl.n0) > 0) {
+            const uint32_t qf = smem_u32(&bar.q_full[t]);
+            if (!mbar_wait(smem_u32(&bar.q_empty[t]), q_phase >> t & 1, abort_flag)) { ok = false; break; }
+            q_phase ^= 1u << t;
+            ++q_issued[t];
+            mbar_arrive_expect_tx(qf, kBytes);
 #pragma unroll
-          for (int b = 0; b < kBoxes; ++b) tma_load_3d(sq + kBytes + b * kBox, &maps.q, b * 64, sl.head, qrow + kTile, qf);
+            for (int b = 0; b < kBoxes; ++b) tma_load_3d(sq + t * kBytes + b * kBox, &maps.q, b * 64, sl.head, sl.job.start + (sl.job.tile * 2 + t) * kTile, qf);
+          }
+          if (t == 0 && ok && keys > 0) ok = load(&maps.k, kvh, sl.job.kv_start);
         }
-        const int kvh = sl.head / group;
         for (int j = 0; ok && j < keys; ++j) {
           const int key = sl.job.kv_start + j * kTile;
-          ok = load(&maps.k, kvh, key) && load(&maps.v, kvh, key);
+          ok = (j == 0 || load(&maps.k, kvh, key)) && load(&maps.v, kvh, key);
         }
       }
+      // the last arrivals at these barriers come before the block ends
+      for (int t = 0; ok && t < 2; ++t)
+        if (q_issued[t] > 0) ok = mbar_wait(smem_u32(&bar.q_empty[t]), q_phase >> t & 1, abort_flag);
+      for (int i = issued > kRing ? issued - kRing : 0; ok && i < issued; ++i) ok = mbar_wait(smem_u32(&bar.empty[i % kRing]), (uint32_t)(i / kRing) & 1, abort_flag);
       if (!ok) {
         fail(abort_flag, p.status);
         int never = 0;  // the copies in flight end before the block does (each of these waits is bounded too)
-        if (jobs > 0) mbar_wait(qf, (jobs - 1) & 1, &never);
+        for (int t = 0; t < 2; ++t)
+          if (q_issued[t] > 0) mbar_wait(smem_u32(&bar.q_full[t]), (uint32_t)(q_issued[t] - 1) & 1, &never);
         for (int i = issued > kRing ? issued - kRing : 0; i < issued; ++i) mbar_wait(smem_u32(&bar.full[i % kRing]), (uint32_t)(i / kRing) & 1, &never);
       }
     }
     if (warp == kWarpMma && elect_one()) {
       constexpr uint32_t type = std::is_same<T, __half>::value ? 0u : (1u << 7) | (1u << 10);
       const uint32_t id_s = idesc_e4m3(kTile) | type, id_o = idesc_e4m3(D) | type | 1u << 16;  // (bit 16: B's rows are K)
-      // Scores run up to kBufs steps ahead of the weights' products, into the next jobs where there are some: two places in the sequence of all
-      // steps. (This thread's own instructions, at about ten cycles each beside the rows' warps, could bound a step: places move by additions, descriptors
-      // by their low words.)
-      struct Cursor {
-        int slot, used;              // the next job's slot, and the parity of its use
-        int j, t, n0, n1;            // step of the job
-        uint32_t stage, phase, buf;  // of its tile of keys (or values) in the ring; its score buffer
-        __device__ __forceinline__ bool end() const { return j >= n0 && j >= n1; }
-        __device__ __forceinline__ bool first_use() const { return t == 0 || j >= n0; }  // of the tile of keys
-        __device__ __forceinline__ bool last_use() const { return t == 1 || j >= n1; }
-        __device__ __forceinline__ void advance() {
-          if (t == 0 && j < n1) {
-            t = 1;
-          } else {
-            ++j;
-            t = j < n0 ? 0 : 1;
-            stage += 2;
-            if (stage >= (uint32_t)kRing) { stage -= kRing; phase ^= 1; }
-          }
-          if (++buf == (uint32_t)kBufs) buf = 0;
-        }
-        __device__ __forceinline__ void take(const Slot& sl) {
-          n0 = sl.n0; n1 = sl.n1;
-          j = 0;
-          t = n0 > 0 ? 0 : 1;
-          if (++slot == kSlots) { slot = 0; used ^= 1; }
-        }
-      };
-      Cursor a{0, 0, 0, 0, 0, 0, 0, 0, 0}, c{0, 0, 0, 0, 0, 0, 1, 0, 0};
-      int ahead = 0, behind = 0;  // steps, and jobs, by which products are behind scores
-      uint32_t q_phase = 0, fix_phase = 0, p_phase = 0, s_buf[2] = {0, 0}, o_phase = 3;
-      int want = 0;
-      bool ok = true, more = true, cut = false;
-      const uint64_t dq = sdesc_sw128(sq), dk = sdesc_sw128(ring0), dv = sdesc_sw128_mn(ring0, kBox);
-      auto scores = [&] {
-        while (a.end()) {
-          const uint32_t bar_job = smem_u32(&bar.job_full[a.slot]);
-          if (!mbar_test(bar_job, a.used)) return false;  // not known yet
-          const Slot& sl = bar.slots[a.slot];
-          if (!sl.valid) {
-            more = false;
-            return false;
-          }
-          a.take(sl);
-          ++behind;
-          if (!a.end()) {
-            if (!mbar_poll(smem_u32(&bar.q_full), q_phase, abort_flag)) { ok = false; return false; }
-            q_phase ^= 1;
-          }
-        }
-        if (a.first_use() && !mbar_poll(smem_u32(&bar.full[a.stage]), a.phase, abort_flag)) { ok = false; return false; }
-        tc_fence_after();
-        const uint64_t q = dq + (uint32_t)a.t * (kBytes >> 4), k = dk + a.stage * (kBytes >> 4);
-        const uint32_t d = tmem + a.buf * kTile;
+      // (This thread's own instructions, at about ten cycles each beside the rows' warps, could bound a step: descriptors move by their low words, places in the
+      // ring by additions.)
+      const uint32_t dq = desc_low(sq, 16), dk = desc_low(ring0, 16), dv = desc_low(ring0, kBox);
+      int slot = 0;
+      uint32_t used = 0, ks = 0, kp = 0, vs = 1, vp = 0;  // the job's slot and its use; the next tiles of keys and of values in the ring
+      uint32_t q_phase = 0, o_phase = 3, p_phase = 0, fix_phase = 0;
+      bool ok = true, begun[2] = {false, false};
+      auto scores = [&](int t, uint32_t stage) {
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) mma_f16(d, q + ((s >> 2) * kBox + (s & 3) * 32 >> 4), k + ((s >> 2) * kBox + (s & 3) * 32 >> 4), id_s, s > 0);
-        const uint32_t n = a.t ? s_buf[1] : s_buf[0];
-        mma_commit(smem_u32(&bar.s_full[a.t][n]));
-        if (a.t) s_buf[1] = n + 1 == kBufs ? 0 : n + 1;
-        else s_buf[0] = n + 1 == kBufs ? 0 : n + 1;
-        if (a.last_use()) mma_commit(smem_u32(&bar.empty[a.stage]));
-        a.advance();
-        if (a.end()) mma_commit(smem_u32(&bar.q_empty));
-        ++ahead;
-        return true;
+        for (int s = 0; s < D / 16; ++s) {
+          const uint32_t at = ((s >> 2) * kBox + (s & 3) * 32) >> 4;
+          mma_ss(tmem + t * kTile, dq + t * (kBytes >> 4) + at, dk + stage * (kBytes >> 4) + at, id_s, s > 0);
+        }
+        mma_commit(smem_u32(&bar.s_full[t]));
       };
-      while (ok && more && ahead < kBufs && scores()) {}
       while (ok) {
-        if (c.end()) {  // the next job
-          if (!wait_long(smem_u32(&bar.job_full[c.slot]), c.used, abort_flag)) { ok = false; break; }
-          const Slot& sl = bar.slots[c.slot];
-          if (!sl.valid) break;
-          const int slot = c.slot, keys = sl.n0 > sl.n1 ? sl.n0 : sl.n1;
-          cut = keys * kTile > sl.job.keys;
-          want = keys > kAhead / 2 ? keys - kAhead / 2 : 0;
-          c.take(sl);
-          --behind;
-          if (c.end() && behind < 0) {  // a job without steps: its slot may be another's by the time that scores come to it
-            a.take(sl);
-            ++behind;
-          }
-          mbar_arrive(smem_u32(&bar.job_empty[slot]));
-          if (c.end()) mbar_arrive(smem_u32(&bar.want));
+        if (!wait_long(smem_u32(&bar.job_full[slot]), used, abort_flag)) { ok = false; break; }
+        const Slot& sl = bar.slots[slot];
+        if (!sl.valid) break;
+        const int n0 = sl.n0, n1 = sl.n1, n = n0 > n1 ? n0 : n1, want = n > kAhead ? n - kAhead : 0;
+        const bool cut = n * kTile > sl.job.keys;
+        mbar_arrive(smem_u32(&bar.job_empty[slot]));
+        if (++slot == kSlots) { slot = 0; used ^= 1; }
+        if (n == 0) {
+          mbar_arrive(smem_u32(&bar.want));
           continue;
         }
-        if (c.j == want) {
-          mbar_arrive(smem_u32(&bar.want));
-          want = -1;
-        }
-        while (ok && ahead == 0) scores();  // (this step's own: its job is known)
-        // (a buffer is free for new scores once the products of its weights are issued: the tensor cores take them in order)
-        while (ok && more && ahead < kBufs && scores()) {}
-        if (!ok) break;
-        if (c.first_use() && !mbar_poll(smem_u32(&bar.full[c.stage]), c.phase, abort_flag)) { ok = false; break; }
-        if (cut && c.first_use() && c.j + 1 >= c.n0 && c.j + 1 >= c.n1) {
-          mbar_arrive(smem_u32(&bar.last_v));
-          if (!mbar_poll(smem_u32(&bar.fixed), fix_phase, abort_flag)) { ok = false; break; }
-          fix_phase ^= 1;
-        }
-        if (c.j == 0) {  // the last job's outputs have been read
-          if (!mbar_poll(smem_u32(&bar.o_free[c.t]), o_phase >> c.t & 1, abort_flag)) { ok = false; break; }
-          o_phase ^= 1u << c.t;
-        }
-        if (!mbar_poll(smem_u32(&bar.p_full[c.buf]), p_phase >> c.buf & 1, abort_flag)) { ok = false; break; }
-        p_phase ^= 1u << c.buf;
-        tc_fence_after();
-        const uint64_t v = dv + c.stage * (kBytes >> 4);
-        const uint32_t o = tmem + kO + c.t * D, w = tmem + c.buf * kTile;
+        // the first scores, where they were not begun beside the last job's end
+        if (!mbar_poll(smem_u32(&bar.full[ks]), kp, abort_flag)) { ok = false; break; }
 #pragma unroll
-        for (int s = 0; s < kTile / 16; ++s) mma_f16_ta(o, w + s * 8, v + (s * 2048 >> 4), id_o, c.j > 0 || s > 0);
-        mma_commit(smem_u32(&bar.o_done[c.t]));
-        if (c.last_use()) mma_commit(smem_u32(&bar.empty[c.stage]));
-        c.advance();
-        --ahead;
+        for (int t = 0; t < 2; ++t) {
+          if ((t ? n1 : n0) == 0) continue;
+          if (!begun[t]) {
+            if (!mbar_poll(smem_u32(&bar.q_full[t]), q_phase >> t & 1, abort_flag)) { ok = false; break; }
+            tc_fence_after();
+            scores(t, ks);
+          }
+          begun[t] = false;
+          q_phase ^= 1u << t;
+          if ((t ? n1 : n0) == 1) mma_commit(smem_u32(&bar.q_empty[t]));
+        }
+        if (!ok) break;
+        mma_commit(smem_u32(&bar.empty[ks]));
+        ks += 2;
+        if (ks >= (uint32_t)kRing) { ks -= kRing; kp ^= 1; }
+        for (int j = 0; j < n; ++j) {
+          if (j == want) mbar_arrive(smem_u32(&bar.want));
+          if (!mbar_poll(smem_u32(&bar.full[vs]), vp, abort_flag)) { ok = false; break; }
+          if (cut && j == n - 1) {
+            mbar_arrive(smem_u32(&bar.last_v));
+            if (!mbar_poll(smem_u32(&bar.fixed), fix_phase, abort_flag)) { ok = false; break; }
+            fix_phase ^= 1;
+          }
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const int nt = t ? n1 : n0;
+            if (j < nt) {
+              if (j == 0) {  // the last job's outputs have been read
+                if (!mbar_poll(smem_u32(&bar.o_free[t]), o_phase >> t & 1, abort_flag)) { ok = false; break; }
+                o_phase ^= 1u << t;
+              }
+              if (!mbar_poll(smem_u32(&bar.p_full[t]), p_phase >> t & 1, abort_flag)) { ok = false; break; }
+              p_phase ^= 1u << t;
+              tc_fence_after();
+#pragma unroll
+              for (int s = 0; s < kTile / 16; ++s) mma_ts(tmem + kO + t * D, tmem + t * kTile + s * 8, dv + vs * (kBytes >> 4) + (s * 2048 >> 4), id_o, j > 0 || s > 0);
+              if (j + 1 == nt) mma_commit(smem_u32(&bar.o_done[t]));
+            }
+            if (j + 1 < nt) {  // scores of the next step, behind the products that read the last ones' weights
+              if (!mbar_poll(smem_u32(&bar.full[ks]), kp, abort_flag)) { ok = false; break; }
+              tc_fence_after();
+              scores(t, ks);
+              if (j + 2 == nt) mma_commit(smem_u32(&bar.q_empty[t]));
+            } else if (j == n - 1 && !begun[t]) {  // or of the next job's first one, if that is known and its copies are there
+              const Slot& nx = bar.slots[slot];
+              if (mbar_test(smem_u32(&bar.job_full[slot]), used) && nx.valid && (t ? nx.n1 : nx.n0) > 0 && mbar_test(smem_u32(&bar.q_full[t]), q_phase >> t & 1) &&
+                  mbar_test(smem_u32(&bar.full[ks]), kp)) {
+                tc_fence_after();
+                scores(t, ks);
+                begun[t] = true;
+              }
+            }
+          }
+          if (!ok) break;
+          mma_commit(smem_u32(&bar.empty[vs]));
+          vs += 2;
+          if (vs >= (uint32_t)kRing) { vs -= kRing; vp ^= 1; }
+          if (j + 1 < n) {
+            mma_commit(smem_u32(&bar.empty[ks]));
+            ks += 2;
+            if (ks >= (uint32_t)kRing) { ks -= kRing; kp ^= 1; }
+          }
+        }
       }
       if (!ok) fail(abort_flag, p.status);
     }
@@ -450,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
       uint32_t ring_at = 0, ends = 0;
       for (int i = 0;; ++i) {
         const int slot = i % kSlots;
-        if (!wait_long(smem_u32(&bar.job_full[slot]), (uint32_t)(i / kSlots) & 1, abort_flag)) break;
+        if (!wait_asleep(smem_u32(&bar.job_full[slot]), (uint32_t)(i / kSlots) & 1, abort_flag)) break;
         const Slot sl = bar.slots[slot];
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bar.job_empty[slot]));
@@ -459,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
         ring_at += 2 * keys;
         if (keys * kTile <= sl.job.keys) continue;
         // the last tile's value rows behind the sequence's end are another's: 0 instead, so that weights of 0 meet no NaN
-        if (!wait_long(smem_u32(&bar.last_v), ends & 1, abort_flag)) break;
+        if (!wait_asleep(smem_u32(&bar.last_v), ends & 1, abort_flag)) break;
         ++ends;
         uint8_t* v = smem + (2 + (ring_at - 1) % kRing) * kBytes;
         for (int r = (sl.job.keys - (keys - 1) * kTile) * 8 + lane; r < kTile * 8; r += 32)
@@ -474,26 +470,24 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
     const int t = warp >> 2, row = (warp & 3) * 32 + lane;  // (a warp reads the quarter of TMEM's lanes that its number gives)
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, to = tmem + kO + t * D + lanes;
     const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f), grow = kGrowth / c2;
-    uint32_t first = 0, sums = 0;  // steps of all jobs so far, and this tile's
+    uint32_t steps = 0, ends = 0;  // this tile's steps so far, and jobs
+    const uint32_t ts = tmem + t * kTile + lanes;
     bool ok = true;
     for (int i = 0; ok; ++i) {
       const int slot = i % kSlots;
       if (!wait_long(smem_u32(&bar.job_full[slot]), (uint32_t)(i / kSlots) & 1, abort_flag)) { ok = false; break; }
       const Job jb = bar.slots[slot].job;
-      const int head = bar.slots[slot].head, valid = bar.slots[slot].valid, n0 = bar.slots[slot].n0, n1 = bar.slots[slot].n1;
+      const int head = bar.slots[slot].head, valid = bar.slots[slot].valid, nt = t ? bar.slots[slot].n1 : bar.slots[slot].n0;
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bar.job_empty[slot]));
       if (!valid) break;
-      // both tiles' steps in turn while both have one, then the rest of the longer one's
-      const int nt = t ? n1 : n0, both = n0 < n1 ? n0 : n1, at = jb.tile * 2 * kTile + t * kTile + row;  // this thread's row of the sequence
+      const int at = jb.tile * 2 * kTile + t * kTile + row;  // this thread's row of the sequence
       int64_t see = p.causal ? (int64_t)at + (jb.keys - jb.queries) + 1 : jb.keys;
       const int lim = (int)(see < 0 ? 0 : see > jb.keys ? jb.keys : see);
       float m = -INFINITY, l = 0.0f;
       for (int j = 0; j < nt; ++j) {
-        const uint32_t place = first + (j < both ? 2 * j + t : j + both), buf = place % kBufs, ts = tmem + buf * kTile + lanes;
-        const uint32_t mine = sums + j;  // this tile's steps
-        bool last_done = j == 0;         // whether the last step's products are known to be done
-        if (!mbar_wait_inline(smem_u32(&bar.s_full[t][mine % kBufs]), mine / kBufs & 1, abort_flag)) { ok = false; break; }
+        if (!mbar_wait_inline(smem_u32(&bar.s_full[t]), steps & 1, abort_flag)) { ok = false; break; }
+        ++steps;
         tc_fence_after();
         float s[kTile];
 #pragma unroll
@@ -519,9 +513,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
           if (grew) m = top;
           l *= f;
           if (j > 0) {
-            if (!mbar_wait_inline(smem_u32(&bar.o_done[t]), mine - 1 & 1, abort_flag)) { ok = false; break; }
-            last_done = true;
-            tc_fence_after();
+            // (the last step's products are done: this step's scores were issued behind them and have arrived)
 #pragma unroll
             for (int i2 = 0; i2 < D; i2 += 16) {
               uint32_t o[16];
@@ -561,15 +553,13 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
         one_each(add2(sum[0], sum[1]), u, v);
         l += u + v;
         tmem_wait_st();
-        if (!last_done && !mbar_wait_inline(smem_u32(&bar.o_done[t]), mine - 1 & 1, abort_flag)) { ok = false; break; }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bar.p_full[buf]));
+        if (lane == 0) mbar_arrive(smem_u32(&bar.p_full[t]));
       }
-      if (ok && nt > 0 && !mbar_wait_inline(smem_u32(&bar.o_done[t]), sums + nt - 1 & 1, abort_flag)) ok = false;
+      if (ok && nt > 0 && !mbar_wait_inline(smem_u32(&bar.o_done[t]), ends & 1, abort_flag)) ok = false;
       if (!ok) break;
-      first += n0 + n1;
-      sums += nt;
+      ends += nt > 0;
       tc_fence_after();
       const int behind = jb.queries - jb.tile * 2 * kTile - t * kTile;
       const bool live = row < behind;
