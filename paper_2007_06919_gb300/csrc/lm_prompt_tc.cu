@@ -4,8 +4,10 @@
 // live in TMEM; a thread per row reads its scores from there, subtracts the running maximum, takes exponentials, and writes the weights over the
 // scores as 16-bit numbers, from where they are the A operand of O += P V (V as it lies: its rows are K of that product). While one
 // tile's rows are at their exponentials, the tensor cores have the other tile's two products. For heads of 128 a step of
-// both takes four products of 128 x 128 x 128 (4 x 512 cycles); for heads of 64 the exponentials bound it (2 x 128 x 128 at 32 a cycle, 1024). (A third score
-// buffer there, which has the next scores ready when a row is through, gave nothing.)
+// both takes four products of 128 x 128 x 128 (4 x 512 cycles). For heads of 64 the exponentials bound it (2 x 128 x 128 at 32 a cycle, 1024), and a row must not
+// wait for its next scores: TMEM has 192 columns for a tile there, in three blocks X, Y, Z. Even steps have their scores in XY and their weights in X, odd ones in YZ
+// and Z: Y is free once a row's scores are read, so the next scores come while the exponentials run. (Scores behind the products that read the last
+// weights, as for heads of 128: 8192 tokens of 32 heads 263 us.)
 //
 // The outputs are brought to a new maximum only where it grew by more than a factor of 2^8 since the last time: weights stay below that, sums are
 // float32, and the division at the end is exact in it. So after the first few tiles of keys no row touches its outputs before the end.
@@ -56,9 +58,10 @@ struct Slot {
   Job job;
   int32_t head, valid, n0, n1;  // n: steps of the two tiles
 };
-// Whoever waits on a barrier meets every one of its phases, and none of them runs two ahead of it.
+// Whoever waits on a barrier meets every one of its phases, and none of them runs two ahead of it. Where scores run ahead, a warp may hand over its next
+// weights before another warp of the tile has its last ones ready: weights of even and odd steps have barriers of their own.
 struct Barriers {
-  uint64_t q_full[2], q_empty[2], full[8], empty[8], s_full[2], p_full[2], o_done[2], o_free[2], last_v, fixed, job_full[kSlots], job_empty[kSlots], want, answer;
+  uint64_t q_full[2], q_empty[2], full[8], empty[8], s_full[2], p_full[2][2], o_done[2], o_free[2], s_read[2], last_v, fixed, job_full[kSlots], job_empty[kSlots], want, answer;
   alignas(16) uint4 response;
   Slot slots[kSlots];
   uint32_t tmem;
@@ -168,7 +171,10 @@ __device__ __forceinline__ bool wait_asleep(uint32_t bar, uint32_t parity, volat
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ PromptArgs p) {
   constexpr int kBytes = tile_bytes(D), kRing = ring(D), kBoxes = D / 64, kBox = kTile * 128;
-  constexpr uint32_t kO = 2 * kTile;  // TMEM: scores of the tiles from columns 0 and 128 on (weights over them), then their outputs
+  // TMEM: 128 columns for each tile's scores, weights over them, or 192 (see above); then their outputs
+  constexpr bool kAhead2 = D == 64;
+  constexpr uint32_t kCols = kAhead2 ? 192 : 128, kO = 2 * kCols;
+  static_assert(kO + 2 * D <= 512, "");
   extern __shared__ __align__(1024) uint8_t smem[];  // queries of both tiles, the ring of keys and values, Barriers
   Barriers& bar = *reinterpret_cast<Barriers*>(smem + (2 + kRing) * kBytes);
   volatile int* abort_flag = &bar.abort_flag;
@@ -184,9 +190,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
       mbar_init(smem_u32(&bar.q_full[t]), 1);
       mbar_init(smem_u32(&bar.q_empty[t]), 1);
       mbar_init(smem_u32(&bar.s_full[t]), 1);
-      mbar_init(smem_u32(&bar.p_full[t]), 4);
+      mbar_init(smem_u32(&bar.p_full[t][0]), 4);
+      mbar_init(smem_u32(&bar.p_full[t][1]), 4);
       mbar_init(smem_u32(&bar.o_done[t]), 1);
       mbar_init(smem_u32(&bar.o_free[t]), 4);
+      mbar_init(smem_u32(&bar.s_read[t]), 4);
     }
     for (int i = 0; i < kSlots; ++i) {
       mbar_init(smem_u32(&bar.job_full[i]), 1);
@@ -352,15 +360,19 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
       int slot = 0;
       uint32_t used = 0, ks = 0, kp = 0, vs = 1, vp = 0;  // the job's slot and its use; the next tiles of keys and of values in the ring
       uint32_t q_phase = 0, o_phase = 3, p_phase = 0, fix_phase = 0;
+      uint32_t odd = 0, weights = 0, read_phase = 3;  // a bit for each tile: whether its next scores, and products, are those of an odd step
       bool ok = true, begun[2] = {false, false};
       auto scores = [&](int t, uint32_t stage) {
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
           const uint32_t at = ((s >> 2) * kBox + (s & 3) * 32) >> 4;
-          mma_ss(tmem + t * kTile, dq + t * (kBytes >> 4) + at, dk + stage * (kBytes >> 4) + at, id_s, s > 0);
+          mma_ss(tmem + t * kCols + (kAhead2 ? (odd >> t & 1) * 64 : 0), dq + t * (kBytes >> 4) + at, dk + stage * (kBytes >> 4) + at, id_s, s > 0);
         }
         mma_commit(smem_u32(&bar.s_full[t]));
+        if (kAhead2) { odd ^= 1u << t; read_phase ^= 1u << t; }
       };
+      // (the rows have read the last step's scores, whose place these take in part)
+      auto read = [&](int t) { return !kAhead2 || mbar_poll(smem_u32(&bar.s_read[t]), read_phase >> t & 1, abort_flag); };
       while (ok) {
         if (!wait_long(smem_u32(&bar.job_full[slot]), used, abort_flag)) { ok = false; break; }
         const Slot& sl = bar.slots[slot];
@@ -379,7 +391,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
         for (int t = 0; t < 2; ++t) {
           if ((t ? n1 : n0) == 0) continue;
           if (!begun[t]) {
-            if (!mbar_poll(smem_u32(&bar.q_full[t]), q_phase >> t & 1, abort_flag)) { ok = false; break; }
+            if (!mbar_poll(smem_u32(&bar.q_full[t]), q_phase >> t & 1, abort_flag) || !read(t)) { ok = false; break; }
             tc_fence_after();
             scores(t, ks);
           }
@@ -402,32 +414,39 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             const int nt = t ? n1 : n0;
-            if (j < nt) {
+            auto products = [&] {
+              if (j >= nt) return true;
               if (j == 0) {  // the last job's outputs have been read
-                if (!mbar_poll(smem_u32(&bar.o_free[t]), o_phase >> t & 1, abort_flag)) { ok = false; break; }
+                if (!mbar_poll(smem_u32(&bar.o_free[t]), o_phase >> t & 1, abort_flag)) return false;
                 o_phase ^= 1u << t;
               }
-              if (!mbar_poll(smem_u32(&bar.p_full[t]), p_phase >> t & 1, abort_flag)) { ok = false; break; }
-              p_phase ^= 1u << t;
+              const uint32_t even_odd = kAhead2 ? weights >> t & 1 : 0;
+              if (!mbar_poll(smem_u32(&bar.p_full[t][even_odd]), p_phase >> (2 * t + even_odd) & 1, abort_flag)) return false;
+              p_phase ^= 1u << (2 * t + even_odd);
               tc_fence_after();
+              const uint32_t w = tmem + t * kCols + even_odd * 128;
 #pragma unroll
-              for (int s = 0; s < kTile / 16; ++s) mma_ts(tmem + kO + t * D, tmem + t * kTile + s * 8, dv + vs * (kBytes >> 4) + (s * 2048 >> 4), id_o, j > 0 || s > 0);
-              if (j + 1 == nt) mma_commit(smem_u32(&bar.o_done[t]));
-            }
-            if (j + 1 < nt) {  // scores of the next step, behind the products that read the last ones' weights
-              if (!mbar_poll(smem_u32(&bar.full[ks]), kp, abort_flag)) { ok = false; break; }
+              for (int s = 0; s < kTile / 16; ++s) mma_ts(tmem + kO + t * D, w + s * 8, dv + vs * (kBytes >> 4) + (s * 2048 >> 4), id_o, j > 0 || s > 0);
+              if (kAhead2) weights ^= 1u << t;
+              if (j + 1 == nt || (kAhead2 && j + 2 == nt)) mma_commit(smem_u32(&bar.o_done[t]));
+              return true;
+            };
+            if (!kAhead2 && !products()) { ok = false; break; }
+            if (j + 1 < nt) {  // scores of the next step
+              if (!mbar_poll(smem_u32(&bar.full[ks]), kp, abort_flag) || !read(t)) { ok = false; break; }
               tc_fence_after();
               scores(t, ks);
               if (j + 2 == nt) mma_commit(smem_u32(&bar.q_empty[t]));
             } else if (j == n - 1 && !begun[t]) {  // or of the next job's first one, if that is known and its copies are there
               const Slot& nx = bar.slots[slot];
               if (mbar_test(smem_u32(&bar.job_full[slot]), used) && nx.valid && (t ? nx.n1 : nx.n0) > 0 && mbar_test(smem_u32(&bar.q_full[t]), q_phase >> t & 1) &&
-                  mbar_test(smem_u32(&bar.full[ks]), kp)) {
+                  mbar_test(smem_u32(&bar.full[ks]), kp) && (!kAhead2 || mbar_test(smem_u32(&bar.s_read[t]), read_phase >> t & 1))) {
                 tc_fence_after();
                 scores(t, ks);
                 begun[t] = true;
               }
             }
+            if (kAhead2 && !products()) { ok = false; break; }
           }
           if (!ok) break;
           mma_commit(smem_u32(&bar.empty[vs]));
@@ -470,8 +489,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
     const int t = warp >> 2, row = (warp & 3) * 32 + lane;  // (a warp reads the quarter of TMEM's lanes that its number gives)
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, to = tmem + kO + t * D + lanes;
     const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f), grow = kGrowth / c2;
-    uint32_t steps = 0, ends = 0;  // this tile's steps so far, and jobs
-    const uint32_t ts = tmem + t * kTile + lanes;
+    uint32_t steps = 0, ends = 0;  // this tile's steps so far, and phases of o_done
+    const uint32_t tile = tmem + t * kCols + lanes;
     bool ok = true;
     for (int i = 0; ok; ++i) {
       const int slot = i % kSlots;
@@ -485,8 +504,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
       int64_t see = p.causal ? (int64_t)at + (jb.keys - jb.queries) + 1 : jb.keys;
       const int lim = (int)(see < 0 ? 0 : see > jb.keys ? jb.keys : see);
       float m = -INFINITY, l = 0.0f;
+      bool before = false;  // whether the end of the products before the last has been met
       for (int j = 0; j < nt; ++j) {
         if (!mbar_wait_inline(smem_u32(&bar.s_full[t]), steps & 1, abort_flag)) { ok = false; break; }
+        const uint32_t ts = tile + (kAhead2 ? (steps & 1) * 64 : 0), tp = tile + (kAhead2 ? (steps & 1) * 128 : 0);
+        const uint32_t handed = smem_u32(&bar.p_full[t][kAhead2 ? steps & 1 : 0]);
         ++steps;
         tc_fence_after();
         float s[kTile];
@@ -495,6 +517,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
         tmem_wait_ld();
 #pragma unroll
         for (int i2 = 0; i2 < kTile; i2 += 32) settle(s + i2);
+        if (kAhead2) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&bar.s_read[t]));
+        }
         const int here = lim - j * kTile;  // places of this tile that the row sees
         if (__any_sync(0xffffffffu, here < kTile)) {
 #pragma unroll
@@ -513,7 +540,17 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
           if (grew) m = top;
           l *= f;
           if (j > 0) {
-            // (the last step's products are done: this step's scores were issued behind them and have arrived)
+            // The last step's products are done: this step's scores were issued behind them and have arrived; or, where scores run ahead, the next
+            // step's are (of which there is none behind the last, where the products tell it themselves).
+            if (kAhead2 && j + 1 < nt) {
+              if (!mbar_wait_inline(smem_u32(&bar.s_full[t]), steps & 1, abort_flag)) { ok = false; break; }
+              tc_fence_after();
+            } else if (kAhead2) {
+              if (!mbar_wait_inline(smem_u32(&bar.o_done[t]), ends & 1, abort_flag)) { ok = false; break; }
+              ++ends;
+              before = true;
+              tc_fence_after();
+            }
 #pragma unroll
             for (int i2 = 0; i2 < D; i2 += 16) {
               uint32_t o[16];
@@ -547,15 +584,20 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
             sum[i2 & 1] = add2(sum[i2 & 1], two_of(x, y));
             w[i2] = pack(x, y, (T*)nullptr);
           }
-          tmem_st16(ts + 16 * h, w);
+          tmem_st16(tp + 16 * h, w);
         }
         float u, v;
         one_each(add2(sum[0], sum[1]), u, v);
         l += u + v;
+        // (every phase of a barrier is met)
+        if (kAhead2 && j > 0 && j + 1 == nt && !before) {
+          if (!mbar_wait_inline(smem_u32(&bar.o_done[t]), ends & 1, abort_flag)) { ok = false; break; }
+          ++ends;
+        }
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bar.p_full[t]));
+        if (lane == 0) mbar_arrive(handed);
       }
       if (ok && nt > 0 && !mbar_wait_inline(smem_u32(&bar.o_done[t]), ends & 1, abort_flag)) ok = false;
       if (!ok) break;
