@@ -37,6 +37,8 @@ template <> __device__ __forceinline__ float from_f32<float>(float v) { return v
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+__device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
+
 template <class T, int V>
 struct alignas(sizeof(T) * V) Vec {
   T x[V];
@@ -394,20 +396,8 @@ __global__ void __launch_bounds__(kThreads, kPlain ? 4 : kCache ? 2 : 3) rows_ke
   const int per = kThreads / 32 / share, warp = threadIdx.x >> 5, half = p.rot >> 1;
   const int64_t t0 = (int64_t)blockIdx.x * per;
   const int here = (int)(p.tokens - t0 < per ? p.tokens - t0 : per);
-  if constexpr (!kPlain) {
-    if (half > 0) {
-      // a thread keeps to one frequency, where there are as many threads
-      const int wide = half < kThreads ? half : kThreads, f0 = threadIdx.x % wide, step = kThreads / wide;
-      for (int f = f0; f < half; f += wide) {
-        const uint64_t rate = turn_rate(p.inv_freq[f]);
-        for (int t = threadIdx.x / wide; t < here && (int)threadIdx.x < wide * step; t += step) turns[t * half + f] = turn_of(rate, p.positions[t0 + t]);
-      }
-    }
-    __syncthreads();
-  }
   const int t = warp / share;
-  if (t >= here) return;
-  const int64_t token = t0 + t;
+  const int64_t token = t0 + (t < here ? t : 0);
   const int lane = threadIdx.x & (lanes - 1), group = (threadIdx.x & 31) >> lanes_log2, groups = 32 >> lanes_log2;
   const int first = (warp % share) * groups, step = share * groups;
   // this lane's two vectors
@@ -419,6 +409,31 @@ __global__ void __launch_bounds__(kThreads, kPlain ? 4 : kCache ? 2 : 3) rows_ke
   int row = 0;
   uint8_t* blk = kept ? place(p.cache, slot, 0, row) : nullptr;
   const int64_t head_bytes = ((int64_t)1 << (p.cache.page_shift - 4)) * 16 * (p.cache.dim + 8);
+  // the first rows are on their way while sines and cosines are made
+  if (!kPlain && in) {
+    if (first + group < p.heads) {
+      const T* x = static_cast<const T*>(p.q) + token * p.ldq + (int64_t)(first + group) * p.ldqh;
+      prefetch(x + ia);
+      prefetch(x + ib);
+    }
+    if (first + group < p.kv_heads) {
+      const T* x = static_cast<const T*>(p.k) + token * p.ldk + (int64_t)(first + group) * p.ldkh;
+      prefetch(x + ia);
+      prefetch(x + ib);
+    }
+  }
+  if constexpr (!kPlain) {
+    if (half > 0) {
+      // a thread keeps to one frequency, where there are as many threads
+      const int wide = half < kThreads ? half : kThreads, f0 = threadIdx.x % wide, each = kThreads / wide;
+      for (int f = f0; f < half; f += wide) {
+        const uint64_t rate = turn_rate(p.inv_freq[f]);
+        for (int s = threadIdx.x / wide; s < here && (int)threadIdx.x < wide * each; s += each) turns[s * half + f] = turn_of(rate, p.positions[t0 + s]);
+      }
+    }
+    __syncthreads();
+  }
+  if (t >= here) return;
 
   auto to_cache = [&](int head, bool live, bool values, const uint4& a, const uint4& b) {
     float lo, hi;
