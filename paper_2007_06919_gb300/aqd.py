@@ -904,7 +904,8 @@ def _out_heads(out: torch.Tensor | None, like: torch.Tensor, name: str, stream):
 
 class KVCache:
     """A 4-bit cache of keys and values (aqd_kv_cache): `pages` pages of page_size places (a power of two, 16..1024), each
-    place a key and a value row of every head. Its memory belongs to the stream current at construction, or to `stream`."""
+    place a key and a value row of every head. Its memory belongs to the stream current at construction, or to `stream`: it has to outlive
+    the calls on others."""
 
     def __init__(self, pages: int, page_size: int, kv_heads: int, head_dim: int, device="cuda", stream=None):
         nbytes = int(_calls().aqd_kv_cache_bytes(pages, page_size, kv_heads, head_dim))

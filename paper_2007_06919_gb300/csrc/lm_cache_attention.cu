@@ -280,7 +280,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
   uint32_t there = 0;          // two bits a stage: its blocks were copied
 
   const uint8_t* mine_data = p.cache.data + (int64_t)head * blocks_of_page * kBlock;  // this head's part of page 0
-  const uint32_t page_bytes = (uint32_t)p.cache.kv_heads * (uint32_t)blocks_of_page * kBlock;
+  const uint64_t page_bytes = (uint64_t)p.cache.kv_heads * (uint32_t)(blocks_of_page * kBlock);
   int blk = idle ? 0 : (step0 * 2) & (blocks_of_page - 1);  // the next step's first block within its page
   int ist = 0;                                              // its stage
 
@@ -610,7 +610,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
       }
     }
   }
-  if (!goes_on && threadIdx.x == 0) span->last = 0;
+  if (!sp.whole && !goes_on && threadIdx.x == 0) span->last = 0;
 }
 
 // A block for a row of the group of runs that begins in block blockIdx.x and goes on: its parts, in a fixed order.
@@ -685,7 +685,7 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant
 struct Sizes {
   int rows;             // of a tile
   int warps;            // tasks that fill the GPU
-  int64_t tiles, blocks; // bounds: row tiles; blocks
+  int64_t tiles, blocks; // bounds: row tiles; blocks where runs are split
   size_t part_off, bytes;
 };
 static Sizes sizes(int64_t tokens, int32_t seqs, int32_t heads, int32_t kv_heads, int32_t dim) {
@@ -697,8 +697,8 @@ static Sizes sizes(int64_t tokens, int32_t seqs, int32_t heads, int32_t kv_heads
   s.tiles = tokens == seqs ? seqs * ((group + s.rows - 1) / s.rows) : tokens * group / s.rows + seqs;
   // (tokens == seqs with starts: each of n > 0 queries has at most ceil(n group / rows) <= n ceil(group / rows) tiles)
   s.warps = 152 * (two || dim > 128 ? 1 : 2) * kWarps;
-  // tasks: a run each for `warps` of them at most (twice as many beside many tiles), and one more for each tile and head; or a block for each
-  s.blocks = (s.warps + kWarps - 1) / kWarps + s.tiles * kv_heads;
+  // tasks: at most `warps`, and one more for each tile and head
+  s.blocks = (s.warps + s.tiles * kv_heads + kWarps - 1) / kWarps;
   s.part_off = ((size_t)s.blocks * sizeof(Span) + 255) / 256 * 256;
   s.bytes = s.part_off + (size_t)s.blocks * 2 * s.rows * (dim + 4) * 4;
   return s;
@@ -721,7 +721,7 @@ static cudaError_t run(const CacheAttnArgs& a, const Sizes& s, cudaStream_t stre
   cudaError_t e = cudaFuncSetAttribute(cache_attention_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   const int64_t heads_tiles = s.tiles * a.cache.kv_heads;
-  const int64_t blocks = sp.whole ? heads_tiles : (s.warps + heads_tiles + kWarps - 1) / kWarps;
+  const int64_t blocks = sp.whole ? heads_tiles : s.blocks;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)blocks);
   cfg.blockDim = dim3(kThreads);
@@ -757,7 +757,7 @@ size_t cache_attention_workspace_bytes(int64_t tokens, int32_t seqs, int32_t hea
 
 int launch_cache_attention(const CacheAttnArgs& a, cudaStream_t stream, std::string* err) {
   const cacheattn::Sizes s = cacheattn::sizes(a.tokens, a.seqs, a.heads, a.cache.kv_heads, a.cache.dim);
-  if (s.blocks > (1 << 27)) {  // (tasks are counted in 32 bits)
+  if (s.tiles * a.cache.kv_heads > (1 << 27)) {  // (tasks are counted in 32 bits)
     *err = "too many tokens in one call";
     return 2;
   }

@@ -231,3 +231,30 @@ def test_no_sequences():
     none = torch.zeros(1, dtype=torch.int32, device="cuda")
     aqd.cache_attention(out.clone(), c.cache, c.table[:0], c.lengths[:0], starts=none, out=out)
     assert (out == 4).all()
+
+
+def test_pages_of_more_than_32_bits():
+    kv, dim = 65535, 64
+    cache = aqd.KVCache(2, 1024, kv, dim)
+    assert cache.data.numel() // 2 > 1 << 32
+    torch.manual_seed(11)
+    n = 20
+    k, v = (torch.randn(n, kv, dim, device="cuda", dtype=BF16) for _ in range(2))
+    slots = torch.arange(n, device="cuda") + 1024
+    aqd.cache_write(cache, k, v, slots)
+    q = torch.randn(1, kv, dim, device="cuda", dtype=BF16)
+    for columns in (1, 2):  # a block for each head, and runs
+        table = torch.full((1, columns), 1, dtype=torch.int32, device="cuda")
+        got = aqd.cache_attention(q, cache, table, torch.tensor([n], dtype=torch.int32, device="cuda"))
+        ck, cv = aqd.cache_read(cache, slots, dtype=F32)
+        p = (torch.einsum("hd,mhd->hm", q[0].double(), ck.double()) / 8).softmax(1)
+        want = torch.einsum("hm,mhd->hd", p, cv.double())
+        # (the sums of the scores' and weights' bounds above, for values of 5 and steps of 0.6)
+        close(got[0], want, 0.02 + U[BF16] * want.abs())
+
+
+def test_broadcast_queries():
+    c = Case([90, 33], [1, 1], 6, 2, 64, 16, BF16, seed=12)
+    c.q = c.q[:, :1].expand(2, 6, 64)
+    o, tol, _, _ = c.want(0.125)
+    close(aqd.cache_attention(c.q, c.cache, c.table, c.lengths, out=torch.empty(2, 6, 64, device="cuda", dtype=BF16)), o, tol)

@@ -202,3 +202,20 @@ def test_no_tokens():
     assert aqd.qk_norm_rope(e, e, i, freqs(64)).q.shape == (0, 2, 64)
     aqd.cache_write(cache, e, e, i)
     assert aqd.cache_read(cache, i)[0].shape == (0, 2, 64)
+
+
+def test_keys_alone_and_broadcast_inputs():
+    q, k, v = inputs(10, 30, 4, 2, 64, BF16)
+    pos, f = torch.arange(30, device="cuda"), freqs(64)
+    want = aqd.qk_norm_rope(q, k, pos, f)
+    none = aqd.qk_norm_rope(q[:, :0], k, pos, f)
+    assert none.q.shape == (30, 0, 64) and torch.equal(none.k, want.k)
+    one = q[:1, :1].expand(30, 4, 64)
+    out = aqd.qk_norm_rope(one, k, pos, f, q_out=torch.empty(30, 4, 64, device="cuda", dtype=BF16)).q
+    exact, size = rotated(one, None, pos, f, False, 0)
+    close(out, exact, bound(exact, size, BF16))
+    cache, slots = aqd.KVCache(4, 16, 2, 64), torch.arange(30, device="cuda")
+    aqd.cache_write(cache, k[:, :1].expand(30, 2, 64), v, slots)
+    gk, gv = aqd.cache_read(cache, slots)
+    check_held(gk, k[:, :1].expand(30, 2, 64))
+    check_held(gv, v)

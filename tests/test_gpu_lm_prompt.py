@@ -175,3 +175,38 @@ def test_no_sequences():
     aqd.prompt_attention(q, k, v, torch.zeros(1, dtype=torch.int32, device="cuda"), out=out)
     assert (out == 4).all()
     assert aqd.prompt_attention(q[:0], k[:0], v[:0], torch.zeros(3, dtype=torch.int32, device="cuda")).shape == (0, 2, 64)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_broadcast_keys_and_two_calls_at_once(dim):
+    at, starts = starts_of([300, 41])
+    q, k, v = inputs(7, 341, 341, 4, 2, dim, BF16)
+    k = k[:, :1].expand(341, 2, dim)
+    o, tol, _, _ = reference(q, k, v, at, at, True, dim ** -0.5)
+    close(aqd.prompt_attention(q, k, v, starts), o, tol)
+    k = k.contiguous()
+    want = aqd.prompt_attention(q, k, v, starts)
+    close(want, o, tol)
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(2_000_000)
+    got = [aqd.prompt_attention(q, k, v, starts, stream=s) for s in streams for _ in range(3)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want) for g in got)
+
+
+def test_many_short_prompts():
+    """More jobs than blocks, most of them a row or two; sequences without queries and without keys among them."""
+    torch.manual_seed(8)
+    lens = [int(n) for n in torch.randint(0, 5, (900,))]
+    klens = [int(n) for n in torch.randint(0, 7, (900,))]
+    lens[450], klens[450] = 700, 900
+    at, starts = starts_of(lens)
+    kat, kstarts = starts_of(klens)
+    q, k, v = inputs(9, at[-1], kat[-1], 2, 1, 64, F16)
+    for causal in (True, False):
+        o, tol, e, et = reference(q, k, v, at, kat, causal, 0.125)
+        got, lse = aqd.prompt_attention(q, k, v, starts, kv_starts=kstarts, causal=causal, lse=True)
+        close(got, o, tol)
+        close(lse, e, et)
+    assert aqd.device_status() == 0
