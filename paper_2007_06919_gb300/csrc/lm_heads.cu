@@ -402,7 +402,8 @@ __global__ void __launch_bounds__(kThreads, kPlain ? 4 : kCache ? 2 : 3) rows_ke
   const int first = (warp % share) * groups, step = share * groups;
   // this lane's two vectors
   const bool in = 2 * lane * V < p.dim, between = !kInter && lane * V < half;  // (pairs between the two)
-  const int ia = between ? lane * V : 2 * lane * V, ib = between ? ia + half : ia + V;
+  // (with no pairs to keep, adjacent vectors are in adjacent lanes all the same: an access takes whole sectors)
+  const int ia = kPlain || between ? lane * V : 2 * lane * V, ib = kPlain ? ia + (p.dim >> 1) : between ? ia + half : ia + V;
   const bool turn_a = kInter ? ia < p.rot : between, turn_b = kInter ? ib < p.rot : between;
   const int64_t slot = kCache ? p.slots[token] : -1;
   const bool kept = kCache && in_cache(p.cache, slot);
@@ -577,70 +578,83 @@ __global__ void __launch_bounds__(kThreads, kPlain ? 4 : kCache ? 2 : 3) rows_ke
   }
 }
 
-// A warp, or several, to a token, as above; a lane takes 16 codes (8 bytes) of a row, `lanes` lanes a row, keys' rows and then values'.
-template <class T, bool kVec>
+// `share` warps to kTokens tokens; a lane takes two words of 8 codes of a row, half a row apart (its values' stores are then whole sectors with its
+// neighbours'), `lanes` lanes a row, keys' rows and then values'. Four rows' loads are on the way together, of each token.
+template <class T, bool kVec, int kTokens>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheReadArgs p, const int share, const int lanes, const int lanes_log2) {
   tc::grid_dep_wait();
   const CacheGeom& c = p.cache;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & (lanes - 1), groups = 32 >> lanes_log2;
-  const int64_t token = ((int64_t)blockIdx.x * (kThreads / 32) + warp) / share;
-  if (token >= p.tokens || lane * 16 >= c.dim) return;
-  const int64_t slot = p.slots[token];
-  const bool kept = in_cache(c, slot);
-  int row = 0;
-  const uint8_t* blk = kept ? place(c, slot, 0, row) : nullptr;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & (lanes - 1), groups = 32 >> lanes_log2, wide = c.dim >> 4;
+  const int64_t token0 = ((int64_t)blockIdx.x * (kThreads / 32) + warp) / share * kTokens;
+  if (token0 >= p.tokens || lane >= wide) return;
   const int64_t head_bytes = ((int64_t)1 << (c.page_shift - 4)) * 16 * (c.dim + 8);
-  // four rows at a time: their loads are on the way together
-  for (int r0 = (warp % share) * groups + ((threadIdx.x & 31) >> lanes_log2); r0 < 2 * c.kv_heads; r0 += 4 * share * groups) {
-    uint2 words[4];
-    uint32_t steps[4];
+  const uint8_t* blk[kTokens];
+  int row[kTokens];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int r = r0 + k * share * groups, h = r >= c.kv_heads ? r - c.kv_heads : r;
-      words[k] = make_uint2(0, 0);
-      steps[k] = 0;
-      if (kept && r < 2 * c.kv_heads) {
-        const uint8_t* x = blk + h * head_bytes;
-        words[k] = *reinterpret_cast<const uint2*>(x + (r >= c.kv_heads ? 8 * c.dim : 0) + row * (c.dim >> 1) + 8 * lane);
-        steps[k] = *reinterpret_cast<const uint32_t*>(x + 16 * c.dim + (r >= c.kv_heads ? 64 : 0) + 4 * row);
+  for (int t = 0; t < kTokens; ++t) {
+    const int64_t slot = token0 + t < p.tokens ? p.slots[token0 + t] : -1;
+    row[t] = 0;
+    blk[t] = in_cache(c, slot) ? place(c, slot, 0, row[t]) : nullptr;
+  }
+  const int step = share * groups;
+  for (int r0 = (warp % share) * groups + ((threadIdx.x & 31) >> lanes_log2); r0 < 2 * c.kv_heads; r0 += 4 * step) {
+    uint2 words[kTokens][4];
+    uint32_t steps[kTokens][4];
+#pragma unroll
+    for (int t = 0; t < kTokens; ++t)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int r = r0 + k * step;
+        const bool is_v = r >= c.kv_heads;
+        words[t][k] = make_uint2(0, 0);
+        steps[t][k] = 0;
+        if (blk[t] && r < 2 * c.kv_heads) {
+          const uint8_t* x = blk[t] + (is_v ? r - c.kv_heads : r) * head_bytes;
+          const uint32_t* w = reinterpret_cast<const uint32_t*>(x + (is_v ? 8 * c.dim : 0) + row[t] * (c.dim >> 1)) + lane;
+          words[t][k] = make_uint2(w[0], w[wide]);
+          steps[t][k] = *reinterpret_cast<const uint32_t*>(x + 16 * c.dim + (is_v ? 64 : 0) + 4 * row[t]);
+        }
       }
-    }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-    const int r = r0 + k * share * groups;
-    const bool is_v = r >= c.kv_heads;
-    T* y = is_v ? static_cast<T*>(p.v) : static_cast<T*>(p.k);
-    if (r >= 2 * c.kv_heads || !y) continue;
-    y += token * (is_v ? p.ldv : p.ldk) + (is_v ? r - c.kv_heads : r) * (is_v ? p.ldvh : p.ldkh) + lane * 16;
-    const uint2 w = words[k];
-    const uint32_t ls = steps[k];
-    const float low = __uint_as_float(ls << 16), step = __uint_as_float(ls & 0xffff0000u);
-    const uint64_t low2 = two_of(low, low), step2 = two_of(step, step), less = two_of(-8388608.0f, -8388608.0f);
-    uint64_t f[8];
+    for (int t = 0; t < kTokens; ++t)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {  // (a code under the exponent of 2^23 is 2^23 + n)
-      const uint32_t u = (j < 4 ? w.x : w.y) >> (8 * (j & 3));
-      f[j] = fma2(add2(two_of(__uint_as_float((u & 15u) | 0x4b000000u), __uint_as_float((u >> 4 & 15u) | 0x4b000000u)), less), step2, low2);
-    }
-    if constexpr (kVec) {
-      constexpr int kPairs = 8 / sizeof(T);
+      for (int k = 0; k < 4; ++k) {
+        const int r = r0 + k * step;
+        const bool is_v = r >= c.kv_heads;
+        T* y = is_v ? static_cast<T*>(p.v) : static_cast<T*>(p.k);
+        if (token0 + t >= p.tokens || r >= 2 * c.kv_heads || !y) continue;
+        y += (token0 + t) * (is_v ? p.ldv : p.ldk) + (is_v ? r - c.kv_heads : r) * (is_v ? p.ldvh : p.ldkh) + lane * 8;
+        const float low = __uint_as_float(steps[t][k] << 16), size = __uint_as_float(steps[t][k] & 0xffff0000u);
+        const uint64_t low2 = two_of(low, low), step2 = two_of(size, size), less = two_of(-8388608.0f, -8388608.0f);
 #pragma unroll
-      for (int i = 0; i < 8; i += kPairs) {
-        uint64_t v[kPairs];
+        for (int h = 0; h < 2; ++h, y += c.dim >> 1) {
+          const uint32_t w = h ? words[t][k].y : words[t][k].x;
+          uint64_t f[4];
 #pragma unroll
-        for (int e = 0; e < kPairs; ++e) v[e] = f[i + e];
-        *reinterpret_cast<uint4*>(y + 2 * i) = from_pairs<T>(v);
+          for (int j = 0; j < 4; ++j) {  // (a code under the exponent of 2^23 is 2^23 + n)
+            const uint32_t u = w >> (8 * j);
+            f[j] = fma2(add2(two_of(__uint_as_float((u & 15u) | 0x4b000000u), __uint_as_float((u >> 4 & 15u) | 0x4b000000u)), less), step2, low2);
+          }
+          if constexpr (kVec) {
+            constexpr int kPairs = 8 / sizeof(T);
+#pragma unroll
+            for (int i = 0; i < 4; i += kPairs) {
+              uint64_t v[kPairs];
+#pragma unroll
+              for (int e = 0; e < kPairs; ++e) v[e] = f[i + e];
+              *reinterpret_cast<uint4*>(y + 2 * i) = from_pairs<T>(v);
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              float a, b;
+              one_each(f[j], a, b);
+              y[2 * j] = from_f32<T>(a);
+              y[2 * j + 1] = from_f32<T>(b);
+            }
+          }
+        }
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float a, b;
-        one_each(f[j], a, b);
-        y[2 * j] = from_f32<T>(a);
-        y[2 * j + 1] = from_f32<T>(b);
-      }
-    }
-    }
   }
 }
 
@@ -706,9 +720,12 @@ static cudaError_t run_read(const CacheReadArgs& a, cudaStream_t stream) {
   const int share = share_of(a.tokens, 2 * a.cache.kv_heads, 32 / lanes);
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute at[1];
-  config(cfg, at, (a.tokens * share + kThreads / 32 - 1) / (kThreads / 32), 0, stream);
-  if (vec) return cudaLaunchKernelEx(&cfg, cache_read_kernel<T, true>, a, share, lanes, log2);
-  return cudaLaunchKernelEx(&cfg, cache_read_kernel<T, false>, a, share, lanes, log2);
+  // two tokens a warp where there are tokens for every warp that fits: twice the bytes on their way
+  const bool two = vec && share == 1 && a.tokens >= 2 * 152 * 32;
+  config(cfg, at, ((two ? (a.tokens + 1) / 2 : a.tokens) * share + kThreads / 32 - 1) / (kThreads / 32), 0, stream);
+  if (two) return cudaLaunchKernelEx(&cfg, cache_read_kernel<T, true, 2>, a, share, lanes, log2);
+  if (vec) return cudaLaunchKernelEx(&cfg, cache_read_kernel<T, true, 1>, a, share, lanes, log2);
+  return cudaLaunchKernelEx(&cfg, cache_read_kernel<T, false, 1>, a, share, lanes, log2);
 }
 
 }  // namespace headrows
