@@ -734,7 +734,8 @@ static cudaError_t run(const CacheAttnArgs& a, const Sizes& s, cudaStream_t stre
   cfg.numAttrs = 1;
   e = cudaLaunchKernelEx(&cfg, cache_attention_kernel<T, D, NT>, a, sp);
   if (e != cudaSuccess || sp.whole) return e;
-  cfg.gridDim = dim3((unsigned)blocks, (unsigned)s.rows);
+  const int most = a.starts || sp.group > s.rows ? s.rows : sp.group;  // rows of a tile that can be there
+  cfg.gridDim = dim3((unsigned)blocks, (unsigned)most);
   cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, combine_kernel<T, D>, a, sp, s.rows);
 }
