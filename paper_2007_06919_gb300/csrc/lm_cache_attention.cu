@@ -13,10 +13,17 @@
 // registers with no exchange between lanes. (tcgen05 would want the expanded codes in shared memory or TMEM first, and its 128 rows mostly empty.)
 //
 // The unit of work is a warp's: one key-value head, 8 or 16 rows (queries x heads of the group) and a run of steps of 32 places, through the warp's own
-// ring of bulk copies (a step is one or two runs of bytes in the cache). The runs' length follows from all sequences' lengths, so that they fill
-// the GPU once and are even however the lengths differ; a block's 8 warps take runs that follow one another, of one sequence or of several, and join
-// what belongs together; combine_kernel joins what lies in several blocks. (64 sequences of 1 to 8192 places: blocks of one sequence each, of which the short ones
-// left most warps idle, 47 us.) Tables of few places give each sequence and head a block, and need no second kernel.
+// ring of bulk copies (a step is one or two runs of bytes in the cache). How many runs a sequence has follows from its part of all sequences' steps, so
+// that they fill the GPU once and are even however the lengths differ; a block's 8 warps take runs that follow one another, of one sequence or of several,
+// and join what belongs together; combine_kernel joins what lies in several blocks. (64 sequences of 1 to 8192 places: 24.0 us; blocks of one sequence
+// each, of which the short ones left most warps idle, 47.) Few rows over tables of few places take a cluster of one to eight blocks a row tile and head
+// instead, which join in shared memory: no second kernel (one sequence of 1000 places, 8 heads: 6.2 us in clusters of four, 9.2 in one block each;
+// 4000 places 7.8, 10.3).
+//
+// What a call spends, in cycles of a block (200,001 places, 2 heads; 22 us): 600 for the launch's order, 2,600 to find its work, 3,000 for page numbers
+// and query rows, 1,000 until the first copy is there, 14,000 to 19,000 in five or six steps, 3,000 to join, and 6,500 in the second kernel. A step of
+// 32 places is 590 instructions of a warp, 2,360 cycles where 16 warps share the SM: with 800,001 places the cache comes in at 4.1 TB/s, with 64 sequences
+// of 8192 at 4.3.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -34,6 +41,7 @@ namespace cacheattn {
 using namespace tc;
 
 constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kMostBlocks = 8;            // of a cluster
 constexpr int kStep = 32;                 // places of a step
 constexpr float kGrowth = 4.0f;           // powers of two that a maximum may grow by before sums are brought to it
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -44,9 +52,9 @@ __host__ __device__ constexpr int row_tiles(int dim) { return dim <= 128 ? 2 : 1
 
 struct Split {
   int32_t warps;        // tasks that fill the GPU
-  int32_t whole;        // a block for each sequence, tile and head
+  int32_t whole;        // blocks for each sequence, tile and head: this many, a cluster (0: runs of even lengths instead)
   int32_t group;        // query heads of a key-value head
-  uint64_t group_magic;
+  uint64_t group_magic, kv_magic;
   int32_t q_vec;        // rows of q on 16 bytes
   int32_t* meta;        // [block][8]: Span
   float* part;          // [block][2][row]: dim sums, then maximum, sum, factor
@@ -122,9 +130,9 @@ __device__ __forceinline__ void lds(uint32_t addr, uint32_t (&w)[kWords]) {
 __device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float step_of(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// A warp's task: run `run` of `runs`, `steps` steps each, of a sequence's tile of rows and a head; seq -1: none.
+// A warp's task: run `run` of `runs` of a sequence's tile of rows and a head, `steps` steps from `step0` on; seq -1: none.
 struct Job {
-  int32_t seq, tile, head, run, runs, steps, start, queries, len;
+  int32_t seq, tile, head, run, runs, step0, steps, start, queries, len;
 };
 
 // A sequence's queries, first token and length, within what the caller's tensors hold.
@@ -142,73 +150,117 @@ __device__ __forceinline__ void sequence(const CacheAttnArgs& p, int s, int& sta
   len = n < 0 ? 0 : n > most ? (int)most : n;
 }
 
-// The tasks of this block's warps. (Counts are 32 bits wide: the host refuses more. Starts that fall may make more; every job is one of its
-// sequence's all the same.)
+// Tasks fill the GPU once (or, beside many tiles, half of it): runs for a step. steps: of all tiles and heads.
+__device__ __forceinline__ float runs_for_a_step(const Split& sp, uint32_t tiles, float steps) {
+  const uint32_t most = tiles < (uint32_t)(sp.warps / 2) ? sp.warps - tiles : sp.warps / 2;
+  return steps > 0.0f ? (float)most / steps : 0.0f;
+}
+// A sequence's tiles and how its steps are split into runs.
 template <int kRows>
-__device__ __forceinline__ void find_jobs(const CacheAttnArgs& p, const Split& sp, Job* jobs, uint64_t* red) {
-  const int kv = p.cache.kv_heads, first_task = blockIdx.x * kWarps, lane = threadIdx.x & 31;
-  if (threadIdx.x < kWarps) jobs[threadIdx.x].seq = -1;
-  const int s0 = threadIdx.x;
+struct Cut {
+  uint32_t tiles, steps, count;  // (count: tasks)
+  int32_t runs;
+  __device__ __forceinline__ Cut(const Split& sp, int queries, int len)
+      : tiles((uint32_t)(((int64_t)queries * sp.group + kRows - 1) / kRows)), steps((uint32_t)(len + kStep - 1) / kStep), count(0), runs(1) {}
+  __device__ __forceinline__ void split(const Split& sp, int kv, float ratio) {
+    if (sp.whole) {
+      runs = kWarps * sp.whole;
+    } else {
+      // (each tile's rounding up is less than one run, and rounding in `ratio` far less than one of all: no more than `most` and the tiles)
+      const float x = ceilf((float)steps * ratio);
+      runs = x < (float)steps ? (int)x : (int)steps;
+      if (runs < 1) runs = 1;
+    }
+    count = tiles * (uint32_t)(kv * runs);
+  }
+  // task `at` of this sequence
+  __device__ __forceinline__ Job job(const Split& sp, int kv, int seq, int at, int start, int queries, int len) const {
+    const int group = (int)((uint32_t)at / (uint32_t)runs), run = at - group * runs, tile = fast_div(group, sp.kv_magic);
+    const int each = (int)(steps / (uint32_t)runs), over = (int)steps - each * runs;  // (so many runs have a step more)
+    return {seq, tile, group - tile * kv, run, runs, run * each + (run < over ? run : over), each + (run < over ? 1 : 0), start, queries, len};
+  }
+};
+// The task of this warp, of up to 32 sequences: every warp looks for its own, and none waits for another (2,600
+// cycles, 3,500 in find_jobs).
+template <int kRows>
+__device__ __forceinline__ Job find_job(const CacheAttnArgs& p, const Split& sp, bool& none) {
+  const int kv = p.cache.kv_heads, lane = threadIdx.x & 31, task0 = blockIdx.x * kWarps, task = task0 + (threadIdx.x >> 5);
   int start = 0, n = 0, len = 0;
-  if (s0 < p.seqs) sequence(p, s0, start, n, len);
-  int steps = 1;
+  if (lane < p.seqs) sequence(p, lane, start, n, len);
+  Cut<kRows> c(sp, n, len);
+  float ratio = 0.0f;
   if (!sp.whole) {
-    // all tiles, and the steps of all tiles: runs fill the GPU once (or, beside many tiles, half of it)
-    uint64_t all = 0, tiles = 0;
-    for (int s = s0; s < p.seqs; s += kThreads) {
-      int st = start, ns = n, ls = len;
-      if (s != s0) sequence(p, s, st, ns, ls);
-      const uint32_t t = (uint32_t)(((int64_t)ns * sp.group + kRows - 1) / kRows);
-      tiles += t;
-      all += (uint64_t)t * (uint32_t)((ls + kStep - 1) / kStep);
-    }
-    for (int o = 16; o > 0; o >>= 1) {
-      all += __shfl_xor_sync(0xffffffffu, all, o);
-      tiles += __shfl_xor_sync(0xffffffffu, tiles, o);
-    }
-    if (lane == 0) { red[2 * (threadIdx.x >> 5)] = all; red[2 * (threadIdx.x >> 5) + 1] = tiles; }
-    __syncthreads();
-    all = tiles = 0;
+    const uint32_t tiles = __reduce_add_sync(0xffffffffu, c.tiles);
+    float steps = (float)c.tiles * (float)c.steps;
+    for (int o = 16; o > 0; o >>= 1) steps += __shfl_xor_sync(0xffffffffu, steps, o);
+    ratio = runs_for_a_step(sp, tiles * (uint32_t)kv, steps * (float)kv);
+  }
+  c.split(sp, kv, ratio);
+  uint32_t upto = c.count;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) { all += red[2 * w]; tiles += red[2 * w + 1]; }
-    all *= kv;
-    tiles *= kv;
-    const uint32_t most = tiles < (uint64_t)(sp.warps / 2) ? sp.warps - (uint32_t)tiles : sp.warps / 2;
-    const uint64_t per = all < (1u << 31) ? ((uint32_t)all + most - 1) / most : (all + most - 1) / most;
-    steps = per < 1 ? 1 : per > 0x3fffffff ? 0x3fffffff : (int)per;
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t u = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += u;
+  }
+  none = (int)__shfl_sync(0xffffffffu, upto, 31) <= task0;
+  const int first = (int)(upto - c.count);
+  const bool has = task >= first && task < first + (int)c.count;
+  Job mine = {-1};
+  if (has) mine = c.job(sp, kv, lane, task - first, start, n, len);
+  const uint32_t who = __ballot_sync(0xffffffffu, has);
+  const int src = who ? __ffs(who) - 1 : 0;
+  int32_t* w = reinterpret_cast<int32_t*>(&mine);
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(Job) / 4); ++i) w[i] = __shfl_sync(0xffffffffu, w[i], src);
+  return mine;
+}
+// The tasks of this block's warps, of any number of sequences. (Counts are 32 bits wide: the host refuses more. Starts that fall may make more; every
+// job is one of its sequence's all the same.)
+template <int kRows>
+__device__ __forceinline__ void find_jobs(const CacheAttnArgs& p, const Split& sp, Job* jobs, float* red) {
+  const int kv = p.cache.kv_heads, first_task = blockIdx.x * kWarps, lane = threadIdx.x & 31, s0 = threadIdx.x;
+  uint32_t* sums = reinterpret_cast<uint32_t*>(red + kWarps);
+  if (threadIdx.x < kWarps) jobs[threadIdx.x].seq = -1;
+  int start = 0, n = 0, len = 0;
+  float ratio = 0.0f;
+  if (!sp.whole) {
+    uint32_t tiles = 0;
+    uint64_t mine = 0;
+    for (int s = s0; s < p.seqs; s += kThreads) {
+      sequence(p, s, start, n, len);
+      const Cut<kRows> c(sp, n, len);
+      tiles += c.tiles;
+      mine += (uint64_t)c.tiles * c.steps;
+    }
+    float steps = (float)mine;
+    tiles = __reduce_add_sync(0xffffffffu, tiles);
+    for (int o = 16; o > 0; o >>= 1) steps += __shfl_xor_sync(0xffffffffu, steps, o);
+    if (lane == 0) { red[threadIdx.x >> 5] = steps; sums[threadIdx.x >> 5] = tiles; }
+    __syncthreads();
+    steps = 0.0f;
+    tiles = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) { steps += red[w]; tiles += sums[w]; }
+    ratio = runs_for_a_step(sp, tiles * (uint32_t)kv, steps * (float)kv);
   }
   uint32_t base = 0;
   for (int b = 0; b < p.seqs; b += kThreads) {
-    int runs = 1, each = steps;
-    uint32_t count = 0;
-    if (b > 0) {
-      start = n = len = 0;
-      if (b + s0 < p.seqs) sequence(p, b + s0, start, n, len);
-    }
-    if (b + s0 < p.seqs) {
-      const uint32_t all = (uint32_t)(len + kStep - 1) / kStep;
-      if (sp.whole) {
-        runs = kWarps;
-        each = (int)(all + kWarps - 1) / kWarps;
-      } else {
-        runs = (int)((all + each - 1) / (uint32_t)each);
-        if (runs < 1) runs = 1;
-      }
-      count = (uint32_t)(((int64_t)n * sp.group + kRows - 1) / kRows) * (uint32_t)(kv * runs);
-    }
+    start = n = len = 0;
+    if (b + s0 < p.seqs) sequence(p, b + s0, start, n, len);
+    Cut<kRows> c(sp, n, len);
+    c.split(sp, kv, ratio);
     // counts before this thread's
-    uint32_t before = count;
+    uint32_t before = c.count;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const uint32_t u = __shfl_up_sync(0xffffffffu, before, o);
       if (lane >= o) before += u;
     }
-    uint32_t* sums = reinterpret_cast<uint32_t*>(red + 2 * kWarps);
     __syncthreads();  // (sums may still be read from the last 256 sequences)
     if (lane == 31) sums[threadIdx.x >> 5] = before;
     __syncthreads();
     uint32_t total = 0;
-    before -= count;
+    before -= c.count;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
       const uint32_t u = sums[w];
@@ -216,22 +268,28 @@ __device__ __forceinline__ void find_jobs(const CacheAttnArgs& p, const Split& s
       total += u;
     }
     const int first = (int)(base + before);
-    if (first < first_task + kWarps && first + (int)count > first_task) {
-      const int lo = first > first_task ? first : first_task;
-      int run = lo - first, group = run / runs, tile = group / kv, head = group - tile * kv;
-      run -= group * runs;
-      for (int at = lo; at < first_task + kWarps && at < first + (int)count; ++at) {
-        jobs[at - first_task] = {b + s0, tile, head, run, runs, each, start, n, len};
-        if (++run == runs) {
-          run = 0;
-          if (++head == kv) { head = 0; ++tile; }
-        }
-      }
-    }
+    for (int at = first > first_task ? first : first_task; at < first_task + kWarps && at < first + (int)c.count; ++at)
+      jobs[at - first_task] = c.job(sp, kv, b + s0, at - first, start, n, len);
     base += total;
     if ((int)base >= first_task + kWarps) break;
   }
   __syncthreads();
+}
+
+// Four channels of a row out, and its logarithm of the sum.
+template <class T>
+__device__ __forceinline__ void finish(const CacheAttnArgs& p, const Split& sp, int start, int head, int rr, int ch, float4 sum, float all, float top, float cs) {
+  const int j = fast_div(rr, sp.group_magic), h = head * sp.group + rr - j * sp.group;
+  const int64_t token = start + j;
+  const float inv = top == -INFINITY && all == 0.0f ? 0.0f : 1.0f / all;
+  T* y = static_cast<T*>(p.out) + token * p.ldo + (int64_t)h * p.ldoh + ch;
+  put(y, sum.x * inv); put(y + 1, sum.y * inv); put(y + 2, sum.z * inv); put(y + 3, sum.w * inv);
+  if (p.lse && ch == 0) p.lse[token * p.heads + h] = fmaf(top, cs, log2f(all)) * kLn2;
+}
+__device__ __forceinline__ float4 load_cluster(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+  return v;
 }
 
 // Places that row r of a tile sees.
@@ -245,7 +303,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
   constexpr int kStages = stages(D), kStage = stage_bytes(D), kBlock = kStage / 2, kRows = 8 * NT;
   constexpr int KW = D / 32, VW = D / 64;  // words of a key row, and of a value row, that a lane reads
   extern __shared__ __align__(128) uint8_t smem[];  // [warp][stage]; at the end the warps' sums
-  __shared__ uint64_t bars[kWarps * kStages], red[2 * kWarps + kWarps / 2];
+  __shared__ uint64_t bars[kWarps * kStages], red[kWarps];
   __shared__ Job jobs[kWarps];
   __shared__ int abort_word;
   __shared__ float wm[kWarps][kRows], wl[kWarps][kRows], wc[kWarps][kRows];  // rows' maxima, sums, factors of scores
@@ -254,10 +312,23 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
   if (threadIdx.x < kWarps * kStages) mbar_init(smem_u32(&bars[threadIdx.x]), 1);
   if (threadIdx.x == 0) abort_word = 0;
   fence_barrier_init();
+  __syncthreads();
   grid_dep_wait();
-  find_jobs<kRows>(p, sp, jobs, red);
+  Job jb;
+  bool none;
+  if (p.seqs <= 32) {
+    jb = find_job<kRows>(p, sp, none);
+    if (lane == 0) jobs[warp] = jb;
+  } else {
+    find_jobs<kRows>(p, sp, jobs, reinterpret_cast<float*>(red));
+    jb = jobs[warp];
+    none = jobs[0].seq < 0;
+  }
   grid_dep_launch();
-  const Job jb = jobs[warp];
+  if (none) {  // (a cluster's blocks all have none, or none of them)
+    if (!sp.whole && threadIdx.x == 0) reinterpret_cast<Span*>(sp.meta)[blockIdx.x] = Span{};
+    return;
+  }
   const int head = jb.head;
   const bool idle = jb.seq < 0;
   const int last_row = idle ? 0 : jb.queries * sp.group - jb.tile * kRows;  // rows of this tile and behind it
@@ -269,7 +340,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
   }
 
   // the steps of the run that lie before the last place that a row sees
-  const int step0 = idle ? 0 : jb.run * jb.steps;
+  const int step0 = idle ? 0 : jb.step0;
   int end = (lim_any + kStep - 1) / kStep;  // (lim_any <= 0: none)
   end = idle ? 0 : end < step0 + jb.steps ? end : step0 + jb.steps;
   const int mine = end > step0 ? end - step0 : 0;
@@ -310,7 +381,25 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
     blk = (blk + 2) & (blocks_of_page - 1);
     ist = ist == kStages - 1 ? 0 : ist + 1;
   };
-  // (the barriers were set up before find_jobs's barriers of the block)
+  // the query rows' loads, and the first copies (the warp's barriers are set up)
+  uint4 qraw[NT][KW];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int r = t * 8 + g;
+    const bool live = r < last_row;
+    const int j = live ? fast_div(jb.tile * kRows + r, sp.group_magic) : 0, h = jb.tile * kRows + r - j * sp.group;
+    const T* x = static_cast<const T*>(p.q) + (live ? (int64_t)(jb.start + j) * p.ldq + (int64_t)(head * sp.group + h) * p.ldqh : 0) + q * (D / 4);
+#pragma unroll
+    for (int w = 0; w < KW; ++w) {
+      qraw[t][w] = make_uint4(0, 0, 0, 0);
+      if (live && sp.q_vec) {
+        qraw[t][w] = *reinterpret_cast<const uint4*>(x + 8 * w);
+      } else if (live) {
+        const uint16_t* y = reinterpret_cast<const uint16_t*>(x + 8 * w);
+        qraw[t][w] = make_uint4(y[0] | (uint32_t)y[1] << 16, y[2] | (uint32_t)y[3] << 16, y[4] | (uint32_t)y[5] << 16, y[6] | (uint32_t)y[7] << 16);
+      }
+    }
+  }
   for (int i = 0; i < kStages - 1 && i < mine; ++i) issue(i);
 
   // this lane's query rows (column g of each tile) as float16 with a power of two in front; the sums and factors of columns 2q, 2q + 1
@@ -318,24 +407,15 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
   float qs[NT][2], qb[NT][2], c2[NT][2];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int r = t * 8 + g;
     float f[KW][8], top = 0.0f, sum = 0.0f, odd = 0.0f;
-    const bool live = r < last_row;
-    const int j = live ? fast_div(jb.tile * kRows + r, sp.group_magic) : 0, h = jb.tile * kRows + r - j * sp.group;
-    const T* x = static_cast<const T*>(p.q) + (live ? (int64_t)(jb.start + j) * p.ldq + (int64_t)(head * sp.group + h) * p.ldqh : 0) + q * (D / 4);
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
-      if (live && sp.q_vec) {
-        const uint4 v = *reinterpret_cast<const uint4*>(x + 8 * w);
-        const T* e = reinterpret_cast<const T*>(&v);
+      const T* e = reinterpret_cast<const T*>(&qraw[t][w]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[w][i] = to_f32(e[i]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[w][i] = live ? to_f32(x[8 * w + i]) : 0.0f;
+      for (int i = 0; i < 8; ++i) {
+        f[w][i] = to_f32(e[i]);
+        top = fmaxf(top, fabsf(f[w][i]));
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[w][i]));
     }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
@@ -571,19 +651,12 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
                                      fmaf(o[t][4 * u + 3][c + 2 * h], back, z));
     }
   __syncthreads();
-  // groups of runs that belong together, the block's warps from `w0` to `w1`
-  Span* span = reinterpret_cast<Span*>(sp.meta) + blockIdx.x;
-  int goes_on = 0;
-  for (int w0 = 0, w1; w0 < kWarps && jobs[w0].seq >= 0; w0 = w1) {
-    const Job j0 = jobs[w0];
-    w1 = w0 + j0.runs - j0.run < kWarps ? w0 + j0.runs - j0.run : kWarps;
-    const bool whole = j0.run == 0 && w0 + j0.runs == w1;
-    const int behind = j0.queries * sp.group - j0.tile * kRows, rows = behind < kRows ? behind : kRows;
-    if (j0.run == 0 && !whole) {
-      goes_on = 1;
-      if (threadIdx.x == 0) *span = {(int)((blockIdx.x * kWarps + w0 + j0.runs - 1) / kWarps), j0.start, j0.queries, j0.tile, j0.head, {0, 0, 0}};
-    }
-    for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
+  // groups of runs that belong together: the block's warps from `w0` to `w1` join theirs
+  if (!idle) {
+    const int w0 = warp > jb.run ? warp - jb.run : 0, run0 = jb.run - (warp - w0), w1 = w0 + jb.runs - run0 < kWarps ? w0 + jb.runs - run0 : kWarps;
+    const bool whole = run0 == 0 && w0 + jb.runs == w1;
+    const int rows = last_row < kRows ? last_row : kRows;
+    for (int i = threadIdx.x - w0 * 32; i < rows * (D / 4); i += (w1 - w0) * 32) {
       const int row = i / (D / 4), ch = (i - row * (D / 4)) * 4;
       float top = -INFINITY;
       for (int w = w0; w < w1; ++w) top = fmaxf(top, wm[w][row]);
@@ -597,47 +670,138 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
         sum.x = fmaf(v.x, f, sum.x); sum.y = fmaf(v.y, f, sum.y); sum.z = fmaf(v.z, f, sum.z); sum.w = fmaf(v.w, f, sum.w);
       }
       if (whole) {
-        const int rr = j0.tile * kRows + row, j = fast_div(rr, sp.group_magic), h = j0.head * sp.group + rr - j * sp.group;
-        const int64_t token = j0.start + j;
-        const float inv = top == -INFINITY && all == 0.0f ? 0.0f : 1.0f / all;
-        T* y = static_cast<T*>(p.out) + token * p.ldo + (int64_t)h * p.ldoh + ch;
-        put(y, sum.x * inv); put(y + 1, sum.y * inv); put(y + 2, sum.z * inv); put(y + 3, sum.w * inv);
-        if (p.lse && ch == 0) p.lse[token * p.heads + h] = fmaf(top, cs, log2f(all)) * kLn2;
+        finish<T>(p, sp, jb.start, head, jb.tile * kRows + row, ch, sum, all, top, cs);
       } else {
-        float* part = sp.part + (((int64_t)blockIdx.x * 2 + (j0.run == 0 ? 1 : 0)) * kRows + row) * (D + 4);
+        float* part = sp.whole ? reinterpret_cast<float*>(smem) + (kWarps * kRows + row) * kPitch
+                               : sp.part + (((int64_t)blockIdx.x * 2 + (run0 == 0 ? 1 : 0)) * kRows + row) * (D + 4);
         *reinterpret_cast<float4*>(part + ch) = sum;
         if (ch == 0) *reinterpret_cast<float4*>(part + D) = make_float4(top, all, cs, 0.0f);
       }
     }
   }
-  if (!sp.whole && !goes_on && threadIdx.x == 0) span->last = 0;
+  if (sp.whole > 1) {
+    // a cluster's blocks have one group: each joins its share of the rows from all of them
+    cluster_sync();
+    const uint32_t rank = cluster_ctarank(), parts = smem_u32(smem) + kWarps * kRows * kPitch * 4;
+    const int items = idle ? 0 : (last_row < kRows ? last_row : kRows) * (D / 4), share = (items + sp.whole - 1) / sp.whole;
+    const int to = items < ((int)rank + 1) * share ? items : ((int)rank + 1) * share;
+    for (int i = (int)rank * share + threadIdx.x; i < to; i += kThreads) {
+      const int row = i / (D / 4), ch = (i - row * (D / 4)) * 4;
+      const uint32_t at = parts + row * kPitch * 4;
+      float4 v[kMostBlocks], z[kMostBlocks];
+      float top = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < kMostBlocks; ++b)
+        if (b < sp.whole) {
+          v[b] = load_cluster(mapa_shared(at + 4 * ch, b));
+          z[b] = load_cluster(mapa_shared(at + 4 * D, b));
+          top = fmaxf(top, z[b].x);
+        }
+      const float ref = top == -INFINITY ? 0.0f : top;
+      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      float all = 0.0f;
+#pragma unroll
+      for (int b = 0; b < kMostBlocks; ++b)
+        if (b < sp.whole) {
+          const float f = ex2((z[b].x - ref) * z[0].z);
+          all = fmaf(z[b].y, f, all);
+          sum.x = fmaf(v[b].x, f, sum.x); sum.y = fmaf(v[b].y, f, sum.y); sum.z = fmaf(v[b].z, f, sum.z); sum.w = fmaf(v[b].w, f, sum.w);
+        }
+      finish<T>(p, sp, jb.start, head, jb.tile * kRows + row, ch, sum, all, top, z[0].z);
+    }
+    __syncwarp();
+    cluster_sync();  // no block goes while another reads from it
+  } else if (!sp.whole && threadIdx.x == 0) {
+    // the group that begins in this block and goes on
+    const Job last = jobs[kWarps - 1];
+    const int run0 = last.run - (kWarps - 1);  // of the first warp, if this group has it
+    const bool begins = last.seq >= 0 && run0 <= 0, goes_on = last.run + 1 < last.runs;
+    Span sn = {0, last.start, last.queries, last.tile, last.head, {0, 0, 0}};
+    if (begins && goes_on) sn.last = (int)(((int64_t)blockIdx.x * kWarps - run0 + last.runs - 1) / kWarps);
+    reinterpret_cast<Span*>(sp.meta)[blockIdx.x] = sn;
+  }
 }
 
-// A block for a row of the group of runs that begins in block blockIdx.x and goes on: its parts, in a fixed order.
+// Joins the parts of the group of runs that begins in block blockIdx.x and goes on, in a fixed order: a warp to a row where a warp's lanes hold all maxima,
+// as those of most groups, and else a block to a row (its loads are shared out then: 152 parts take 3.4 us, 17 a warp, where 5 take 1.3).
 template <class T, int D>
-__global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_constant__ Split sp, const int rows) {
-  constexpr int kMost = 152 * 2 + 4;  // parts: a group has at most as many runs as fill the GPU
-  __shared__ float weight[kMost], so[kWarps][D], red[kWarps];
+__global__ void __launch_bounds__(kThreads, 3) combine_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_constant__ Split sp, const int rows) {
+  constexpr int kParts = 152 * 2 + 4;  // a group has at most as many runs as fill the GPU
+  constexpr int kQuads = D / 4, kSlots = kThreads / kQuads, kAhead = 8;
+  __shared__ float weight[kParts], red[kWarps];
+  __shared__ __align__(16) float so[kSlots][D];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   grid_dep_wait();
   const Span span = reinterpret_cast<const Span*>(sp.meta)[blockIdx.x];
-  const int row = blockIdx.y, rr = span.tile * rows + row, first = blockIdx.x;
-  const int parts = span.last - first + 1;
+  const int first = blockIdx.x, parts = span.last - first + 1, behind = span.queries * sp.group - span.tile * rows;
   // (starts that fall make more tasks than there are blocks: such groups are left)
-  if (span.last <= first || span.last >= (int)gridDim.x || parts > kMost || rr >= span.queries * sp.group) return;
+  if (span.last <= first || span.last >= (int)gridDim.x || parts > kParts) return;
+  const bool few = parts <= 32;
+  const int row = few ? blockIdx.y * kWarps + warp : blockIdx.y;
+  if (row >= rows || row >= behind) return;
   // (what a block goes on with comes first among its two parts, what it begins second)
   const float* part = sp.part + ((int64_t)first * 2 * rows + row) * (D + 4);
   const int64_t pitch = (int64_t)2 * rows * (D + 4), begin = rows * (D + 4);
+  const int rr = span.tile * rows + row;
+  float4 v[kAhead], z[2];
+  if (few) {
+    constexpr int kWide = D < 128 ? D / 4 : 32, kAt = 32 / kWide;  // lanes across a row, rows of parts at once
+    const int at = lane / kWide;
+    z[0] = make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
+    if (lane < parts) z[0] = *reinterpret_cast<const float4*>(part + lane * pitch + (lane == 0 ? begin : 0) + D);
+    float top, all = 0.0f, cs = 0.0f, f = 0.0f;
+#pragma unroll 1
+    for (int ch = 4 * (lane & (kWide - 1)); ch - 4 * (lane & (kWide - 1)) < D; ch += 128) {
+      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      for (int c0 = 0; c0 < parts; c0 += kAhead * kAt) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int c = c0 + k * kAt + at;
+          v[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          if (c < parts && ch < D) v[k] = *reinterpret_cast<const float4*>(part + c * pitch + (c == 0 ? begin : 0) + ch);
+        }
+        if (c0 == 0 && ch < 128) {  // (every lane at once)
+          top = z[0].x;
+          for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          cs = __shfl_sync(0xffffffffu, z[0].z, 0);
+          f = ex2((z[0].x - (top == -INFINITY ? 0.0f : top)) * cs);
+          all = z[0].y * f;
+          for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int c = c0 + k * kAt + at;
+          const float e = __shfl_sync(0xffffffffu, f, c & 31);
+          if (c < parts) { sum.x = fmaf(v[k].x, e, sum.x); sum.y = fmaf(v[k].y, e, sum.y); sum.z = fmaf(v[k].z, e, sum.z); sum.w = fmaf(v[k].w, e, sum.w); }
+        }
+      }
+      if constexpr (kAt == 2) {
+        sum.x += __shfl_xor_sync(0xffffffffu, sum.x, 16); sum.y += __shfl_xor_sync(0xffffffffu, sum.y, 16);
+        sum.z += __shfl_xor_sync(0xffffffffu, sum.z, 16); sum.w += __shfl_xor_sync(0xffffffffu, sum.w, 16);
+      }
+      if (at == 0 && ch < D) finish<T>(p, sp, span.start, span.head, rr, ch, sum, all, top, cs);
+    }
+    return;
+  }
+  const int slot = threadIdx.x / kQuads, quad = threadIdx.x - slot * kQuads;
+  // all that these loads need is known: the first sums come beside the maxima
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, cs = part[begin + D + 2], top = -INFINITY;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int c = threadIdx.x + k * kThreads;
-    if (c < parts) {
-      const float4 v = *reinterpret_cast<const float4*>(part + c * pitch + (c == 0 ? begin : 0) + D);
-      m[k] = v.x; l[k] = v.y;
-      top = fmaxf(top, v.x);
-    }
+    if (c < parts) z[k] = *reinterpret_cast<const float4*>(part + c * pitch + (c == 0 ? begin : 0) + D);
   }
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    const int c = slot + k * kSlots;
+    if (slot < kSlots && c < parts) v[k] = *reinterpret_cast<const float4*>(part + c * pitch + (c == 0 ? begin : 0) + 4 * quad);
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if ((int)threadIdx.x + k * kThreads < parts) {
+      m[k] = z[k].x; l[k] = z[k].y;
+      top = fmaxf(top, m[k]);
+    }
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   if (lane == 0) red[warp] = top;
   __syncthreads();
@@ -655,30 +819,37 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant
   for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
   __syncthreads();
   if (lane == 0) red[warp] = all;
-  float o[D / 32];
+  float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (slot < kSlots) {
+    for (int c0 = slot; c0 < parts; c0 += kAhead * kSlots) {
+      if (c0 > slot) {
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) o[i] = 0.0f;
-#pragma unroll 8
-  for (int c = warp; c < parts; c += kWarps) {
-    const float f = weight[c];
-    const float* x = part + c * pitch + (c == 0 ? begin : 0) + lane;
+        for (int k = 0; k < kAhead; ++k) {
+          const int c = c0 + k * kSlots;
+          if (c < parts) v[k] = *reinterpret_cast<const float4*>(part + c * pitch + 4 * quad);
+        }
+      }
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) o[i] = fmaf(x[32 * i], f, o[i]);
+      for (int k = 0; k < kAhead; ++k) {
+        const int c = c0 + k * kSlots;
+        if (c < parts) {
+          const float f = weight[c];
+          sum.x = fmaf(v[k].x, f, sum.x); sum.y = fmaf(v[k].y, f, sum.y); sum.z = fmaf(v[k].z, f, sum.z); sum.w = fmaf(v[k].w, f, sum.w);
+        }
+      }
+    }
+    *reinterpret_cast<float4*>(&so[slot][4 * quad]) = sum;
   }
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) so[warp][lane + 32 * i] = o[i];
   __syncthreads();
   all = 0.0f;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) all += red[w];
-  for (int ch = threadIdx.x; ch < D; ch += kThreads) {
-    float sum = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) sum += so[w][ch];
-    const int j = fast_div(rr, sp.group_magic), h = span.head * sp.group + rr - j * sp.group;
-    const int64_t token = span.start + j;
-    put(static_cast<T*>(p.out) + token * p.ldo + (int64_t)h * p.ldoh + ch, top == -INFINITY && all == 0.0f ? 0.0f : sum / all);
-    if (p.lse && ch == 0) p.lse[token * p.heads + h] = fmaf(top, cs, log2f(all)) * kLn2;
+  if (slot == 0) {
+    for (int k = 1; k < kSlots; ++k) {
+      const float4 u = *reinterpret_cast<const float4*>(&so[k][4 * quad]);
+      sum.x += u.x; sum.y += u.y; sum.z += u.z; sum.w += u.w;
+    }
+    finish<T>(p, sp, span.start, span.head, rr, 4 * quad, sum, all, top, cs);
   }
 }
 
@@ -697,8 +868,9 @@ static Sizes sizes(int64_t tokens, int32_t seqs, int32_t heads, int32_t kv_heads
   s.tiles = tokens == seqs ? seqs * ((group + s.rows - 1) / s.rows) : tokens * group / s.rows + seqs;
   // (tokens == seqs with starts: each of n > 0 queries has at most ceil(n group / rows) <= n ceil(group / rows) tiles)
   s.warps = 152 * (two || dim > 128 ? 1 : 2) * kWarps;
-  // tasks: at most `warps`, and one more for each tile and head
-  s.blocks = (s.warps + s.tiles * kv_heads + kWarps - 1) / kWarps;
+  // tasks: at most `warps`, or half of that beside more tiles and heads than the other half
+  const int64_t tasks = s.warps / 2 + s.tiles * kv_heads;
+  s.blocks = ((tasks > s.warps ? tasks : s.warps) + kWarps - 1) / kWarps;
   s.part_off = ((size_t)s.blocks * sizeof(Span) + 255) / 256 * 256;
   s.bytes = s.part_off + (size_t)s.blocks * 2 * s.rows * (dim + 4) * 4;
   return s;
@@ -708,30 +880,38 @@ template <class T, int D, int NT>
 static cudaError_t run(const CacheAttnArgs& a, const Sizes& s, cudaStream_t stream) {
   Split sp{};
   sp.warps = s.warps;
-  // up to four steps a warp: a second kernel's launch costs more than a finer split gives
-  sp.whole = ((int64_t)a.columns << a.cache.page_shift) <= 4 * kWarps * kStep;
   sp.group = a.heads / a.cache.kv_heads;
   sp.group_magic = div_magic(sp.group);
+  sp.kv_magic = div_magic(a.cache.kv_heads);
   sp.q_vec = (reinterpret_cast<uintptr_t>(a.q) & 15) == 0 && (a.ldq | a.ldqh) % 8 == 0;
   sp.meta = reinterpret_cast<int32_t*>(a.ws);
   sp.part = reinterpret_cast<float*>(a.ws + s.part_off);
-  constexpr int ring = kWarps * stages(D) * stage_bytes(D), join = kWarps * 8 * NT * (D + 4) * 4;
+  constexpr int ring = kWarps * stages(D) * stage_bytes(D), join = (kWarps + 1) * 8 * NT * (D + 4) * 4;
   constexpr int smem = ring > join ? ring : join;
   static_assert(smem <= 227 * 1024 - 4096, "");
   cudaError_t e = cudaFuncSetAttribute(cache_attention_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   const int64_t heads_tiles = s.tiles * a.cache.kv_heads;
-  const int64_t blocks = sp.whole ? heads_tiles : s.blocks;
+  const int64_t places = (int64_t)a.columns << a.cache.page_shift;
+  // As many blocks a row tile and head as leave each warp a step, within one block an SM; taken while a warp has no more than four steps (2 heads, clusters of
+  // eight: 2000 places 6.6 us, 10.0 in split runs; 4000 7.8, 10.3; 8000 10.3, 10.9; where one block each fills the GPU, 1024 places take 12.6 either way).
+  int cluster = 1;
+  while (cluster < kMostBlocks && cluster * kWarps * kStep < places && 2 * cluster * heads_tiles <= 152) cluster *= 2;
+  sp.whole = places <= 4 * kWarps * kStep * cluster ? cluster : 0;
+  const int64_t blocks = sp.whole ? heads_tiles * sp.whole : s.blocks;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)blocks);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
-  cudaLaunchAttribute at[1];
+  cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = sp.whole ? sp.whole : 1;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = sp.whole > 1 ? 2 : 1;
   e = cudaLaunchKernelEx(&cfg, cache_attention_kernel<T, D, NT>, a, sp);
   if (e != cudaSuccess || sp.whole) return e;
   const int most = a.starts || sp.group > s.rows ? s.rows : sp.group;  // rows of a tile that can be there

@@ -119,6 +119,33 @@ def test_many_sequences_of_uneven_lengths():
     close(lse, e, et)
 
 
+# Few sequences and heads: one, two, four or eight blocks join a row; longer tables split it among all. Without a place, with one, and with fewer steps than warps.
+@pytest.mark.parametrize("lens,asked,heads,kv,dim,dtype", [([1024], [1], 8, 8, 128, BF16), ([8192, 1, 0], [1, 1, 1], 12, 3, 64, F16), ([700, 300, 2, 0], [3, 5, 4, 1], 14, 2, 64, BF16),
+                                                           ([2000], [9], 6, 1, 192, F16), ([4096, 33], [1, 1], 20, 1, 256, BF16), ([513] * 19, [1] * 19, 16, 8, 128, F16),
+                                                           ([8193, 8193], [1, 1], 4, 1, 128, BF16), ([3000] * 9, [2] * 9, 8, 1, 128, F16)])
+def test_few_rows_in_several_blocks(lens, asked, heads, kv, dim, dtype):
+    c = Case(lens, asked, heads, kv, dim, 64, dtype, seed=13)
+    o, tol, e, et = c.want(dim ** -0.5)
+    for _ in range(2):
+        got, lse = c.run(lse=True)
+        close(got, o, tol)
+        close(lse, e, et)
+    assert aqd.device_status() == 0
+
+
+# (a warp looks through up to 128 sequences by itself; a block looks through more together)
+@pytest.mark.parametrize("count", [31, 33, 128, 129, 257])
+@pytest.mark.parametrize("longest", [100, 5000])
+def test_any_number_of_sequences(count, longest):
+    lens = [(7 * i) % 90 for i in range(count)]
+    lens[count // 2] = longest
+    c = Case(lens, [1 + i % 2 for i in range(count)], 4, 1, 64, 16, BF16, seed=14)
+    o, tol, e, et = c.want(0.125)
+    got, lse = c.run(lse=True)
+    close(got, o, tol)
+    close(lse, e, et)
+
+
 def test_strides_and_rows_left_as_they_were():
     c = Case([100, 40, 300], [3, 1, 2], 6, 2, 128, 32, BF16, seed=4)
     want = c.run()
