@@ -5,9 +5,12 @@
 // i + rot / 2), or that hold its pairs themselves (interleaved), so norm, rotation and codes take one read and one write, and what crosses
 // lanes is a sum of squares and a row's lowest and highest value. Bound by memory, if the instructions for a value stay below about eight: a
 // warp takes a token's heads in turn (rows_kernel), its lanes keep their places in the row, and with them the products of weights, cosines and sines;
-// float32 goes in pairs; 16-bit minima and maxima stay packed; codes come out of the bits of one multiply-add. (A row at a time with indexes, weights and turns
-// looked up for each: 8192 tokens of 40 heads of 128 in bfloat16 47 us, 16,384 tokens' 16 rows to codes 46 and back 34.)
-// Rows at any address, and rotations of any even length, take heads_kernel, a value at a time.
+// float32 goes in pairs; 16-bit minima and maxima stay packed; codes come out of the bits of one multiply-add.
+//   8192 tokens of 40 heads of 128 in bfloat16: 38.4 us, 168 MB at 4.4 TB/s (47 with a row at a time, its indexes, weights and turns looked up for
+//   each); with keys and values to the cache 47.3, 171 MB. 16,384 tokens' 16 rows to codes: 20.3 us, 85 MB at 4.2 TB/s (46), and back 14.8 (34).
+// What holds them back is bytes on their way: 80 registers leave 24 warps an SM, with two rows' loads each (counters: 52 to 68% of the issue slots,
+// most waits for loads). Four rows at once (75 registers for codes, fewer warps) 21.7, weights and turns in shared memory 52 to 78.
+// Rows at any address, and rotations of any even length, take heads_kernel, a value at a time (14 heads of 64 in float32, 777 tokens: 4.4 us).
 //
 // The angle of position p at frequency f is p f / 2 pi turns, of which the whole ones do not count: with u = frac(f / 2 pi) 2^64 cut to
 // an integer, p u mod 2^64 is the fraction, exact but for |p| (1 + |f|) 2^-64 of a turn, whatever the position. A block's sines and cosines are computed
@@ -386,10 +389,15 @@ __device__ __forceinline__ uint32_t codes_of(const RowStep& rs, const uint4& v) 
   return rs.inv > 0.0f ? w - kRest : 0u;
 }
 
+template <bool k>
+struct Bool {
+  static constexpr bool value = k;
+};
+
 // A warp, or several, to a token: the lanes of a row keep their places in it while the warp goes through the heads. lanes: a power of two, those past the
 // row's end idle. `share` warps (1, 2, 4 or 8) take a token's rows in turn. kPlain: keys and values to the cache as they are.
 template <class T, bool kCache, bool kInter, bool kPlain>
-__global__ void __launch_bounds__(kThreads, kPlain ? 4 : kCache ? 2 : 3) rows_kernel(const QkArgs p, const int share, const int lanes, const int lanes_log2) {
+__global__ void __launch_bounds__(kThreads, kPlain ? 4 : 3) rows_kernel(const QkArgs p, const int share, const int lanes, const int lanes_log2) {
   constexpr int V = 16 / sizeof(T), kPairs = V / 2;
   extern __shared__ float2 turns[];  // [tokens of the block][rot / 2]: cosine, sine
   tc::grid_dep_wait();
@@ -455,9 +463,9 @@ __global__ void __launch_bounds__(kThreads, kPlain ? 4 : kCache ? 2 : 3) rows_ke
     }
   };
   // two rows' vectors at once: their loads are on the way together
-  auto fetch = [&](const T* x, int64_t ldh, int h, int n, uint4 (&a)[2], uint4 (&b)[2]) {
+  auto fetch = [&](auto& a, auto& b, const T* x, int64_t ldh, int h, int n) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < (int)(sizeof(a) / sizeof(uint4)); ++k) {
       a[k] = b[k] = make_uint4(0, 0, 0, 0);
       if (in && h + k * step < n) {
         const T* y = x + (int64_t)(h + k * step) * ldh;
@@ -468,7 +476,8 @@ __global__ void __launch_bounds__(kThreads, kPlain ? 4 : kCache ? 2 : 3) rows_ke
   };
   const float per_value = 1.0f / (float)p.dim;
   // rows of queries or keys: norm, turn, out, and keys to the cache
-  auto run = [&](const T* x, int64_t ldh, int n, const void* weight, T* y, int64_t ldyh, bool keys) {
+  auto run = [&](auto cached, const T* x, int64_t ldh, int n, const void* weight, T* y, int64_t ldyh) {
+    constexpr bool kCached = decltype(cached)::value;
     // out = in * own + partner * other, and times 1 / rms at the end
     uint64_t own_a[kPairs], own_b[kPairs], other_a[kPairs], other_b[kPairs];
     const bool plain = kPlain || (!weight && half == 0);
@@ -501,11 +510,12 @@ __global__ void __launch_bounds__(kThreads, kPlain ? 4 : kCache ? 2 : 3) rows_ke
         own_b[j / 2] = two_of(wb[j] * d0.x, wb[j + 1] * d1.x);
       }
     }
-    for (int h0 = first; h0 < n; h0 += 2 * step) {
-      uint4 va[2], vb[2];
-      fetch(x, ldh, h0 + group, n, va, vb);
+    constexpr int kAtOnce = kCached && !kPlain ? 1 : 2;  // (with the codes' numbers, two rows would not fit three blocks' registers)
+    for (int h0 = first; h0 < n; h0 += kAtOnce * step) {
+      uint4 va[kAtOnce], vb[kAtOnce];
+      fetch(va, vb, x, ldh, h0 + group, n);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
+      for (int k = 0; k < kAtOnce; ++k) {
         if (h0 + k * step >= n) break;
         const int h = h0 + group + k * step;
         uint4 a = va[k], b = vb[k];
@@ -555,19 +565,17 @@ __global__ void __launch_bounds__(kThreads, kPlain ? 4 : kCache ? 2 : 3) rows_ke
           *reinterpret_cast<uint4*>(z + ia) = a;
           *reinterpret_cast<uint4*>(z + ib) = b;
         }
-        if constexpr (kCache) {
-          if (keys) to_cache(h, h < n, false, a, b);  // codes are of the rounded values, whether these are stored or not
-        }
+        if constexpr (kCached) to_cache(h, h < n, false, a, b);  // codes are of the rounded values, whether these are stored or not
       }
     }
   };
-  if (!kPlain && p.heads > 0) run(static_cast<const T*>(p.q) + token * p.ldq, p.ldqh, p.heads, p.q_weight, static_cast<T*>(p.q_out) + token * p.ldqo, p.ldqoh, false);
-  run(static_cast<const T*>(p.k) + token * p.ldk, p.ldkh, p.kv_heads, p.k_weight, p.k_out ? static_cast<T*>(p.k_out) + token * p.ldko : nullptr, p.ldkoh, true);
+  if (!kPlain && p.heads > 0) run(Bool<false>(), static_cast<const T*>(p.q) + token * p.ldq, p.ldqh, p.heads, p.q_weight, static_cast<T*>(p.q_out) + token * p.ldqo, p.ldqoh);
+  run(Bool<kCache>(), static_cast<const T*>(p.k) + token * p.ldk, p.ldkh, p.kv_heads, p.k_weight, p.k_out ? static_cast<T*>(p.k_out) + token * p.ldko : nullptr, p.ldkoh);
   if constexpr (kCache) {
     const T* x = static_cast<const T*>(p.v) + token * p.ldv;
     for (int h0 = first; h0 < p.kv_heads; h0 += 2 * step) {
       uint4 a[2], b[2];
-      fetch(x, p.ldvh, h0 + group, p.kv_heads, a, b);
+      fetch(a, b, x, p.ldvh, h0 + group, p.kv_heads);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         if (h0 + k * step >= p.kv_heads) break;
@@ -578,83 +586,74 @@ __global__ void __launch_bounds__(kThreads, kPlain ? 4 : kCache ? 2 : 3) rows_ke
   }
 }
 
-// `share` warps to kTokens tokens; a lane takes two words of 8 codes of a row, half a row apart (its values' stores are then whole sectors with its
-// neighbours'), `lanes` lanes a row, keys' rows and then values'. Four rows' loads are on the way together, of each token.
-template <class T, bool kVec, int kTokens>
+// `share` warps to a token, as above; a lane takes two words of 8 codes of a row, half a row apart (its values' stores are whole sectors with its neighbours':
+// 16,384 tokens of 8 heads of 128 back to bfloat16 in 14.2 us, 19 with 16 codes together), `lanes` lanes a row, keys' rows and then values'.
+template <class T, bool kVec>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheReadArgs p, const int share, const int lanes, const int lanes_log2) {
   tc::grid_dep_wait();
   const CacheGeom& c = p.cache;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & (lanes - 1), groups = 32 >> lanes_log2, wide = c.dim >> 4;
-  const int64_t token0 = ((int64_t)blockIdx.x * (kThreads / 32) + warp) / share * kTokens;
-  if (token0 >= p.tokens || lane >= wide) return;
-  const int64_t head_bytes = ((int64_t)1 << (c.page_shift - 4)) * 16 * (c.dim + 8);
-  const uint8_t* blk[kTokens];
-  int row[kTokens];
-#pragma unroll
-  for (int t = 0; t < kTokens; ++t) {
-    const int64_t slot = token0 + t < p.tokens ? p.slots[token0 + t] : -1;
-    row[t] = 0;
-    blk[t] = in_cache(c, slot) ? place(c, slot, 0, row[t]) : nullptr;
-  }
+  const int64_t token = ((int64_t)blockIdx.x * (kThreads / 32) + warp) / share;
+  if (token >= p.tokens || lane >= wide) return;
+  const int64_t slot = p.slots[token], head_bytes = ((int64_t)1 << (c.page_shift - 4)) * 16 * (c.dim + 8);
+  int row = 0;
+  const uint8_t* blk = in_cache(c, slot) ? place(c, slot, 0, row) : nullptr;
   const int step = share * groups;
   for (int r0 = (warp % share) * groups + ((threadIdx.x & 31) >> lanes_log2); r0 < 2 * c.kv_heads; r0 += 4 * step) {
-    uint2 words[kTokens][4];
-    uint32_t steps[kTokens][4];
+    // four rows' loads on the way together
+    uint2 words[4];
+    uint32_t steps[4];
 #pragma unroll
-    for (int t = 0; t < kTokens; ++t)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int r = r0 + k * step;
-        const bool is_v = r >= c.kv_heads;
-        words[t][k] = make_uint2(0, 0);
-        steps[t][k] = 0;
-        if (blk[t] && r < 2 * c.kv_heads) {
-          const uint8_t* x = blk[t] + (is_v ? r - c.kv_heads : r) * head_bytes;
-          const uint32_t* w = reinterpret_cast<const uint32_t*>(x + (is_v ? 8 * c.dim : 0) + row[t] * (c.dim >> 1)) + lane;
-          words[t][k] = make_uint2(w[0], w[wide]);
-          steps[t][k] = *reinterpret_cast<const uint32_t*>(x + 16 * c.dim + (is_v ? 64 : 0) + 4 * row[t]);
-        }
+    for (int k = 0; k < 4; ++k) {
+      const int r = r0 + k * step;
+      const bool is_v = r >= c.kv_heads;
+      words[k] = make_uint2(0, 0);
+      steps[k] = 0;
+      if (blk && r < 2 * c.kv_heads) {
+        const uint8_t* x = blk + (is_v ? r - c.kv_heads : r) * head_bytes;
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(x + (is_v ? 8 * c.dim : 0) + row * (c.dim >> 1)) + lane;
+        words[k] = make_uint2(w[0], w[wide]);
+        steps[k] = *reinterpret_cast<const uint32_t*>(x + 16 * c.dim + (is_v ? 64 : 0) + 4 * row);
       }
+    }
 #pragma unroll
-    for (int t = 0; t < kTokens; ++t)
+    for (int k = 0; k < 4; ++k) {
+      const int r = r0 + k * step;
+      const bool is_v = r >= c.kv_heads;
+      T* y = is_v ? static_cast<T*>(p.v) : static_cast<T*>(p.k);
+      if (r >= 2 * c.kv_heads || !y) continue;
+      y += token * (is_v ? p.ldv : p.ldk) + (is_v ? r - c.kv_heads : r) * (is_v ? p.ldvh : p.ldkh) + lane * 8;
+      const float low = __uint_as_float(steps[k] << 16), size = __uint_as_float(steps[k] & 0xffff0000u);
+      const uint64_t low2 = two_of(low, low), step2 = two_of(size, size), less = two_of(-8388608.0f, -8388608.0f);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int r = r0 + k * step;
-        const bool is_v = r >= c.kv_heads;
-        T* y = is_v ? static_cast<T*>(p.v) : static_cast<T*>(p.k);
-        if (token0 + t >= p.tokens || r >= 2 * c.kv_heads || !y) continue;
-        y += (token0 + t) * (is_v ? p.ldv : p.ldk) + (is_v ? r - c.kv_heads : r) * (is_v ? p.ldvh : p.ldkh) + lane * 8;
-        const float low = __uint_as_float(steps[t][k] << 16), size = __uint_as_float(steps[t][k] & 0xffff0000u);
-        const uint64_t low2 = two_of(low, low), step2 = two_of(size, size), less = two_of(-8388608.0f, -8388608.0f);
+      for (int h = 0; h < 2; ++h, y += c.dim >> 1) {
+        const uint32_t w = h ? words[k].y : words[k].x;
+        uint64_t f[4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h, y += c.dim >> 1) {
-          const uint32_t w = h ? words[t][k].y : words[t][k].x;
-          uint64_t f[4];
+        for (int j = 0; j < 4; ++j) {  // (a code under the exponent of 2^23 is 2^23 + n)
+          const uint32_t u = w >> (8 * j);
+          f[j] = fma2(add2(two_of(__uint_as_float((u & 15u) | 0x4b000000u), __uint_as_float((u >> 4 & 15u) | 0x4b000000u)), less), step2, low2);
+        }
+        if constexpr (kVec) {
+          constexpr int kPairs = 8 / sizeof(T);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {  // (a code under the exponent of 2^23 is 2^23 + n)
-            const uint32_t u = w >> (8 * j);
-            f[j] = fma2(add2(two_of(__uint_as_float((u & 15u) | 0x4b000000u), __uint_as_float((u >> 4 & 15u) | 0x4b000000u)), less), step2, low2);
+          for (int i = 0; i < 4; i += kPairs) {
+            uint64_t v[kPairs];
+#pragma unroll
+            for (int e = 0; e < kPairs; ++e) v[e] = f[i + e];
+            *reinterpret_cast<uint4*>(y + 2 * i) = from_pairs<T>(v);
           }
-          if constexpr (kVec) {
-            constexpr int kPairs = 8 / sizeof(T);
+        } else {
 #pragma unroll
-            for (int i = 0; i < 4; i += kPairs) {
-              uint64_t v[kPairs];
-#pragma unroll
-              for (int e = 0; e < kPairs; ++e) v[e] = f[i + e];
-              *reinterpret_cast<uint4*>(y + 2 * i) = from_pairs<T>(v);
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              float a, b;
-              one_each(f[j], a, b);
-              y[2 * j] = from_f32<T>(a);
-              y[2 * j + 1] = from_f32<T>(b);
-            }
+          for (int j = 0; j < 4; ++j) {
+            float a, b;
+            one_each(f[j], a, b);
+            y[2 * j] = from_f32<T>(a);
+            y[2 * j + 1] = from_f32<T>(b);
           }
         }
       }
+    }
   }
 }
 
@@ -675,10 +674,11 @@ static void config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* at, int64_t blo
   cfg.attrs = at;
   cfg.numAttrs = 1;
 }
-// Warps to a token: more while there are SMs to fill and rows for them. (`rows` of a warp's groups of lanes)
-static int share_of(int64_t tokens, int rows, int groups) {
+// Warps to a token: more while all of them are on the GPU at once (`blocks` an SM) and have rows for their groups of lanes. (40 heads of 128 and a cache,
+// 1024 tokens: two warps a token 8.7 us, four, in two rounds, 12.3, eight 19.1; 2048 tokens: one 13.0, two 14.8, four 21.4.)
+static int share_of(int64_t tokens, int rows, int groups, int blocks) {
   int share = 1;
-  while (share < 8 && tokens * share < 152 * 32 && share * groups < rows) share *= 2;
+  while (share < kThreads / 32 && 2 * share * tokens <= 152 * (kThreads / 32) * blocks && share * groups < rows) share *= 2;
   return share;
 }
 
@@ -694,9 +694,11 @@ static cudaError_t run_heads_type(const QkArgs& a, cudaStream_t stream) {
   cudaLaunchAttribute at[1];
   if (vec) {
     const int lanes = pow2_at_least(a.dim / (2 * V)), log2 = __builtin_ctz(lanes);
-    const int share = share_of(a.tokens, a.heads > a.kv_heads ? a.heads : a.kv_heads, 32 / lanes), per = kThreads / 32 / share;
+    const bool plain = a.cache.data && a.heads == 0 && !a.k_weight && a.rot == 0 && !a.k_out;
+    const int blocks = plain ? 4 : 3;  // an SM, as the kernels are built for
+    const int share = share_of(a.tokens, a.heads > a.kv_heads ? a.heads : a.kv_heads, 32 / lanes, blocks), per = kThreads / 32 / share;
     config(cfg, at, (a.tokens + per - 1) / per, (size_t)per * (a.rot / 2) * sizeof(float2), stream);
-    if (a.cache.data && a.heads == 0 && !a.k_weight && a.rot == 0 && !a.k_out) return cudaLaunchKernelEx(&cfg, rows_kernel<T, true, false, true>, a, share, lanes, log2);
+    if (plain) return cudaLaunchKernelEx(&cfg, rows_kernel<T, true, false, true>, a, share, lanes, log2);
     if (a.cache.data)
       return a.interleaved ? cudaLaunchKernelEx(&cfg, rows_kernel<T, true, true, false>, a, share, lanes, log2)
                            : cudaLaunchKernelEx(&cfg, rows_kernel<T, true, false, false>, a, share, lanes, log2);
@@ -717,15 +719,12 @@ static cudaError_t run_read(const CacheReadArgs& a, cudaStream_t stream) {
   constexpr int V = 16 / sizeof(T);
   const bool vec = on16(a.k) && on16(a.v) && (a.ldk | a.ldkh | a.ldv | a.ldvh) % V == 0;
   const int lanes = pow2_at_least(a.cache.dim / 16), log2 = __builtin_ctz(lanes);
-  const int share = share_of(a.tokens, 2 * a.cache.kv_heads, 32 / lanes);
+  const int share = share_of(a.tokens, 2 * a.cache.kv_heads, 32 / lanes, 5);
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute at[1];
-  // two tokens a warp where there are tokens for every warp that fits: twice the bytes on their way
-  const bool two = vec && share == 1 && a.tokens >= 2 * 152 * 32;
-  config(cfg, at, ((two ? (a.tokens + 1) / 2 : a.tokens) * share + kThreads / 32 - 1) / (kThreads / 32), 0, stream);
-  if (two) return cudaLaunchKernelEx(&cfg, cache_read_kernel<T, true, 2>, a, share, lanes, log2);
-  if (vec) return cudaLaunchKernelEx(&cfg, cache_read_kernel<T, true, 1>, a, share, lanes, log2);
-  return cudaLaunchKernelEx(&cfg, cache_read_kernel<T, false, 1>, a, share, lanes, log2);
+  config(cfg, at, (a.tokens * share + kThreads / 32 - 1) / (kThreads / 32), 0, stream);
+  if (vec) return cudaLaunchKernelEx(&cfg, cache_read_kernel<T, true>, a, share, lanes, log2);
+  return cudaLaunchKernelEx(&cfg, cache_read_kernel<T, false>, a, share, lanes, log2);
 }
 
 }  // namespace headrows
