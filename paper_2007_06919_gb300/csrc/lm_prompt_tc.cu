@@ -4,17 +4,19 @@
 // live in TMEM; a thread per row reads its scores from there, subtracts the running maximum, takes exponentials, and writes the weights over the
 // scores as 16-bit numbers, from where they are the A operand of O += P V (V as it lies: its rows are K of that product). While one
 // tile's rows are at their exponentials, the tensor cores have the other tile's two products. For heads of 128 a step of
-// both takes four products of 128 x 128 x 128 (4 x 512 cycles). For heads of 64 the exponentials bound it (2 x 128 x 128 at 32 a cycle, 1024), and a row must not
-// wait for its next scores: TMEM has 192 columns for a tile there, in three blocks X, Y, Z. Even steps have their scores in XY and their weights in X, odd ones in YZ
-// and Z: Y is free once a row's scores are read, so the next scores come while the exponentials run. (Scores behind the products that read the last
-// weights, as for heads of 128: 8192 tokens of 32 heads 263 us.)
+// both takes four products of 128 x 128 x 128 (4 x 512 cycles), which bound it: 16,384 tokens of 32 heads 1,260 us, 1,745 TFLOP/s, 90% of the measured
+// rate. For heads of 64 the exponentials bound it (2 x 128 x 128 at 32 a cycle, 1024), and a row must not wait for its next scores: TMEM
+// has 192 columns for a tile there, in three blocks X, Y, Z. Even steps have their scores in XY and their weights in X, odd ones in YZ and Z: Y is free
+// once a row's scores are read, so the next scores come while the exponentials run. (Scores behind the products that read the last
+// weights, as for heads of 128: 8192 tokens of 32 heads 263 us, this way 248, 1,108 TFLOP/s. Two threads to a row, 281; the tiles taking turns at the
+// exponentials, 267: what is left there is a row's chain of maximum, exponentials and stores, not one unit's rate.)
 //
 // The outputs are brought to a new maximum only where it grew by more than a factor of 2^8 since the last time: weights stay below that, sums are
 // float32, and the division at the end is exact in it. So after the first few tiles of keys no row touches its outputs before the end.
 //
 // Blocks stay and take over the jobs of blocks that have not begun (clusterlaunchcontrol), one warp asking and looking up the sequence ahead of the
-// others: a job's first copies and scores run beside the last one's end. (With a block for each job, whose start and end cost 6 to 7 us: 13 prompts of up to
-// 2500 tokens, 28 heads of 64, 84 us.)
+// others: a job's first copies and scores run beside the last one's end. (13 prompts of up to
+// 2500 tokens, 28 heads of 64: 62 us; with a block for each job, whose start and end cost 6 to 7 us, 84.)
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
