@@ -1,4 +1,4 @@
-// lm_prompt_tc.cu -- attention over packed prompts on the fifth-generation tensor cores, for heads of 64 and 128.
+// lm_prompt_tc.cu -- attention over packed prompts on the fifth-generation tensor cores: heads of 64 and 128 (first), of 192 and 256.
 //
 // A job is 256 query rows of one head, as two tiles of 128, and keys 128 at a time. Scores S = Q K^T and the outputs O of both tiles
 // live in TMEM; a thread per row reads its scores from there, subtracts the running maximum, takes exponentials, and writes the weights over the
@@ -55,6 +55,7 @@ constexpr float kGrowth = 8.0f;             // powers of two that a maximum may 
 
 __host__ __device__ constexpr int tile_bytes(int dim) { return kTile * dim * 2; }
 __host__ __device__ constexpr int ring(int dim) { return dim == 128 ? 5 : 8; }
+__host__ __device__ constexpr int job_rows(int dim) { return dim > 128 ? kTile : 2 * kTile; }
 
 struct Slot {
   Job job;
@@ -646,6 +647,292 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
   }
 }
 
+// ---------------------------------------------------------------- heads of 192 and 256
+
+// Two such tiles' outputs would leave TMEM no room for scores: a block takes one tile of 128 rows, whose outputs have up to 256 columns, and its scores go
+// to the other two times 128 in turn. The tensor cores have the next step's scores, and the last step's products, while the four warps of the rows are at
+// their exponentials. Keys and values come in pieces that a product takes whole: 128 x 128 numbers of a head of 256, 128 x 192 of 192. Bound by the products
+// (8192 tokens of 32 heads of 256: 651 us, 1,689 TFLOP/s) and, for 192, the rows' chain beside shorter ones (534 us, 1,543). A block takes one job: its
+// start and end, about 7 us, show where jobs are short (13 prompts of up to 2500 tokens, 28 heads of 256: 182 us, 844 TFLOP/s).
+struct WideBarriers {
+  uint64_t q_full, full[8], empty[8], s_full[2], p_full[2], o_done[2], last_v, fixed;  // (even and odd steps have barriers of their own)
+  uint64_t red[8];
+  Job job;
+  uint32_t tmem;
+  int abort_flag;
+};
+__host__ __device__ constexpr int pieces(int dim) { return dim == 256 ? 2 : 1; }
+__host__ __device__ constexpr int wide_ring(int dim) { return dim == 256 ? 5 : 3; }
+__host__ __device__ constexpr size_t wide_smem(int dim) { return (size_t)tile_bytes(dim) + wide_ring(dim) * (tile_bytes(dim) / pieces(dim)) + sizeof(WideBarriers); }
+constexpr int kWideThreads = 256, kWideTma = 4, kWideMma = 5, kWideFix = 6;
+
+template <class T, int D>
+__global__ void __launch_bounds__(kWideThreads, 1) prompt_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ PromptArgs p) {
+  constexpr int kPieces = pieces(D), kRing = wide_ring(D), kBox = kTile * 128, kBoxes = D / 64 / kPieces, kPiece = kBoxes * kBox;
+  constexpr uint32_t kO = 2 * kTile;
+  static_assert(kO + D <= 512 && kPieces <= kRing && kRing <= 8, "");
+  extern __shared__ __align__(1024) uint8_t smem[];  // queries, the ring of keys and values, WideBarriers
+  WideBarriers& bar = *reinterpret_cast<WideBarriers*>(smem + tile_bytes(D) + kRing * kPiece);
+  volatile int* abort_flag = &bar.abort_flag;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t sq = smem_u32(smem), ring0 = sq + tile_bytes(D);
+  if (threadIdx.x == 0) {
+    mbar_init(smem_u32(&bar.q_full), 1);
+    for (int i = 0; i < kRing; ++i) {
+      mbar_init(smem_u32(&bar.full[i]), 1);
+      mbar_init(smem_u32(&bar.empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&bar.s_full[i]), 1);
+      mbar_init(smem_u32(&bar.p_full[i]), 4);
+      mbar_init(smem_u32(&bar.o_done[i]), 1);
+    }
+    mbar_init(smem_u32(&bar.last_v), 1);
+    mbar_init(smem_u32(&bar.fixed), 1);
+    bar.abort_flag = 0;
+    fence_barrier_init();
+  }
+  grid_dep_wait();
+  if (!prompt::find_job(p, kTile, blockIdx.y, &bar.job, bar.red)) return;
+  const Job jb = bar.job;
+  if (warp == kWideMma) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bar.tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *const_cast<volatile uint32_t*>(&bar.tmem);
+  const int head = blockIdx.x, kvh = head / (p.heads / p.kv_heads), row0 = jb.tile * kTile, behind = jb.queries - row0, rows = behind < kTile ? behind : kTile;
+  int64_t most = p.causal ? (int64_t)row0 + rows + (jb.keys - jb.queries) : jb.keys;
+  most = most < 0 ? 0 : most > jb.keys ? jb.keys : most;
+  const int n = (int)((most + kTile - 1) / kTile);  // steps
+  const bool cut = n * kTile > jb.keys;             // the last step's tile ends behind the sequence
+
+  if (warp == kWideTma && elect_one() && n > 0) {
+    const uint32_t qf = smem_u32(&bar.q_full);
+    mbar_arrive_expect_tx(qf, tile_bytes(D));
+#pragma unroll
+    for (int b = 0; b < D / 64; ++b) tma_load_3d(sq + b * kBox, &maps.q, b * 64, head, jb.start + row0, qf);
+    uint32_t st = 0, ph = 0;
+    int issued = 0;
+    bool ok = true;
+    auto load = [&](const CUtensorMap* map, int key) {
+#pragma unroll
+      for (int c = 0; c < kPieces; ++c) {
+        if (!mbar_wait(smem_u32(&bar.empty[st]), ph ^ 1, abort_flag)) { ok = false; return; }
+        const uint32_t full = smem_u32(&bar.full[st]);
+        mbar_arrive_expect_tx(full, kPiece);
+#pragma unroll
+        for (int b = 0; b < kBoxes; ++b) tma_load_3d(ring0 + st * kPiece + b * kBox, map, (c * kBoxes + b) * 64, kvh, key, full);
+        ++issued;
+        if (++st == (uint32_t)kRing) { st = 0; ph ^= 1; }
+      }
+    };
+    // in the order of the products: two steps' scores lead
+    for (int j = -2; ok && j < n; ++j) {
+      const int key = jb.kv_start + j * kTile;
+      if (j >= 0) load(&maps.v, key);
+      if (ok && j + 2 < n) load(&maps.k, key + 2 * kTile);
+    }
+    // the last arrivals at these barriers come before the block ends
+    for (int i = issued > kRing ? issued - kRing : 0; ok && i < issued; ++i) ok = mbar_wait(smem_u32(&bar.empty[i % kRing]), (uint32_t)(i / kRing) & 1, abort_flag);
+    if (!ok) {
+      fail(abort_flag, p.status);
+      int never = 0;  // the copies in flight end before the block does (each of these waits is bounded too)
+      mbar_wait(qf, 0, &never);
+      for (int i = issued > kRing ? issued - kRing : 0; i < issued; ++i) mbar_wait(smem_u32(&bar.full[i % kRing]), (uint32_t)(i / kRing) & 1, &never);
+    }
+  }
+  if (warp == kWideMma && elect_one() && n > 0) {
+    constexpr uint32_t type = std::is_same<T, __half>::value ? 0u : (1u << 7) | (1u << 10);
+    const uint32_t id_s = idesc_e4m3(kTile) | type, id_o = idesc_e4m3(kBoxes * 64) | type | 1u << 16;  // (bit 16: B's rows are K)
+    const uint32_t dq = desc_low(sq, 16), dk = desc_low(ring0, 16), dv = desc_low(ring0, kBox);
+    uint32_t st = 0, ph = 0;
+    bool ok = mbar_poll(smem_u32(&bar.q_full), 0, abort_flag);
+    auto there = [&] {
+      ok = ok && mbar_poll(smem_u32(&bar.full[st]), ph, abort_flag);
+      tc_fence_after();
+      return ok;
+    };
+    auto used = [&] {
+      mma_commit(smem_u32(&bar.empty[st]));
+      if (++st == (uint32_t)kRing) { st = 0; ph ^= 1; }
+    };
+    auto scores = [&](int j) {
+#pragma unroll
+      for (int c = 0; c < kPieces; ++c) {
+        if (!there()) return;
+#pragma unroll
+        for (int s = 0; s < kBoxes * 4; ++s) {
+          const uint32_t at = ((s >> 2) * kBox + (s & 3) * 32) >> 4;
+          mma_ss(tmem + (j & 1) * kTile, dq + c * (kPiece >> 4) + at, dk + st * (kPiece >> 4) + at, id_s, c > 0 || s > 0);
+        }
+        used();
+      }
+      mma_commit(smem_u32(&bar.s_full[j & 1]));
+    };
+    if (ok) scores(0);
+    if (ok && n > 1) scores(1);
+    for (int j = 0; ok && j < n; ++j) {
+      if (cut && j == n - 1) {
+        // (all of the last values: the pieces behind this one are in the next places)
+#pragma unroll
+        for (int c = 0; c < kPieces; ++c) {
+          const bool over = st + c >= (uint32_t)kRing;
+          ok = ok && mbar_poll(smem_u32(&bar.full[over ? st + c - kRing : st + c]), over ? ph ^ 1 : ph, abort_flag);
+        }
+        if (ok) mbar_arrive(smem_u32(&bar.last_v));
+        ok = ok && mbar_poll(smem_u32(&bar.fixed), 0, abort_flag);
+      }
+      ok = ok && mbar_poll(smem_u32(&bar.p_full[j & 1]), (uint32_t)(j >> 1) & 1, abort_flag);
+#pragma unroll
+      for (int c = 0; c < kPieces; ++c) {
+        if (!there()) break;
+#pragma unroll
+        for (int s = 0; s < kTile / 16; ++s)
+          mma_ts(tmem + kO + c * (kBoxes * 64), tmem + (j & 1) * kTile + s * 8, dv + st * (kPiece >> 4) + (s * 2048 >> 4), id_o, j > 0 || s > 0);
+        used();
+      }
+      if (!ok) break;
+      mma_commit(smem_u32(&bar.o_done[j & 1]));
+      if (j + 2 < n) scores(j + 2);
+    }
+    if (!ok) fail(abort_flag, p.status);
+  }
+  if (warp == kWideFix && cut && n > 0) {
+    // the last tile's value rows behind the sequence's end are another's: 0 instead, so that weights of 0 meet no NaN
+    if (mbar_wait(smem_u32(&bar.last_v), 0, abort_flag)) {
+      for (int c = 0; c < kPieces; ++c) {
+        uint8_t* v = smem + tile_bytes(D) + ((2 * n - 1) * kPieces + c) % kRing * kPiece;
+        for (int i = (jb.keys - (n - 1) * kTile) * 8 + lane; i < kTile * 8; i += 32)
+          for (int b = 0; b < kBoxes; ++b) reinterpret_cast<uint4*>(v + b * kBox)[i] = make_uint4(0, 0, 0, 0);
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bar.fixed));
+    } else {
+      fail(abort_flag, p.status);
+    }
+  }
+  if (warp < 4) {
+    const int row = warp * 32 + lane, at = row0 + row;  // this thread's row of the tile, and of the sequence
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16, to = tmem + kO + lanes;
+    const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f), grow = kGrowth / c2;
+    int64_t see = p.causal ? (int64_t)at + (jb.keys - jb.queries) + 1 : jb.keys;
+    const int lim = (int)(see < 0 ? 0 : see > jb.keys ? jb.keys : see);
+    float m = -INFINITY, l = 0.0f;
+    bool ok = true;
+    for (int j = 0; j < n; ++j) {
+      const uint32_t ts = tmem + (j & 1) * kTile + lanes;
+      if (!mbar_wait_inline(smem_u32(&bar.s_full[j & 1]), (uint32_t)(j >> 1) & 1, abort_flag)) { ok = false; break; }
+      // (every phase of a barrier is met: these products came before the scores)
+      if (j >= 2 && !mbar_wait_inline(smem_u32(&bar.o_done[j & 1]), (uint32_t)((j - 2) >> 1) & 1, abort_flag)) { ok = false; break; }
+      tc_fence_after();
+      float s[kTile];
+#pragma unroll
+      for (int i = 0; i < kTile; i += 32) tmem_ld32(ts + i, s + i);
+      tmem_wait_ld();
+#pragma unroll
+      for (int i = 0; i < kTile; i += 32) settle(s + i);
+      const int here = lim - j * kTile;  // places of this tile that the row sees
+      if (__any_sync(0xffffffffu, here < kTile)) {
+#pragma unroll
+        for (int i = 0; i < kTile; ++i)
+          if (i >= here) s[i] = -INFINITY;
+      }
+      float a[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+      for (int i = 4; i < kTile; i += 4)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) a[c] = fmaxf(a[c], s[i + c]);
+      const float top = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
+      const bool grew = top > m + grow;  // (from -infinity: any score)
+      if (__any_sync(0xffffffffu, grew)) {
+        const float f = grew ? ex2((m - top) * c2) : 1.0f;
+        if (grew) m = top;
+        l *= f;
+        if (j > 0) {
+          // (the last step's products come behind these scores)
+          if (!mbar_wait_inline(smem_u32(&bar.o_done[(j - 1) & 1]), (uint32_t)((j - 1) >> 1) & 1, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+#pragma unroll
+          for (int i = 0; i < D; i += 16) {
+            uint32_t o[16];
+            tmem_ld16(to + i, o);
+            tmem_wait_ld();
+            reg_fence16(o);
+#pragma unroll
+            for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
+            tmem_st16(to + i, o);
+          }
+        }
+      }
+      float ref = m == -INFINITY ? 0.0f : m;
+      // the factor goes into one multiply-add with the maximum, but where scores are so large that its rounding shows
+      if (__any_sync(0xffffffffu, fabsf(ref * c2) > 1e5f)) {
+#pragma unroll
+        for (int i = 0; i < kTile; ++i) s[i] -= ref;
+        ref = 0.0f;
+      }
+      const uint64_t c22 = two_of(c2, c2), r22 = two_of(-ref * c2, -ref * c2);
+      uint64_t sum[2] = {0, 0};
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float x, y;
+          one_each(fma2(two_of(s[32 * h + 2 * i], s[32 * h + 2 * i + 1]), c22, r22), x, y);
+          x = ex2(x);
+          y = ex2(y);
+          sum[i & 1] = add2(sum[i & 1], two_of(x, y));
+          w[i] = pack(x, y, (T*)nullptr);
+        }
+        tmem_st16(ts + 16 * h, w);
+      }
+      float u, v;
+      one_each(add2(sum[0], sum[1]), u, v);
+      l += u + v;
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bar.p_full[j & 1]));
+    }
+    for (int j = n > 1 ? n - 2 : 0; ok && j < n; ++j) ok = mbar_wait_inline(smem_u32(&bar.o_done[j & 1]), (uint32_t)(j >> 1) & 1, abort_flag);
+    if (!ok) fail(abort_flag, p.status);
+    tc_fence_after();
+    const bool live = row < behind;
+    const float inv = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
+    T* y = static_cast<T*>(p.out) + (int64_t)(jb.start + at) * p.ldo + (int64_t)head * p.ldoh;
+#pragma unroll 2
+    for (int i = 0; i < D; i += 32) {
+      float o[32];
+      if (n > 0) {
+        tmem_ld32(to + i, o);
+        tmem_wait_ld();
+        settle(o);
+      } else {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) o[c] = 0.0f;
+      }
+      if (live && ok) {
+#pragma unroll
+        for (int c = 0; c < 32; c += 8)
+          *reinterpret_cast<uint4*>(y + i + c) = make_uint4(pack(o[c] * inv, o[c + 1] * inv, (T*)nullptr), pack(o[c + 2] * inv, o[c + 3] * inv, (T*)nullptr),
+                                                            pack(o[c + 4] * inv, o[c + 5] * inv, (T*)nullptr), pack(o[c + 6] * inv, o[c + 7] * inv, (T*)nullptr));
+      }
+    }
+    if (live && ok && p.lse) p.lse[(int64_t)(jb.start + at) * p.heads + head] = fmaf(m, c2, log2f(l)) * kLn2;
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (warp == kWideMma) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
 // ---------------------------------------------------------------- host side
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -678,13 +965,17 @@ static bool encode(CUtensorMap* map, bool half, const void* base, int64_t dim, i
 
 template <class T, int D>
 static cudaError_t run(const PromptArgs& a, const Maps& maps, cudaStream_t stream) {
-  constexpr size_t smem = (2 + ring(D)) * tile_bytes(D) + sizeof(Barriers);
+  constexpr bool kWide = D > 128;
+  constexpr size_t smem = kWide ? wide_smem(D) : (2 + ring(D)) * tile_bytes(D) + sizeof(Barriers);
   static_assert(smem <= kSmemLimit, "");
-  cudaError_t e = cudaFuncSetAttribute(prompt_tc_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  void (*kernel)(Maps, PromptArgs);
+  if constexpr (kWide) kernel = prompt_wide_kernel<T, D>;
+  else kernel = prompt_tc_kernel<T, D>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)a.heads, (unsigned)(a.tokens / (2 * kTile) + a.seqs));
-  cfg.blockDim = dim3(kThreads);
+  cfg.gridDim = dim3((unsigned)a.heads, (unsigned)(a.tokens / job_rows(D) + a.seqs));
+  cfg.blockDim = dim3(kWide ? kWideThreads : kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute at[1];
@@ -692,7 +983,16 @@ static cudaError_t run(const PromptArgs& a, const Maps& maps, cudaStream_t strea
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, prompt_tc_kernel<T, D>, maps, a);
+  return cudaLaunchKernelEx(&cfg, kernel, maps, a);
+}
+template <class T>
+static cudaError_t run_type(const PromptArgs& a, const Maps& maps, cudaStream_t stream) {
+  switch (a.dim) {
+    case 64: return run<T, 64>(a, maps, stream);
+    case 128: return run<T, 128>(a, maps, stream);
+    case 192: return run<T, 192>(a, maps, stream);
+    default: return run<T, 256>(a, maps, stream);
+  }
 }
 
 }  // namespace prompttc
@@ -703,7 +1003,7 @@ bool prompt_tc_takes(const PromptArgs& a) {
   const int64_t ld[6] = {a.ldq, a.ldqh, a.ldk, a.ldkh, a.ldv, a.ldvh};
   for (int i = 0; i < 6; ++i)
     if (ld[i] < 1 || ld[i] > most) return false;
-  return (a.dim == 64 || a.dim == 128) && a.kv_tokens > 0 && a.tokens / (2 * prompttc::kTile) + a.seqs <= 65535;
+  return a.kv_tokens > 0 && a.tokens / prompttc::job_rows(a.dim) + a.seqs <= 65535;
 }
 
 int launch_prompt_tc(const PromptArgs& a, cudaStream_t stream, std::string* err) {
@@ -715,8 +1015,7 @@ int launch_prompt_tc(const PromptArgs& a, cudaStream_t stream, std::string* err)
     *err = "cuTensorMapEncodeTiled failed";
     return AQD_ERR_CUDA;
   }
-  const cudaError_t e = half ? (a.dim == 64 ? run<__half, 64>(a, maps, stream) : run<__half, 128>(a, maps, stream))
-                             : (a.dim == 64 ? run<__nv_bfloat16, 64>(a, maps, stream) : run<__nv_bfloat16, 128>(a, maps, stream));
+  const cudaError_t e = half ? run_type<__half>(a, maps, stream) : run_type<__nv_bfloat16>(a, maps, stream);
   if (e == cudaSuccess) return 0;
   *err = std::string("prompt attention: ") + cudaGetErrorString(e);
   return AQD_ERR_CUDA;

@@ -210,3 +210,46 @@ def test_many_short_prompts():
         close(got, o, tol)
         close(lse, e, et)
     assert aqd.device_status() == 0
+
+
+# Heads of 192 and 256 have a kernel of their own: one to many steps, tiles that end in a sequence, maxima that grow, weights that vanish.
+@pytest.mark.parametrize("dim,dtype", [(192, BF16), (256, F16), (192, F16), (256, BF16)])
+def test_wide_heads(dim, dtype):
+    lens = [1, 128, 129, 256, 257, 383, 384, 385, 640, 2000]
+    at, starts = starts_of(lens)
+    q, k, v = inputs(10 + dim, at[-1], at[-1], 3, 1, dim, dtype)
+    for scale, ramp in ((dim ** -0.5, False), (0.25, True)):
+        kk = k * torch.linspace(0.1, 15, at[-1], device="cuda").to(dtype)[:, None, None] if ramp else k
+        o, tol, e, et = reference(q, kk, v, at, at, True, scale)
+        for _ in range(2):
+            got, lse = aqd.prompt_attention(q, kk, v, starts, scale=scale, lse=True)
+            close(got, o, tol)
+            close(lse, e, et)
+    assert aqd.device_status() == 0
+
+
+@pytest.mark.parametrize("dim", [192, 256])
+def test_wide_heads_of_many_short_prompts_broadcast_and_at_once(dim):
+    torch.manual_seed(11)
+    lens = [int(n) for n in torch.randint(0, 4, (400,))]
+    klens = [int(n) for n in torch.randint(0, 6, (400,))]
+    lens[200], klens[200] = 500, 700
+    at, starts = starts_of(lens)
+    kat, kstarts = starts_of(klens)
+    q, k, v = inputs(12, at[-1], kat[-1], 4, 2, dim, BF16)
+    for causal in (True, False):
+        o, tol, e, et = reference(q, k, v, at, kat, causal, 0.08)
+        got, lse = aqd.prompt_attention(q, k, v, starts, kv_starts=kstarts, causal=causal, scale=0.08, lse=True)
+        close(got, o, tol)
+        close(lse, e, et)
+    want = got
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(2_000_000)
+    runs = [aqd.prompt_attention(q, k, v, starts, kv_starts=kstarts, causal=False, scale=0.08, stream=s) for s in streams for _ in range(3)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want) for g in runs)
+    k = k[:, :1].expand(-1, 2, -1)  # (a stride of zero: the other kernel)
+    o, tol, _, _ = reference(q, k, v, at, kat, True, 0.08)
+    close(aqd.prompt_attention(q, k, v, starts, kv_starts=kstarts, scale=0.08), o, tol)
+    assert aqd.device_status() == 0
