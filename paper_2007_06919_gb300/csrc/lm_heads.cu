@@ -6,10 +6,11 @@
 // lanes is a sum of squares and a row's lowest and highest value. Bound by memory, if the instructions for a value stay below about eight: a
 // warp takes a token's heads in turn (rows_kernel), its lanes keep their places in the row, and with them the products of weights, cosines and sines;
 // float32 goes in pairs; 16-bit minima and maxima stay packed; codes come out of the bits of one multiply-add.
-//   8192 tokens of 40 heads of 128 in bfloat16: 38.4 us, 168 MB at 4.4 TB/s (47 with a row at a time, its indexes, weights and turns looked up for
-//   each); with keys and values to the cache 47.3, 171 MB. 16,384 tokens' 16 rows to codes: 20.3 us, 85 MB at 4.2 TB/s (46), and back 14.8 (34).
-// What holds them back is bytes on their way: 80 registers leave 24 warps an SM, with two rows' loads each (counters: 52 to 68% of the issue slots,
-// most waits for loads). Four rows at once (75 registers for codes, fewer warps) 21.7, weights and turns in shared memory 52 to 78.
+//   8192 tokens of 40 heads of 128 in bfloat16: 32.7 us, 168 MB at 5.1 TB/s (47 with a row at a time, its indexes, weights and turns looked up for
+//   each); with keys and values to the cache 41.1, 177 MB. 16,384 tokens' 16 rows to codes: 19.6 us, 85 MB at 4.3 TB/s (46), and back 13.8 (34).
+// What holds them back is bytes on their way: 90 registers leave 20 warps an SM, with two rows' loads each and the next two's lines asked for without a
+// register (38.4 us, and 47.3, with 24 warps and none asked for ahead; 36.8 with all of a token's asked for at once; 39 with 16 warps). Four rows at once
+// (75 registers for codes, fewer warps) 21.7, weights and turns in shared memory 52 to 78.
 // Rows at any address, and rotations of any even length, take heads_kernel, a value at a time (14 heads of 64 in float32, 777 tokens: 4.4 us).
 //
 // The angle of position p at frequency f is p f / 2 pi turns, of which the whole ones do not count: with u = frac(f / 2 pi) 2^64 cut to
@@ -30,7 +31,7 @@
 namespace aqd {
 namespace headrows {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
@@ -395,9 +396,9 @@ struct Bool {
 };
 
 // A warp, or several, to a token: the lanes of a row keep their places in it while the warp goes through the heads. lanes: a power of two, those past the
-// row's end idle. `share` warps (1, 2, 4 or 8) take a token's rows in turn. kPlain: keys and values to the cache as they are.
+// row's end idle. `share` warps (1, 2 or 4) take a token's rows in turn. kPlain: keys and values to the cache as they are.
 template <class T, bool kCache, bool kInter, bool kPlain>
-__global__ void __launch_bounds__(kThreads, kPlain ? 4 : 3) rows_kernel(const QkArgs p, const int share, const int lanes, const int lanes_log2) {
+__global__ void __launch_bounds__(kThreads, kPlain ? 8 : 5) rows_kernel(const QkArgs p, const int share, const int lanes, const int lanes_log2) {
   constexpr int V = 16 / sizeof(T), kPairs = V / 2;
   extern __shared__ float2 turns[];  // [tokens of the block][rot / 2]: cosine, sine
   tc::grid_dep_wait();
@@ -418,18 +419,17 @@ __global__ void __launch_bounds__(kThreads, kPlain ? 4 : 3) rows_kernel(const Qk
   int row = 0;
   uint8_t* blk = kept ? place(p.cache, slot, 0, row) : nullptr;
   const int64_t head_bytes = ((int64_t)1 << (p.cache.page_shift - 4)) * 16 * (p.cache.dim + 8);
-  // the first rows are on their way while sines and cosines are made
-  if (!kPlain && in) {
-    if (first + group < p.heads) {
-      const T* x = static_cast<const T*>(p.q) + token * p.ldq + (int64_t)(first + group) * p.ldqh;
-      prefetch(x + ia);
-      prefetch(x + ib);
+  // rows to come begin their way, a lane to a line of 128 bytes; the first ones while sines and cosines are made
+  auto begin = [&](const T* x, int64_t ldh, int h0, int n, int count) {
+    if (lane * (int)(128 / sizeof(T)) < p.dim) {
+#pragma unroll
+      for (int k = 0; k < count; ++k)
+        if (h0 + group + k * step < n) prefetch(x + (h0 + group + k * step) * ldh + lane * (int)(128 / sizeof(T)));
     }
-    if (first + group < p.kv_heads) {
-      const T* x = static_cast<const T*>(p.k) + token * p.ldk + (int64_t)(first + group) * p.ldkh;
-      prefetch(x + ia);
-      prefetch(x + ib);
-    }
+  };
+  if constexpr (!kPlain) {
+    begin(static_cast<const T*>(p.q) + token * p.ldq, p.ldqh, first, p.heads, kCache ? 1 : 2);
+    begin(static_cast<const T*>(p.k) + token * p.ldk, p.ldkh, first, p.kv_heads, kCache ? 1 : 2);
   }
   if constexpr (!kPlain) {
     if (half > 0) {
@@ -514,6 +514,7 @@ __global__ void __launch_bounds__(kThreads, kPlain ? 4 : 3) rows_kernel(const Qk
     for (int h0 = first; h0 < n; h0 += kAtOnce * step) {
       uint4 va[kAtOnce], vb[kAtOnce];
       fetch(va, vb, x, ldh, h0 + group, n);
+      if constexpr (!kPlain) begin(x, ldh, h0 + kAtOnce * step, n, kAtOnce);
 #pragma unroll
       for (int k = 0; k < kAtOnce; ++k) {
         if (h0 + k * step >= n) break;
@@ -587,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, kPlain ? 4 : 3) rows_kernel(const Qk
 }
 
 // `share` warps to a token, as above; a lane takes two words of 8 codes of a row, half a row apart (its values' stores are whole sectors with its neighbours':
-// 16,384 tokens of 8 heads of 128 back to bfloat16 in 14.2 us, 19 with 16 codes together), `lanes` lanes a row, keys' rows and then values'.
+// 16,384 tokens of 8 heads of 128 back to bfloat16 in 13.8 us, 19 with 16 codes together), `lanes` lanes a row, keys' rows and then values'.
 template <class T, bool kVec>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheReadArgs p, const int share, const int lanes, const int lanes_log2) {
   tc::grid_dep_wait();
@@ -675,7 +676,7 @@ static void config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* at, int64_t blo
   cfg.numAttrs = 1;
 }
 // Warps to a token: more while all of them are on the GPU at once (`blocks` an SM) and have rows for their groups of lanes. (40 heads of 128 and a cache,
-// 1024 tokens: two warps a token 8.7 us, four, in two rounds, 12.3, eight 19.1; 2048 tokens: one 13.0, two 14.8, four 21.4.)
+// 1024 tokens: two warps a token 8.7 us, four, in two rounds, 12.3, eight 19.1; 2048 tokens: one 13.0, two 14.8, four 21.4. These with 24 warps an SM.)
 static int share_of(int64_t tokens, int rows, int groups, int blocks) {
   int share = 1;
   while (share < kThreads / 32 && 2 * share * tokens <= 152 * (kThreads / 32) * blocks && share * groups < rows) share *= 2;
@@ -695,7 +696,7 @@ static cudaError_t run_heads_type(const QkArgs& a, cudaStream_t stream) {
   if (vec) {
     const int lanes = pow2_at_least(a.dim / (2 * V)), log2 = __builtin_ctz(lanes);
     const bool plain = a.cache.data && a.heads == 0 && !a.k_weight && a.rot == 0 && !a.k_out;
-    const int blocks = plain ? 4 : 3;  // an SM, as the kernels are built for
+    const int blocks = plain ? 8 : 5;  // an SM, as the kernels are built for
     const int share = share_of(a.tokens, a.heads > a.kv_heads ? a.heads : a.kv_heads, 32 / lanes, blocks), per = kThreads / 32 / share;
     config(cfg, at, (a.tokens + per - 1) / per, (size_t)per * (a.rot / 2) * sizeof(float2), stream);
     if (plain) return cudaLaunchKernelEx(&cfg, rows_kernel<T, true, false, true>, a, share, lanes, log2);
