@@ -319,6 +319,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
   if (p.seqs <= 32) {
     jb = find_job<kRows>(p, sp, none);
     if (lane == 0) jobs[warp] = jb;
+    __syncwarp();
   } else {
     find_jobs<kRows>(p, sp, jobs, reinterpret_cast<float*>(red));
     jb = jobs[warp];
@@ -450,6 +451,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
   // the value steps' power of two: weights p s reach float16 times `up_v`, so that the largest step lies in [2^10, 2^11) (and p may be 2^kGrowth); an
   // exponent field, which only falls (0: no step so far)
   int up_v = 0;
+  uint32_t within = 0xffffu;  // the greatest word of a step that this power is for
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -501,7 +503,8 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
 #pragma unroll
         for (int c = 0; c < 4; ++c) x[b][t][c] = fmaf(acc[t][c], step_of(kz[c >> 1]), low_of(kz[c >> 1]) * qs[t][c & 1]);
     }
-    if (place + kStep > lim_all || here != 3u) {
+    const bool partly = place + kStep > lim_all || here != 3u;  // not every row sees every place
+    if (partly) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -513,24 +516,15 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
           for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              const int lim = lim_of(jb, sp, kRows, t * 8 + 2 * q + c, last_row);
+              const int lim = lim_of(jobs[warp], sp, kRows, t * 8 + 2 * q + c, last_row);
               if (gone || at >= lim) x[b][t][2 * h + c] = -INFINITY;
             }
         }
     }
     // Maxima so far, of each column's scores and of the value steps. What was summed is brought to a new maximum only where it grew by 2^kGrowth.
-    uint32_t tops = 0;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t e = vz[b][h] & 0x7f800000u;
-        if (e != 0x7f800000u) tops = max(tops, e);
-      }
-    const int top_e = (int)(__reduce_max_sync(0xffffffffu, tops) >> 23);
-    const int up_new = top_e == 0 ? up_v : top_e < 11 ? 253 : 264 - top_e;
+    const uint32_t steepest = max(max(vz[0][0], vz[0][1]), max(vz[1][0], vz[1][1]));  // (a step is the word's upper half)
     float mx[NT][2];
-    bool grew = up_new < up_v || up_v == 0;
+    bool grew = steepest > within;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -541,9 +535,20 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
       }
     if (__any_sync(0xffffffffu, grew)) {
       float fs = 1.0f;
+      uint32_t tops = 0;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t e = vz[b][h] & 0x7f800000u;
+          if (e != 0x7f800000u) tops = max(tops, e);
+        }
+      const int top_e = (int)(__reduce_max_sync(0xffffffffu, tops) >> 23);
+      const int up_new = top_e == 0 ? up_v : top_e < 11 ? 253 : 264 - top_e;
       if (up_new < up_v || up_v == 0) {
         fs = up_new - up_v > -127 ? __uint_as_float((uint32_t)(127 + (up_v == 0 ? 0 : up_new - up_v)) << 23) : 0.0f;
         up_v = up_new;
+        within = up_v == 0 ? 0xffffu : (uint32_t)(up_v == 253 ? 11 : 264 - up_v) << 23 | 0x7fffffu;
       }
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
@@ -575,21 +580,16 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
       const float z0 = fmaf(8.0f, step_of(vz[b][0]), low_of(vz[b][0])), z1 = fmaf(8.0f, step_of(vz[b][1]), low_of(vz[b][1]));
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        float w[4], z[4];
+        float w[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const float pr = ex2((x[b][t][c] - (m[t][c & 1] == -INFINITY ? 0.0f : m[t][c & 1])) * c2[t][c & 1]);
           l[t][c & 1] += pr;
           w[c] = pr * (c < 2 ? s0 : s1);
-          z[c] = pr * (c < 2 ? z0 : z1);
+          float z = c < 2 ? z0 : z1;
+          if (partly && x[b][t][c] == -INFINITY) w[c] = z = 0.0f;  // (a place that only later queries see may hold a NaN)
+          zs[t][c & 1] = fmaf(pr, z, zs[t][c & 1]);
         }
-        if (place + kStep > lim_all || here != 3u) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (x[b][t][c] == -INFINITY) w[c] = z[c] = 0.0f;  // (a place that only later queries see may hold a NaN)
-        }
-        zs[t][0] += z[0] + z[2];
-        zs[t][1] += z[1] + z[3];
         const __half2 h0 = __floats2half2_rn(w[0], w[1]), h1 = __floats2half2_rn(w[2], w[3]);
         pw[b][t][0] = transposed(*reinterpret_cast<const uint32_t*>(&h0));
         pw[b][t][1] = transposed(*reinterpret_cast<const uint32_t*>(&h1));
@@ -651,10 +651,11 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
                                      fmaf(o[t][4 * u + 3][c + 2 * h], back, z));
     }
   __syncthreads();
+  const Job je = jobs[warp];  // (read again: its numbers are not kept through the steps)
   // groups of runs that belong together: the block's warps from `w0` to `w1` join theirs
   if (!idle) {
-    const int w0 = warp > jb.run ? warp - jb.run : 0, run0 = jb.run - (warp - w0), w1 = w0 + jb.runs - run0 < kWarps ? w0 + jb.runs - run0 : kWarps;
-    const bool whole = run0 == 0 && w0 + jb.runs == w1;
+    const int w0 = warp > je.run ? warp - je.run : 0, run0 = je.run - (warp - w0), w1 = w0 + je.runs - run0 < kWarps ? w0 + je.runs - run0 : kWarps;
+    const bool whole = run0 == 0 && w0 + je.runs == w1;
     const int rows = last_row < kRows ? last_row : kRows;
     for (int i = threadIdx.x - w0 * 32; i < rows * (D / 4); i += (w1 - w0) * 32) {
       const int row = i / (D / 4), ch = (i - row * (D / 4)) * 4;
@@ -670,7 +671,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
         sum.x = fmaf(v.x, f, sum.x); sum.y = fmaf(v.y, f, sum.y); sum.z = fmaf(v.z, f, sum.z); sum.w = fmaf(v.w, f, sum.w);
       }
       if (whole) {
-        finish<T>(p, sp, jb.start, head, jb.tile * kRows + row, ch, sum, all, top, cs);
+        finish<T>(p, sp, je.start, je.head, je.tile * kRows + row, ch, sum, all, top, cs);
       } else {
         float* part = sp.whole ? reinterpret_cast<float*>(smem) + (kWarps * kRows + row) * kPitch
                                : sp.part + (((int64_t)blockIdx.x * 2 + (run0 == 0 ? 1 : 0)) * kRows + row) * (D + 4);
@@ -707,7 +708,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
           all = fmaf(z[b].y, f, all);
           sum.x = fmaf(v[b].x, f, sum.x); sum.y = fmaf(v[b].y, f, sum.y); sum.z = fmaf(v[b].z, f, sum.z); sum.w = fmaf(v[b].w, f, sum.w);
         }
-      finish<T>(p, sp, jb.start, head, jb.tile * kRows + row, ch, sum, all, top, z[0].z);
+      finish<T>(p, sp, je.start, je.head, je.tile * kRows + row, ch, sum, all, top, z[0].z);
     }
     __syncwarp();
     cluster_sync();  // no block goes while another reads from it
