@@ -6,9 +6,8 @@
 //
 // This kernel takes 64 query rows of one head, four warps of 16, and keys in tiles of 64 (or 32) through two stages of shared memory. It serves what the
 // tensor-memory kernels do not: strides of zero, which no tensor map holds, and more jobs than a grid's second axis. Bound by mma.sync, whose rate is a
-// fraction of theirs: 8192 tokens of 32 heads of 192 3,750 us (220 TFLOP/s; 534 there), of 256 4,239 (259; 651). Only for prompts of less than a
-// tile's 128 rows, and hundreds of them, it is the faster one (100 of 64 tokens, 32 heads of 256: 113 us, 163 there); lengths are not known where the
-// kernel is chosen.
+// fraction of theirs: 8192 tokens of 32 heads of 192 3,750 us (220 TFLOP/s; 511 there), of 256 4,239 (259; 639). Prompts of less than
+// a tile's 128 rows come near: 100 of 64 tokens, 32 heads of 256, 113 us (99 there).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>

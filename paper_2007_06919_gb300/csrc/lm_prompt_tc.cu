@@ -143,8 +143,9 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 }
 
 // Steps of query tile t of a job: tiles of keys that its rows see.
+template <int kTiles>
 __device__ __forceinline__ int steps_of(const Job& jb, int t, int causal) {
-  const int row0 = jb.tile * 2 * kTile + t * kTile, behind = jb.queries - row0, rows = behind < kTile ? behind : kTile;
+  const int row0 = (jb.tile * kTiles + t) * kTile, behind = jb.queries - row0, rows = behind < kTile ? behind : kTile;
   int64_t see = causal ? (int64_t)row0 + rows + (jb.keys - jb.queries) : jb.keys;
   see = see < 0 ? 0 : see > jb.keys ? jb.keys : see;
   return rows > 0 ? (int)((see + kTile - 1) / kTile) : 0;
@@ -263,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
             const int32_t* ks = p.kv_starts ? p.kv_starts : p.starts;
             const int k0 = prompt::clamp_at(ks[q], p.kv_tokens), k1 = prompt::clamp_at(ks[q + 1], p.kv_tokens);
             const Job jb{1, start, queries, k0, k1 > k0 ? k1 - k0 : 0, upto - 1 - y};
-            bar.slots[slot] = {jb, x, 1, steps_of(jb, 0, p.causal), steps_of(jb, 1, p.causal)};
+            bar.slots[slot] = {jb, x, 1, steps_of<2>(jb, 0, p.causal), steps_of<2>(jb, 1, p.causal)};
             mbar_arrive(smem_u32(&bar.job_full[slot]));
           }
           if (!ok || !wait_asleep(smem_u32(&bar.want), (uint32_t)i & 1, abort_flag)) { ok = false; break; }
@@ -652,19 +653,101 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
 // Two such tiles' outputs would leave TMEM no room for scores: a block takes one tile of 128 rows, whose outputs have up to 256 columns, and its scores go
 // to the other two times 128 in turn. The tensor cores have the next step's scores, and the last step's products, while the four warps of the rows are at
 // their exponentials. Keys and values come in pieces that a product takes whole: 128 x 128 numbers of a head of 256, 128 x 192 of 192. Bound by the products
-// (8192 tokens of 32 heads of 256: 651 us, 1,689 TFLOP/s) and, for 192, the rows' chain beside shorter ones (534 us, 1,543). A block takes one job: its
-// start and end, about 7 us, show where jobs are short (13 prompts of up to 2500 tokens, 28 heads of 256: 182 us, 844 TFLOP/s).
+// (8192 tokens of 32 heads of 256: 639 us, 1,720 TFLOP/s) and, for 192, the rows' chain beside shorter ones (511 us, 1,613). Blocks stay, as above: with
+// a block for each job 651 and 534; 13 prompts of up to 2500 tokens, 28 heads of 256: 152 us and 182, 100 prompts of 64 tokens 99 and 163.
 struct WideBarriers {
-  uint64_t q_full, full[8], empty[8], s_full[2], p_full[2], o_done[2], last_v, fixed;  // (even and odd steps have barriers of their own)
-  uint64_t red[8];
-  Job job;
+  uint64_t q_full, q_empty, full[8], empty[8], s_full[2], p_full[2], o_done[2], o_free, last_v, fixed, job_full[kSlots], job_empty[kSlots], want, answer;
+  alignas(16) uint4 response;
+  Slot slots[kSlots];
   uint32_t tmem;
   int abort_flag;
 };
 __host__ __device__ constexpr int pieces(int dim) { return dim == 256 ? 2 : 1; }
 __host__ __device__ constexpr int wide_ring(int dim) { return dim == 256 ? 5 : 3; }
 __host__ __device__ constexpr size_t wide_smem(int dim) { return (size_t)tile_bytes(dim) + wide_ring(dim) * (tile_bytes(dim) / pieces(dim)) + sizeof(WideBarriers); }
-constexpr int kWideThreads = 256, kWideTma = 4, kWideMma = 5, kWideFix = 6;
+constexpr int kWideThreads = 256, kWideTma = 4, kWideMma = 5, kWideFix = 6, kWideJobs = 7, kWideReaders = 4 + 3;
+
+// One warp's part: this block's job, and others' of blocks that have not begun, to the slots. (The kernel above has the same written out: its part as a
+// function takes 16,384 tokens of 32 heads of 128 from 1,262 to 1,285 us.)
+__device__ __forceinline__ void hand_out_jobs(const PromptArgs& p, WideBarriers& bar, volatile int* abort_flag, int lane) {
+  // this block's own job first, then others'
+  int x = blockIdx.x, y = blockIdx.y, i = 0;
+  int seq0 = 0, base = 0, start = 0, queries = 0, tiles = 0, upto = 0;  // 32 sequences, a lane each: tiles of them, and up to the lane's end
+  auto load = [&] {
+    const int q = seq0 + lane;
+    start = queries = 0;
+    if (q < p.seqs) {
+      start = prompt::clamp_at(p.starts[q], p.tokens);
+      const int end = prompt::clamp_at(p.starts[q + 1], p.tokens);
+      queries = end > start ? end - start : 0;
+    }
+    tiles = (queries + kTile - 1) / kTile;
+    upto = tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += u;
+    }
+    upto += base;
+  };
+  load();
+  bool ok = true;
+  for (uint32_t asked = 0;; ++asked) {
+    // the sequence of unit y, and its tile: the last tiles of a sequence, which see the most keys, first
+    if (y < base) { seq0 = base = 0; load(); }
+    int end;
+    while (y >= (end = __shfl_sync(0xffffffffu, upto, 31)) && seq0 + 32 < p.seqs) {
+      base = end;
+      seq0 += 32;
+      load();
+    }
+    if (y < end) {
+      const int slot = i % kSlots;
+      if (!wait_asleep(smem_u32(&bar.job_empty[slot]), (uint32_t)(i / kSlots & 1) ^ 1, abort_flag)) ok = false;
+      if (ok && y >= upto - tiles && y < upto) {
+        const int q = seq0 + lane;
+        const int32_t* ks = p.kv_starts ? p.kv_starts : p.starts;
+        const int k0 = prompt::clamp_at(ks[q], p.kv_tokens), k1 = prompt::clamp_at(ks[q + 1], p.kv_tokens);
+        const Job jb{1, start, queries, k0, k1 > k0 ? k1 - k0 : 0, upto - 1 - y};
+        bar.slots[slot] = {jb, x, 1, steps_of<1>(jb, 0, p.causal), 0};
+        mbar_arrive(smem_u32(&bar.job_full[slot]));
+      }
+      if (!ok || !wait_asleep(smem_u32(&bar.want), (uint32_t)i & 1, abort_flag)) { ok = false; break; }
+      ++i;
+    }
+    if (lane == 0) {
+      fence_proxy_async();  // (the last answer has been read)
+      mbar_arrive_expect_tx(smem_u32(&bar.answer), 16);
+      asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+                   ::"r"(smem_u32(&bar.response)), "r"(smem_u32(&bar.answer)) : "memory");
+    }
+    if (!mbar_wait_inline(smem_u32(&bar.answer), asked & 1, abort_flag)) {
+      int never = 0;
+      if (!mbar_wait_inline(smem_u32(&bar.answer), asked & 1, &never)) ok = false;
+    }
+    uint32_t taken, nx, ny;
+    asm volatile(
+        "{\n\t.reg .b128 r;\n\t.reg .pred p;\n\t.reg .b32 z, u;\n\t"
+        "ld.shared.b128 r, [%3];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t"
+        "mov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, %2, z, u}, r;\n\t}"
+        : "=r"(taken), "=r"(nx), "=r"(ny) : "r"(smem_u32(&bar.response)) : "memory");
+    __syncwarp();
+    if (!taken || !ok) break;
+    x = (int)nx;
+    y = (int)ny;
+  }
+  const int slot = i % kSlots;
+  if (ok && !wait_asleep(smem_u32(&bar.job_empty[slot]), (uint32_t)(i / kSlots & 1) ^ 1, abort_flag)) ok = false;
+  if (!ok) fail(abort_flag, p.status);
+  __syncwarp();
+  if (lane == 0) {
+    bar.slots[slot].valid = 0;
+    mbar_arrive(smem_u32(&bar.job_full[slot]));
+  }
+}
 
 template <class T, int D>
 __global__ void __launch_bounds__(kWideThreads, 1) prompt_wide_kernel(const __grid_constant__ Maps maps, const __grid_constant__ PromptArgs p) {
@@ -678,6 +761,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) prompt_wide_kernel(const __gr
   const uint32_t sq = smem_u32(smem), ring0 = sq + tile_bytes(D);
   if (threadIdx.x == 0) {
     mbar_init(smem_u32(&bar.q_full), 1);
+    mbar_init(smem_u32(&bar.q_empty), 1);
     for (int i = 0; i < kRing; ++i) {
       mbar_init(smem_u32(&bar.full[i]), 1);
       mbar_init(smem_u32(&bar.empty[i]), 1);
@@ -687,37 +771,35 @@ __global__ void __launch_bounds__(kWideThreads, 1) prompt_wide_kernel(const __gr
       mbar_init(smem_u32(&bar.p_full[i]), 4);
       mbar_init(smem_u32(&bar.o_done[i]), 1);
     }
+    for (int i = 0; i < kSlots; ++i) {
+      mbar_init(smem_u32(&bar.job_full[i]), 1);
+      mbar_init(smem_u32(&bar.job_empty[i]), kWideReaders);
+    }
+    mbar_init(smem_u32(&bar.o_free), 4);
     mbar_init(smem_u32(&bar.last_v), 1);
     mbar_init(smem_u32(&bar.fixed), 1);
+    mbar_init(smem_u32(&bar.want), 1);
+    mbar_init(smem_u32(&bar.answer), 1);
     bar.abort_flag = 0;
     fence_barrier_init();
   }
-  grid_dep_wait();
-  if (!prompt::find_job(p, kTile, blockIdx.y, &bar.job, bar.red)) return;
-  const Job jb = bar.job;
   if (warp == kWideMma) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bar.tmem)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  grid_dep_wait();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *const_cast<volatile uint32_t*>(&bar.tmem);
-  const int head = blockIdx.x, kvh = head / (p.heads / p.kv_heads), row0 = jb.tile * kTile, behind = jb.queries - row0, rows = behind < kTile ? behind : kTile;
-  int64_t most = p.causal ? (int64_t)row0 + rows + (jb.keys - jb.queries) : jb.keys;
-  most = most < 0 ? 0 : most > jb.keys ? jb.keys : most;
-  const int n = (int)((most + kTile - 1) / kTile);  // steps
-  const bool cut = n * kTile > jb.keys;             // the last step's tile ends behind the sequence
+  const int group = p.heads / p.kv_heads;
 
-  if (warp == kWideTma && elect_one() && n > 0) {
-    const uint32_t qf = smem_u32(&bar.q_full);
-    mbar_arrive_expect_tx(qf, tile_bytes(D));
-#pragma unroll
-    for (int b = 0; b < D / 64; ++b) tma_load_3d(sq + b * kBox, &maps.q, b * 64, head, jb.start + row0, qf);
-    uint32_t st = 0, ph = 0;
+  if (warp == kWideJobs) hand_out_jobs(p, bar, abort_flag, lane);
+  if (warp == kWideTma && elect_one()) {
+    uint32_t st = 0, ph = 0, with_keys = 0;  // (with_keys: jobs that have steps so far)
     int issued = 0;
     bool ok = true;
-    auto load = [&](const CUtensorMap* map, int key) {
+    auto load = [&](const CUtensorMap* map, int kvh, int key) {
 #pragma unroll
       for (int c = 0; c < kPieces; ++c) {
         if (!mbar_wait(smem_u32(&bar.empty[st]), ph ^ 1, abort_flag)) { ok = false; return; }
@@ -729,27 +811,43 @@ __global__ void __launch_bounds__(kWideThreads, 1) prompt_wide_kernel(const __gr
         if (++st == (uint32_t)kRing) { st = 0; ph ^= 1; }
       }
     };
-    // in the order of the products: two steps' scores lead
-    for (int j = -2; ok && j < n; ++j) {
-      const int key = jb.kv_start + j * kTile;
-      if (j >= 0) load(&maps.v, key);
-      if (ok && j + 2 < n) load(&maps.k, key + 2 * kTile);
+    for (int i = 0; ok; ++i) {
+      const int slot = i % kSlots;
+      if (!wait_asleep(smem_u32(&bar.job_full[slot]), (uint32_t)(i / kSlots) & 1, abort_flag)) { ok = false; break; }
+      const Slot sl = bar.slots[slot];
+      mbar_arrive(smem_u32(&bar.job_empty[slot]));
+      if (!sl.valid) break;
+      const int n = sl.n0, kvh = sl.head / group;
+      if (n == 0) continue;
+      if (!mbar_wait(smem_u32(&bar.q_empty), (with_keys & 1) ^ 1, abort_flag)) { ok = false; break; }
+      ++with_keys;
+      const uint32_t qf = smem_u32(&bar.q_full);
+      mbar_arrive_expect_tx(qf, tile_bytes(D));
+#pragma unroll
+      for (int b = 0; b < D / 64; ++b) tma_load_3d(sq + b * kBox, &maps.q, b * 64, sl.head, sl.job.start + sl.job.tile * kTile, qf);
+      // in the order of the products: two steps' scores lead
+      for (int j = -2; ok && j < n; ++j) {
+        const int key = sl.job.kv_start + j * kTile;
+        if (j >= 0) load(&maps.v, kvh, key);
+        if (ok && j + 2 < n) load(&maps.k, kvh, key + 2 * kTile);
+      }
     }
     // the last arrivals at these barriers come before the block ends
+    if (ok && with_keys > 0) ok = mbar_wait(smem_u32(&bar.q_empty), (with_keys - 1) & 1, abort_flag);
     for (int i = issued > kRing ? issued - kRing : 0; ok && i < issued; ++i) ok = mbar_wait(smem_u32(&bar.empty[i % kRing]), (uint32_t)(i / kRing) & 1, abort_flag);
     if (!ok) {
       fail(abort_flag, p.status);
       int never = 0;  // the copies in flight end before the block does (each of these waits is bounded too)
-      mbar_wait(qf, 0, &never);
+      if (with_keys > 0) mbar_wait(smem_u32(&bar.q_full), (with_keys - 1) & 1, &never);
       for (int i = issued > kRing ? issued - kRing : 0; i < issued; ++i) mbar_wait(smem_u32(&bar.full[i % kRing]), (uint32_t)(i / kRing) & 1, &never);
     }
   }
-  if (warp == kWideMma && elect_one() && n > 0) {
+  if (warp == kWideMma && elect_one()) {
     constexpr uint32_t type = std::is_same<T, __half>::value ? 0u : (1u << 7) | (1u << 10);
     const uint32_t id_s = idesc_e4m3(kTile) | type, id_o = idesc_e4m3(kBoxes * 64) | type | 1u << 16;  // (bit 16: B's rows are K)
     const uint32_t dq = desc_low(sq, 16), dk = desc_low(ring0, 16), dv = desc_low(ring0, kBox);
-    uint32_t st = 0, ph = 0;
-    bool ok = mbar_poll(smem_u32(&bar.q_full), 0, abort_flag);
+    uint32_t st = 0, ph = 0, base = 0, with_keys = 0, fix_phase = 0;  // (base: steps of the jobs so far)
+    bool ok = true;
     auto there = [&] {
       ok = ok && mbar_poll(smem_u32(&bar.full[st]), ph, abort_flag);
       tc_fence_after();
@@ -759,171 +857,222 @@ __global__ void __launch_bounds__(kWideThreads, 1) prompt_wide_kernel(const __gr
       mma_commit(smem_u32(&bar.empty[st]));
       if (++st == (uint32_t)kRing) { st = 0; ph ^= 1; }
     };
-    auto scores = [&](int j) {
-#pragma unroll
-      for (int c = 0; c < kPieces; ++c) {
-        if (!there()) return;
-#pragma unroll
-        for (int s = 0; s < kBoxes * 4; ++s) {
-          const uint32_t at = ((s >> 2) * kBox + (s & 3) * 32) >> 4;
-          mma_ss(tmem + (j & 1) * kTile, dq + c * (kPiece >> 4) + at, dk + st * (kPiece >> 4) + at, id_s, c > 0 || s > 0);
-        }
-        used();
+    for (int i = 0; ok; ++i) {
+      const int slot = i % kSlots;
+      if (!wait_long(smem_u32(&bar.job_full[slot]), (uint32_t)(i / kSlots) & 1, abort_flag)) { ok = false; break; }
+      const int valid = bar.slots[slot].valid, n = bar.slots[slot].n0, want = n > kAhead ? n - kAhead : 0;
+      const bool cut = n * kTile > bar.slots[slot].job.keys;  // the last step's tile ends behind the sequence
+      mbar_arrive(smem_u32(&bar.job_empty[slot]));
+      if (!valid) break;
+      if (n == 0) {
+        mbar_arrive(smem_u32(&bar.want));
+        continue;
       }
-      mma_commit(smem_u32(&bar.s_full[j & 1]));
-    };
-    if (ok) scores(0);
-    if (ok && n > 1) scores(1);
-    for (int j = 0; ok && j < n; ++j) {
-      if (cut && j == n - 1) {
-        // (all of the last values: the pieces behind this one are in the next places)
+      auto scores = [&](int j) {
+        const uint32_t odd = (base + j) & 1;
 #pragma unroll
         for (int c = 0; c < kPieces; ++c) {
-          const bool over = st + c >= (uint32_t)kRing;
-          ok = ok && mbar_poll(smem_u32(&bar.full[over ? st + c - kRing : st + c]), over ? ph ^ 1 : ph, abort_flag);
+          if (!there()) return;
+#pragma unroll
+          for (int s = 0; s < kBoxes * 4; ++s) {
+            const uint32_t at = ((s >> 2) * kBox + (s & 3) * 32) >> 4;
+            mma_ss(tmem + odd * kTile, dq + c * (kPiece >> 4) + at, dk + st * (kPiece >> 4) + at, id_s, c > 0 || s > 0);
+          }
+          used();
         }
-        if (ok) mbar_arrive(smem_u32(&bar.last_v));
-        ok = ok && mbar_poll(smem_u32(&bar.fixed), 0, abort_flag);
-      }
-      ok = ok && mbar_poll(smem_u32(&bar.p_full[j & 1]), (uint32_t)(j >> 1) & 1, abort_flag);
+        mma_commit(smem_u32(&bar.s_full[odd]));
+        if (j + 1 == n) mma_commit(smem_u32(&bar.q_empty));
+      };
+      if (!mbar_poll(smem_u32(&bar.q_full), with_keys & 1, abort_flag)) { ok = false; break; }
+      scores(0);
+      if (ok && n > 1) scores(1);
+      for (int j = 0; ok && j < n; ++j) {
+        const uint32_t step = base + j, odd = step & 1;
+        if (j == want) mbar_arrive(smem_u32(&bar.want));
+        if (cut && j == n - 1) {
+          // (all of the last values: the pieces behind this one are in the next places)
 #pragma unroll
-      for (int c = 0; c < kPieces; ++c) {
-        if (!there()) break;
+          for (int c = 0; c < kPieces; ++c) {
+            const bool over = st + c >= (uint32_t)kRing;
+            ok = ok && mbar_poll(smem_u32(&bar.full[over ? st + c - kRing : st + c]), over ? ph ^ 1 : ph, abort_flag);
+          }
+          if (ok) mbar_arrive(smem_u32(&bar.last_v));
+          ok = ok && mbar_poll(smem_u32(&bar.fixed), fix_phase, abort_flag);
+          fix_phase ^= 1;
+        }
+        // (the last job's outputs have been read)
+        if (j == 0) ok = ok && mbar_poll(smem_u32(&bar.o_free), (with_keys & 1) ^ 1, abort_flag);
+        ok = ok && mbar_poll(smem_u32(&bar.p_full[odd]), (step >> 1) & 1, abort_flag);
 #pragma unroll
-        for (int s = 0; s < kTile / 16; ++s)
-          mma_ts(tmem + kO + c * (kBoxes * 64), tmem + (j & 1) * kTile + s * 8, dv + st * (kPiece >> 4) + (s * 2048 >> 4), id_o, j > 0 || s > 0);
-        used();
+        for (int c = 0; c < kPieces; ++c) {
+          if (!there()) break;
+#pragma unroll
+          for (int s = 0; s < kTile / 16; ++s)
+            mma_ts(tmem + kO + c * (kBoxes * 64), tmem + odd * kTile + s * 8, dv + st * (kPiece >> 4) + (s * 2048 >> 4), id_o, j > 0 || s > 0);
+          used();
+        }
+        if (!ok) break;
+        mma_commit(smem_u32(&bar.o_done[odd]));
+        if (j + 2 < n) scores(j + 2);
       }
-      if (!ok) break;
-      mma_commit(smem_u32(&bar.o_done[j & 1]));
-      if (j + 2 < n) scores(j + 2);
+      base += n;
+      ++with_keys;
     }
     if (!ok) fail(abort_flag, p.status);
   }
-  if (warp == kWideFix && cut && n > 0) {
-    // the last tile's value rows behind the sequence's end are another's: 0 instead, so that weights of 0 meet no NaN
-    if (mbar_wait(smem_u32(&bar.last_v), 0, abort_flag)) {
-      for (int c = 0; c < kPieces; ++c) {
-        uint8_t* v = smem + tile_bytes(D) + ((2 * n - 1) * kPieces + c) % kRing * kPiece;
-        for (int i = (jb.keys - (n - 1) * kTile) * 8 + lane; i < kTile * 8; i += 32)
-          for (int b = 0; b < kBoxes; ++b) reinterpret_cast<uint4*>(v + b * kBox)[i] = make_uint4(0, 0, 0, 0);
+  if (warp == kWideFix) {
+    uint32_t ring_at = 0, ends = 0;
+    for (int i = 0;; ++i) {
+      const int slot = i % kSlots;
+      if (!wait_asleep(smem_u32(&bar.job_full[slot]), (uint32_t)(i / kSlots) & 1, abort_flag)) break;
+      const Slot sl = bar.slots[slot];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bar.job_empty[slot]));
+      if (!sl.valid) break;
+      const int n = sl.n0;
+      ring_at += 2 * n * kPieces;
+      if (n * kTile <= sl.job.keys) continue;
+      // the last tile's value rows behind the sequence's end are another's: 0 instead, so that weights of 0 meet no NaN
+      if (!wait_asleep(smem_u32(&bar.last_v), ends & 1, abort_flag)) break;
+      ++ends;
+      for (int c = 1; c <= kPieces; ++c) {
+        uint8_t* v = smem + tile_bytes(D) + (ring_at - c) % kRing * kPiece;
+        for (int r = (sl.job.keys - (n - 1) * kTile) * 8 + lane; r < kTile * 8; r += 32)
+          for (int b = 0; b < kBoxes; ++b) reinterpret_cast<uint4*>(v + b * kBox)[r] = make_uint4(0, 0, 0, 0);
       }
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bar.fixed));
-    } else {
-      fail(abort_flag, p.status);
     }
   }
   if (warp < 4) {
-    const int row = warp * 32 + lane, at = row0 + row;  // this thread's row of the tile, and of the sequence
+    const int row = warp * 32 + lane;  // this thread's row of the tile
     const uint32_t lanes = (uint32_t)(warp * 32) << 16, to = tmem + kO + lanes;
     const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f), grow = kGrowth / c2;
-    int64_t see = p.causal ? (int64_t)at + (jb.keys - jb.queries) + 1 : jb.keys;
-    const int lim = (int)(see < 0 ? 0 : see > jb.keys ? jb.keys : see);
-    float m = -INFINITY, l = 0.0f;
+    uint32_t base = 0;
     bool ok = true;
-    for (int j = 0; j < n; ++j) {
-      const uint32_t ts = tmem + (j & 1) * kTile + lanes;
-      if (!mbar_wait_inline(smem_u32(&bar.s_full[j & 1]), (uint32_t)(j >> 1) & 1, abort_flag)) { ok = false; break; }
-      // (every phase of a barrier is met: these products came before the scores)
-      if (j >= 2 && !mbar_wait_inline(smem_u32(&bar.o_done[j & 1]), (uint32_t)((j - 2) >> 1) & 1, abort_flag)) { ok = false; break; }
-      tc_fence_after();
-      float s[kTile];
+    for (int i = 0; ok; ++i) {
+      const int slot = i % kSlots;
+      if (!wait_long(smem_u32(&bar.job_full[slot]), (uint32_t)(i / kSlots) & 1, abort_flag)) { ok = false; break; }
+      const Job jb = bar.slots[slot].job;
+      const int head = bar.slots[slot].head, valid = bar.slots[slot].valid, n = bar.slots[slot].n0;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bar.job_empty[slot]));
+      if (!valid) break;
+      const int at = jb.tile * kTile + row;  // and of the sequence
+      int64_t see = p.causal ? (int64_t)at + (jb.keys - jb.queries) + 1 : jb.keys;
+      const int lim = (int)(see < 0 ? 0 : see > jb.keys ? jb.keys : see);
+      float m = -INFINITY, l = 0.0f;
+      auto products = [&](uint32_t step) { return mbar_wait_inline(smem_u32(&bar.o_done[step & 1]), (step >> 1) & 1, abort_flag); };
+      for (int j = 0; j < n; ++j) {
+        const uint32_t step = base + j, ts = tmem + (step & 1) * kTile + lanes;
+        if (!mbar_wait_inline(smem_u32(&bar.s_full[step & 1]), (step >> 1) & 1, abort_flag)) { ok = false; break; }
+        // (every phase of a barrier is met: these products came before the scores)
+        if (j >= 2 && !products(step - 2)) { ok = false; break; }
+        tc_fence_after();
+        float s[kTile];
 #pragma unroll
-      for (int i = 0; i < kTile; i += 32) tmem_ld32(ts + i, s + i);
-      tmem_wait_ld();
+        for (int k = 0; k < kTile; k += 32) tmem_ld32(ts + k, s + k);
+        tmem_wait_ld();
 #pragma unroll
-      for (int i = 0; i < kTile; i += 32) settle(s + i);
-      const int here = lim - j * kTile;  // places of this tile that the row sees
-      if (__any_sync(0xffffffffu, here < kTile)) {
+        for (int k = 0; k < kTile; k += 32) settle(s + k);
+        const int here = lim - j * kTile;  // places of this tile that the row sees
+        if (__any_sync(0xffffffffu, here < kTile)) {
 #pragma unroll
-        for (int i = 0; i < kTile; ++i)
-          if (i >= here) s[i] = -INFINITY;
-      }
-      float a[4] = {s[0], s[1], s[2], s[3]};
+          for (int k = 0; k < kTile; ++k)
+            if (k >= here) s[k] = -INFINITY;
+        }
+        float a[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-      for (int i = 4; i < kTile; i += 4)
+        for (int k = 4; k < kTile; k += 4)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) a[c] = fmaxf(a[c], s[i + c]);
-      const float top = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
-      const bool grew = top > m + grow;  // (from -infinity: any score)
-      if (__any_sync(0xffffffffu, grew)) {
-        const float f = grew ? ex2((m - top) * c2) : 1.0f;
-        if (grew) m = top;
-        l *= f;
-        if (j > 0) {
-          // (the last step's products come behind these scores)
-          if (!mbar_wait_inline(smem_u32(&bar.o_done[(j - 1) & 1]), (uint32_t)((j - 1) >> 1) & 1, abort_flag)) { ok = false; break; }
-          tc_fence_after();
+          for (int c = 0; c < 4; ++c) a[c] = fmaxf(a[c], s[k + c]);
+        const float top = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
+        const bool grew = top > m + grow;  // (from -infinity: any score)
+        if (__any_sync(0xffffffffu, grew)) {
+          const float f = grew ? ex2((m - top) * c2) : 1.0f;
+          if (grew) m = top;
+          l *= f;
+          if (j > 0) {
+            // (the last step's products come behind these scores)
+            if (!products(step - 1)) { ok = false; break; }
+            tc_fence_after();
 #pragma unroll
-          for (int i = 0; i < D; i += 16) {
-            uint32_t o[16];
-            tmem_ld16(to + i, o);
-            tmem_wait_ld();
-            reg_fence16(o);
+            for (int k = 0; k < D; k += 16) {
+              uint32_t o[16];
+              tmem_ld16(to + k, o);
+              tmem_wait_ld();
+              reg_fence16(o);
 #pragma unroll
-            for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
-            tmem_st16(to + i, o);
+              for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
+              tmem_st16(to + k, o);
+            }
           }
         }
-      }
-      float ref = m == -INFINITY ? 0.0f : m;
-      // the factor goes into one multiply-add with the maximum, but where scores are so large that its rounding shows
-      if (__any_sync(0xffffffffu, fabsf(ref * c2) > 1e5f)) {
+        float ref = m == -INFINITY ? 0.0f : m;
+        // the factor goes into one multiply-add with the maximum, but where scores are so large that its rounding shows
+        if (__any_sync(0xffffffffu, fabsf(ref * c2) > 1e5f)) {
 #pragma unroll
-        for (int i = 0; i < kTile; ++i) s[i] -= ref;
-        ref = 0.0f;
-      }
-      const uint64_t c22 = two_of(c2, c2), r22 = two_of(-ref * c2, -ref * c2);
-      uint64_t sum[2] = {0, 0};
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        uint32_t w[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float x, y;
-          one_each(fma2(two_of(s[32 * h + 2 * i], s[32 * h + 2 * i + 1]), c22, r22), x, y);
-          x = ex2(x);
-          y = ex2(y);
-          sum[i & 1] = add2(sum[i & 1], two_of(x, y));
-          w[i] = pack(x, y, (T*)nullptr);
+          for (int k = 0; k < kTile; ++k) s[k] -= ref;
+          ref = 0.0f;
         }
-        tmem_st16(ts + 16 * h, w);
+        const uint64_t c22 = two_of(c2, c2), r22 = two_of(-ref * c2, -ref * c2);
+        uint64_t sum[2] = {0, 0};
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          uint32_t w[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            float x, y;
+            one_each(fma2(two_of(s[32 * h + 2 * k], s[32 * h + 2 * k + 1]), c22, r22), x, y);
+            x = ex2(x);
+            y = ex2(y);
+            sum[k & 1] = add2(sum[k & 1], two_of(x, y));
+            w[k] = pack(x, y, (T*)nullptr);
+          }
+          tmem_st16(ts + 16 * h, w);
+        }
+        float u, v;
+        one_each(add2(sum[0], sum[1]), u, v);
+        l += u + v;
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bar.p_full[step & 1]));
       }
-      float u, v;
-      one_each(add2(sum[0], sum[1]), u, v);
-      l += u + v;
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bar.p_full[j & 1]));
+      for (int j = n > 1 ? n - 2 : 0; ok && j < n; ++j) ok = products(base + j);
+      if (!ok) break;
+      base += n;
+      tc_fence_after();
+      const bool live = at < jb.queries;
+      const float inv = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
+      T* y = static_cast<T*>(p.out) + (int64_t)(jb.start + at) * p.ldo + (int64_t)head * p.ldoh;
+#pragma unroll
+      for (int k = 0; k < D; k += 32) {
+        float o[32];
+        if (n > 0) {
+          tmem_ld32(to + k, o);
+          tmem_wait_ld();
+          settle(o);
+        } else {
+#pragma unroll
+          for (int c = 0; c < 32; ++c) o[c] = 0.0f;
+        }
+        if (k + 32 == D && n > 0) {  // read: the next job's products may come
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&bar.o_free));
+        }
+        if (live) {
+#pragma unroll
+          for (int c = 0; c < 32; c += 8)
+            *reinterpret_cast<uint4*>(y + k + c) = make_uint4(pack(o[c] * inv, o[c + 1] * inv, (T*)nullptr), pack(o[c + 2] * inv, o[c + 3] * inv, (T*)nullptr),
+                                                              pack(o[c + 4] * inv, o[c + 5] * inv, (T*)nullptr), pack(o[c + 6] * inv, o[c + 7] * inv, (T*)nullptr));
+        }
+      }
+      if (live && p.lse) p.lse[(int64_t)(jb.start + at) * p.heads + head] = fmaf(m, c2, log2f(l)) * kLn2;
     }
-    for (int j = n > 1 ? n - 2 : 0; ok && j < n; ++j) ok = mbar_wait_inline(smem_u32(&bar.o_done[j & 1]), (uint32_t)(j >> 1) & 1, abort_flag);
     if (!ok) fail(abort_flag, p.status);
-    tc_fence_after();
-    const bool live = row < behind;
-    const float inv = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
-    T* y = static_cast<T*>(p.out) + (int64_t)(jb.start + at) * p.ldo + (int64_t)head * p.ldoh;
-#pragma unroll 2
-    for (int i = 0; i < D; i += 32) {
-      float o[32];
-      if (n > 0) {
-        tmem_ld32(to + i, o);
-        tmem_wait_ld();
-        settle(o);
-      } else {
-#pragma unroll
-        for (int c = 0; c < 32; ++c) o[c] = 0.0f;
-      }
-      if (live && ok) {
-#pragma unroll
-        for (int c = 0; c < 32; c += 8)
-          *reinterpret_cast<uint4*>(y + i + c) = make_uint4(pack(o[c] * inv, o[c + 1] * inv, (T*)nullptr), pack(o[c + 2] * inv, o[c + 3] * inv, (T*)nullptr),
-                                                            pack(o[c + 4] * inv, o[c + 5] * inv, (T*)nullptr), pack(o[c + 6] * inv, o[c + 7] * inv, (T*)nullptr));
-      }
-    }
-    if (live && ok && p.lse) p.lse[(int64_t)(jb.start + at) * p.heads + head] = fmaf(m, c2, log2f(l)) * kLn2;
     tc_fence_before();
   }
   __syncthreads();
