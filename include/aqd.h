@@ -468,8 +468,9 @@ aqd_status aqd_linear_int8(const aqd_linear_args* args, const aqd_linear_weights
  * slot g * page_size + p. A place holds, of each head, a key row and a value row: head_dim (64, 128, 192 or 256) codes of 4 bits,
  * the row's lowest value and its step, both bfloat16:
  *   low = the largest bfloat16 <= min_k x_k,  step = the least bfloat16 >= (max_k x_k - low) / 15 (at least 2^-126, but 0 where max = low),
- *   code_k = (x_k - low) / step to the nearest, ties to even (0 where step = 0);  value = low + step * code.
- * So a value is off by half a step at most. Rows that hold a NaN or an infinity, or whose values span more than float32's range, read back
+ *   code_k = (x_k - low) / step to the nearest, ties to even (0 where step = 0; what is within 2^-18 of a tie without being one may go to
+ *   either side);  value = low + step * code.
+ * So a value is off by half a step at most, and by 2^-18 of one more beside a tie. Rows that hold a NaN or an infinity, or whose values span more than float32's range, read back
  * as NaN. The layout within a page is the library's own. */
 typedef struct {
   void* data; /* aqd_kv_cache_bytes(...) bytes (device), 256-byte aligned; its first contents do not matter */

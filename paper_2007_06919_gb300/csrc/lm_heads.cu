@@ -7,7 +7,7 @@
 // warp takes a token's heads in turn (rows_kernel), its lanes keep their places in the row, and with them the products of weights, cosines and sines;
 // float32 goes in pairs; 16-bit minima and maxima stay packed; codes come out of the bits of one multiply-add.
 //   8192 tokens of 40 heads of 128 in bfloat16: 32.7 us, 168 MB at 5.1 TB/s (47 with a row at a time, its indexes, weights and turns looked up for
-//   each); with keys and values to the cache 41.1, 177 MB. 16,384 tokens' 16 rows to codes: 19.6 us, 85 MB at 4.3 TB/s (46), and back 13.8 (34).
+//   each); with keys and values to the cache 41.6, 177 MB. 16,384 tokens' 16 rows to codes: 20.1 us, 85 MB at 4.2 TB/s (46), and back 13.8 (34).
 // What holds them back is bytes on their way: 90 registers leave 20 warps an SM, with two rows' loads each and the next two's lines asked for without a
 // register (38.4 us, and 47.3, with 24 warps and none asked for ahead; 36.8 with all of a token's asked for at once; 39 with 16 warps). Four rows at once
 // (75 registers for codes, fewer warps) 21.7, weights and turns in shared memory 52 to 78.
@@ -107,6 +107,10 @@ struct RowStep {
     low = __uint_as_float(l);
     const float span = __fsub_rn(hi, low);
     uint32_t s = __float_as_uint(quotient(span, 15.0f, 1.0f / 15.0f)) + 0xffffu & 0xffff0000u;
+    // The span and the quotient are rounded, each maybe down to 15 steps and to a step: the next step then, if 15 of these are less than the span and what
+    // its rounding left over (12 bits against a number beside them: the difference is exact).
+    const float back = __fsub_rn(span, hi), over = __fsub_rn(__fsub_rn(hi, __fsub_rn(span, back)), __fadd_rn(low, back));
+    if (__fmaf_rn(15.0f, __uint_as_float(s), -span) < over) s += 0x10000u;
     s = hi == low ? 0u : s < 0x00800000u ? 0x00800000u : s;
     const bool fine = fabsf(low) < INFINITY && span < INFINITY;
     word = fine ? l >> 16 | s : 0x7fc07fc0u;

@@ -113,6 +113,22 @@ def check_held(got, x):
     assert ((got == want) | (tie & ((got == other[0]) | (got == other[1])))).all()
 
 
+# Spans a little over 15 times a bfloat16, which float32 rounds down to it: the step is the next one.
+@pytest.mark.parametrize("dtype,low,high", [(F32, -8.0, 7 + 2.0 ** -21), (F32, -2.0 ** -30, 15.0), (F16, -2.0 ** -24, 15.0), (BF16, -2.0 ** -40, 30.0), (F32, -3.0, 12 + 2.0 ** -20),
+                                            (F32, 0.0, 15 + 2.0 ** -20), (F32, -8.0, 7 - 2.0 ** -21)])
+@pytest.mark.parametrize("pad", [0, 1])
+def test_step_of_a_span_just_over_fifteen(dtype, low, high, pad):
+    cache = aqd.KVCache(2, 16, 2, 64)
+    _, k, v = inputs(5, 9, 1, 2, 64, dtype, pad)
+    k, v = (x.abs().clamp(0.5, 6.5) for x in (k, v))
+    k[..., 5], k[..., 60], v[..., 31], v[..., 0] = low, high, low, high
+    slots = slots_for(cache, 9)
+    aqd.cache_write(cache, k, v, slots)
+    gk, gv = aqd.cache_read(cache, slots, dtype=F32)
+    check_held(gk, k)
+    check_held(gv, v)
+
+
 @pytest.mark.parametrize("pad", [0, 1])
 @pytest.mark.parametrize("tokens,kv,dim,page,dtype", [(1, 8, 128, 64, BF16), (100, 2, 64, 16, F16), (77, 3, 192, 32, F32), (300, 1, 256, 1024, BF16),
                                                       (1000, 5, 128, 128, F32), (40, 4, 64, 256, BF16)])
