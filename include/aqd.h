@@ -485,6 +485,7 @@ size_t aqd_kv_cache_bytes(int64_t pages, int32_t page_size, int32_t kv_heads, in
  *   u_k = x_k / sqrt(mean(x^2) + eps) * weight_k  (weight NULL: u = x, for queries and keys each; head_dim values of weight_dtype),
  *   then pair f of the first rot_dim places turns by the angle a = positions[token] * inv_freq[f], f < rot_dim / 2:
  *   (u_i, u_j) -> (u_i cos a - u_j sin a, u_j cos a + u_i sin a), with i = f, j = f + rot_dim / 2, or, if interleaved, i = 2 f, j = 2 f + 1.
+ * eps >= 0. Rows of any finite values are normalized alike, those whose squares leave float32's range too (a row of zeros with eps = 0: NaN).
  * The angle is exact to 2^-24 of a turn while |position| (1 + |inv_freq|) < 2^38 (it is reduced in fixed point). rot_dim: even, 0..head_dim.
  * head_dim: even, 2..512 (with a cache: its own). q_out may be q, and k_out k (same pointer and strides).
  * heads may be 0 (keys alone). cache NULL: v and slots are not read. With a cache, each token's keys (rotated and rounded to `dtype`) and

@@ -90,6 +90,24 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
+// Norms whose mean of squares and eps lie outside [2^-100, infinity): below, squares (each off by up to 2^-150) and products with weights lose bits that count in the
+// result; above, the sum is infinite. The row is taken times a power of two that brings the larger of its largest value and the root of that mean to [1, 4)
+// (a subnormal value to 2^-23 at least), and eps times its square. So rows of any finite values come out as ordinary ones do; one of zeros with eps = 0 is
+// 0 / 0, and what holds a NaN or an infinity stays as it is.
+__device__ __forceinline__ bool off_range(float mean_eps) { return __float_as_uint(mean_eps) - 0x0d800000u >= 0x7f800000u - 0x0d800000u; }
+// 1 / sqrt of a mean within it
+__device__ __forceinline__ float root(float mean_eps) {
+  float r;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(mean_eps));
+  return r;
+}
+// That power for a row whose largest magnitude is `top`; 1 for rows that stay as they are.
+__device__ __forceinline__ float into_range(float mean_eps, float top) {
+  if (!off_range(mean_eps) || isnan(mean_eps) || !(top > 0.0f && top < INFINITY)) return 1.0f;
+  const int e = 254 - (int)(__float_as_uint(mean_eps < INFINITY ? fmaxf(top, sqrtf(mean_eps)) : top) >> 23);
+  return __uint_as_float((uint32_t)(e < 1 ? 1 : e > 253 ? 253 : e) << 23);
+}
+
 // The quotient a / b from inv, 1 / b to about a step: what a first one leaves over corrects it. Exact where the quotient is a float32 (16-bit rows meet
 // codes exactly halfway between two often, and those have to stay there).
 __device__ __forceinline__ float quotient(float a, float b, float inv) {
@@ -201,7 +219,24 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const QkArgs p, const i
     const void* w = is_v ? nullptr : is_q ? p.q_weight : p.k_weight;
     if (w) {
       for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      const float rms = rsqrtf(ss / (float)p.dim + p.eps);
+      float mean = ss / (float)p.dim + p.eps;
+      if (off_range(mean)) {  // (every lane has the same sum)
+        float top = 0.0f;
+#pragma unroll
+        for (int c = 0; c < kC; ++c) top = fmaxf(top, fmaxf(fabsf(a[c]), fabsf(b[c])));
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float s = into_range(mean, top);
+        ss = 0.0f;
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+          a[c] *= s;
+          b[c] *= s;
+          ss = fmaf(a[c], a[c], fmaf(b[c], b[c], ss));
+        }
+        for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        mean = ss / (float)p.dim + p.eps * s * s;
+      }
+      const float rms = rsqrtf(mean);
 #pragma unroll
       for (int c = 0; c < kC; ++c) {
         if (ia[c] < 0) continue;
@@ -530,17 +565,41 @@ __global__ void __launch_bounds__(kThreads, kPlain ? 8 : 5) rows_kernel(const Qk
           to_pairs<T>(b, v);
           uint64_t f = two_of(1.0f, 1.0f);
           if (weight) {
-            uint64_t s0 = 0, s1 = 0;
+            auto squares = [&] {
+              uint64_t s0 = 0, s1 = 0;
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
-              s0 = fma2(u[i], u[i], s0);
-              s1 = fma2(v[i], v[i], s1);
+              for (int i = 0; i < kPairs; ++i) {
+                s0 = fma2(u[i], u[i], s0);
+                s1 = fma2(v[i], v[i], s1);
+              }
+              float ss, s2;
+              one_each(add2(s0, s1), ss, s2);
+              ss += s2;
+              for (int o = lanes >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+              return ss;
+            };
+            const float mean = fmaf(squares(), per_value, p.eps);
+            float rms = root(mean);
+            if (__any_sync(0xffffffffu, off_range(mean))) {
+              float top = 0.0f;
+#pragma unroll
+              for (int i = 0; i < kPairs; ++i) {
+                float c, d;
+                one_each(u[i], c, d);
+                top = fmaxf(top, fmaxf(fabsf(c), fabsf(d)));
+                one_each(v[i], c, d);
+                top = fmaxf(top, fmaxf(fabsf(c), fabsf(d)));
+              }
+              for (int o = lanes >> 1; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+              const float s = into_range(mean, top);  // (1 for the other rows of the warp: theirs come out as before)
+              const uint64_t by = two_of(s, s);
+#pragma unroll
+              for (int i = 0; i < kPairs; ++i) {
+                u[i] = mul2(u[i], by);
+                v[i] = mul2(v[i], by);
+              }
+              rms = rsqrtf(fmaf(squares(), per_value, p.eps * s * s));
             }
-            float ss, s2;
-            one_each(add2(s0, s1), ss, s2);
-            ss += s2;
-            for (int o = lanes >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            const float rms = rsqrtf(fmaf(ss, per_value, p.eps));
             f = two_of(rms, rms);
           }
           uint64_t ya[kPairs], yb[kPairs];
