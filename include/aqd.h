@@ -550,7 +550,7 @@ typedef struct {
   float* lse;               /* [tokens][heads] or NULL */
   const int32_t* starts;    /* [seqs + 1] or NULL */
   const int32_t* lengths;   /* [seqs] */
-  const int32_t* page_table; /* [seqs][ld_table], `columns` of them used */
+  const int32_t* page_table; /* [seqs][ld_table], `columns` of them used; ld_table 0: one row for all */
   int64_t ld_table;
   int32_t columns;
 } aqd_cache_attention_args;

@@ -1029,7 +1029,7 @@ def cache_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, l
                     starts: torch.Tensor | None = None, scale: float | None = None, out: torch.Tensor | None = None,
                     lse: bool | torch.Tensor = False, workspace: torch.Tensor | None = None, stream=None):
     """Attention of each sequence's last tokens over the cache (aqd_cache_attention): q [tokens, heads, head_dim], page_table int32
-    [seqs, columns], lengths int32 [seqs] (places of each sequence, its queries' own among them), starts int32 [seqs + 1] for several
+    [seqs, columns] (expanded: one row for all), lengths int32 [seqs] (places of each sequence, its queries' own among them), starts int32 [seqs + 1] for several
     queries a sequence. scale: 1 / sqrt(head_dim) where not given. Returns the output, or (output, lse [tokens, heads]) where lse is wanted.
     workspace: cache_attention_workspace(q, cache, seqs), which calls that may overlap in time must not share."""
     dev = cache.index
@@ -1044,6 +1044,10 @@ def cache_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, l
     lt, last = page_table.stride()
     if last != 1 and cols > 1:
         raise ValueError("the entries of a row of page_table must be adjacent")
+    if seqs < 2:
+        lt = max(lt, cols)
+    elif 0 < lt < cols:
+        raise ValueError("rows of page_table must not overlap (but one row may be all sequences')")
     lp = _vector(lengths, seqs, torch.int32, "lengths", dev)
     stp = 0 if starts is None else _vector(starts, seqs + 1, torch.int32, "starts", dev)
     o, lo, loh = _out_heads(out, q, "out", stream)
@@ -1056,7 +1060,7 @@ def cache_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, l
     elif not workspace.is_cuda or workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous CUDA tensor on the call's device")
     args = _CACHE_ATTENTION.pack(n, seqs, h, dt, d ** -0.5 if scale is None else scale, q.data_ptr(), lq, lqh, o.data_ptr(), lo, loh, ep,
-                                 stp, lp, page_table.data_ptr(), max(lt, cols), cols)
+                                 stp, lp, page_table.data_ptr(), lt, cols)
     _check(_calls().aqd_cache_attention(args, cache.desc, workspace.data_ptr(), workspace.nbytes, _stream(stream)),
            "aqd_cache_attention")
     return o if e is None else (o, e)

@@ -1194,8 +1194,8 @@ aqd_status aqd_cache_attention(const aqd_cache_attention_args* n, const aqd_kv_c
   if (!f && n->dtype != AQD_F16 && n->dtype != AQD_BF16) f = "dtype must be AQD_F16 or AQD_BF16";
   if (!f && !(n->scale > 0.0f && std::isfinite(n->scale))) f = "scale must be positive and finite";
   if (!f && !n->starts && n->tokens != n->seqs) f = "without starts there is one token for each sequence";
-  if (!f && (n->columns < 0 || n->ld_table < n->columns || (int64_t)n->columns * cache->page_size > INT_MAX - 1024))
-    f = "columns must be >= 0, at most ld_table, and its places below 2^31 - 1024";
+  if (!f && (n->columns < 0 || (n->ld_table < n->columns && n->ld_table != 0) || (int64_t)n->columns * cache->page_size > INT_MAX - 1024))
+    f = "columns must be >= 0, at most ld_table (or ld_table 0), and its places below 2^31 - 1024";
   if (!f && n->tokens > 0 && n->seqs > 0) {
     f = heads_fault(n->q, n->ldq, n->ldqh, 2);
     if (!f) f = heads_out_fault(n->out, n->ldo, n->ldoh, 2, n->tokens, n->heads, cache->head_dim);
