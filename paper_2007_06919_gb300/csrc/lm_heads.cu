@@ -769,10 +769,10 @@ static cudaError_t run_heads_type(const QkArgs& a, cudaStream_t stream) {
     return a.interleaved ? cudaLaunchKernelEx(&cfg, rows_kernel<T, false, true, false>, a, share, lanes, log2)
                          : cudaLaunchKernelEx(&cfg, rows_kernel<T, false, false, false>, a, share, lanes, log2);
   }
-  // a block's tokens: one while that leaves SMs without a block, else enough for four rows a warp
+  // a block's tokens: one while that leaves SMs without a block, else enough for four rows a warp, as far as their cosines and sines fit in 32 KB
   const int each = a.heads + a.kv_heads * (a.cache.data ? 2 : 1);
   int per = 1;
-  while (per * 2 * each <= 32 && a.tokens / (per * 2) >= 4 * 152) per *= 2;
+  while (per * 2 * each <= 32 && a.tokens / (per * 2) >= 4 * 152 && per * 2 * (a.rot / 2) * sizeof(float2) <= 32768) per *= 2;
   config(cfg, at, (a.tokens + per - 1) / per, (size_t)per * (a.rot / 2) * sizeof(float2), stream);
   if (a.cache.data) return cudaLaunchKernelEx(&cfg, heads_kernel<T, true>, a, per, div_magic(each));
   return cudaLaunchKernelEx(&cfg, heads_kernel<T, false>, a, per, div_magic(each));
