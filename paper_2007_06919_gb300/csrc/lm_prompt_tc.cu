@@ -492,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
     const int t = warp >> 2, row = (warp & 3) * 32 + lane;  // (a warp reads the quarter of TMEM's lanes that its number gives)
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, to = tmem + kO + t * D + lanes;
-    const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f), grow = kGrowth / c2;
+    const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f), grow = fminf(kGrowth / c2, 3.402823466e38f);
     uint32_t steps = 0, ends = 0;  // this tile's steps so far, and phases of o_done
     const uint32_t tile = tmem + t * kCols + lanes;
     bool ok = true;
@@ -538,7 +538,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
 #pragma unroll
           for (int c = 0; c < 4; ++c) a[c] = fmaxf(a[c], s[i2 + c]);
         const float top = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
-        const bool grew = top > m + grow;  // (from -infinity: any score)
+        const bool grew = top > m + grow;  // (from -infinity: any score; `grow` is finite for that)
         if (__any_sync(0xffffffffu, grew)) {
           const float f = grew ? ex2((m - top) * c2) : 1.0f;
           if (grew) m = top;
@@ -948,7 +948,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) prompt_wide_kernel(const __gr
   if (warp < 4) {
     const int row = warp * 32 + lane;  // this thread's row of the tile
     const uint32_t lanes = (uint32_t)(warp * 32) << 16, to = tmem + kO + lanes;
-    const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f), grow = kGrowth / c2;
+    const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f), grow = fminf(kGrowth / c2, 3.402823466e38f);
     uint32_t base = 0;
     bool ok = true;
     for (int i = 0; ok; ++i) {
@@ -988,7 +988,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) prompt_wide_kernel(const __gr
 #pragma unroll
           for (int c = 0; c < 4; ++c) a[c] = fmaxf(a[c], s[k + c]);
         const float top = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
-        const bool grew = top > m + grow;  // (from -infinity: any score)
+        const bool grew = top > m + grow;  // (from -infinity: any score; `grow` is finite for that)
         if (__any_sync(0xffffffffu, grew)) {
           const float f = grew ? ex2((m - top) * c2) : 1.0f;
           if (grew) m = top;
