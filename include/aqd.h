@@ -561,8 +561,7 @@ aqd_status aqd_cache_attention(const aqd_cache_attention_args* args, const aqd_k
  * kv_starts[s] .. kv_starts[s+1] - 1 (kv_starts NULL: the same). causal: query j of n sees the first m - n + j + 1 of its sequence's m keys; else all.
  * o and lse as above; a query that sees nothing gets 0 and -infinity; rows behind the last sequence are left as they were. dtype (q, k, v, out): AQD_F16 or
  * AQD_BF16; head_dim 64, 128, 192 or 256; every pointer of them 16-byte aligned, every stride a multiple of 8 elements. Scores, statistics and sums
- * are float32; p is rounded to dtype before it meets v. Within a sequence, a NaN or infinity in a value row may reach queries up to 255 places before
- * it; other sequences' rows are never read into a result. tokens and kv_tokens: rows of q and of k. */
+ * are float32; p is rounded to dtype before it meets v. A key or value that a query does not see reaches no output of it, be it NaN or infinite. tokens and kv_tokens: rows of q and of k. */
 typedef struct {
   int64_t tokens, kv_tokens;
   int32_t seqs, heads, kv_heads, head_dim, dtype, causal;

@@ -50,8 +50,9 @@ __device__ __forceinline__ uint32_t at(uint32_t base, int r, int c) {
   return base + r * (D * 2) + ((c & ~7) | ((c ^ r) & 7)) * 16;
 }
 
+// (heads of 128: two blocks an SM by shared memory, not three by registers, which would spill)
 template <class T, int D>
-__global__ void __launch_bounds__(kThreads) prompt_kernel(const __grid_constant__ PromptArgs p) {
+__global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 0) prompt_kernel(const __grid_constant__ PromptArgs p) {
   constexpr int kKeys = keys_of(D), kTile = kKeys * D * 2, kChunks = D / 8;
   extern __shared__ __align__(128) uint8_t smem[];  // queries, two stages of keys and values
   __shared__ Job job;
@@ -181,6 +182,20 @@ __global__ void __launch_bounds__(kThreads) prompt_kernel(const __grid_constant_
     for (int i = 0; i < D / 8; ++i) *reinterpret_cast<uint32_t*>(y + 8 * i) = pack(o[i][2 * h] * inv, o[i][2 * h + 1] * inv, (T*)nullptr);
     if (p.lse && (lane & 3) == 0) p.lse[token * p.heads + head] = fmaf(m[h], c2, log2f(l[h])) * kLn2;
   }
+  // rows that a hidden value reached, a warp its own
+  const Job je = job;  // (read again: its numbers are not kept through the tiles)
+  const int first = je.tile * kRows + warp * 16;
+  if (!p.causal || first >= je.queries) return;
+  const int last = last_not_finite<T, D>(seen_by(je, first), tiles * kKeys < je.keys ? tiles * kKeys : je.keys, [&](int t, int i) {
+    const int tile = t / kKeys;  // (the last two tiles' values are still here)
+    uint4 x;
+    if (tile >= tiles - 2) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at<D>(sk + ((tile & 1) * 2 + 1) * kTile, t - tile * kKeys, i)));
+    else x = reinterpret_cast<const uint4*>(v + t * p.ldv)[i];
+    return x;
+  });
+  __syncwarp();  // (the rows' first outputs come before)
+#pragma unroll 1
+  for (int at = first; at < first + 16 && at < je.queries && seen_by(je, at) <= last; ++at) attend_again<T, D>(p, je, head, at, seen_by(je, at));
 }
 
 template <class T, int D>

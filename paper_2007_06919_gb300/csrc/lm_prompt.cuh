@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "kernels.h"
 #include "lm_seq.cuh"
@@ -60,6 +61,106 @@ static __device__ __forceinline__ bool find_job(const PromptArgs& p, int rows, i
   return job->found != 0;
 }
 
+// Values that the causal order hides from a row, in the last tiles of keys that its block takes: a weight of 0 does not keep out a NaN or an infinity, since 0
+// times it is NaN. Rows behind whose last key such a value lies are taken again after the products, key by key, one warp a row.
+
+__device__ __forceinline__ void pairs_of(const uint4& w, float2 (&f)[4], __half*) {
+  f[0] = __half22float2(*reinterpret_cast<const __half2*>(&w.x));
+  f[1] = __half22float2(*reinterpret_cast<const __half2*>(&w.y));
+  f[2] = __half22float2(*reinterpret_cast<const __half2*>(&w.z));
+  f[3] = __half22float2(*reinterpret_cast<const __half2*>(&w.w));
+}
+__device__ __forceinline__ float2 pair_of(uint32_t w, __half*) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+__device__ __forceinline__ float2 pair_of(uint32_t w, __nv_bfloat16*) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ void pairs_of(const uint4& w, float2 (&f)[4], __nv_bfloat16* t) {
+  f[0] = pair_of(w.x, t); f[1] = pair_of(w.y, t); f[2] = pair_of(w.z, t); f[3] = pair_of(w.w, t);
+}
+
+// The last of the keys lo .. hi - 1 whose value row has a NaN or an infinity, or -1: a lane to a key. row(t, i): 16 bytes of it.
+template <class T, int D, class Row>
+__device__ __forceinline__ int last_not_finite(int lo, int hi, Row row) {
+  constexpr uint32_t kExponent = std::is_same<T, __half>::value ? 0x7c007c00u : 0x7f807f80u, kLow = kExponent & 0xffffu;
+  const int lane = threadIdx.x & 31;
+  for (int end = hi; end > lo; end -= 32) {
+    const int t = end - 32 + lane;
+    bool bad = false;
+    if (t >= lo) {
+#pragma unroll 4
+      for (int i = 0; i < D / 8; ++i) {
+        const uint4 x = row(t, i);
+        const uint32_t w[4] = {x.x & kExponent, x.y & kExponent, x.z & kExponent, x.w & kExponent};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) bad = bad || (w[j] & 0xffffu) == kLow || w[j] >= kLow << 16;
+      }
+    }
+    const uint32_t found = __ballot_sync(0xffffffffu, bad);
+    if (found) return end - 1 - __clz(found);
+  }
+  return -1;
+}
+// Output of row `at` of a job's sequence over the first `lim` keys: scores with a lane to a key, weights times values with D / 32 channels a lane, as above.
+template <class T, int D>
+__device__ __forceinline__ void attend_again(const PromptArgs& p, const Job& jb, int head, int at, int lim) {
+  constexpr int kPairs = D / 64;
+  const int lane = threadIdx.x & 31, kvh = head / (p.heads / p.kv_heads);
+  const T* q = static_cast<const T*>(p.q) + (int64_t)(jb.start + at) * p.ldq + (int64_t)head * p.ldqh;
+  const T* k = static_cast<const T*>(p.k) + (int64_t)jb.kv_start * p.ldk + (int64_t)kvh * p.ldkh;
+  const T* v = static_cast<const T*>(p.v) + (int64_t)jb.kv_start * p.ldv + (int64_t)kvh * p.ldvh + lane * (D / 32);
+  const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f);
+  float m = -INFINITY, l = 0.0f;
+  float2 o[kPairs];
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) o[i] = make_float2(0.0f, 0.0f);
+  for (int t0 = 0; t0 < lim; t0 += 32) {
+    const int here = lim - t0 < 32 ? lim - t0 : 32;
+    float s = -INFINITY;
+    if (lane < here) {
+      const uint4* row = reinterpret_cast<const uint4*>(k + (t0 + lane) * p.ldk);
+      float a = 0.0f, b = 0.0f;
+#pragma unroll 4
+      for (int i = 0; i < D / 8; ++i) {
+        float2 x[4], y[4];
+        pairs_of(reinterpret_cast<const uint4*>(q)[i], x, (T*)nullptr);
+        pairs_of(row[i], y, (T*)nullptr);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { a = fmaf(x[j].x, y[j].x, a); b = fmaf(x[j].y, y[j].y, b); }
+      }
+      s = a + b;
+    }
+    float top = s;
+    for (int n = 16; n > 0; n >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, n));
+    top = fmaxf(m, top);
+    const float ref = top == -INFINITY ? 0.0f : top, f = ex2((m - ref) * c2), w = ex2((s - ref) * c2);
+    const uint32_t w2 = pack(w, w, (T*)nullptr);
+    m = top;
+    l = fmaf(l, f, w);
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) { o[i].x *= f; o[i].y *= f; }
+    for (int j = 0; j < here; ++j) {
+      const float x = pair_of(__shfl_sync(0xffffffffu, w2, j), (T*)nullptr).x;
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        const float2 y = pair_of(*reinterpret_cast<const uint32_t*>(v + (t0 + j) * p.ldv + 2 * i), (T*)nullptr);
+        o[i].x = fmaf(x, y.x, o[i].x);
+        o[i].y = fmaf(x, y.y, o[i].y);
+      }
+    }
+    bool lost = true;
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) lost = lost && isnan(o[i].x) && isnan(o[i].y);
+    if (__all_sync(0xffffffffu, lost)) break;  // (nothing is left to find)
+  }
+  for (int n = 16; n > 0; n >>= 1) l += __shfl_xor_sync(0xffffffffu, l, n);
+  const float inv = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
+  T* y = static_cast<T*>(p.out) + (int64_t)(jb.start + at) * p.ldo + (int64_t)head * p.ldoh + lane * (D / 32);
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) *reinterpret_cast<uint32_t*>(y + 2 * i) = pack(o[i].x * inv, o[i].y * inv, (T*)nullptr);
+}
+// Keys that row `at` of a job's sequence sees, in causal order.
+__device__ __forceinline__ int seen_by(const Job& jb, int at) {
+  const int64_t see = (int64_t)at + (jb.keys - jb.queries) + 1;
+  return (int)(see < 0 ? 0 : see > jb.keys ? jb.keys : see);
+}
 
 }  // namespace prompt
 }  // namespace aqd

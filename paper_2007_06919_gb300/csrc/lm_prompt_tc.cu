@@ -61,12 +61,40 @@ struct Slot {
   Job job;
   int32_t head, valid, n0, n1;  // n: steps of the two tiles
 };
+// Jobs with outputs that are not finite, of which a value that their rows do not see may be the reason: those rows are taken again at the block's end. The rows' warps mark
+// a job by its number, modulo kMarks; the warp that hands jobs out, which gives out one more when they have begun the one kSlots before it, keeps the one before
+// that if it is marked, and takes over no more jobs once it has kSpoiled.
+constexpr int kSpoiled = 8, kMarks = 8;
+static_assert(kMarks > kSlots + 1 && (kMarks & (kMarks - 1)) == 0, "");
+struct Marked {
+  Job job;
+  int32_t head;
+};
+struct Spoiled {
+  int32_t mark[kMarks];
+  Marked last[kMarks];                    // the jobs of these numbers
+  Marked jobs[kSpoiled];
+  int32_t count;
+  // (a whole warp, which counts)
+  __device__ __forceinline__ void keep(int number, int lane, int& kept) {
+    const int at = number & (kMarks - 1);
+    if (*const_cast<volatile int32_t*>(&mark[at])) {
+      __syncwarp();
+      if (lane == 0) {
+        jobs[kept] = last[at];
+        mark[at] = 0;
+      }
+      ++kept;
+    }
+  }
+};
 // Whoever waits on a barrier meets every one of its phases, and none of them runs two ahead of it. Where scores run ahead, a warp may hand over its next
 // weights before another warp of the tile has its last ones ready: weights of even and odd steps have barriers of their own.
 struct Barriers {
   uint64_t q_full[2], q_empty[2], full[8], empty[8], s_full[2], p_full[2][2], o_done[2], o_free[2], s_read[2], last_v, fixed, job_full[kSlots], job_empty[kSlots], want, answer;
   alignas(16) uint4 response;
   Slot slots[kSlots];
+  Spoiled spoiled;
   uint32_t tmem;
   int abort_flag;
 };
@@ -172,6 +200,32 @@ __device__ __forceinline__ bool wait_asleep(uint32_t bar, uint32_t parity, volat
   }
 }
 
+// At the end of a job's row: its mark where an output is not finite (sums of its row's products with 0 are NaN then).
+__device__ __forceinline__ void mark_if_spoiled(const uint64_t (&sums)[2], bool live, uint32_t mark) {
+  float a, b;
+  one_each(add2(sums[0], sums[1]), a, b);
+  // (without a branch: the loop around keeps its registers)
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 q, %1, 0;\n\tsetp.neu.and.f32 p, %0, 0f00000000, q;\n\t@p st.shared.u32 [%2], 1;\n\t}" ::"f"(a + b), "r"((int)live), "r"(mark) : "memory");
+}
+// The block's end: each row of the kept jobs, and of the last ones that are marked, whose last key lies before a value that is not finite. For the four warps beside the
+// rows' (it takes 70 registers), as a call, with a copy of the arguments: what the compiler does to the jobs' loop for the code here, for a call of theirs, or for one that
+// might change the arguments, costs heads of 64 1 to 4% more (8192 tokens, 32 heads 248 us, 245 with neither marks nor this).
+template <class T, int D, int kTiles>
+static __device__ __noinline__ void take_rows_again(const PromptArgs& p, const Spoiled& spoiled, int warp) {
+  for (int i = 0; i < spoiled.count + kMarks; ++i) {
+    const int number = i - spoiled.count;  // (behind the kept jobs the last ones)
+    if (number >= 0 && !spoiled.mark[number]) continue;
+    const Marked& which = number < 0 ? spoiled.jobs[i] : spoiled.last[number];
+    const Job jb = which.job;
+    const int head = which.head, n0 = steps_of<kTiles>(jb, 0, 1), n1 = kTiles > 1 ? steps_of<kTiles>(jb, 1, 1) : 0, keys = (n0 > n1 ? n0 : n1) * kTile;
+    const int first = jb.tile * kTiles * kTile, end = first + kTiles * kTile < jb.queries ? first + kTiles * kTile : jb.queries;
+    const T* v = static_cast<const T*>(p.v) + (int64_t)jb.kv_start * p.ldv + (int64_t)(head / (p.heads / p.kv_heads)) * p.ldvh;
+    const int last = prompt::last_not_finite<T, D>(prompt::seen_by(jb, first), keys < jb.keys ? keys : jb.keys,
+                                                   [&](int t, int c) { return reinterpret_cast<const uint4*>(v + t * p.ldv)[c]; });
+    for (int at = first + warp; at < end && prompt::seen_by(jb, at) <= last; at += 4) prompt::attend_again<T, D>(p, jb, head, at, prompt::seen_by(jb, at));
+  }
+}
+
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ PromptArgs p) {
   constexpr int kBytes = tile_bytes(D), kRing = ring(D), kBoxes = D / 64, kBox = kTile * 128;
@@ -208,6 +262,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
     mbar_init(smem_u32(&bar.fixed), 1);
     mbar_init(smem_u32(&bar.want), 1);
     mbar_init(smem_u32(&bar.answer), 1);
+    for (int i = 0; i < kMarks; ++i) bar.spoiled.mark[i] = 0;
     bar.abort_flag = 0;
     fence_barrier_init();
   }
@@ -226,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
     if (warp == kWarpJobs) {
       // this block's own job first, then others'
-      int x = blockIdx.x, y = blockIdx.y, i = 0;
+      int x = blockIdx.x, y = blockIdx.y, i = 0, kept = 0;
       int seq0 = 0, base = 0, start = 0, queries = 0, tiles = 0, upto = 0;  // 32 sequences, a lane each: tiles of them, and up to the lane's end
       auto load = [&] {
         const int q = seq0 + lane;
@@ -264,12 +319,15 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
             const int32_t* ks = p.kv_starts ? p.kv_starts : p.starts;
             const int k0 = prompt::clamp_at(ks[q], p.kv_tokens), k1 = prompt::clamp_at(ks[q + 1], p.kv_tokens);
             const Job jb{1, start, queries, k0, k1 > k0 ? k1 - k0 : 0, upto - 1 - y};
+            bar.spoiled.last[i & (kMarks - 1)] = {jb, x};
             bar.slots[slot] = {jb, x, 1, steps_of<2>(jb, 0, p.causal), steps_of<2>(jb, 1, p.causal)};
             mbar_arrive(smem_u32(&bar.job_full[slot]));
           }
+          bar.spoiled.keep(i - kSlots - 1, lane, kept);
           if (!ok || !wait_asleep(smem_u32(&bar.want), (uint32_t)i & 1, abort_flag)) { ok = false; break; }
           ++i;
         }
+        if (kept >= kSpoiled) break;
         if (lane == 0) {
           fence_proxy_async();  // (the last answer has been read)
           mbar_arrive_expect_tx(smem_u32(&bar.answer), 16);
@@ -300,6 +358,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
       __syncwarp();
       if (lane == 0) {
         bar.slots[slot].valid = 0;
+        bar.spoiled.count = kept;
         mbar_arrive(smem_u32(&bar.job_full[slot]));
       }
     }
@@ -492,6 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
     const int t = warp >> 2, row = (warp & 3) * 32 + lane;  // (a warp reads the quarter of TMEM's lanes that its number gives)
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, to = tmem + kO + t * D + lanes;
+    const uint32_t marks = smem_u32(bar.spoiled.mark);
     const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f), grow = fminf(kGrowth / c2, 3.402823466e38f);
     uint32_t steps = 0, ends = 0;  // this tile's steps so far, and phases of o_done
     const uint32_t tile = tmem + t * kCols + lanes;
@@ -612,6 +672,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
       const float inv = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
       T* y = static_cast<T*>(p.out) + (int64_t)(jb.start + at) * p.ldo + (int64_t)head * p.ldoh;
       if (behind > 0) {
+        uint64_t zero[2] = {0, 0};
 #pragma unroll
         for (int i2 = 0; i2 < D; i2 += 32) {
           float o[32];
@@ -628,6 +689,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bar.o_free[t]));
           }
+#pragma unroll
+          for (int c = 0; c < 32; c += 2) zero[c >> 1 & 1] = fma2(two_of(o[c], o[c + 1]), 0, zero[c >> 1 & 1]);
           if (live) {
 #pragma unroll
             for (int c = 0; c < 32; c += 8)
@@ -636,12 +699,17 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
           }
         }
         if (live && p.lse) p.lse[(int64_t)(jb.start + at) * p.heads + head] = fmaf(m, c2, log2f(l)) * kLn2;
+        mark_if_spoiled(zero, live, marks + (i & (kMarks - 1)) * 4);
       }
     }
     if (!ok) fail(abort_flag, p.status);
     tc_fence_before();
   }
   __syncthreads();
+  if (warp >= kSoftWarps && p.causal && !bar.abort_flag && (bar.spoiled.count > 0 || __any_sync(0xffffffffu, bar.spoiled.mark[lane & (kMarks - 1)]))) {
+    const PromptArgs copy = p;
+    take_rows_again<T, D, 2>(copy, bar.spoiled, warp - kSoftWarps);
+  }
   if (warp == kWarpMma) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
@@ -659,6 +727,7 @@ struct WideBarriers {
   uint64_t q_full, q_empty, full[8], empty[8], s_full[2], p_full[2], o_done[2], o_free, last_v, fixed, job_full[kSlots], job_empty[kSlots], want, answer;
   alignas(16) uint4 response;
   Slot slots[kSlots];
+  Spoiled spoiled;
   uint32_t tmem;
   int abort_flag;
 };
@@ -671,7 +740,7 @@ constexpr int kWideThreads = 256, kWideTma = 4, kWideMma = 5, kWideFix = 6, kWid
 // function takes 16,384 tokens of 32 heads of 128 from 1,262 to 1,285 us.)
 __device__ __forceinline__ void hand_out_jobs(const PromptArgs& p, WideBarriers& bar, volatile int* abort_flag, int lane) {
   // this block's own job first, then others'
-  int x = blockIdx.x, y = blockIdx.y, i = 0;
+  int x = blockIdx.x, y = blockIdx.y, i = 0, kept = 0;
   int seq0 = 0, base = 0, start = 0, queries = 0, tiles = 0, upto = 0;  // 32 sequences, a lane each: tiles of them, and up to the lane's end
   auto load = [&] {
     const int q = seq0 + lane;
@@ -709,12 +778,15 @@ __device__ __forceinline__ void hand_out_jobs(const PromptArgs& p, WideBarriers&
         const int32_t* ks = p.kv_starts ? p.kv_starts : p.starts;
         const int k0 = prompt::clamp_at(ks[q], p.kv_tokens), k1 = prompt::clamp_at(ks[q + 1], p.kv_tokens);
         const Job jb{1, start, queries, k0, k1 > k0 ? k1 - k0 : 0, upto - 1 - y};
+        bar.spoiled.last[i & (kMarks - 1)] = {jb, x};
         bar.slots[slot] = {jb, x, 1, steps_of<1>(jb, 0, p.causal), 0};
         mbar_arrive(smem_u32(&bar.job_full[slot]));
       }
+      bar.spoiled.keep(i - kSlots - 1, lane, kept);
       if (!ok || !wait_asleep(smem_u32(&bar.want), (uint32_t)i & 1, abort_flag)) { ok = false; break; }
       ++i;
     }
+    if (kept >= kSpoiled) break;
     if (lane == 0) {
       fence_proxy_async();  // (the last answer has been read)
       mbar_arrive_expect_tx(smem_u32(&bar.answer), 16);
@@ -745,6 +817,7 @@ __device__ __forceinline__ void hand_out_jobs(const PromptArgs& p, WideBarriers&
   __syncwarp();
   if (lane == 0) {
     bar.slots[slot].valid = 0;
+    bar.spoiled.count = kept;
     mbar_arrive(smem_u32(&bar.job_full[slot]));
   }
 }
@@ -780,6 +853,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) prompt_wide_kernel(const __gr
     mbar_init(smem_u32(&bar.fixed), 1);
     mbar_init(smem_u32(&bar.want), 1);
     mbar_init(smem_u32(&bar.answer), 1);
+    for (int i = 0; i < kMarks; ++i) bar.spoiled.mark[i] = 0;
     bar.abort_flag = 0;
     fence_barrier_init();
   }
@@ -948,6 +1022,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) prompt_wide_kernel(const __gr
   if (warp < 4) {
     const int row = warp * 32 + lane;  // this thread's row of the tile
     const uint32_t lanes = (uint32_t)(warp * 32) << 16, to = tmem + kO + lanes;
+    const uint32_t marks = smem_u32(bar.spoiled.mark);
     const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f), grow = fminf(kGrowth / c2, 3.402823466e38f);
     uint32_t base = 0;
     bool ok = true;
@@ -1047,6 +1122,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) prompt_wide_kernel(const __gr
       const bool live = at < jb.queries;
       const float inv = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
       T* y = static_cast<T*>(p.out) + (int64_t)(jb.start + at) * p.ldo + (int64_t)head * p.ldoh;
+      uint64_t zero[2] = {0, 0};
 #pragma unroll
       for (int k = 0; k < D; k += 32) {
         float o[32];
@@ -1063,6 +1139,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) prompt_wide_kernel(const __gr
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&bar.o_free));
         }
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) zero[c >> 1 & 1] = fma2(two_of(o[c], o[c + 1]), 0, zero[c >> 1 & 1]);
         if (live) {
 #pragma unroll
           for (int c = 0; c < 32; c += 8)
@@ -1071,11 +1149,16 @@ __global__ void __launch_bounds__(kWideThreads, 1) prompt_wide_kernel(const __gr
         }
       }
       if (live && p.lse) p.lse[(int64_t)(jb.start + at) * p.heads + head] = fmaf(m, c2, log2f(l)) * kLn2;
+      mark_if_spoiled(zero, live, marks + (i & (kMarks - 1)) * 4);
     }
     if (!ok) fail(abort_flag, p.status);
     tc_fence_before();
   }
   __syncthreads();
+  if (warp >= 4 && p.causal && !bar.abort_flag && (bar.spoiled.count > 0 || __any_sync(0xffffffffu, bar.spoiled.mark[lane & (kMarks - 1)]))) {
+    const PromptArgs copy = p;
+    take_rows_again<T, D, 1>(copy, bar.spoiled, warp - 4);
+  }
   if (warp == kWideMma) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
