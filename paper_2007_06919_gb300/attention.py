@@ -19,11 +19,20 @@ from .feedforward import FeedForward, Head, _Part, _workspace
 class Tokens:
     """Where a call's tokens lie: device tensors for the operators. starts [seqs + 1]: the tokens of each sequence; positions and slots [tokens];
     lengths [seqs]: places of each sequence with these tokens; table [seqs, columns]: its pages; fresh: whether all sequences begin here; one:
-    whether each has one token."""
+    whether each has one token. They may be dropped while a stream still reads them."""
 
     def __init__(self, starts, positions, slots, lengths, table, fresh: bool, one: bool):
         self.starts, self.positions, self.slots, self.lengths, self.table = starts, positions, slots, lengths, table
         self.fresh, self.one = fresh, one
+        self._readers = set()
+
+    def _read_on(self, stream):
+        """Keeps the tensors' memory, once they are dropped, until this stream has finished with it."""
+        handle = aqd._stream(stream)
+        if handle not in self._readers:
+            for t in (self.starts, self.positions, self.slots, self.lengths, self.table):
+                t.record_stream(torch.cuda.current_stream() if stream is None else stream)
+            self._readers.add(handle)
 
 
 class Sequences:
@@ -94,6 +103,7 @@ class Attention(_Part):
     def __call__(self, x: torch.Tensor, residual: torch.Tensor | None, tokens: Tokens, cache: aqd.KVCache, stream=None, workspace=None):
         """(block's output, x + residual) of x [tokens, d], whose keys and values go into the cache. workspace: as a feed-forward block's."""
         self._read_on(stream)
+        tokens._read_on(stream)
         if workspace is None:
             workspace = _workspace(x.shape[0], (self.qkv, self.out), stream)
         q8 = aqd.rms_norm_quant(x, self.norm, eps=self.eps, residual=residual, stream=stream)
