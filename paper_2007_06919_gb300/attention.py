@@ -101,7 +101,11 @@ class Attention(_Part):
         self._memory += [t for t in (q_norm, k_norm, inv_freq) if t is not None]
 
     def __call__(self, x: torch.Tensor, residual: torch.Tensor | None, tokens: Tokens, cache: aqd.KVCache, stream=None, workspace=None):
-        """(block's output, x + residual) of x [tokens, d], whose keys and values go into the cache. workspace: as a feed-forward block's."""
+        """(block's output, x + residual) of x [tokens, d] in 16 bits, whose keys and values go into the cache. workspace: as a feed-forward block's."""
+        if x.dtype not in (torch.float16, torch.bfloat16):
+            raise ValueError(f"attention takes float16 or bfloat16, not {x.dtype}")
+        if (cache.kv_heads, cache.head_dim) != (self.kv_heads, self.dim):
+            raise ValueError("the cache has other heads than the block")
         self._read_on(stream)
         tokens._read_on(stream)
         if workspace is None:
@@ -133,11 +137,14 @@ class CausalDecoder:
         return [aqd.KVCache(pages, page_size, a.kv_heads, a.dim, device) for a, _ in self.blocks]
 
     def __call__(self, x: torch.Tensor, tokens: Tokens, caches: list[aqd.KVCache], stream=None) -> torch.Tensor:
-        """Logits [tokens, vocab] of tokens x [tokens, d]: whole prompts of new sequences, or further tokens of others."""
+        """Logits [tokens, vocab] of tokens x [tokens, d] in 16 bits: whole prompts of new sequences, or further tokens of others. Types and caches that do
+        not fit are refused before any cache is written."""
+        if len(caches) != len(self.blocks) or any((c.kv_heads, c.head_dim) != (a.kv_heads, a.dim) for c, (a, _) in zip(caches, self.blocks)):
+            raise ValueError("one cache for each layer, of its heads")
         layers = [w for a, f in self.blocks for w in (a.qkv, a.out, f.both, f.down)] + [self.head.proj]
         ws = _workspace(x.shape[0], layers, stream)
         residual = None
-        for (attention, feed), cache in zip(self.blocks, caches, strict=True):
+        for (attention, feed), cache in zip(self.blocks, caches):
             x, residual = attention(x, residual, tokens, cache, stream=stream, workspace=ws)
             x, residual = feed(x, residual, stream=stream, workspace=ws)
         return self.head(x, residual, stream=stream, workspace=ws)
