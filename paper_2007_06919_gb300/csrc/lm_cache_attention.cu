@@ -443,7 +443,7 @@ cache_attention_kernel(const __grid_constant__ CacheAttnArgs p, const __grid_con
     for (int c = 0; c < 2; ++c) {
       qs[t][c] = __shfl_sync(0xffffffffu, sum, (2 * q + c) * 4);
       qb[t][c] = -64.0f * __shfl_sync(0xffffffffu, odd, (2 * q + c) * 4);
-      c2[t][c] = fmaxf(__shfl_sync(0xffffffffu, down, (2 * q + c) * 4), 1.4e-45f);
+      c2[t][c] = fminf(fmaxf(__shfl_sync(0xffffffffu, down, (2 * q + c) * 4), 1.4e-45f), 3.402823466e38f);  // (a difference of 0 times it is 0)
     }
   }
 

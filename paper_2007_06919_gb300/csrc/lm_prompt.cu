@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 0) prompt_kernel(cons
   for (int i = 0; i < D / 8; ++i)
 #pragma unroll
     for (int c = 0; c < 4; ++c) o[i][c] = 0.0f;
-  const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f);
+  const float c2 = factor(p.scale);
   const int r0 = row0 + warp * 16 + (lane >> 2);  // this lane's rows: r0 and r0 + 8
   for (int t = 0; t < tiles; ++t) {
     const uint32_t kt = sk + (t & 1) * 2 * kTile, vt = kt + kTile;

@@ -20,6 +20,8 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Scores' factor in powers of two, neither 0 nor infinite (a difference of 0 times it is 0).
+__device__ __forceinline__ float factor(float scale) { return fminf(fmaxf(scale * kLog2e, 1.4e-45f), 3.402823466e38f); }
 __device__ __forceinline__ uint32_t pack(float a, float b, __half*) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -106,7 +108,7 @@ __device__ __forceinline__ void attend_again(const PromptArgs& p, const Job& jb,
   const T* q = static_cast<const T*>(p.q) + (int64_t)(jb.start + at) * p.ldq + (int64_t)head * p.ldqh;
   const T* k = static_cast<const T*>(p.k) + (int64_t)jb.kv_start * p.ldk + (int64_t)kvh * p.ldkh;
   const T* v = static_cast<const T*>(p.v) + (int64_t)jb.kv_start * p.ldv + (int64_t)kvh * p.ldvh + lane * (D / 32);
-  const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f);
+  const float c2 = factor(p.scale);
   float m = -INFINITY, l = 0.0f;
   float2 o[kPairs];
 #pragma unroll

@@ -552,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_tc_kernel(const __grid_con
     const int t = warp >> 2, row = (warp & 3) * 32 + lane;  // (a warp reads the quarter of TMEM's lanes that its number gives)
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, to = tmem + kO + t * D + lanes;
     const uint32_t marks = smem_u32(bar.spoiled.mark);
-    const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f), grow = fminf(kGrowth / c2, 3.402823466e38f);
+    const float c2 = prompt::factor(p.scale), grow = fminf(kGrowth / c2, 3.402823466e38f);
     uint32_t steps = 0, ends = 0;  // this tile's steps so far, and phases of o_done
     const uint32_t tile = tmem + t * kCols + lanes;
     bool ok = true;
@@ -1023,7 +1023,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) prompt_wide_kernel(const __gr
     const int row = warp * 32 + lane;  // this thread's row of the tile
     const uint32_t lanes = (uint32_t)(warp * 32) << 16, to = tmem + kO + lanes;
     const uint32_t marks = smem_u32(bar.spoiled.mark);
-    const float c2 = fmaxf(p.scale * kLog2e, 1.4e-45f), grow = fminf(kGrowth / c2, 3.402823466e38f);
+    const float c2 = prompt::factor(p.scale), grow = fminf(kGrowth / c2, 3.402823466e38f);
     uint32_t base = 0;
     bool ok = true;
     for (int i = 0; ok; ++i) {
