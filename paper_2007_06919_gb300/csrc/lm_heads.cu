@@ -6,12 +6,13 @@
 // lanes is a sum of squares and a row's lowest and highest value. Bound by memory, if the instructions for a value stay below about eight: a
 // warp takes a token's heads in turn (rows_kernel), its lanes keep their places in the row, and with them the products of weights, cosines and sines;
 // float32 goes in pairs; 16-bit minima and maxima stay packed; codes come out of the bits of one multiply-add.
-//   8192 tokens of 40 heads of 128 in bfloat16: 32.7 us, 168 MB at 5.1 TB/s (47 with a row at a time, its indexes, weights and turns looked up for
+//   8192 tokens of 40 heads of 128 in bfloat16: 32.6 us, 168 MB at 5.1 TB/s (47 with a row at a time, its indexes, weights and turns looked up for
 //   each); with keys and values to the cache 41.6, 177 MB. 16,384 tokens' 16 rows to codes: 20.1 us, 85 MB at 4.2 TB/s (46), and back 13.8 (34).
 // What holds them back is bytes on their way: 90 registers leave 20 warps an SM, with two rows' loads each and the next two's lines asked for without a
 // register (38.4 us, and 47.3, with 24 warps and none asked for ahead; 36.8 with all of a token's asked for at once; 39 with 16 warps). Four rows at once
 // (75 registers for codes, fewer warps) 21.7, weights and turns in shared memory 52 to 78.
-// Rows at any address, and rotations of any even length, take heads_kernel, a value at a time (14 heads of 64 in float32, 777 tokens: 4.4 us).
+// Rows at any address, and rotations of any even length, take heads_kernel, a value at a time: the 8192 tokens at odd addresses 129 us, bound by its instructions; 777 tokens
+// of 14 + 2 heads of 64 in float32 7.1, where rows_kernel takes 4.7.
 //
 // The angle of position p at frequency f is p f / 2 pi turns, of which the whole ones do not count: with u = frac(f / 2 pi) 2^64 cut to
 // an integer, p u mod 2^64 is the fraction, exact but for |p| (1 + |f|) 2^-64 of a turn, whatever the position. A block's sines and cosines are computed
@@ -549,7 +550,7 @@ __global__ void __launch_bounds__(kThreads, kPlain ? 8 : 5) rows_kernel(const Qk
         own_b[j / 2] = two_of(wb[j] * d0.x, wb[j + 1] * d1.x);
       }
     }
-    constexpr int kAtOnce = kCached && !kPlain ? 1 : 2;  // (with the codes' numbers, two rows would not fit three blocks' registers)
+    constexpr int kAtOnce = kCached && !kPlain ? 1 : 2;  // (with the codes' numbers, two rows would not fit the registers of five blocks an SM)
     for (int h0 = first; h0 < n; h0 += kAtOnce * step) {
       uint4 va[kAtOnce], vb[kAtOnce];
       fetch(va, vb, x, ldh, h0 + group, n);
@@ -738,8 +739,8 @@ static void config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* at, int64_t blo
   cfg.attrs = at;
   cfg.numAttrs = 1;
 }
-// Warps to a token: more while all of them are on the GPU at once (`blocks` an SM) and have rows for their groups of lanes. (40 heads of 128 and a cache,
-// 1024 tokens: two warps a token 8.7 us, four, in two rounds, 12.3, eight 19.1; 2048 tokens: one 13.0, two 14.8, four 21.4. These with 24 warps an SM.)
+// Warps to a token: more while all of them are on the GPU at once (`blocks` an SM) and have rows for their groups of lanes. (40 heads of 128 and a cache, us with
+// one, two and four warps a token: 512 tokens 9.1, 7.1, 6.9; 1024 tokens 10.4, 8.7, 11.8; 2048 tokens 12.9, 14.4, 17.6; 4096 tokens 24.4, 25.1, 34.4.)
 static int share_of(int64_t tokens, int rows, int groups, int blocks) {
   int share = 1;
   while (share < kThreads / 32 && 2 * share * tokens <= 152 * (kThreads / 32) * blocks && share * groups < rows) share *= 2;

@@ -6,8 +6,7 @@
 namespace aqd {
 namespace seq {
 
-// Sum over a block's threads and the sum before each, of two numbers at once (hi and lo halves of 64 bits; lo sums stay below 2^32).
-// red: one word for each warp and one more.
+// Sum of a block's threads' counts, and the sum before each. red: a word for each warp.
 __device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* red, uint64_t& before) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   uint64_t s = v;
