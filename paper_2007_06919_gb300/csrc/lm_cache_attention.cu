@@ -23,8 +23,9 @@
 // What a call spends, in cycles of a block (200,001 places, 2 heads; 22 us): 600 for the launch's order, 2,600 to find its work, 3,000 for page numbers
 // and query rows, 1,000 until the first copy is there, 14,000 to 19,000 in five or six steps, 3,000 to join, and 6,500 in the second kernel. A step of
 // 32 places is 590 instructions of a warp: 2,360 cycles where 16 warps share the SM, whose copies (70 KB) need 3,200 at 6.8 TB/s. Neither is what the steps take,
-// 4,600 to 5,000: with 800,001 places the cache comes in at 4.2 TB/s, with 64 sequences of 8192 at 4.4, with 16 of 32,768 at 4.8. Half of the issue slots are used:
-// four warps a scheduler do not hide a step's chain of shared-memory reads, products, exponentials and transposes.
+// 4,600 to 5,000: with 800,001 places the cache comes in at 4.2 TB/s, with 64 sequences of 8192 at 4.4, with 16 of 32,768 at 4.8. Over a whole
+// block the issue slots are 52% busy and the ALU pipe (shifts, logic: two cycles each) 56%, in the steps more; the warps' waits are spread over fixed latencies, that
+// pipe, each other and shared memory.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
