@@ -50,6 +50,11 @@ __device__ __forceinline__ uint32_t at(uint32_t base, int r, int c) {
   return base + r * (D * 2) + ((c & ~7) | ((c ^ r) & 7)) * 16;
 }
 
+// (a call, with copies: heads of 256 have no registers left for it)
+template <class T, int D>
+static __device__ __noinline__ void take_row_again(const PromptArgs p, const Job jb, int head, int at) {
+  attend_again<T, D>(p, jb, head, at);
+}
 // (heads of 128: two blocks an SM by shared memory, not three by registers, which would spill)
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 0) prompt_kernel(const __grid_constant__ PromptArgs p) {
@@ -195,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 0) prompt_kernel(cons
   });
   __syncwarp();  // (the rows' first outputs come before)
 #pragma unroll 1
-  for (int at = first; at < first + 16 && at < je.queries && seen_by(je, at) <= last; ++at) attend_again<T, D>(p, je, head, at, seen_by(je, at));
+  for (int at = first; at < first + 16 && at < je.queries && seen_by(je, at) <= last; ++at) take_row_again<T, D>(p, je, head, at);
 }
 
 template <class T, int D>

@@ -64,19 +64,11 @@ static __device__ __forceinline__ bool find_job(const PromptArgs& p, int rows, i
 }
 
 // Values that the causal order hides from a row, in the last tiles of keys that its block takes: a weight of 0 does not keep out a NaN or an infinity, since 0
-// times it is NaN. Rows behind whose last key such a value lies are taken again after the products, key by key, one warp a row.
+// times it is NaN. Rows behind whose last key such a value lies are taken again after the products, key by key, one warp a row. (16,384 tokens of 32 heads of 128 whose
+// last value row holds a NaN, 127 rows a head: 41 ms, where the call takes 1.3; with a lane to a key, and its 32 rows' sectors in turn, 157.)
 
-__device__ __forceinline__ void pairs_of(const uint4& w, float2 (&f)[4], __half*) {
-  f[0] = __half22float2(*reinterpret_cast<const __half2*>(&w.x));
-  f[1] = __half22float2(*reinterpret_cast<const __half2*>(&w.y));
-  f[2] = __half22float2(*reinterpret_cast<const __half2*>(&w.z));
-  f[3] = __half22float2(*reinterpret_cast<const __half2*>(&w.w));
-}
 __device__ __forceinline__ float2 pair_of(uint32_t w, __half*) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 __device__ __forceinline__ float2 pair_of(uint32_t w, __nv_bfloat16*) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
-__device__ __forceinline__ void pairs_of(const uint4& w, float2 (&f)[4], __nv_bfloat16* t) {
-  f[0] = pair_of(w.x, t); f[1] = pair_of(w.y, t); f[2] = pair_of(w.z, t); f[3] = pair_of(w.w, t);
-}
 
 // The last of the keys lo .. hi - 1 whose value row has a NaN or an infinity, or -1: a lane to a key. row(t, i): 16 bytes of it.
 template <class T, int D, class Row>
@@ -100,51 +92,77 @@ __device__ __forceinline__ int last_not_finite(int lo, int hi, Row row) {
   }
   return -1;
 }
-// Output of row `at` of a job's sequence over the first `lim` keys: scores with a lane to a key, weights times values with D / 32 channels a lane, as above.
+// Keys that row `at` of a job's sequence sees, in causal order.
+__device__ __forceinline__ int seen_by(const Job& jb, int at) {
+  const int64_t see = (int64_t)at + (jb.keys - jb.queries) + 1;
+  return (int)(see < 0 ? 0 : see > jb.keys ? jb.keys : see);
+}
+// Output of row `at` of a job's sequence, eight keys at a time: a lane has D / 32 channels of each, adds up its part of their scores, and the lanes' parts are
+// added so that lane n is left with key n's (and those lanes with it that have its number but for higher bits); weights times values as above.
 template <class T, int D>
-__device__ __forceinline__ void attend_again(const PromptArgs& p, const Job& jb, int head, int at, int lim) {
-  constexpr int kPairs = D / 64;
-  const int lane = threadIdx.x & 31, kvh = head / (p.heads / p.kv_heads);
-  const T* q = static_cast<const T*>(p.q) + (int64_t)(jb.start + at) * p.ldq + (int64_t)head * p.ldqh;
-  const T* k = static_cast<const T*>(p.k) + (int64_t)jb.kv_start * p.ldk + (int64_t)kvh * p.ldkh;
+__device__ __forceinline__ void attend_again(const PromptArgs& p, const Job& jb, int head, int at) {
+  constexpr int kPairs = D / 64, kKeys = 8;
+  const int lane = threadIdx.x & 31, kvh = head / (p.heads / p.kv_heads), lim = seen_by(jb, at);
+  const T* k = static_cast<const T*>(p.k) + (int64_t)jb.kv_start * p.ldk + (int64_t)kvh * p.ldkh + lane * (D / 32);
   const T* v = static_cast<const T*>(p.v) + (int64_t)jb.kv_start * p.ldv + (int64_t)kvh * p.ldvh + lane * (D / 32);
   const float c2 = factor(p.scale);
   float m = -INFINITY, l = 0.0f;
-  float2 o[kPairs];
+  float2 q[kPairs], o[kPairs];
 #pragma unroll
-  for (int i = 0; i < kPairs; ++i) o[i] = make_float2(0.0f, 0.0f);
-  for (int t0 = 0; t0 < lim; t0 += 32) {
-    const int here = lim - t0 < 32 ? lim - t0 : 32;
-    float s = -INFINITY;
-    if (lane < here) {
-      const uint4* row = reinterpret_cast<const uint4*>(k + (t0 + lane) * p.ldk);
-      float a = 0.0f, b = 0.0f;
-#pragma unroll 4
-      for (int i = 0; i < D / 8; ++i) {
-        float2 x[4], y[4];
-        pairs_of(reinterpret_cast<const uint4*>(q)[i], x, (T*)nullptr);
-        pairs_of(row[i], y, (T*)nullptr);
+  for (int i = 0; i < kPairs; ++i) {
+    q[i] = pair_of(*reinterpret_cast<const uint32_t*>(static_cast<const T*>(p.q) + (int64_t)(jb.start + at) * p.ldq + (int64_t)head * p.ldqh + lane * (D / 32) + 2 * i), (T*)nullptr);
+    o[i] = make_float2(0.0f, 0.0f);
+  }
+  for (int t0 = 0; t0 < lim; t0 += kKeys) {
+    const int here = lim - t0 < kKeys ? lim - t0 : kKeys;
+    uint32_t x[kKeys][kPairs];
+    auto load = [&](const T* rows, int64_t ld) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { a = fmaf(x[j].x, y[j].x, a); b = fmaf(x[j].y, y[j].y, b); }
+      for (int j = 0; j < kKeys; ++j)
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) x[j][i] = j < here ? *reinterpret_cast<const uint32_t*>(rows + (t0 + j) * ld + 2 * i) : 0u;
+    };
+    load(k, p.ldk);
+    float s[kKeys];
+#pragma unroll
+    for (int j = 0; j < kKeys; ++j) {
+      s[j] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        const float2 u = pair_of(x[j][i], (T*)nullptr);
+        s[j] = fmaf(q[i].x, u.x, fmaf(q[i].y, u.y, s[j]));
       }
-      s = a + b;
     }
-    float top = s;
-    for (int n = 16; n > 0; n >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, n));
+    load(v, p.ldv);  // (on its way while the scores are added)
+#pragma unroll
+    for (int n = kKeys / 2; n > 0; n >>= 1)
+#pragma unroll
+      for (int j = 0; j < n; ++j) {  // a lane keeps one of keys j and j + n, and gives the other away
+        const bool upper = lane & n;
+        const float mine = upper ? s[j + n] : s[j], other = upper ? s[j] : s[j + n];
+        s[j] = mine + __shfl_xor_sync(0xffffffffu, other, n);
+      }
+    float score = s[0];
+#pragma unroll
+    for (int n = kKeys; n < 32; n <<= 1) score += __shfl_xor_sync(0xffffffffu, score, n);
+    if ((lane & (kKeys - 1)) >= here) score = -INFINITY;
+    float top = score;
+    for (int n = kKeys / 2; n > 0; n >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, n));
     top = fmaxf(m, top);
-    const float ref = top == -INFINITY ? 0.0f : top, f = ex2((m - ref) * c2), w = ex2((s - ref) * c2);
+    const float ref = top == -INFINITY ? 0.0f : top, f = ex2((m - ref) * c2), w = ex2((score - ref) * c2);
     const uint32_t w2 = pack(w, w, (T*)nullptr);
     m = top;
     l = fmaf(l, f, w);
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) { o[i].x *= f; o[i].y *= f; }
-    for (int j = 0; j < here; ++j) {
-      const float x = pair_of(__shfl_sync(0xffffffffu, w2, j), (T*)nullptr).x;
+#pragma unroll
+    for (int j = 0; j < kKeys; ++j) {  // (keys behind the last: weights of 0, values of 0)
+      const float y = pair_of(__shfl_sync(0xffffffffu, w2, j), (T*)nullptr).x;
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) {
-        const float2 y = pair_of(*reinterpret_cast<const uint32_t*>(v + (t0 + j) * p.ldv + 2 * i), (T*)nullptr);
-        o[i].x = fmaf(x, y.x, o[i].x);
-        o[i].y = fmaf(x, y.y, o[i].y);
+        const float2 u = pair_of(x[j][i], (T*)nullptr);
+        o[i].x = fmaf(y, u.x, o[i].x);
+        o[i].y = fmaf(y, u.y, o[i].y);
       }
     }
     bool lost = true;
@@ -152,16 +170,11 @@ __device__ __forceinline__ void attend_again(const PromptArgs& p, const Job& jb,
     for (int i = 0; i < kPairs; ++i) lost = lost && isnan(o[i].x) && isnan(o[i].y);
     if (__all_sync(0xffffffffu, lost)) break;  // (nothing is left to find)
   }
-  for (int n = 16; n > 0; n >>= 1) l += __shfl_xor_sync(0xffffffffu, l, n);
+  for (int n = kKeys / 2; n > 0; n >>= 1) l += __shfl_xor_sync(0xffffffffu, l, n);
   const float inv = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
   T* y = static_cast<T*>(p.out) + (int64_t)(jb.start + at) * p.ldo + (int64_t)head * p.ldoh + lane * (D / 32);
 #pragma unroll
   for (int i = 0; i < kPairs; ++i) *reinterpret_cast<uint32_t*>(y + 2 * i) = pack(o[i].x * inv, o[i].y * inv, (T*)nullptr);
-}
-// Keys that row `at` of a job's sequence sees, in causal order.
-__device__ __forceinline__ int seen_by(const Job& jb, int at) {
-  const int64_t see = (int64_t)at + (jb.keys - jb.queries) + 1;
-  return (int)(see < 0 ? 0 : see > jb.keys ? jb.keys : see);
 }
 
 }  // namespace prompt

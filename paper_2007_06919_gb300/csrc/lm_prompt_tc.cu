@@ -211,9 +211,9 @@ __device__ __forceinline__ void mark_if_spoiled(const uint64_t (&sums)[2], bool 
   // (without a branch: the loop around keeps its registers)
   asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 q, %1, 0;\n\tsetp.neu.and.f32 p, %0, 0f00000000, q;\n\t@p st.shared.u32 [%2], 1;\n\t}" ::"f"(a + b), "r"((int)live), "r"(mark) : "memory");
 }
-// The block's end: each row of the kept jobs, and of the last ones that are marked, whose last key lies before a value that is not finite. For the four warps beside the
-// rows' (it takes 70 registers), as a call, with a copy of the arguments: what the compiler does to the jobs' loop for the code here, for a call of theirs, or for one that
-// might change the arguments, costs heads of 64 1 to 4% more (8192 tokens, 32 heads 248 us, 245 with neither marks nor this).
+// The block's end: the rows of the kept jobs, and of the last ones that are marked, whose last key lies before a value that is not finite. For the four warps beside the
+// rows' (it takes up to 88 registers, of their 104), as a call, with a copy of the arguments: what the compiler does to the jobs' loop for the code here, for a call of theirs, or for one that
+// might change the arguments, costs heads of 64 1 to 4% more (8192 tokens, 32 heads 247 us, 245 with neither marks nor this).
 template <class T, int D, int kTiles>
 static __device__ __noinline__ void take_rows_again(const PromptArgs& p, const Spoiled& spoiled, int warp) {
   for (int i = 0; i < spoiled.count + kMarks; ++i) {
@@ -221,12 +221,15 @@ static __device__ __noinline__ void take_rows_again(const PromptArgs& p, const S
     if (number >= 0 && !spoiled.mark[number]) continue;
     const Marked& which = number < 0 ? spoiled.jobs[i] : spoiled.last[number];
     const Job jb = which.job;
-    const int head = which.head, n0 = steps_of<kTiles>(jb, 0, 1), n1 = kTiles > 1 ? steps_of<kTiles>(jb, 1, 1) : 0, keys = (n0 > n1 ? n0 : n1) * kTile;
-    const int first = jb.tile * kTiles * kTile, end = first + kTiles * kTile < jb.queries ? first + kTiles * kTile : jb.queries;
+    const int head = which.head;
     const T* v = static_cast<const T*>(p.v) + (int64_t)jb.kv_start * p.ldv + (int64_t)(head / (p.heads / p.kv_heads)) * p.ldvh;
-    const int last = prompt::last_not_finite<T, D>(prompt::seen_by(jb, first), keys < jb.keys ? keys : jb.keys,
-                                                   [&](int t, int c) { return reinterpret_cast<const uint4*>(v + t * p.ldv)[c]; });
-    for (int at = first + warp; at < end && prompt::seen_by(jb, at) <= last; at += 4) prompt::attend_again<T, D>(p, jb, head, at, prompt::seen_by(jb, at));
+    for (int t = 0; t < kTiles; ++t) {
+      const int first = (jb.tile * kTiles + t) * kTile, end = first + kTile < jb.queries ? first + kTile : jb.queries, keys = steps_of<kTiles>(jb, t, 1) * kTile;
+      if (first >= end) break;
+      const int last = prompt::last_not_finite<T, D>(prompt::seen_by(jb, first), keys < jb.keys ? keys : jb.keys,
+                                                     [&](int key, int c) { return reinterpret_cast<const uint4*>(v + key * p.ldv)[c]; });
+      for (int at = first + warp; at < end && prompt::seen_by(jb, at) <= last; at += 4) prompt::attend_again<T, D>(p, jb, head, at);
+    }
   }
 }
 
