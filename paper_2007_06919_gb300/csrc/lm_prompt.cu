@@ -6,8 +6,8 @@
 //
 // This kernel takes 64 query rows of one head, four warps of 16, and keys in tiles of 64 (or 32) through two stages of shared memory. It serves what the
 // tensor-memory kernels do not: strides of zero, which no tensor map holds, and more jobs than a grid's second axis. Bound by mma.sync, whose rate is a
-// fraction of theirs: 8192 tokens of 32 heads of 192 3,750 us (220 TFLOP/s; 511 there), of 256 4,239 (259; 639). Prompts of less than
-// a tile's 128 rows come near: 100 of 64 tokens, 32 heads of 256, 113 us (99 there).
+// fraction of theirs: 8192 tokens of 32 heads of 192 3,730 us (221 TFLOP/s; 511 there), of 256 4,193 (262; 639). Prompts of less than
+// a tile's 128 rows come near: 100 of 64 tokens, 32 heads of 256, 112 us (99 there).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -50,14 +50,19 @@ __device__ __forceinline__ uint32_t at(uint32_t base, int r, int c) {
   return base + r * (D * 2) + ((c & ~7) | ((c ^ r) & 7)) * 16;
 }
 
-// (a call, with copies: heads of 256 have no registers left for it)
+// The rows of a warp, from row `first` on, that a hidden value reached. (A call, with copies: heads of 256 have no registers left for it.)
 template <class T, int D>
-static __device__ __noinline__ void take_row_again(const PromptArgs p, const Job jb, int head, int at) {
-  attend_again<T, D>(p, jb, head, at);
+static __device__ __noinline__ void take_rows_again(const PromptArgs p, const Job jb, int head, int first) {
+  const int end = first + 16 < jb.queries ? first + 16 : jb.queries, seen = seen_by(jb, (jb.tile + 1) * kRows - 1 < jb.queries ? (jb.tile + 1) * kRows - 1 : jb.queries - 1);
+  const int keys = (seen + keys_of(D) - 1) / keys_of(D) * keys_of(D);  // that the block's products took
+  const T* v = static_cast<const T*>(p.v) + (int64_t)jb.kv_start * p.ldv + (int64_t)(head / (p.heads / p.kv_heads)) * p.ldvh;
+  const int last = last_not_finite<T, D>(seen_by(jb, first), keys < jb.keys ? keys : jb.keys, [&](int t, int i) { return reinterpret_cast<const uint4*>(v + t * p.ldv)[i]; });
+  __syncwarp();  // (the rows' first outputs come before)
+  for (int at = first; at < end && seen_by(jb, at) <= last; ++at) attend_again<T, D>(p, jb, head, at);
 }
-// (heads of 128: two blocks an SM by shared memory, not three by registers, which would spill)
+// (Blocks an SM: heads of 64 three, 4096 tokens of 8 heads 94 us, 111 with four and 122 with five; of 128 two by shared memory, three by registers would spill.)
 template <class T, int D>
-__global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 0) prompt_kernel(const __grid_constant__ PromptArgs p) {
+__global__ void __launch_bounds__(kThreads, D == 64 ? 3 : D == 128 ? 2 : 0) prompt_kernel(const __grid_constant__ PromptArgs p) {
   constexpr int kKeys = keys_of(D), kTile = kKeys * D * 2, kChunks = D / 8;
   extern __shared__ __align__(128) uint8_t smem[];  // queries, two stages of keys and values
   __shared__ Job job;
@@ -174,6 +179,7 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 0) prompt_kernel(cons
     }
   }
   cp_async_wait<0>();
+  float zero = 0.0f;  // (a sum of outputs times 0: NaN where one is not finite)
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
@@ -184,23 +190,13 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 0) prompt_kernel(cons
     const int64_t token = jb.start + row0 + r;
     T* y = static_cast<T*>(p.out) + token * p.ldo + (int64_t)head * p.ldoh + (lane & 3) * 2;
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) *reinterpret_cast<uint32_t*>(y + 8 * i) = pack(o[i][2 * h] * inv, o[i][2 * h + 1] * inv, (T*)nullptr);
+    for (int i = 0; i < D / 8; ++i) {
+      *reinterpret_cast<uint32_t*>(y + 8 * i) = pack(o[i][2 * h] * inv, o[i][2 * h + 1] * inv, (T*)nullptr);
+      zero = fmaf(o[i][2 * h], 0.0f, fmaf(o[i][2 * h + 1], 0.0f, zero));
+    }
     if (p.lse && (lane & 3) == 0) p.lse[token * p.heads + head] = fmaf(m[h], c2, log2f(l[h])) * kLn2;
   }
-  // rows that a hidden value reached, a warp its own
-  const Job je = job;  // (read again: its numbers are not kept through the tiles)
-  const int first = je.tile * kRows + warp * 16;
-  if (!p.causal || first >= je.queries) return;
-  const int last = last_not_finite<T, D>(seen_by(je, first), tiles * kKeys < je.keys ? tiles * kKeys : je.keys, [&](int t, int i) {
-    const int tile = t / kKeys;  // (the last two tiles' values are still here)
-    uint4 x;
-    if (tile >= tiles - 2) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at<D>(sk + ((tile & 1) * 2 + 1) * kTile, t - tile * kKeys, i)));
-    else x = reinterpret_cast<const uint4*>(v + t * p.ldv)[i];
-    return x;
-  });
-  __syncwarp();  // (the rows' first outputs come before)
-#pragma unroll 1
-  for (int at = first; at < first + 16 && at < je.queries && seen_by(je, at) <= last; ++at) take_row_again<T, D>(p, je, head, at);
+  if (p.causal && __any_sync(0xffffffffu, isnan(zero))) take_rows_again<T, D>(p, job, head, job.tile * kRows + warp * 16);
 }
 
 template <class T, int D>
