@@ -213,7 +213,8 @@ __device__ __forceinline__ void mark_if_spoiled(const uint64_t (&sums)[2], bool 
 }
 // The block's end: the rows of the kept jobs, and of the last ones that are marked, whose last key lies before a value that is not finite. For the four warps beside the
 // rows' (it takes up to 88 registers, of their 104), as a call, with a copy of the arguments: what the compiler does to the jobs' loop for the code here, for a call of theirs, or for one that
-// might change the arguments, costs heads of 64 1 to 4% more (8192 tokens, 32 heads 247 us, 245 with neither marks nor this).
+// might change the arguments, costs heads of 64 1 to 4% more. (With marks and this against neither: 8192 tokens, 32 heads of 64 247 us and 245, of 128 336 and 336; 200 prompts of up
+// to 64 tokens 148 and 143, 155 and 149, of 192 159 and 148, of 256 191 and 184. A look at the values instead, by the warp that clears those behind a sequence: 255, 339; 155, 176, 177, 206.)
 template <class T, int D, int kTiles>
 static __device__ __noinline__ void take_rows_again(const PromptArgs& p, const Spoiled& spoiled, int warp) {
   for (int i = 0; i < spoiled.count + kMarks; ++i) {
